@@ -48,7 +48,7 @@ typedef enum {
     GLEAM_E_DIMS = -2,              /* non-positive or inconsistent dimension, ndim_fft not 1, 2 or 3  */
     GLEAM_E_UNSUPPORTED_SIZE = -3,  /* a transformed length has no kernel (see gleam_fft_size_supported) */
     GLEAM_E_WORKSPACE = -4,         /* ws / saved too small or misaligned                              */
-    GLEAM_E_DESC = -5,              /* prox description is not a valid / supported network             */
+    GLEAM_E_DESC = -5,              /* a description (prox, layer operator) is not valid / supported   */
     GLEAM_E_LAUNCH = -6             /* the HIP runtime refused a launch                                */
 } gleam_status;
 
@@ -298,6 +298,93 @@ int gleam_unrolled_infer(const gleam_geom* geom, const gleam_prox_desc* prox, in
                          const gleam_c64* x0, const gleam_c64* S, const uint8_t* M, const gleam_c64* y,
                          float alpha, const float* theta, gleam_c64* x_out, gleam_c64* x_tmp,
                          void* ws, size_t ws_bytes, void* stream);
+
+/* ---- Layers between the convolutions: layer norm, dropout, linear attention along the frames ------------------------
+ * The operators below take feature maps [..][channels] as the prox network holds them (channels last) and mix the frames of a
+ * dynamic series, or the tokens of any sequence: y = layer_norm(x); q, k, v = projections of y; h = x + dropout(projection of
+ * linear_attention(q, k, v)).  Activations are float32 (dtype 0) or bfloat16 (dtype 1) and are computed on in float32 (products of
+ * bfloat16 arrays on the bfloat16 matrix cores with float32 sums); scales, shifts, statistics, decays and states are float32.
+ * Conventions are those above, except that arrays may have strides.  Pointers need the alignment of their element type; accesses are
+ * fastest where base addresses and strides are multiples of 16 bytes. */
+
+/* Layer norm over the last dimension of `rows` rows of n elements: mean m and variance s^2 (over n) of the row,
+ *     y = (x - m) * r * gamma + beta,   r = 1 / sqrt(s^2 + eps)
+ * ld_in, ld_out: elements between the starts of neighbouring rows of x and g_x, and of y and g_y (>= n).  eps > 0. */
+typedef struct {
+    int32_t dtype;
+    float eps;
+    int64_t rows, n, ld_in, ld_out;
+} gleam_layer_norm_desc;
+
+/* gamma, beta: [n], either may be NULL (1 and 0).  mean, rstd: [rows], m and r for the backward pass, either may be NULL.  y may be x
+ * where ld_in = ld_out. */
+int gleam_layer_norm_fwd(const gleam_layer_norm_desc* desc, const void* x, const float* gamma, const float* beta, void* y,
+                         float* mean, float* rstd, void* stream);
+
+/* Gradients of the same call from g_y = dL/dy: with xh = (x - m) r and gg = g_y gamma,
+ *     g_x = r (gg - mean(gg) - xh mean(gg xh)),   g_gamma = sum over rows of g_y xh,   g_beta = sum over rows of g_y
+ * g_gamma, g_beta: [n], overwritten, either may be NULL (not wanted).  g_x may be g_y where ld_in = ld_out, and may not be x.
+ * Sums over rows are formed in a fixed order.  ws: gleam_layer_norm_workspace_bytes, 256-byte aligned, not read where it is 0. */
+int gleam_layer_norm_workspace_bytes(const gleam_layer_norm_desc* desc, size_t* ws_bytes);
+int gleam_layer_norm_bwd(const gleam_layer_norm_desc* desc, const void* x, const float* gamma, const float* mean,
+                         const float* rstd, const void* g_y, void* g_x, float* g_gamma, float* g_beta, void* ws,
+                         size_t ws_bytes, void* stream);
+
+/* Dropout with rate p of `rows` rows of n elements, a residual added in the same pass.  The mask is never stored: element
+ * e = row * n + column is kept where its draw of 16 bits is below K = round(65536 (1 - p)), and then multiplied by 65536 / K, so that
+ * the expectation is exact for the rate 1 - K/65536 that is in force (within 8e-6 of p).  Draws are the 16-bit halves, low halves
+ * first, of Philox 4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011): block e / 8 has the
+ * counter (e/8 low word, high word, c low word, high word), c = offset + *step, and the key (seed low word, high word).  They depend
+ * on seed, c and e alone, not on strides, types or the launch.
+ * ld_in, ld_res, ld_out: elements between rows of x and g_x, of residual, and of out and g_out. */
+typedef struct {
+    int32_t dtype;
+    float p;                        /* 0 <= p <= 1; 1 drops everything */
+    int64_t rows, n, ld_in, ld_res, ld_out;
+    uint64_t seed, offset;          /* one offset for each dropout layer and training step */
+} gleam_dropout_desc;
+
+/* out = residual + dropout(x); residual may be NULL.  out may be x or residual where their strides are equal.  A dropped element is
+ * not read into the result, whatever it holds.  step: device uint64 added to the offset, or NULL; a captured graph that is
+ * replayed draws a new mask for each value it finds there. */
+int gleam_dropout_fwd(const gleam_dropout_desc* desc, const void* x, const void* residual, void* out, const uint64_t* step,
+                      void* stream);
+/* g_x = the same mask and factor on g_out; the gradient of the residual is g_out itself.  g_x may be g_out where ld_in = ld_out. */
+int gleam_dropout_bwd(const gleam_dropout_desc* desc, const void* g_out, void* g_x, const uint64_t* step, void* stream);
+
+/* Linear attention with a decay for each head, over B sequences of T tokens at each of P pixels:
+ *     S_t = exp(log_decay[h]) S_{t-1} + k_t v_t^T,    o_t = scale * S_t^T q_t     (S: dk x dv, one for each sequence, pixel and head)
+ * so o_t = scale * sum over s <= t of exp(log_decay[h] (t - s)) (q_t . k_s) v_s.  log_decay <= 0 (-inf: no memory); it is a constant of the
+ * layer and has no gradient.  Heads: `heads` of the output and the states; q, k and v have heads of their own number, each a
+ * divisor of `heads`, and output head h uses head h / (heads / their number).
+ * Arrays: element [b][t][p][head][c] of an activation lies at b*s.b + t*s.t + p*s.p + head*s.h + c (strides in elements, >= 0).  Strides of arrays that are written - o, and in the backward pass those of q, k and v - must not let elements
+ * overlap.  States are [B][P][heads][dk][dv] float32, row-major.
+ * lengths: device int32 [B] or NULL (all T), tokens of each sequence that are there; others are not read, their outputs and
+ * gradients are written as zeros; values outside 0..T count as the nearest of them.  A sequence of length 0 leaves its state as it is.
+ * A token that is not finite can reach the outputs of up to 63 tokens before it (and in the gradients behind it) as NaN: they share a
+ * matrix product.
+ * 1 <= dk, dv <= 128.  One token (T = 1) takes the recurrent form: every state is read once and written once. */
+typedef struct { int64_t b, t, p, h; } gleam_seq_strides;
+typedef struct {
+    int32_t dtype, heads, q_heads, k_heads, v_heads, dk, dv;
+    float scale;
+    int64_t B, T, P;
+    gleam_seq_strides q, k, v, o;
+} gleam_linattn_desc;
+
+/* Scratch of either direction; 0 where none is needed (then ws may be NULL). */
+int gleam_linattn_workspace_bytes(const gleam_linattn_desc* desc, size_t* fwd_bytes, size_t* bwd_bytes);
+/* state_in: state before the first token, or NULL (zero).  state_out: state behind the last token, or NULL (not wanted); may be
+ * state_in.  o may not overlap q, k or v. */
+int gleam_linattn_fwd(const gleam_linattn_desc* desc, const void* q, const void* k, const void* v, const float* log_decay,
+                      const int32_t* lengths, const float* state_in, void* o, float* state_out, void* ws, size_t ws_bytes,
+                      void* stream);
+/* Gradients of the same call from g_o = dL/do (strides of o) and g_state_out = dL/d state_out (or NULL: zero).  g_q, g_k, g_v have the
+ * strides of q, k, v; heads that are shared receive the sum over the output heads that use them, in a fixed order.  g_state_in
+ * (or NULL) = dL/d state_in, may be g_state_out.  No gradient may overlap an input. */
+int gleam_linattn_bwd(const gleam_linattn_desc* desc, const void* q, const void* k, const void* v, const float* log_decay,
+                      const int32_t* lengths, const float* state_in, const void* g_o, const float* g_state_out, void* g_q,
+                      void* g_k, void* g_v, float* g_state_in, void* ws, size_t ws_bytes, void* stream);
 
 /* Measurement aid (not part of the method): between gleam_profile_begin and gleam_profile_end every kernel
  * this library launches is bracketed by HIP events on the caller's stream.  gleam_profile_end synchronises

@@ -46,6 +46,25 @@ class gleam_adam(C.Structure):
     _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float)]
 
 
+class gleam_layer_norm_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("eps", C.c_float), ("rows", C.c_int64), ("n", C.c_int64), ("ld_in", C.c_int64),
+                ("ld_out", C.c_int64)]
+
+
+class gleam_dropout_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("p", C.c_float), ("rows", C.c_int64), ("n", C.c_int64), ("ld_in", C.c_int64),
+                ("ld_res", C.c_int64), ("ld_out", C.c_int64), ("seed", C.c_uint64), ("offset", C.c_uint64)]
+
+
+class gleam_seq_strides(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("b", "t", "p", "h")]
+
+
+class gleam_linattn_desc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("dtype", "heads", "q_heads", "k_heads", "v_heads", "dk", "dv")] + [("scale", C.c_float)] +
+                [(n, C.c_int64) for n in ("B", "T", "P")] + [(n, gleam_seq_strides) for n in ("q", "k", "v", "o")])
+
+
 class GleamError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -91,6 +110,15 @@ def lib() -> C.CDLL:
         L.gleam_greedy_iteration.argtypes = [pg, pp, C.c_int, vp, vp, vp, vp, C.c_float, vp, vp, vp, C.POINTER(gleam_adam),
                                              C.c_int64, vp, vp, vp, vp, vp, vp, sz, vp, sz, vp]
         L.gleam_unrolled_infer.argtypes = [pg, pp, C.c_int, vp, vp, vp, vp, C.c_float, vp, vp, vp, vp, sz, vp]
+        pn, pd, pl = C.POINTER(gleam_layer_norm_desc), C.POINTER(gleam_dropout_desc), C.POINTER(gleam_linattn_desc)
+        L.gleam_layer_norm_fwd.argtypes = [pn, vp, vp, vp, vp, vp, vp, vp]
+        L.gleam_layer_norm_workspace_bytes.argtypes = [pn, C.POINTER(sz)]
+        L.gleam_layer_norm_bwd.argtypes = [pn, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.gleam_dropout_fwd.argtypes = [pd, vp, vp, vp, vp, vp]
+        L.gleam_dropout_bwd.argtypes = [pd, vp, vp, vp, vp]
+        L.gleam_linattn_workspace_bytes.argtypes = [pl, C.POINTER(sz), C.POINTER(sz)]
+        L.gleam_linattn_fwd.argtypes = [pl, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.gleam_linattn_bwd.argtypes = [pl, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.gleam_profile_begin.argtypes = []
         L.gleam_profile_end.argtypes = [C.POINTER(gleam_kernel_record), C.c_int, C.POINTER(C.c_int)]
         _lib = L
@@ -102,7 +130,9 @@ EXPORTS = ("gleam_strerror", "gleam_fft_size_supported", "gleam_set_kernel_polic
            "gleam_deep_module_fwd", "gleam_deep_module_bwd", "gleam_sense_adjoint", "gleam_kspace_to_hybrid",
            "gleam_mask_constant_along_outer_axis", "gleam_modl_workspace_bytes",
            "gleam_modl_module_fwd", "gleam_modl_module_bwd", "gleam_adam_step",
-           "gleam_greedy_iteration", "gleam_unrolled_infer", "gleam_profile_begin", "gleam_profile_end")
+           "gleam_greedy_iteration", "gleam_unrolled_infer", "gleam_layer_norm_fwd", "gleam_layer_norm_workspace_bytes", "gleam_layer_norm_bwd",
+           "gleam_dropout_fwd", "gleam_dropout_bwd", "gleam_linattn_workspace_bytes", "gleam_linattn_fwd", "gleam_linattn_bwd",
+           "gleam_profile_begin", "gleam_profile_end")
 
 
 def strerror(status: int) -> str:
@@ -294,6 +324,154 @@ def gleam_unrolled_infer(geom, prox, n_modules, x0, S, M, y, alpha, theta, x_out
     _check(lib().gleam_unrolled_infer(C.byref(geom), C.byref(prox), int(n_modules), _ptr(x0), _ptr(S), _ptr(M), _ptr(y),
                                       C.c_float(alpha), _ptr(theta), _ptr(x_out), _ptr(x_tmp), _ptr(ws), _nbytes(ws),
                                       _stream(stream)), "gleam_unrolled_infer")
+
+
+# ---- layer norm, dropout, linear attention: arrays may have strides, so what a call reads is checked against its description
+def _dtype_code(dtype) -> int:
+    """0 or 1 from a code or from torch.float32 / torch.bfloat16."""
+    import torch
+    code = {torch.float32: 0, torch.bfloat16: 1, 0: 0, 1: 1}.get(dtype)
+    if code is None:
+        raise ValueError(f"dtype {dtype}: float32 (0) and bfloat16 (1) have kernels")
+    return code
+
+
+_DTYPES = []
+
+
+def _array(t, code: int, count: int, what: str) -> Optional[int]:
+    """Address of a device array of `count` elements of type code 0 / 1 (2: int32, 3: int64 words); strides are the description's."""
+    if t is None or isinstance(t, int):
+        return t
+    if not _DTYPES:
+        import torch
+        _DTYPES.extend((torch.float32, torch.bfloat16, torch.int32, torch.int64))
+    if t.dtype is not _DTYPES[code] or t.numel() != count or not t.is_cuda:
+        raise ValueError(f"{what}: {t.numel()} elements of {t.dtype} on {t.device}, the description has {count} of {_DTYPES[code]} on the GPU")
+    return t.data_ptr()
+
+
+def _flat(t, code: int, count: int, what: str) -> Optional[int]:
+    if t is not None and not isinstance(t, int) and not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    return _array(t, code, count, what)
+
+
+def _rows(t, code: int, rows: int, n: int, ld: int, what: str) -> Optional[int]:
+    """A rows x n array with `ld` elements from row to row: contiguous (ld = n) of any shape, or two-dimensional with that stride."""
+    if t is not None and not isinstance(t, int):
+        if t.is_contiguous():
+            if ld != n and rows > 1:
+                raise ValueError(f"{what} is contiguous, the description has {ld} elements from row to row of {n}")
+        elif t.shape != (rows, n) or (n > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) != ld):
+            raise ValueError(f"{what}: shape {tuple(t.shape)} with strides {t.stride()}, the description has {rows} rows of {n}, {ld} apart")
+    return _array(t, code, rows * n, what)
+
+
+def make_layer_norm(dtype, rows, n, eps=1e-5, ld=None, ld_out=None) -> gleam_layer_norm_desc:
+    """ld: elements from row to row of x and g_x (default n); ld_out: of y and g_y (default ld)."""
+    ld = n if ld is None else ld
+    return gleam_layer_norm_desc(_dtype_code(dtype), float(eps), int(rows), int(n), int(ld), int(ld if ld_out is None else ld_out))
+
+
+def gleam_layer_norm_fwd(desc, x, gamma, beta, y, mean=None, rstd=None, stream=None):
+    rows, n = desc.rows, desc.n
+    _check(lib().gleam_layer_norm_fwd(C.byref(desc), _rows(x, desc.dtype, rows, n, desc.ld_in, "x"), _flat(gamma, 0, n, "gamma"),
+                                      _flat(beta, 0, n, "beta"), _rows(y, desc.dtype, rows, n, desc.ld_out, "y"),
+                                      _flat(mean, 0, rows, "mean"), _flat(rstd, 0, rows, "rstd"), _stream(stream)),
+           "gleam_layer_norm_fwd")
+
+
+def gleam_layer_norm_workspace_bytes(desc) -> int:
+    n = C.c_size_t(0)
+    _check(lib().gleam_layer_norm_workspace_bytes(C.byref(desc), C.byref(n)), "gleam_layer_norm_workspace_bytes")
+    return n.value
+
+
+def gleam_layer_norm_bwd(desc, x, gamma, mean, rstd, g_y, g_x, g_gamma, g_beta, ws, stream=None):
+    rows, n = desc.rows, desc.n
+    _check(lib().gleam_layer_norm_bwd(C.byref(desc), _rows(x, desc.dtype, rows, n, desc.ld_in, "x"), _flat(gamma, 0, n, "gamma"),
+                                      _flat(mean, 0, rows, "mean"), _flat(rstd, 0, rows, "rstd"),
+                                      _rows(g_y, desc.dtype, rows, n, desc.ld_out, "g_y"),
+                                      _rows(g_x, desc.dtype, rows, n, desc.ld_in, "g_x"), _flat(g_gamma, 0, n, "g_gamma"),
+                                      _flat(g_beta, 0, n, "g_beta"), _ptr(ws), _nbytes(ws), _stream(stream)), "gleam_layer_norm_bwd")
+
+
+def make_dropout(dtype, rows, n, p, seed, offset=0, ld=None, ld_res=None, ld_out=None) -> gleam_dropout_desc:
+    """ld: elements from row to row of x and g_x (default n); ld_res, ld_out: of residual, of out and g_out (default ld)."""
+    ld = n if ld is None else ld
+    return gleam_dropout_desc(_dtype_code(dtype), float(p), int(rows), int(n), int(ld), int(ld if ld_res is None else ld_res),
+                              int(ld if ld_out is None else ld_out), int(seed), int(offset))
+
+
+def gleam_dropout_fwd(desc, x, residual, out, step=None, stream=None):
+    """step: int64 tensor of one element on the device, added to the offset, or None."""
+    rows, n = desc.rows, desc.n
+    _check(lib().gleam_dropout_fwd(C.byref(desc), _rows(x, desc.dtype, rows, n, desc.ld_in, "x"),
+                                   _rows(residual, desc.dtype, rows, n, desc.ld_res, "residual"),
+                                   _rows(out, desc.dtype, rows, n, desc.ld_out, "out"), _flat(step, 3, 1, "step"), _stream(stream)),
+           "gleam_dropout_fwd")
+
+
+def gleam_dropout_bwd(desc, g_out, g_x, step=None, stream=None):
+    rows, n = desc.rows, desc.n
+    _check(lib().gleam_dropout_bwd(C.byref(desc), _rows(g_out, desc.dtype, rows, n, desc.ld_out, "g_out"),
+                                   _rows(g_x, desc.dtype, rows, n, desc.ld_in, "g_x"), _flat(step, 3, 1, "step"), _stream(stream)),
+           "gleam_dropout_bwd")
+
+
+def make_linattn(q, k, v, o, scale=1.0) -> gleam_linattn_desc:
+    """From the arrays of a call, or others of their shapes and strides: [B][T][P][heads][width] with any strides but the last.
+    Gradients have the strides of the arrays they belong to."""
+    for name, t in (("q", q), ("k", k), ("v", v), ("o", o)):
+        if t.dim() != 5 or t.dtype is not o.dtype or t.shape[:3] != o.shape[:3] or (t.shape[4] > 1 and t.stride(4) != 1):
+            raise ValueError(f"{name}: [B][T][P][heads][width] of one type with contiguous widths expected, got {tuple(t.shape)} with strides "
+                             f"{t.stride()} of {t.dtype}")
+    if q.shape[4] != k.shape[4] or v.shape[4] != o.shape[4]:
+        raise ValueError("q and k, and v and o, have the same width")
+    B, T, P, H, dv = o.shape
+    return gleam_linattn_desc(_dtype_code(o.dtype), H, q.shape[3], k.shape[3], v.shape[3], q.shape[4], dv, float(scale), B, T, P,
+                              *(gleam_seq_strides(*t.stride()[:4]) for t in (q, k, v, o)))
+
+
+def _seq(t, desc, s: gleam_seq_strides, heads: int, width: int, what: str) -> Optional[int]:
+    if t is not None and not isinstance(t, int):
+        if t.shape != (desc.B, desc.T, desc.P, heads, width):
+            raise ValueError(f"{what}: shape {tuple(t.shape)}, the description has {(desc.B, desc.T, desc.P, heads, width)}")
+        got = t.stride()
+        if got != (s.b, s.t, s.p, s.h, 1) and any(n > 1 and x != y for n, x, y in zip(t.shape, got, (s.b, s.t, s.p, s.h, 1))):
+            raise ValueError(f"{what}: strides {got}, the description has {(s.b, s.t, s.p, s.h, 1)}")
+        return _array(t, desc.dtype, t.numel(), what)
+    return t
+
+
+def gleam_linattn_workspace_bytes(desc):
+    """(forward, backward) bytes; 0: no workspace needed."""
+    fwd, bwd = C.c_size_t(0), C.c_size_t(0)
+    _check(lib().gleam_linattn_workspace_bytes(C.byref(desc), C.byref(fwd), C.byref(bwd)), "gleam_linattn_workspace_bytes")
+    return fwd.value, bwd.value
+
+
+def gleam_linattn_fwd(desc, q, k, v, log_decay, lengths, state_in, o, state_out, ws, stream=None):
+    H, dk, dv = desc.heads, desc.dk, desc.dv
+    state = desc.B * desc.P * H * dk * dv
+    _check(lib().gleam_linattn_fwd(C.byref(desc), _seq(q, desc, desc.q, desc.q_heads, dk, "q"), _seq(k, desc, desc.k, desc.k_heads, dk, "k"),
+                                   _seq(v, desc, desc.v, desc.v_heads, dv, "v"), _flat(log_decay, 0, H, "log_decay"),
+                                   _flat(lengths, 2, desc.B, "lengths"), _flat(state_in, 0, state, "state_in"),
+                                   _seq(o, desc, desc.o, H, dv, "o"), _flat(state_out, 0, state, "state_out"), _ptr(ws), _nbytes(ws),
+                                   _stream(stream)), "gleam_linattn_fwd")
+
+
+def gleam_linattn_bwd(desc, q, k, v, log_decay, lengths, state_in, g_o, g_state_out, g_q, g_k, g_v, g_state_in, ws, stream=None):
+    H, dk, dv = desc.heads, desc.dk, desc.dv
+    state = desc.B * desc.P * H * dk * dv
+    _check(lib().gleam_linattn_bwd(C.byref(desc), _seq(q, desc, desc.q, desc.q_heads, dk, "q"), _seq(k, desc, desc.k, desc.k_heads, dk, "k"),
+                                   _seq(v, desc, desc.v, desc.v_heads, dv, "v"), _flat(log_decay, 0, H, "log_decay"),
+                                   _flat(lengths, 2, desc.B, "lengths"), _flat(state_in, 0, state, "state_in"),
+                                   _seq(g_o, desc, desc.o, H, dv, "g_o"), _flat(g_state_out, 0, state, "g_state_out"),
+                                   _seq(g_q, desc, desc.q, desc.q_heads, dk, "g_q"), _seq(g_k, desc, desc.k, desc.k_heads, dk, "g_k"),
+                                   _seq(g_v, desc, desc.v, desc.v_heads, dv, "g_v"), _flat(g_state_in, 0, state, "g_state_in"),
+                                   _ptr(ws), _nbytes(ws), _stream(stream)), "gleam_linattn_bwd")
 
 
 def gleam_profile_begin():

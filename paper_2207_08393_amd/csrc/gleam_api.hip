@@ -150,7 +150,7 @@ const char* gleam_strerror(int status) {
         case GLEAM_E_DIMS: return "invalid geometry";
         case GLEAM_E_UNSUPPORTED_SIZE: return "no transform kernel for one of the Fourier lengths";
         case GLEAM_E_WORKSPACE: return "workspace or saved buffer too small or not 256-byte aligned";
-        case GLEAM_E_DESC: return "invalid or unsupported prox description";
+        case GLEAM_E_DESC: return "invalid or unsupported description";
         case GLEAM_E_LAUNCH: return "HIP launch failed";
         default: return "unknown gleam status";
     }

@@ -1,0 +1,459 @@
+// Layer norm over rows of n elements, forward and backward (gfx950).
+//
+// Forward: one read and one write of the row.  A team of lanes holds a whole row in registers, so the variance is the mean of the
+// squared distances from the mean (no cancellation where the mean is large) without a second read; the mean is the row's first element
+// plus the mean distance from it, so that a row of equal numbers has exactly that mean and becomes zeros.  Backward: one read of x and g_y,
+// one write of g_x; every lane keeps its columns from row to row and sums g_gamma and g_beta in registers, a workgroup writes one
+// partial sum per column and a second launch adds them up in a fixed order.  Both are bound by HBM.
+//
+// Rows too long for the registers of a workgroup are read three times (forward) or twice (backward), see the streaming kernels.
+#include <hip/hip_runtime.h>
+
+#include "layer_common.h"
+#include "layer_ops.h"
+
+namespace gleam {
+namespace {
+
+constexpr int kNormThreads = 256;
+constexpr int kNormGrid = 2048;   // workgroups at most: every one walks rows and keeps gamma, beta and its sums
+
+template <class T>
+constexpr int vec_of() { return 16 / (int)sizeof(T); }
+
+template <int LANES>
+constexpr int threads_of() { return LANES > 64 ? LANES : kNormThreads; }
+
+// Sum over a team of LANES lanes, the same value in all of them.  A team wider than a wave is the workgroup; `red` is then LDS for
+// one float2 a wave, and the barrier in front makes its last use over.
+template <int LANES>
+__device__ __forceinline__ float2 team_sum(float2 v, float2* red) {
+#pragma unroll
+    for (int o = (LANES < 64 ? LANES : 64) / 2; o > 0; o >>= 1) {
+        v.x += __shfl_xor(v.x, o);
+        v.y += __shfl_xor(v.y, o);
+    }
+    if constexpr (LANES > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = red[0];
+#pragma unroll
+        for (int w = 1; w < LANES / 64; ++w) {
+            v.x += red[w].x;
+            v.y += red[w].y;
+        }
+    }
+    return v;
+}
+
+// The columns of a lane's vectors: vector j begins at column (lane + j LANES) VE.  The row's last vector is moved back to end at n;
+// its first elements, [0, lo), are then the vector's before it and stay out of sums (their results are written twice, the same
+// bits).  Rows shorter than a vector: hi < VE, element by element.
+template <int VE>
+struct Columns {
+    long long col;
+    int lo, hi;
+    __device__ __forceinline__ Columns(long long unit, long long n) {
+        col = unit * VE;
+        lo = 0;
+        hi = col < n ? VE : 0;
+        if (hi && col + VE > n) {
+            if (n >= VE) {
+                lo = (int)(col + VE - n);
+                col = n - VE;
+            } else {
+                hi = (int)n;
+            }
+        }
+    }
+};
+template <class T, int VE>
+__device__ __forceinline__ void load_cols(const T* row, const Columns<VE>& c, Pack<T, VE>& p) {
+    if (c.hi == VE) {
+        p.load(row + c.col);
+    } else {
+        float v[VE];
+#pragma unroll
+        for (int i = 0; i < VE; ++i) v[i] = i < c.hi ? to_f32(row[c.col + i]) : 0.f;
+        p.set(v);
+    }
+}
+template <class T, int VE>
+__device__ __forceinline__ void store_cols(T* row, const Columns<VE>& c, const float* v) {
+    if (c.hi == VE) {
+        Pack<T, VE> p;
+        p.set(v);
+        p.store(row + c.col);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VE; ++i)
+            if (i < c.hi) put_f32(row + c.col + i, v[i]);
+    }
+}
+template <int VE>
+__device__ __forceinline__ void load_param(const float* p, const Columns<VE>& c, float fallback, float* v) {
+#pragma unroll
+    for (int i = 0; i < VE; ++i) v[i] = p && i < c.hi ? p[c.col + i] : fallback;
+}
+
+struct NormArgs {
+    const void *x, *g;
+    const float *gamma, *beta, *mean_in, *rstd_in;
+    void* out;
+    float *mean, *rstd;
+    float* part;              // backward: [workgroup][2][n] partial sums, or null
+    long long rows, n, ld_x, ld_y;
+    float eps;
+};
+
+template <class T, int LANES, int NV>
+__global__ __launch_bounds__(threads_of<LANES>()) void norm_fwd_kernel(NormArgs a) {
+    constexpr int VE = vec_of<T>(), TEAMS = threads_of<LANES>() / LANES;
+    __shared__ float2 red[LANES > 64 ? LANES / 64 : 1];
+    const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
+    const float inv_n = 1.f / (float)a.n;
+    const T* x = (const T*)a.x;
+    T* y = (T*)a.out;
+    // a row beyond the last is computed on zeros and not written, so that every lane of a wave takes part in the sums
+    for (long long r0 = (long long)blockIdx.x * TEAMS; r0 < a.rows; r0 += (long long)gridDim.x * TEAMS) {
+        const long long row = r0 + team;
+        const bool there = row < a.rows;
+        const float pivot = there ? to_f32(x[row * a.ld_x]) : 0.f;
+        float v[NV][VE];
+        float2 s = {0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const Columns<VE> c(lane + j * LANES, a.n);
+            if (there && c.hi) {
+                Pack<T, VE> p;
+                load_cols(x + row * a.ld_x, c, p);
+#pragma unroll
+                for (int i = 0; i < VE; ++i) {
+                    v[j][i] = p.get(i);
+                    s.x += i >= c.lo && i < c.hi ? v[j][i] - pivot : 0.f;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < VE; ++i) v[j][i] = 0.f;
+            }
+        }
+        const float mean = pivot + team_sum<LANES>(s, red).x * inv_n;
+        s.x = 0.f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const Columns<VE> c(lane + j * LANES, a.n);
+#pragma unroll
+            for (int i = 0; i < VE; ++i) {
+                v[j][i] -= mean;
+                s.x += i >= c.lo && i < c.hi ? v[j][i] * v[j][i] : 0.f;
+            }
+        }
+        const float rstd = 1.f / sqrtf(team_sum<LANES>(s, red).x * inv_n + a.eps);
+        if (!there) continue;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const Columns<VE> c(lane + j * LANES, a.n);
+            if (!c.hi) continue;
+            float gm[VE], bt[VE], o[VE];
+            load_param(a.gamma, c, 1.f, gm);
+            load_param(a.beta, c, 0.f, bt);
+#pragma unroll
+            for (int i = 0; i < VE; ++i) o[i] = v[j][i] * rstd * gm[i] + bt[i];
+            store_cols(y + row * a.ld_y, c, o);
+        }
+        if (lane == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+    }
+}
+
+template <class T, int LANES, int NV>
+__global__ __launch_bounds__(threads_of<LANES>()) void norm_bwd_kernel(NormArgs a) {
+    constexpr int VE = vec_of<T>(), TEAMS = threads_of<LANES>() / LANES;
+    __shared__ float2 red[LANES > 64 ? LANES / 64 : 1];
+    __shared__ float fold[TEAMS > 1 ? TEAMS : 1][TEAMS > 1 ? LANES * VE : 1];
+    const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
+    const float inv_n = 1.f / (float)a.n;
+    const T *x = (const T*)a.x, *g = (const T*)a.g;
+    T* gx = (T*)a.out;
+    float dg[NV][VE] = {}, db[NV][VE] = {};
+    for (long long r0 = (long long)blockIdx.x * TEAMS; r0 < a.rows; r0 += (long long)gridDim.x * TEAMS) {
+        const long long row = r0 + team;
+        const bool there = row < a.rows;
+        const float mean = there ? a.mean_in[row] : 0.f, rstd = there ? a.rstd_in[row] : 0.f;
+        float xh[NV][VE], gg[NV][VE];
+        float2 s = {0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const Columns<VE> c(lane + j * LANES, a.n);
+            if (there && c.hi) {
+                Pack<T, VE> px, pg;
+                load_cols(x + row * a.ld_x, c, px);
+                load_cols(g + row * a.ld_y, c, pg);
+                float gm[VE];
+                load_param(a.gamma, c, 1.f, gm);
+#pragma unroll
+                for (int i = 0; i < VE; ++i) {
+                    const bool mine = i >= c.lo && i < c.hi;
+                    xh[j][i] = (px.get(i) - mean) * rstd;
+                    const float gy = pg.get(i);
+                    gg[j][i] = gy * gm[i];
+                    dg[j][i] += mine ? gy * xh[j][i] : 0.f;
+                    db[j][i] += mine ? gy : 0.f;
+                    s.x += mine ? gg[j][i] : 0.f;
+                    s.y += mine ? gg[j][i] * xh[j][i] : 0.f;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < VE; ++i) xh[j][i] = gg[j][i] = 0.f;
+            }
+        }
+        s = team_sum<LANES>(s, red);
+        if (!there) continue;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const Columns<VE> c(lane + j * LANES, a.n);
+            if (!c.hi) continue;
+            float o[VE];
+#pragma unroll
+            for (int i = 0; i < VE; ++i) o[i] = rstd * (gg[j][i] - s.x * inv_n - xh[j][i] * (s.y * inv_n));
+            store_cols(gx + row * a.ld_x, c, o);
+        }
+    }
+    if (!a.part) return;
+    float* part = a.part + (long long)blockIdx.x * 2 * a.n;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const Columns<VE> c(lane + j * LANES, a.n);
+            float v[VE];
+#pragma unroll
+            for (int i = 0; i < VE; ++i) v[i] = k ? db[j][i] : dg[j][i];
+            if constexpr (TEAMS > 1) {
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < VE; ++i) fold[team][lane * VE + i] = v[i];
+                __syncthreads();
+                if (team == 0) {
+#pragma unroll
+                    for (int i = 0; i < VE; ++i)
+                        for (int t = 1; t < TEAMS; ++t) v[i] += fold[t][lane * VE + i];
+                }
+            }
+            if (team == 0) {
+#pragma unroll
+                for (int i = 0; i < VE; ++i)
+                    if (i >= c.lo && i < c.hi) part[k * a.n + c.col + i] = v[i];
+            }
+        }
+    }
+}
+
+// Column sums of n_part partial sums [n_part][2][n]; 32 columns and 32 groups of partials a workgroup.
+__global__ __launch_bounds__(1024) void norm_reduce_kernel(const float* __restrict__ part, int n_part, long long n, float* g_gamma,
+                                                           float* g_beta) {
+    __shared__ float red[32][33];
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+    const long long col = (long long)blockIdx.x * 32 + tx;
+    float s = 0.f;
+    if (col < 2 * n)
+        for (int w = ty; w < n_part; w += 32) s += part[(long long)w * 2 * n + col];
+    red[ty][tx] = s;
+    __syncthreads();
+    if (ty == 0 && col < 2 * n) {
+        for (int k = 1; k < 32; ++k) s += red[k][tx];
+        if (col < n) {
+            if (g_gamma) g_gamma[col] = s;
+        } else {
+            if (g_beta) g_beta[col - n] = s;
+        }
+    }
+}
+
+// ------------------------------------------------------------------ rows longer than the registers of a workgroup
+constexpr int kLongThreads = 1024;
+
+// One workgroup a row, the row read three times (from the cache after the first, up to its size).
+template <class T>
+__global__ __launch_bounds__(kLongThreads) void norm_fwd_long_kernel(NormArgs a) {
+    __shared__ float2 red[kLongThreads / 64];
+    const long long row = blockIdx.x;
+    const T* x = (const T*)a.x + row * a.ld_x;
+    T* y = (T*)a.out + row * a.ld_y;
+    const float inv_n = 1.f / (float)a.n;
+    float2 s = {0.f, 0.f};
+    const float pivot = to_f32(x[0]);
+    for (long long c = threadIdx.x; c < a.n; c += kLongThreads) s.x += to_f32(x[c]) - pivot;
+    const float mean = pivot + team_sum<kLongThreads>(s, red).x * inv_n;
+    s.x = 0.f;
+    for (long long c = threadIdx.x; c < a.n; c += kLongThreads) {
+        const float d = to_f32(x[c]) - mean;
+        s.x += d * d;
+    }
+    const float rstd = 1.f / sqrtf(team_sum<kLongThreads>(s, red).x * inv_n + a.eps);
+    for (long long c = threadIdx.x; c < a.n; c += kLongThreads)
+        put_f32(y + c, (to_f32(x[c]) - mean) * rstd * (a.gamma ? a.gamma[c] : 1.f) + (a.beta ? a.beta[c] : 0.f));
+    if (threadIdx.x == 0) {
+        if (a.mean) a.mean[row] = mean;
+        if (a.rstd) a.rstd[row] = rstd;
+    }
+}
+
+template <class T>
+__global__ __launch_bounds__(kLongThreads) void norm_bwd_long_kernel(NormArgs a) {
+    __shared__ float2 red[kLongThreads / 64];
+    const long long row = blockIdx.x;
+    const T *x = (const T*)a.x + row * a.ld_x, *g = (const T*)a.g + row * a.ld_y;
+    T* gx = (T*)a.out + row * a.ld_x;
+    const float inv_n = 1.f / (float)a.n, mean = a.mean_in[row], rstd = a.rstd_in[row];
+    float2 s = {0.f, 0.f};
+    for (long long c = threadIdx.x; c < a.n; c += kLongThreads) {
+        const float gg = to_f32(g[c]) * (a.gamma ? a.gamma[c] : 1.f);
+        s.x += gg;
+        s.y += gg * ((to_f32(x[c]) - mean) * rstd);
+    }
+    s = team_sum<kLongThreads>(s, red);
+    for (long long c = threadIdx.x; c < a.n; c += kLongThreads) {
+        const float gg = to_f32(g[c]) * (a.gamma ? a.gamma[c] : 1.f), xh = (to_f32(x[c]) - mean) * rstd;
+        put_f32(gx + c, rstd * (gg - s.x * inv_n - xh * (s.y * inv_n)));
+    }
+}
+
+// Partial sums over rows blockIdx.y, + gridDim.y, ...: one column a thread.  Runs before norm_bwd_long_kernel, whose output may
+// take the place of g.
+template <class T>
+__global__ __launch_bounds__(kNormThreads) void norm_cols_kernel(NormArgs a) {
+    const long long c = (long long)blockIdx.x * kNormThreads + threadIdx.x;
+    if (c >= a.n) return;
+    float dg = 0.f, db = 0.f;
+    for (long long row = blockIdx.y; row < a.rows; row += gridDim.y) {
+        const float g = to_f32(((const T*)a.g)[row * a.ld_y + c]);
+        dg += g * ((to_f32(((const T*)a.x)[row * a.ld_x + c]) - a.mean_in[row]) * a.rstd_in[row]);
+        db += g;
+    }
+    float* part = a.part + (long long)blockIdx.y * 2 * a.n;
+    part[c] = dg;
+    part[a.n + c] = db;
+}
+
+// ------------------------------------------------------------------ choice of the team
+// The smallest team whose lanes hold the row in one vector each, up to a wave; then more vectors a lane, then the workgroup.
+struct Team {
+    int lanes, nv;
+};
+Team team_for(const gleam_layer_norm_desc& d) {
+    const long long units = (d.n * (d.dtype ? 2 : 4) + 15) / 16;
+    for (Team t : {Team{4, 1}, Team{8, 1}, Team{16, 1}, Team{32, 1}, Team{64, 1}, Team{64, 2}, Team{64, 4}, Team{256, 2}, Team{256, 4},
+                   Team{1024, 2}})
+        if (units <= (long long)t.lanes * t.nv) return t;
+    return Team{0, 0};
+}
+int grid_for(const gleam_layer_norm_desc& d, Team t) {
+    const long long teams = t.lanes > 64 ? 1 : kNormThreads / t.lanes, wgs = (d.rows + teams - 1) / teams;
+    return (int)(wgs < kNormGrid ? wgs : kNormGrid);
+}
+int long_parts(const gleam_layer_norm_desc& d) { return (int)(d.rows < 64 ? d.rows : 64); }
+
+template <class T, class F>
+void with_team(Team t, F&& f) {
+#define GLEAM_TEAM(L, N) \
+    if (t.lanes == L && t.nv == N) return f(std::integral_constant<int, L>{}, std::integral_constant<int, N>{})
+    GLEAM_TEAM(4, 1);
+    GLEAM_TEAM(8, 1);
+    GLEAM_TEAM(16, 1);
+    GLEAM_TEAM(32, 1);
+    GLEAM_TEAM(64, 1);
+    GLEAM_TEAM(64, 2);
+    GLEAM_TEAM(64, 4);
+    GLEAM_TEAM(256, 2);
+    GLEAM_TEAM(256, 4);
+    GLEAM_TEAM(1024, 2);
+#undef GLEAM_TEAM
+}
+
+template <class T>
+hipError_t forward(const gleam_layer_norm_desc& d, const NormArgs& a, hipStream_t st) {
+    const Team t = team_for(d);
+    KernelScope ks("layer_norm_fwd", 7.0 * d.rows * d.n, 2.0 * sizeof(T) * d.rows * d.n, st);
+    if (!t.lanes) {
+        hipLaunchKernelGGL(norm_fwd_long_kernel<T>, dim3((unsigned)d.rows), dim3(kLongThreads), 0, st, a);
+        return hipGetLastError();
+    }
+    with_team<T>(t, [&](auto L, auto N) {
+        hipLaunchKernelGGL((norm_fwd_kernel<T, L(), N()>), dim3(grid_for(d, t)), dim3(threads_of<L()>()), 0, st, a);
+    });
+    return hipGetLastError();
+}
+
+template <class T>
+hipError_t backward(const gleam_layer_norm_desc& d, const NormArgs& a, float* g_gamma, float* g_beta, hipStream_t st) {
+    const Team t = team_for(d);
+    int parts;
+    if (!t.lanes) {
+        parts = long_parts(d);
+        if (a.part) {
+            KernelScope ks("layer_norm_cols", 4.0 * d.rows * d.n, 2.0 * sizeof(T) * d.rows * d.n, st);
+            hipLaunchKernelGGL(norm_cols_kernel<T>, dim3((unsigned)((d.n + kNormThreads - 1) / kNormThreads), parts), dim3(kNormThreads), 0, st, a);
+        }
+        KernelScope ks("layer_norm_bwd", 8.0 * d.rows * d.n, 3.0 * sizeof(T) * d.rows * d.n, st);
+        hipLaunchKernelGGL(norm_bwd_long_kernel<T>, dim3((unsigned)d.rows), dim3(kLongThreads), 0, st, a);
+    } else {
+        parts = grid_for(d, t);
+        KernelScope ks("layer_norm_bwd", 12.0 * d.rows * d.n, 3.0 * sizeof(T) * d.rows * d.n, st);
+        with_team<T>(t, [&](auto L, auto N) {
+            hipLaunchKernelGGL((norm_bwd_kernel<T, L(), N()>), dim3(parts), dim3(threads_of<L()>()), 0, st, a);
+        });
+    }
+    if (a.part) {
+        KernelScope ks("layer_norm_reduce", 2.0 * parts * d.n, 8.0 * parts * d.n, st);
+        hipLaunchKernelGGL(norm_reduce_kernel, dim3((unsigned)((2 * d.n + 31) / 32)), dim3(1024), 0, st, (const float*)a.part, parts,
+                           (long long)d.n, g_gamma, g_beta);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t layer_norm_forward(const gleam_layer_norm_desc& d, const void* x, const float* gamma, const float* beta, void* y, float* mean,
+                              float* rstd, hipStream_t st) {
+    NormArgs a{};
+    a.x = x;
+    a.gamma = gamma;
+    a.beta = beta;
+    a.out = y;
+    a.mean = mean;
+    a.rstd = rstd;
+    a.rows = d.rows;
+    a.n = d.n;
+    a.ld_x = d.ld_in;
+    a.ld_y = d.ld_out;
+    a.eps = d.eps;
+    return d.dtype ? forward<unsigned short>(d, a, st) : forward<float>(d, a, st);
+}
+
+size_t layer_norm_ws_bytes(const gleam_layer_norm_desc& d) {
+    const Team t = team_for(d);
+    return (size_t)(t.lanes ? grid_for(d, t) : long_parts(d)) * 2 * (size_t)d.n * sizeof(float);
+}
+
+hipError_t layer_norm_backward(const gleam_layer_norm_desc& d, const void* x, const float* gamma, const float* mean, const float* rstd,
+                               const void* g_y, void* g_x, float* g_gamma, float* g_beta, void* ws, hipStream_t st) {
+    NormArgs a{};
+    a.x = x;
+    a.g = g_y;
+    a.gamma = gamma;
+    a.mean_in = mean;
+    a.rstd_in = rstd;
+    a.out = g_x;
+    a.part = g_gamma || g_beta ? (float*)ws : nullptr;
+    a.rows = d.rows;
+    a.n = d.n;
+    a.ld_x = d.ld_in;
+    a.ld_y = d.ld_out;
+    return d.dtype ? backward<unsigned short>(d, a, g_gamma, g_beta, st) : backward<float>(d, a, g_gamma, g_beta, st);
+}
+
+}  // namespace gleam
