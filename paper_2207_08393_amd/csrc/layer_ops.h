@@ -33,20 +33,24 @@ struct MixTensor {
     int share;          // output heads that use one head of this tensor
     int d;              // width of a head
 };
-struct MixArgs {
+// One pass over all problems, see linattn.hip; a launch runs up to three of them side by side.
+struct MixRole {
     MixTensor q, k, v, o;
     void* out;
     int out_f32;                        // the output is float32 whatever the type of q, k, v
-    long long B, P, T;
-    int H;
-    const float* log_decay;             // [H]
-    const int* lengths;                 // [B] or null
-    const float* state_in;              // natural layout [B][P][H][dk][dv] of the layer, or null: zero
-    float* state_out;                   // or null
     int state_t;                        // this pass has the roles of dk and dv exchanged
     int reverse;                        // tokens from a sequence's end to its start
     float in_scale, out_scale;          // on k (x) v, and on what a query reads
-    float* seg_state;                   // states at the start of every segment, or null for one segment
+    const float* state_in;              // natural layout [B][P][H][dk][dv] of the layer, or null: zero
+    float* state_out;                   // or null
+    float* seg_state;                   // [problem][segment][D][D], rows dk: states at the segments' starts; or null for one segment
+};
+struct MixArgs {
+    MixRole role[3];
+    long long B, P, T;
+    int H, dk, dv;
+    const float* log_decay;             // [H]
+    const int* lengths;                 // [B] or null
     int n_seg, seg_chunks;
 };
 size_t linattn_fwd_ws_bytes(const gleam_linattn_desc& d);

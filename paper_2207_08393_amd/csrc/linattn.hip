@@ -35,6 +35,20 @@ __device__ __forceinline__ uint2 read_tr16(const unsigned short* p) {
     return __builtin_bit_cast(uint2, v);
 }
 
+// The first `left` of N values.
+template <class O, int N>
+__device__ __forceinline__ void store_part(O* p, int left, const float* v) {
+    if (left >= N) {
+        Pack<O, N> x;
+        x.set(v);
+        x.store(p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < left) put_f32(p + i, v[i]);
+    }
+}
+
 // Operands of a product over a block of kBlock values of the contracted index.  Lane l = 16 g + m holds row (column) m and the
 // kBlock/4 values from g kBlock/4 on, 16 bytes.  Results: column m, rows 4 g .. 4 g + 3 of a 16 x 16 tile.
 //   row_frag : from an LDS array whose rows are the operand's rows
@@ -58,7 +72,7 @@ struct Mma<unsigned short> {
         return __builtin_bit_cast(Frag, make_uint4(lo.x, lo.y, hi.x, hi.y));
     }
     // Parts whose sum is f times w: bfloat16 numbers w[i] f[i] rounded, what that left over rounded, and so on; 8 bits each.
-    static constexpr int kParts = 3, kStateParts = 2;
+    static constexpr int kStateParts = 2;
     static __device__ __forceinline__ void scaled(Frag f, const float* w, Frag* parts, int n) {
         const uint4 u = __builtin_bit_cast(uint4, f);
         const unsigned x[4] = {u.x, u.y, u.z, u.w};
@@ -92,6 +106,14 @@ struct Mma<unsigned short> {
         for (int i = 0; i < 8; ++i) v[i] = x[i >> 2][i & 3];
         split(v, parts, kStateParts);
     }
+    // a lane's results of tiles 0 and 1 of a 32-wide block, which are its elements 8 g .. 8 g + 7
+    template <class O>
+    static __device__ __forceinline__ void store(O* p, int left, int g, const floatx4* o) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = o[i >> 2][i & 3];
+        store_part<O, 8>(p + 8 * g, left - 8 * g, v);
+    }
     static __device__ __forceinline__ void put4(unsigned short* p, floatx4 v) {
         *(uint2*)p = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
     }
@@ -111,9 +133,17 @@ struct Mma<float> {
         const float* q = p + 4 * (lane >> 4) * stride + 16 * t + (lane & 15);
         return Frag{q[0], q[stride], q[2 * stride], q[3 * stride]};
     }
-    static constexpr int kParts = 1, kStateParts = 1;
+    static constexpr int kStateParts = 1;
     static __device__ __forceinline__ void scaled(Frag f, const float* w, Frag* parts, int) { parts[0] = Frag{f[0] * w[0], f[1] * w[1], f[2] * w[2], f[3] * w[3]}; }
     static __device__ __forceinline__ void pack(const floatx4* x, Frag* parts) { parts[0] = x[0]; }
+    template <class O>
+    static __device__ __forceinline__ void store(O* p, int left, int g, const floatx4* o) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const float v[4] = {o[u][0], o[u][1], o[u][2], o[u][3]};
+            store_part<O, 4>(p + 16 * u + 4 * g, left - 16 * u - 4 * g, v);
+        }
+    }
     static __device__ __forceinline__ void put4(float* p, floatx4 v) { *(floatx4*)p = v; }
 };
 
@@ -142,6 +172,58 @@ __device__ __forceinline__ void exchange() {
     }
 }
 
+// The elements [col, col + VE) of rows of d elements that exist.
+template <class T>
+struct Edge {
+    static constexpr int VE = 16 / (int)sizeof(T);
+    int at, back, d;     // where the vector is read, elements in front of those that are wanted, width
+    bool live, narrow;   // whether any exists; rows shorter than a vector go element by element
+    __device__ __forceinline__ Edge(int col, int width) {
+        d = width;
+        narrow = d < VE;
+        live = col < d;
+        back = live && col + VE > d && !narrow ? col + VE - d : 0;
+        at = live ? col - back : 0;
+    }
+    __device__ __forceinline__ void load(const T* row, Pack<T, VE>& x) const {
+        if (!narrow) {
+            x.load(row + at);
+        } else {
+            for (int i = 0; i < 4; ++i) x.w[i] = 0;
+            for (int e = d - 1; e >= 0; --e) {      // the element goes in front of those behind it
+                const T v = row[e];
+                if constexpr (sizeof(T) == 4) {
+                    x.w[2] = x.w[1];
+                    x.w[1] = x.w[0];
+                    x.w[0] = __float_as_uint(v);
+                } else {
+                    x.w[3] = x.w[3] << 16 | x.w[2] >> 16;
+                    x.w[2] = x.w[2] << 16 | x.w[1] >> 16;
+                    x.w[1] = x.w[1] << 16 | x.w[0] >> 16;
+                    x.w[0] = x.w[0] << 16 | v;
+                }
+            }
+        }
+    }
+    // zeros where nothing exists, the rest in its place
+    __device__ __forceinline__ Pack<T, VE> settle(Pack<T, VE> x, bool there) const {
+        if (d % VE && !narrow) {
+            unsigned long long lo = x.w[0] | (unsigned long long)x.w[1] << 32, hi = x.w[2] | (unsigned long long)x.w[3] << 32;
+            const int bits = 8 * (int)sizeof(T) * back, b = bits & 63;
+            const unsigned long long from_hi = b ? hi << (64 - b) : 0;
+            lo = bits >= 64 ? hi >> b : lo >> b | from_hi;
+            hi = bits >= 64 ? 0 : hi >> b;
+            x.w[0] = (unsigned)lo;
+            x.w[1] = (unsigned)(lo >> 32);
+            x.w[2] = (unsigned)hi;
+            x.w[3] = (unsigned)(hi >> 32);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x.w[i] = there && live ? x.w[i] : 0;
+        return x;
+    }
+};
+
 struct Problem {
     long long index;    // (b P + p) H + h
     long long b, p;
@@ -166,20 +248,19 @@ __device__ __forceinline__ const T* base_of(const MixTensor& x, const Problem& r
     return (const T*)x.p + r.b * x.s.b + r.p * x.s.p + (long long)(r.h / x.share) * x.s.h;
 }
 
-// State element (row of dk, column of dv in this pass's roles) in the natural layout of the layer.
-__device__ __forceinline__ long long state_at(const MixArgs& a, int row, int col) {
-    return a.state_t ? (long long)col * a.k.d + row : (long long)row * a.v.d + col;
-}
-
 // STATES: only the sum of k (x) v over segment blockIdx.y, for the scan over segments; seg_state slot blockIdx.y + 1.
-template <class T, int D, bool STATES>
-__global__ __launch_bounds__((Shape<T, D>::kThreads)) void mix_kernel(MixArgs a) {
+// PARTS: numbers a decayed value is the sum of on its way into the state (bfloat16: 3 give 24 bits, for a state that is handed out; 2
+// where the state only feeds outputs, which are rounded to 8 bits).
+template <class T, int D, bool STATES, int PARTS>
+__global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs args) {
+    const MixRole& a = args.role[blockIdx.z];
     typedef Shape<T, D> S;
     typedef Mma<T> M;
     typedef typename M::Frag Frag;
     constexpr int L = S::kL, VE = M::kVec, KB = M::kBlock, W = S::kWaves, NT = 64 * W;
     constexpr int NV = L * D / VE / NT;               // 16-byte vectors of an array a lane stages
     constexpr int kPair = KB / 16;                    // result tiles that make an operand
+    constexpr int kRows = L / 16;                     // row tiles of a chunk
     __shared__ __attribute__((aligned(16))) T lds_q[STATES ? 1 : S::kProblems][STATES ? 8 : L * S::kRow];
     __shared__ __attribute__((aligned(16))) T lds_k[S::kProblems][L * S::kRow];
     __shared__ __attribute__((aligned(16))) T lds_v[S::kProblems][L * S::kRow];
@@ -188,54 +269,52 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads)) void mix_kernel(MixArgs a)
     const int slot = S::kProblems == 1 ? 0 : threadIdx.x >> 6;
     const int tid = S::kProblems == 1 ? threadIdx.x : threadIdx.x & 63;
     const int lane = tid & 63, m = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
     const long long index = (long long)blockIdx.x * S::kProblems + slot;
-    if (index >= a.B * a.P * a.H) return;             // several problems a workgroup: a wave each, and no barriers
-    const Problem r = problem_of(a, index);
+    if (index >= args.B * args.P * args.H) return;             // several problems a workgroup: a wave each, and no barriers
+    const Problem r = problem_of(args, index);
     const int seg = blockIdx.y;
-    const long long r_begin = (long long)seg * a.seg_chunks * L;
-    const int c_begin = seg * a.seg_chunks;
+    const int c_begin = seg * args.seg_chunks;
     int c_end = (r.len + L - 1) / L;
-    if (c_end > c_begin + a.seg_chunks) c_end = c_begin + a.seg_chunks;
+    if (c_end > c_begin + args.seg_chunks) c_end = c_begin + args.seg_chunks;
+    const bool last_seg = (r.len > c_begin * L && c_end * L >= r.len) || (r.len == 0 && seg == 0);
     const int shift = a.reverse;
-    const float decay = a.log_decay[r.h];
+    const float decay = args.log_decay[r.h];
     T *sq = lds_q[STATES ? 0 : slot], *sk = lds_k[slot], *sv = lds_v[slot], *sp = lds_p[STATES ? 0 : slot];
     float* sw = lds_w[slot];
-    const T *gq = base_of<T>(a.q, r), *gk = base_of<T>(a.k, r), *gv = base_of<T>(a.v, r);
     for (int i = tid; i < L + 2; i += NT) sw[i] = decay_of(decay, i);
 
+    // tokens of the chunk from the first one on (or, in reverse, from the last one down)
+    const long long way = a.reverse ? -1 : 1, start = a.reverse ? r.len - 1 : 0;
     // staging: vectors tid + i NT of the chunk's rows
     const int col = tid % (D / VE) * VE, row0 = tid / (D / VE);
     constexpr int kRowStep = NT / (D / VE);
+    const T *gq = base_of<T>(a.q, r), *gk = base_of<T>(a.k, r), *gv = base_of<T>(a.v, r);
+    const long long sq_t = way * a.q.s.t, sk_t = way * a.k.s.t, sv_t = way * a.v.s.t;
+    gq += start * a.q.s.t;
+    gk += start * a.k.s.t;
+    gv += start * a.v.s.t;
+    // Loads always go to a token and a column that exist; what does not belong to the chunk becomes zero on the way into LDS, so that
+    // nothing waits for a load before it has to.  A row's last vector ends with the row and is moved into place there.
     Pack<T, VE> nq[NV], nk[NV], nv[NV];
-    auto fetch_one = [&](const T* base, const MixTensor& x, long long token, bool ok, Pack<T, VE>& p) {
-        if (ok && col + VE <= x.d) {
-            p.load(base + token * x.s.t + col);
-        } else {
-            float f[VE];
-#pragma unroll
-            for (int e = 0; e < VE; ++e) f[e] = ok && col + e < x.d ? to_f32(base[token * x.s.t + col + e]) : 0.f;
-            p.set(f);
-        }
-    };
+    const Edge<T> ek(col, a.k.d), ev(col, a.v.d);
     auto fetch = [&](int c) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int at = c * L + row0 + i * kRowStep;
-            const bool ok = at < r.len;
-            const long long token = a.reverse ? r.len - 1 - at : at;
-            if constexpr (!STATES) fetch_one(gq, a.q, token, ok, nq[i]);
-            fetch_one(gk, a.k, token, ok, nk[i]);
-            fetch_one(gv, a.v, token, ok, nv[i]);
+            int at = c * L + row0 + i * kRowStep;
+            at = at < r.len ? at : r.len - 1;
+            if constexpr (!STATES) ek.load(gq + at * sq_t, nq[i]);
+            ek.load(gk + at * sk_t, nk[i]);
+            ev.load(gv + at * sv_t, nv[i]);
         }
     };
-    auto stage = [&] {
+    auto stage = [&](int count) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int at = (row0 + i * kRowStep) * S::kRow + col;
-            if constexpr (!STATES) nq[i].store_lds(sq + at);
-            nk[i].store_lds(sk + at);
-            nv[i].store_lds(sv + at);
+            const int row = row0 + i * kRowStep, at = row * S::kRow + col;
+            if constexpr (!STATES) ek.settle(nq[i], row < count).store_lds(sq + at);
+            ek.settle(nk[i], row < count).store_lds(sk + at);
+            ev.settle(nv[i], row < count).store_lds(sv + at);
         }
     };
 
@@ -243,10 +322,8 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads)) void mix_kernel(MixArgs a)
     bool have = false;                                // it is not zero
 #pragma unroll
     for (int t = 0; t < S::kTiles; ++t) x[t][0] = x[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
-    auto seg_slot = [&](int s) {
-        return (floatx4*)a.seg_state + (((r.index * a.n_seg + s) * W + wave) * S::kTiles * 2) * 64 + lane;
-    };
-    auto for_state = [&](auto&& f) {                  // f(t, u, i, natural offset) for this lane's elements that exist
+    // f(tile t, u, number i, offset in the layer's [rows dk][columns dv]) of every element of the lane; pitch: elements of a row
+    auto for_state = [&](int pitch, auto&& f) {
 #pragma unroll
         for (int t = 0; t < S::kTiles; ++t)
 #pragma unroll
@@ -254,27 +331,39 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads)) void mix_kernel(MixArgs a)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int row = M::tile(t, 4 * g + i), c = 32 * wave + M::tile(u, m);
-                    if (row < a.k.d && c < a.v.d) f(t, u, i, r.index * a.k.d * a.v.d + state_at(a, row, c));
+                    f(t, u, i, row < a.k.d && c < a.v.d, a.state_t ? c * pitch + row : row * pitch + c);
                 }
     };
+    const long long state_base = r.index * args.dk * args.dv;
+    auto segment = [&](int s) { return a.seg_state + (r.index * args.n_seg + s) * S::kStateFloats; };
+    if (c_begin < c_end) fetch(c_begin);
     if constexpr (!STATES) {
         if (a.seg_state) {
-            const floatx4* s = seg_slot(seg);
-#pragma unroll
-            for (int t = 0; t < S::kTiles; ++t)
-#pragma unroll
-                for (int u = 0; u < 2; ++u) x[t][u] = s[(t * 2 + u) * 64];
-            have = true;
+            const float* s = segment(seg);
+            for_state(D, [&](int t, int u, int i, bool, int at) { x[t][u][i] = s[at]; });
+            have = seg > 0 || a.state_in;
         } else if (a.state_in) {
-            for_state([&](int t, int u, int i, long long at) { x[t][u][i] = a.state_in[at]; });
+            for_state(args.dv, [&](int t, int u, int i, bool there, int at) {
+                if (there) x[t][u][i] = a.state_in[state_base + at];
+            });
             have = true;
         }
     }
-    if (c_begin < c_end) fetch(c_begin);
+    // decays between a row and a column of scores whose tiles are n apart (0 where the column is the later one), and with scale
+    floatx4 wt[STATES ? 1 : kRows];
+    if constexpr (!STATES) {
+#pragma unroll
+        for (int n = 0; n < kRows; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int apart = 16 * n + m - 4 * g - i;
+                wt[n][i] = apart < 0 ? 0.f : a.in_scale * a.out_scale * decay_of(decay, apart);
+            }
+    }
     for (int c = c_begin; c < c_end; ++c) {
         const int left = r.len - c * L, count = left < L ? left : L;
         exchange<W>();                                // everyone is done with the chunk before
-        stage();
+        stage(count);
         exchange<W>();
         if (c + 1 < c_end) fetch(c + 1);
         Frag vf[L / KB][2];
@@ -283,73 +372,74 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads)) void mix_kernel(MixArgs a)
 #pragma unroll
             for (int u = 0; u < 2; ++u) vf[s][u] = M::col_frag(sv + s * KB * S::kRow, S::kRow, 2 * wave + u, lane);
         if constexpr (!STATES) {
-            // scores of rows it (mod waves): the lane has four consecutive columns j of row i
-            for (int it = wave; it < L / 16; it += W) {
-                if (it * 16 >= count) break;
-                Frag qf[D / KB];
+            // scores of rows `it`: the lane has four consecutive columns of row m of the tile
 #pragma unroll
-                for (int s = 0; s < D / KB; ++s) qf[s] = M::row_frag(sq + (16 * it + m) * S::kRow + s * KB + g * VE);
-                const int last = (it * 16 / KB + 1) * (KB / 16);    // tiles up to the end of the diagonal's block
-                for (int jt = 0; jt < last; ++jt) {
-                    floatx4 p{0.f, 0.f, 0.f, 0.f};
-                    if (jt <= it) {
+            for (int rr = 0; rr < (kRows + W - 1) / W; ++rr) {
+                const int it = wave + rr * W;
+                if (it < kRows && it * 16 < count) {
+                    Frag qf[D / KB];
+#pragma unroll
+                    for (int s = 0; s < D / KB; ++s) qf[s] = M::row_frag(sq + (16 * it + m) * S::kRow + s * KB + g * VE);
+#pragma unroll
+                    for (int n = 0; n < kRows; ++n) {
+                        if (n >= rr * W + W) continue;            // n <= it, whatever the wave
+                        const int jt = it > n ? it - n : 0;
+                        floatx4 p{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                         for (int s = 0; s < D / KB; ++s) p = M::mma(M::row_frag(sk + (16 * jt + m) * S::kRow + s * KB + g * VE), qf[s], p);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) p[i] = wt[n][i] != 0.f ? p[i] * wt[n][i] : 0.f;
+                        if (n <= it) M::put4(sp + (16 * it + m) * S::kScoreRow + 16 * jt + 4 * g, p);
+                    }
+                    if (kPair == 2 && !(it & 1)) M::put4(sp + (16 * it + m) * S::kScoreRow + 16 * (it + 1) + 4 * g, floatx4{0.f, 0.f, 0.f, 0.f});
+                }
+            }
+            // what the queries read of the state; needs no scores, so it stands in front of their exchange
+            floatx4 o[kRows][2] = {};
+            if (have) {
+#pragma unroll
+                for (int s = 0; s < D / KB; ++s) {
+                    Frag xf[2][M::kStateParts];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const floatx4 both[2] = {x[kPair * s][u], x[kPair * s + kPair - 1][u]};
+                        M::pack(both, xf[u]);
                     }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int n = 16 * (it - jt) + m - 4 * g - i;
-                        p[i] = n >= 0 ? p[i] * (a.in_scale * a.out_scale * sw[n < 0 ? 0 : n]) : 0.f;
+                    for (int it = 0; it < kRows; ++it) {
+                        const Frag qf = M::row_frag(sq + (16 * it + m) * S::kRow + s * KB + g * VE);
+#pragma unroll
+                        for (int n = 0; n < M::kStateParts; ++n)
+#pragma unroll
+                            for (int u = 0; u < 2; ++u) o[it][u] = M::mma(xf[u][n], qf, o[it][u]);
                     }
-                    M::put4(sp + (16 * it + m) * S::kScoreRow + 16 * jt + 4 * g, p);
+                }
+#pragma unroll
+                for (int it = 0; it < kRows; ++it) {
+                    const float f = a.out_scale * sw[16 * it + m + 1 - shift];
+                    o[it][0] *= f;
+                    o[it][1] *= f;
                 }
             }
             exchange<W>();
-            for (int it = 0; it * 16 < count; ++it) {
-                floatx4 o[2] = {};
-                if (have) {
+            long long at = r.b * a.o.s.b + r.p * a.o.s.p + (long long)(r.h / a.o.share) * a.o.s.h + (start + way * ((long long)c * L + m)) * a.o.s.t + 32 * wave;
 #pragma unroll
-                    for (int s = 0; s < D / KB; ++s) {
-                        const Frag qf = M::row_frag(sq + (16 * it + m) * S::kRow + s * KB + g * VE);
+            for (int it = 0; it < kRows; ++it, at += way * 16 * a.o.s.t) {
+                if (it * 16 >= count) break;
 #pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            const floatx4 both[2] = {x[kPair * s][u], x[kPair * s + kPair - 1][u]};
-                            Frag part[M::kStateParts];
-                            M::pack(both, part);
-#pragma unroll
-                            for (int n = 0; n < M::kStateParts; ++n) o[u] = M::mma(part[n], qf, o[u]);
-                        }
-                    }
-                    const float f = a.out_scale * sw[16 * it + m + 1 - shift];
-                    o[0] *= f;
-                    o[1] *= f;
-                }
-                const int last = it * 16 / KB;
-#pragma unroll
-                for (int s = 0; s < L / KB; ++s) {
-                    if (s > last) break;
+                for (int s = 0; s <= it * 16 / KB; ++s) {
                     const Frag pf = M::row_frag(sp + (16 * it + m) * S::kScoreRow + s * KB + g * VE);
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) o[u] = M::mma(vf[s][u], pf, o[u]);
+                    for (int u = 0; u < 2; ++u) o[it][u] = M::mma(vf[s][u], pf, o[it][u]);
                 }
-                const int i = 16 * it + m;
-                if (i < count) {
-                    const long long token = a.reverse ? r.len - 1 - (c * L + i) : c * L + i;
-                    const long long at = r.b * a.o.s.b + token * a.o.s.t + r.p * a.o.s.p + (long long)(r.h / a.o.share) * a.o.s.h;
-#pragma unroll
-                    for (int u = 0; u < 2; ++u)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int cc = 32 * wave + M::tile(u, 4 * g + e);
-                            if (cc < a.o.d) {
-                                if (a.out_f32) ((float*)a.out)[at + cc] = o[u][e];
-                                else put_f32((T*)a.out + at + cc, o[u][e]);
-                            }
-                        }
+                if (16 * it + m < count) {
+                    if (a.out_f32) M::store((float*)a.out + at, a.o.d - 32 * wave, g, o[it]);
+                    else M::store((T*)a.out + at, a.o.d - 32 * wave, g, o[it]);
                 }
             }
         }
-        // the state: decay over the chunk, then k (x) v with each token's decay to its end
+        // the state: decay over the chunk, then k (x) v with each token's decay to its end; not where nothing reads it
+        if (!STATES && c + 1 == c_end && !(a.state_out && last_seg)) break;
         const float whole = sw[count];
 #pragma unroll
         for (int t = 0; t < S::kTiles; ++t) {
@@ -365,14 +455,14 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads)) void mix_kernel(MixArgs a)
                 const int j = s * KB + g * VE + e;
                 w[e] = j < count ? a.in_scale * sw[count - 1 - j + shift] : 0.f;
             }
-            Frag part[2][M::kParts];
+            Frag part[2][PARTS];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) M::scaled(vf[s][u], w, part[u], M::kParts);
+            for (int u = 0; u < 2; ++u) M::scaled(vf[s][u], w, part[u], PARTS);
 #pragma unroll
             for (int t = 0; t < S::kTiles; ++t) {
                 const Frag kf = M::col_frag(sk + s * KB * S::kRow, S::kRow, t, lane);
 #pragma unroll
-                for (int n = 0; n < M::kParts; ++n)
+                for (int n = 0; n < PARTS; ++n)
 #pragma unroll
                     for (int u = 0; u < 2; ++u) x[t][u] = M::mma(kf, part[u][n], x[t][u]);
             }
@@ -380,51 +470,48 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads)) void mix_kernel(MixArgs a)
         have = true;
     }
     if constexpr (STATES) {
-        floatx4* s = seg_slot(seg + 1);
-#pragma unroll
-        for (int t = 0; t < S::kTiles; ++t)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) s[(t * 2 + u) * 64] = x[t][u];
+        float* s = segment(seg + 1);
+        for_state(D, [&](int t, int u, int i, bool, int at) { s[at] = x[t][u][i]; });
         return;
     }
     // zeros behind the end of the sequence, in this segment's range of tokens
-    long long r_end = r_begin + (long long)a.seg_chunks * L;
-    if (r_end > a.T) r_end = a.T;
+    const long long r_begin = (long long)c_begin * L;
+    long long r_end = r_begin + (long long)args.seg_chunks * L;
+    if (r_end > args.T) r_end = args.T;
     static_assert(NT % D == 0, "a thread keeps its column");
     for (long long t = (r_begin > r.len ? r_begin : r.len) + tid / D; t < r_end && tid % D < a.o.d; t += NT / D) {
         const long long at = r.b * a.o.s.b + t * a.o.s.t + r.p * a.o.s.p + (long long)(r.h / a.o.share) * a.o.s.h + tid % D;
         if (a.out_f32) ((float*)a.out)[at] = 0.f;
         else put_f32((T*)a.out + at, 0.f);
     }
-    if (a.state_out && ((r.len > r_begin && c_end * (long long)L >= r.len) || (r.len == 0 && seg == 0)))
-        for_state([&](int t, int u, int i, long long at) { a.state_out[at] = x[t][u][i]; });
+    if (a.state_out && last_seg)
+        for_state(args.dv, [&](int t, int u, int i, bool there, int at) {
+            if (there) a.state_out[state_base + at] = x[t][u][i];
+        });
 }
 
 // States at the start of every segment from the sums of the segments: X_{s+1} = e^{a n} X_s + sum_s, n tokens a segment.  A thread
 // has four elements; slot 0 is the state that comes in.
-template <class T, int D>
-__global__ __launch_bounds__(256) void mix_scan_kernel(MixArgs a) {
-    typedef Shape<T, D> S;
-    typedef Mma<T> M;
-    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
-    const long long index = at / (S::kStateFloats / 4);
-    if (index >= a.B * a.P * a.H) return;
-    const int e = (int)(at % (S::kStateFloats / 4));
-    const int lane = e & 63, u = (e >> 6) & 1, t = (e >> 7) % S::kTiles, wave = (e >> 7) / S::kTiles;
+template <int D>
+__global__ __launch_bounds__(256) void mix_scan_kernel(MixArgs args, int chunk) {
+    const MixRole& a = args.role[blockIdx.z];
+    constexpr int kQuads = D * D / 4;
+    const long long at = (long long)blockIdx.x * 256 + threadIdx.x, index = at / kQuads;
+    if (index >= args.B * args.P * args.H) return;
+    const int e = (int)(at % kQuads), row = 4 * e / D, col = 4 * e % D;
     floatx4 x{0.f, 0.f, 0.f, 0.f};
     if (a.state_in) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = M::tile(t, 4 * (lane >> 4) + i), c = 32 * wave + M::tile(u, lane & 15);
-            if (row < a.k.d && c < a.v.d) x[i] = a.state_in[index * a.k.d * a.v.d + state_at(a, row, c)];
-        }
+        for (int i = 0; i < 4; ++i)
+            if (row < args.dk && col + i < args.dv) x[i] = a.state_in[(index * args.dk + row) * args.dv + col + i];
     }
-    const float whole = decay_of(a.log_decay[index % a.H], a.seg_chunks * S::kL);
-    floatx4* s = (floatx4*)a.seg_state + index * a.n_seg * (S::kStateFloats / 4) + e;
+    const float whole = decay_of(args.log_decay[index % args.H], args.seg_chunks * chunk);
+    floatx4* s = (floatx4*)a.seg_state + index * args.n_seg * kQuads + e;
     s[0] = x;
-    for (int k = 1; k < a.n_seg; ++k) {
-        x = x * whole + s[(long long)k * (S::kStateFloats / 4)];
-        s[(long long)k * (S::kStateFloats / 4)] = x;
+#pragma unroll 8
+    for (int k = 1; k < args.n_seg; ++k) {
+        x = x * whole + s[(long long)k * kQuads];
+        s[(long long)k * kQuads] = x;
     }
 }
 
@@ -448,9 +535,10 @@ __global__ __launch_bounds__(256) void mix_share_kernel(const float* __restrict_
 // One token: S' = e^a S + k v^T, o = scale q S'.  A workgroup has a problem; a thread has column c of dv and every R-th row.
 constexpr int kStepThreads = 256;
 template <class T>
-__global__ __launch_bounds__(kStepThreads) void mix_step_kernel(MixArgs a) {
+__global__ __launch_bounds__(kStepThreads) void mix_step_kernel(MixArgs args) {
+    const MixRole& a = args.role[0];
     __shared__ float sq[128], sk[128], red[kStepThreads];
-    const Problem r = problem_of(a, blockIdx.x);
+    const Problem r = problem_of(args, blockIdx.x);
     const T *gq = base_of<T>(a.q, r), *gk = base_of<T>(a.k, r), *gv = base_of<T>(a.v, r);
     const int tid = threadIdx.x, dk = a.k.d, dv = a.v.d;
     const bool live = r.len > 0;
@@ -460,7 +548,7 @@ __global__ __launch_bounds__(kStepThreads) void mix_step_kernel(MixArgs a) {
     }
     __syncthreads();
     const int width = dv <= 32 ? 32 : dv <= 64 ? 64 : 128, c = tid % width, rows = kStepThreads / width;
-    const float whole = live ? decay_of(a.log_decay[r.h], 1) : 1.f, v = c < dv && live ? to_f32(gv[c]) : 0.f;
+    const float whole = live ? decay_of(args.log_decay[r.h], 1) : 1.f, v = c < dv && live ? to_f32(gv[c]) : 0.f;
     const long long base = r.index * dk * dv;
     float o = 0.f;
     if (c < dv)
@@ -483,169 +571,171 @@ int width_of(int dk, int dv) {
     const int d = dk > dv ? dk : dv;
     return d <= 32 ? 32 : d <= 64 ? 64 : 128;
 }
-// Segments of a pass: enough workgroups to fill the chip where there are few problems.
+// Segments of a call of `roles` passes: enough workgroups to fill the chip where there are few problems.
 struct Split {
     int n_seg, chunks;
 };
-Split split_of(const gleam_linattn_desc& d) {
+Split split_of(const gleam_linattn_desc& d, int roles) {
     const int D = width_of(d.dk, d.dv), L = d.dtype && D > 32 ? 64 : 32;
     const long long problems = d.B * d.P * d.heads, groups = D == 32 ? (problems + 3) / 4 : problems, chunks = (d.T + L - 1) / L;
-    long long n = 1024 / groups;
-    if (n > chunks / 4) n = chunks / 4;
+    long long n = 1024 / (groups * roles);
+    if (n > chunks / 2) n = chunks / 2;
     if (n < 2) return {1, (int)chunks};
     const long long per = (chunks + n - 1) / n;
     return {(int)((chunks + per - 1) / per), (int)per};
 }
-size_t seg_bytes(const gleam_linattn_desc& d) {
-    const Split s = split_of(d);
+size_t seg_bytes(const gleam_linattn_desc& d, int roles) {
+    const Split s = split_of(d, roles);
     const size_t D = width_of(d.dk, d.dv);
     return s.n_seg < 2 ? 0 : align_up((size_t)(d.B * d.P * d.heads) * s.n_seg * D * D * sizeof(float));
 }
-size_t share_bytes(const gleam_linattn_desc& d) {   // float32 gradients of the widest array whose heads are shared
-    size_t w = 0;
-    if (d.q_heads < d.heads || d.k_heads < d.heads) w = d.dk;
-    if (d.v_heads < d.heads && (size_t)d.dv > w) w = d.dv;
-    return align_up((size_t)(d.B * d.T * d.P * d.heads) * w * sizeof(float));
+// float32 gradients of all output heads of an array whose heads are shared
+size_t share_bytes(const gleam_linattn_desc& d, int heads, int width) {
+    return heads == d.heads ? 0 : align_up((size_t)(d.B * d.T * d.P * d.heads) * width * sizeof(float));
 }
 
-template <class T, int D>
-hipError_t mix_pass(MixArgs& a, const char* name, hipStream_t st) {
+// `roles` passes side by side; `states` of them first, over segments, where there are several.
+template <class T, int D, int PARTS>
+hipError_t mix_passes(const MixArgs& a, int roles, const MixArgs& states, int n_states, const char* name, hipStream_t st) {
     typedef Shape<T, D> S;
     const long long problems = a.B * a.P * a.H;
     const unsigned groups = (unsigned)((problems + S::kProblems - 1) / S::kProblems);
-    const double tokens = (double)problems * a.T;
-    const double state_flops = 2.0 * a.k.d * a.v.d, bytes = sizeof(T);
+    const double tokens = (double)problems * a.T, flops = 2.0 * tokens * a.dk * a.dv, bytes = tokens * sizeof(T) * (a.dk + a.dv);
     if (a.n_seg > 1) {
         {
-            KernelScope ks("linattn_segments", tokens * state_flops, tokens * bytes * (a.k.d + a.v.d), st);
-            hipLaunchKernelGGL((mix_kernel<T, D, true>), dim3(groups, a.n_seg - 1), dim3(S::kThreads), 0, st, a);
+            KernelScope ks("linattn_segments", n_states * flops, n_states * bytes, st);
+            hipLaunchKernelGGL((mix_kernel<T, D, true, PARTS>), dim3(groups, a.n_seg - 1, n_states), dim3(S::kThreads), 0, st, states);
         }
-        const double floats = (double)problems * a.n_seg * S::kStateFloats;
+        const double floats = (double)n_states * problems * a.n_seg * S::kStateFloats;
         KernelScope ks("linattn_scan", 2.0 * floats, 8.0 * floats, st);
-        hipLaunchKernelGGL((mix_scan_kernel<T, D>), dim3((unsigned)((problems * (S::kStateFloats / 4) + 255) / 256)), dim3(256), 0, st, a);
-    } else {
-        a.seg_state = nullptr;
+        const unsigned blocks = (unsigned)((problems * (S::kStateFloats / 4) + 255) / 256);
+        hipLaunchKernelGGL(mix_scan_kernel<D>, dim3(blocks, 1, n_states), dim3(256), 0, st, states, S::kL);
     }
-    KernelScope ks(name, tokens * 2.0 * state_flops, tokens * bytes * (a.q.d + a.k.d + a.v.d + a.o.d), st);
-    hipLaunchKernelGGL((mix_kernel<T, D, false>), dim3(groups, a.n_seg), dim3(S::kThreads), 0, st, a);
+    KernelScope ks(name, roles * 2.0 * flops, roles * 2.0 * bytes, st);
+    hipLaunchKernelGGL((mix_kernel<T, D, false, PARTS>), dim3(groups, a.n_seg, roles), dim3(S::kThreads), 0, st, a);
     return hipGetLastError();
 }
-template <class T>
-hipError_t mix_any(MixArgs& a, const char* name, hipStream_t st) {
-    switch (width_of(a.k.d, a.v.d)) {
-        case 32: return mix_pass<T, 32>(a, name, st);
-        case 64: return mix_pass<T, 64>(a, name, st);
-        default: return mix_pass<T, 128>(a, name, st);
-    }
+template <class T, int D>
+hipError_t mix_parts(const MixArgs& a, int roles, const MixArgs& states, int n_states, bool state_out, const char* name, hipStream_t st) {
+    if constexpr (sizeof(T) == 4) return mix_passes<T, D, 1>(a, roles, states, n_states, name, st);
+    else return state_out ? mix_passes<T, D, 3>(a, roles, states, n_states, name, st) : mix_passes<T, D, 2>(a, roles, states, n_states, name, st);
 }
-hipError_t mix(const gleam_linattn_desc& d, MixArgs& a, const char* name, hipStream_t st) {
-    return d.dtype ? mix_any<unsigned short>(a, name, st) : mix_any<float>(a, name, st);
+template <class T>
+hipError_t mix_any(const MixArgs& a, int roles, const MixArgs& states, int n_states, bool state_out, const char* name, hipStream_t st) {
+    switch (width_of(a.dk, a.dv)) {
+        case 32: return mix_parts<T, 32>(a, roles, states, n_states, state_out, name, st);
+        case 64: return mix_parts<T, 64>(a, roles, states, n_states, state_out, name, st);
+        default: return mix_parts<T, 128>(a, roles, states, n_states, state_out, name, st);
+    }
 }
 
 gleam_seq_strides row_major(const gleam_linattn_desc& d, int heads, int width) {
     return {d.T * d.P * heads * width, d.P * heads * width, (int64_t)heads * width, width};
 }
-MixArgs common(const gleam_linattn_desc& d, const float* log_decay, const int* lengths, void* ws) {
+MixArgs common(const gleam_linattn_desc& d, int roles, const float* log_decay, const int* lengths) {
     MixArgs a{};
     a.B = d.B;
     a.P = d.P;
     a.T = d.T;
     a.H = d.heads;
+    a.dk = d.dk;
+    a.dv = d.dv;
     a.log_decay = log_decay;
     a.lengths = lengths;
-    a.seg_state = (float*)ws;
-    const Split s = split_of(d);
+    const Split s = split_of(d, roles);
     a.n_seg = s.n_seg;
     a.seg_chunks = s.chunks;
     return a;
 }
+MixRole role_of(const MixTensor& q, const MixTensor& k, const MixTensor& v, int state_t, int reverse, float in_scale, float out_scale,
+                const float* state_in, float* seg_state) {
+    MixRole r{};
+    r.q = q;
+    r.k = k;
+    r.v = v;
+    r.state_t = state_t;
+    r.reverse = reverse;
+    r.in_scale = in_scale;
+    r.out_scale = out_scale;
+    r.state_in = state_in;
+    r.seg_state = seg_state;
+    return r;
+}
 
 }  // namespace
 
-size_t linattn_fwd_ws_bytes(const gleam_linattn_desc& d) { return d.T == 1 ? 0 : seg_bytes(d); }
-size_t linattn_bwd_ws_bytes(const gleam_linattn_desc& d) { return seg_bytes(d) + share_bytes(d); }
+size_t linattn_fwd_ws_bytes(const gleam_linattn_desc& d) { return d.T == 1 ? 0 : seg_bytes(d, 1); }
+size_t linattn_bwd_ws_bytes(const gleam_linattn_desc& d) {
+    return 2 * seg_bytes(d, 3) + share_bytes(d, d.q_heads, d.dk) + share_bytes(d, d.k_heads, d.dk) + share_bytes(d, d.v_heads, d.dv);
+}
 
 hipError_t linattn_forward(const gleam_linattn_desc& d, const void* q, const void* k, const void* v, const float* log_decay,
                            const int* lengths, const float* state_in, void* o, float* state_out, void* ws, hipStream_t st) {
-    MixArgs a = common(d, log_decay, lengths, ws);
-    a.q = {q, d.q, d.heads / d.q_heads, d.dk};
-    a.k = {k, d.k, d.heads / d.k_heads, d.dk};
-    a.v = {v, d.v, d.heads / d.v_heads, d.dv};
-    a.o = {nullptr, d.o, 1, d.dv};
-    a.out = o;
-    a.state_in = state_in;
-    a.state_out = state_out;
-    a.in_scale = 1.f;
-    a.out_scale = d.scale;
+    const MixTensor tq = {q, d.q, d.heads / d.q_heads, d.dk}, tk = {k, d.k, d.heads / d.k_heads, d.dk}, tv = {v, d.v, d.heads / d.v_heads, d.dv};
+    MixArgs a = common(d, 1, log_decay, lengths), states = a;
+    float* seg = a.n_seg > 1 ? (float*)ws : nullptr;
+    a.role[0] = role_of(tq, tk, tv, 0, 0, 1.f, d.scale, state_in, seg);
+    a.role[0].o = {nullptr, d.o, 1, d.dv};
+    a.role[0].out = o;
+    a.role[0].state_out = state_out;
     if (d.T == 1) {
-        const double states = (double)d.B * d.P * d.heads * d.dk * d.dv;
-        KernelScope ks("linattn_step", 4.0 * states, 8.0 * states, st);
+        const double floats = (double)d.B * d.P * d.heads * d.dk * d.dv;
+        KernelScope ks("linattn_step", 4.0 * floats, 8.0 * floats, st);
         const dim3 grid((unsigned)(d.B * d.P * d.heads));
         if (d.dtype) hipLaunchKernelGGL(mix_step_kernel<unsigned short>, grid, dim3(kStepThreads), 0, st, a);
         else hipLaunchKernelGGL(mix_step_kernel<float>, grid, dim3(kStepThreads), 0, st, a);
         return hipGetLastError();
     }
-    return mix(d, a, "linattn_fwd", st);
+    states.role[0] = role_of(tq, tv, tk, 1, 0, 1.f, 1.f, state_in, seg);
+    return d.dtype ? mix_any<unsigned short>(a, 1, states, 1, state_out, "linattn_fwd", st)
+                   : mix_any<float>(a, 1, states, 1, state_out, "linattn_fwd", st);
 }
 
 hipError_t linattn_backward(const gleam_linattn_desc& d, const void* q, const void* k, const void* v, const float* log_decay,
                             const int* lengths, const float* state_in, const void* g_o, const float* g_state_out, void* g_q, void* g_k,
                             void* g_v, float* g_state_in, void* ws, hipStream_t st) {
-    const MixTensor tq = {q, d.q, d.heads / d.q_heads, d.dk};
-    const MixTensor tk = {k, d.k, d.heads / d.k_heads, d.dk};
-    const MixTensor tv = {v, d.v, d.heads / d.v_heads, d.dv};
+    const MixTensor tq = {q, d.q, d.heads / d.q_heads, d.dk}, tk = {k, d.k, d.heads / d.k_heads, d.dk}, tv = {v, d.v, d.heads / d.v_heads, d.dv};
     const MixTensor tg = {g_o, d.o, 1, d.dv};
-    float* part = (float*)((unsigned char*)ws + seg_bytes(d));
-    // one pass into `out` of the layout of x, by way of a float32 array of all output heads where heads are shared
-    auto pass = [&](MixArgs& a, const MixTensor& x, void* out, const char* name) {
-        a.o = x;
-        a.out = out;
-        if (x.share > 1) {
-            a.o.s = row_major(d, d.heads, x.d);
-            a.o.share = 1;
-            a.out = part;
-            a.out_f32 = 1;
+    MixArgs a = common(d, 3, log_decay, lengths), states = a;
+    unsigned char* at = (unsigned char*)ws;
+    float* seg_s = a.n_seg > 1 ? (float*)at : nullptr;               // states of the forward pass
+    at += seg_bytes(d, 3);
+    float* seg_g = a.n_seg > 1 ? (float*)at : nullptr;               // their gradients
+    at += seg_bytes(d, 3);
+    a.role[0] = role_of(tg, tv, tk, 1, 0, 1.f, d.scale, state_in, seg_s);
+    a.role[1] = role_of(tv, tg, tq, 1, 1, d.scale, 1.f, g_state_out, seg_g);
+    a.role[2] = role_of(tk, tq, tg, 0, 1, d.scale, 1.f, g_state_out, seg_g);
+    a.role[2].state_out = g_state_in;
+    states.role[0] = role_of(tg, tv, tk, 1, 0, 1.f, 1.f, state_in, seg_s);
+    states.role[1] = role_of(tv, tg, tq, 1, 1, d.scale, 1.f, g_state_out, seg_g);
+    const MixTensor* of[3] = {&tq, &tk, &tv};
+    void* out[3] = {g_q, g_k, g_v};
+    float* part[3] = {};
+    for (int i = 0; i < 3; ++i) {
+        const MixTensor& x = *of[i];
+        a.role[i].o = x;
+        a.role[i].out = out[i];
+        if (x.share > 1) {                                           // by way of a float32 array of all output heads
+            part[i] = (float*)at;
+            at += share_bytes(d, d.heads / x.share, x.d);
+            a.role[i].o = {nullptr, row_major(d, d.heads, x.d), 1, x.d};
+            a.role[i].out = part[i];
+            a.role[i].out_f32 = 1;
         }
-        hipError_t e = mix(d, a, name, st);
-        if (e != hipSuccess || x.share == 1) return e;
+    }
+    hipError_t e = d.dtype ? mix_any<unsigned short>(a, 3, states, 2, g_state_in, "linattn_bwd", st)
+                           : mix_any<float>(a, 3, states, 2, g_state_in, "linattn_bwd", st);
+    for (int i = 0; i < 3 && e == hipSuccess; ++i) {
+        if (!part[i]) continue;
+        const MixTensor& x = *of[i];
         const long long n = d.B * d.T * d.P * (d.heads / x.share) * x.d;
         KernelScope ks("linattn_share", (double)n * x.share, 4.0 * n * x.share + (d.dtype ? 2.0 : 4.0) * n, st);
         const dim3 grid((unsigned)((n + 255) / 256));
-        if (d.dtype) hipLaunchKernelGGL(mix_share_kernel<unsigned short>, grid, dim3(256), 0, st, (const float*)part, x, out, d.T, d.P, d.heads, n);
-        else hipLaunchKernelGGL(mix_share_kernel<float>, grid, dim3(256), 0, st, (const float*)part, x, out, d.T, d.P, d.heads, n);
-        return hipGetLastError();
-    };
-    MixArgs a = common(d, log_decay, lengths, ws);
-    a.q = tg;
-    a.k = tv;
-    a.v = tk;
-    a.state_in = state_in;
-    a.state_t = 1;
-    a.in_scale = 1.f;
-    a.out_scale = d.scale;
-    hipError_t e = pass(a, tq, g_q, "linattn_bwd_q");
-    if (e != hipSuccess) return e;
-    a = common(d, log_decay, lengths, ws);
-    a.reverse = 1;
-    a.q = tv;
-    a.k = tg;
-    a.v = tq;
-    a.state_in = g_state_out;
-    a.state_t = 1;
-    a.in_scale = d.scale;
-    a.out_scale = 1.f;
-    e = pass(a, tk, g_k, "linattn_bwd_k");
-    if (e != hipSuccess) return e;
-    a = common(d, log_decay, lengths, ws);
-    a.reverse = 1;
-    a.q = tk;
-    a.k = tq;
-    a.v = tg;
-    a.state_in = g_state_out;
-    a.state_out = g_state_in;
-    a.in_scale = d.scale;
-    a.out_scale = 1.f;
-    return pass(a, tv, g_v, "linattn_bwd_v");
+        if (d.dtype) hipLaunchKernelGGL(mix_share_kernel<unsigned short>, grid, dim3(256), 0, st, (const float*)part[i], x, out[i], d.T, d.P, d.heads, n);
+        else hipLaunchKernelGGL(mix_share_kernel<float>, grid, dim3(256), 0, st, (const float*)part[i], x, out[i], d.T, d.P, d.heads, n);
+        e = hipGetLastError();
+    }
+    return e;
 }
 
 }  // namespace gleam
