@@ -27,6 +27,7 @@ namespace {
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef short short4v __attribute__((ext_vector_type(4)));
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr int kNear = 1 << 26;   // elements between tokens whose offsets within 16 rows fit 32 bits
 
 // Within each group of 16 lanes, lane s passes the address of 4 consecutive 16-bit values of row s/4; lane j gets column j of the
 // 4 x 16 block, rows 0..3.
@@ -177,7 +178,7 @@ template <class T>
 struct Edge {
     static constexpr int VE = 16 / (int)sizeof(T);
     int at, back, d;     // where the vector is read, elements in front of those that are wanted, width
-    bool live, narrow;   // whether any exists; rows shorter than a vector go element by element
+    bool live, narrow;   // whether any exists; whether a row is shorter than a vector (then none of this is used)
     __device__ __forceinline__ Edge(int col, int width) {
         d = width;
         narrow = d < VE;
@@ -185,29 +186,9 @@ struct Edge {
         back = live && col + VE > d && !narrow ? col + VE - d : 0;
         at = live ? col - back : 0;
     }
-    __device__ __forceinline__ void load(const T* row, Pack<T, VE>& x) const {
-        if (!narrow) {
-            x.load(row + at);
-        } else {
-            for (int i = 0; i < 4; ++i) x.w[i] = 0;
-            for (int e = d - 1; e >= 0; --e) {      // the element goes in front of those behind it
-                const T v = row[e];
-                if constexpr (sizeof(T) == 4) {
-                    x.w[2] = x.w[1];
-                    x.w[1] = x.w[0];
-                    x.w[0] = __float_as_uint(v);
-                } else {
-                    x.w[3] = x.w[3] << 16 | x.w[2] >> 16;
-                    x.w[2] = x.w[2] << 16 | x.w[1] >> 16;
-                    x.w[1] = x.w[1] << 16 | x.w[0] >> 16;
-                    x.w[0] = x.w[0] << 16 | v;
-                }
-            }
-        }
-    }
     // zeros where nothing exists, the rest in its place
     __device__ __forceinline__ Pack<T, VE> settle(Pack<T, VE> x, bool there) const {
-        if (d % VE && !narrow) {
+        if (d % VE) {
             unsigned long long lo = x.w[0] | (unsigned long long)x.w[1] << 32, hi = x.w[2] | (unsigned long long)x.w[3] << 32;
             const int bits = 8 * (int)sizeof(T) * back, b = bits & 63;
             const unsigned long long from_hi = b ? hi << (64 - b) : 0;
@@ -265,7 +246,8 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs
     __shared__ __attribute__((aligned(16))) T lds_k[S::kProblems][L * S::kRow];
     __shared__ __attribute__((aligned(16))) T lds_v[S::kProblems][L * S::kRow];
     __shared__ __attribute__((aligned(16))) T lds_p[STATES ? 1 : S::kProblems][STATES ? 8 : L * S::kScoreRow];
-    __shared__ float lds_w[S::kProblems][L + 2];
+    __shared__ __attribute__((aligned(16))) float lds_w[S::kProblems][L + 4];   // decay over n tokens
+    __shared__ __attribute__((aligned(16))) float lds_e[S::kProblems][L];       // from token j to the end of a whole chunk, with scale
     const int slot = S::kProblems == 1 ? 0 : threadIdx.x >> 6;
     const int tid = S::kProblems == 1 ? threadIdx.x : threadIdx.x & 63;
     const int lane = tid & 63, m = lane & 15, g = lane >> 4;
@@ -281,8 +263,9 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs
     const int shift = a.reverse;
     const float decay = args.log_decay[r.h];
     T *sq = lds_q[STATES ? 0 : slot], *sk = lds_k[slot], *sv = lds_v[slot], *sp = lds_p[STATES ? 0 : slot];
-    float* sw = lds_w[slot];
+    float *sw = lds_w[slot], *se = lds_e[slot];
     for (int i = tid; i < L + 2; i += NT) sw[i] = decay_of(decay, i);
+    for (int i = tid; i < L; i += NT) se[i] = a.in_scale * decay_of(decay, L - 1 - i + shift);
 
     // tokens of the chunk from the first one on (or, in reverse, from the last one down)
     const long long way = a.reverse ? -1 : 1, start = a.reverse ? r.len - 1 : 0;
@@ -290,31 +273,63 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs
     const int col = tid % (D / VE) * VE, row0 = tid / (D / VE);
     constexpr int kRowStep = NT / (D / VE);
     const T *gq = base_of<T>(a.q, r), *gk = base_of<T>(a.k, r), *gv = base_of<T>(a.v, r);
-    const long long sq_t = way * a.q.s.t, sk_t = way * a.k.s.t, sv_t = way * a.v.s.t;
-    gq += start * a.q.s.t;
-    gk += start * a.k.s.t;
-    gv += start * a.v.s.t;
-    // Loads always go to a token and a column that exist; what does not belong to the chunk becomes zero on the way into LDS, so that
-    // nothing waits for a load before it has to.  A row's last vector ends with the row and is moved into place there.
+    // A whole chunk is read at a scalar address plus a lane's own offset.  In a chunk that ends early, and where tokens are too far
+    // apart for 32 bits, every load goes to a token that exists, and what does not belong to the chunk becomes zero on the way into
+    // LDS, so that nothing waits for a load before it has to.  A row's last vector ends with the row and is moved into place there.
     Pack<T, VE> nq[NV], nk[NV], nv[NV];
     const Edge<T> ek(col, a.k.d), ev(col, a.v.d);
-    auto fetch = [&](int c) {
+    const bool narrow = ek.narrow || ev.narrow;
+    const bool near = a.q.s.t < kNear && a.k.s.t < kNear && a.v.s.t < kNear;
+    const int lane_row = a.reverse ? kRowStep - 1 - row0 : row0;
+    auto fetch_array = [&](int c, bool whole, const T* base, long long t, const Edge<T>& e, Pack<T, VE>(&n)[NV]) {
+        if (whole) {
+            const unsigned off = (unsigned)(lane_row * (int)t + e.at);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            int at = c * L + row0 + i * kRowStep;
-            at = at < r.len ? at : r.len - 1;
-            if constexpr (!STATES) ek.load(gq + at * sq_t, nq[i]);
-            ek.load(gk + at * sk_t, nk[i]);
-            ev.load(gv + at * sv_t, nv[i]);
+            for (int i = 0; i < NV; ++i) {
+                const int first = c * L + i * kRowStep;
+                const T* p = base + (a.reverse ? (long long)(r.len - kRowStep - first) : (long long)first) * t;
+                n[i].load(p + off);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                int at = c * L + row0 + i * kRowStep;
+                at = at < r.len ? at : r.len - 1;
+                n[i].load(base + (a.reverse ? r.len - 1 - at : at) * t + e.at);
+            }
         }
     };
-    auto stage = [&](int count) {
+    auto fetch = [&](int c) {
+        if (narrow) return;
+        const bool whole = near && (c + 1) * L <= r.len;
+        if constexpr (!STATES) fetch_array(c, whole, gq, a.q.s.t, ek, nq);
+        fetch_array(c, whole, gk, a.k.s.t, ek, nk);
+        fetch_array(c, whole, gv, a.v.s.t, ev, nv);
+    };
+    auto stage = [&](int c, int count) {
+        if (narrow) {                                 // rows shorter than a vector: element by element, nothing ahead of time
+            for (int e = tid; e < L * S::kRow; e += NT) {
+                const int row = e / S::kRow, cc = e % S::kRow, at = c * L + row;
+                const long long token = a.reverse ? r.len - 1 - at : at;
+                if constexpr (!STATES) sq[e] = row < count && cc < a.q.d ? gq[token * a.q.s.t + cc] : (T)0;
+                sk[e] = row < count && cc < a.k.d ? gk[token * a.k.s.t + cc] : (T)0;
+                sv[e] = row < count && cc < a.v.d ? gv[token * a.v.s.t + cc] : (T)0;
+            }
+            return;
+        }
+        const bool as_is = count == L && a.k.d == D && a.v.d == D;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int row = row0 + i * kRowStep, at = row * S::kRow + col;
-            if constexpr (!STATES) ek.settle(nq[i], row < count).store_lds(sq + at);
-            ek.settle(nk[i], row < count).store_lds(sk + at);
-            ev.settle(nv[i], row < count).store_lds(sv + at);
+            if (as_is) {
+                if constexpr (!STATES) nq[i].store_lds(sq + at);
+                nk[i].store_lds(sk + at);
+                nv[i].store_lds(sv + at);
+            } else {
+                if constexpr (!STATES) ek.settle(nq[i], row < count).store_lds(sq + at);
+                ek.settle(nk[i], row < count).store_lds(sk + at);
+                ev.settle(nv[i], row < count).store_lds(sv + at);
+            }
         }
     };
 
@@ -363,7 +378,7 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs
     for (int c = c_begin; c < c_end; ++c) {
         const int left = r.len - c * L, count = left < L ? left : L;
         exchange<W>();                                // everyone is done with the chunk before
-        stage(count);
+        stage(c, count);
         exchange<W>();
         if (c + 1 < c_end) fetch(c + 1);
         Frag vf[L / KB][2];
@@ -388,7 +403,7 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs
 #pragma unroll
                         for (int s = 0; s < D / KB; ++s) p = M::mma(M::row_frag(sk + (16 * jt + m) * S::kRow + s * KB + g * VE), qf[s], p);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) p[i] = wt[n][i] != 0.f ? p[i] * wt[n][i] : 0.f;
+                        for (int i = 0; i < 4; ++i) p[i] = n > 0 || m >= 4 * g + i ? p[i] * wt[n][i] : 0.f;
                         if (n <= it) M::put4(sp + (16 * it + m) * S::kScoreRow + 16 * jt + 4 * g, p);
                     }
                     if (kPair == 2 && !(it & 1)) M::put4(sp + (16 * it + m) * S::kScoreRow + 16 * (it + 1) + 4 * g, floatx4{0.f, 0.f, 0.f, 0.f});
@@ -450,10 +465,15 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs
         for (int s = 0; s < L / KB; ++s) {
             if (s * KB >= count) break;
             float w[VE];
+            if (count == L) {
 #pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                const int j = s * KB + g * VE + e;
-                w[e] = j < count ? a.in_scale * sw[count - 1 - j + shift] : 0.f;
+                for (int e = 0; e < VE; e += 4) *(floatx4*)(w + e) = *(const floatx4*)(se + s * KB + g * VE + e);
+            } else {
+#pragma unroll
+                for (int e = 0; e < VE; ++e) {
+                    const int j = s * KB + g * VE + e;
+                    w[e] = j < count ? se[j + L - count] : 0.f;
+                }
             }
             Frag part[2][PARTS];
 #pragma unroll
