@@ -72,6 +72,19 @@ struct Mma<unsigned short> {
         const uint2 lo = read_tr16(q), hi = read_tr16(q + 4 * stride);
         return __builtin_bit_cast(Frag, make_uint4(lo.x, lo.y, hi.x, hi.y));
     }
+    // the same with the block's rows in the order in which pack_scores has them
+    static __device__ __forceinline__ Frag col_frag_of_scores(const unsigned short* p, int stride, int col, int lane) {
+        const int g = lane >> 4, s = lane & 15;
+        const unsigned short* q = p + (4 * g + (s >> 2)) * stride + col;
+        const uint2 lo = read_tr16(q), hi = read_tr16(q + 16 * stride);
+        return __builtin_bit_cast(Frag, make_uint4(lo.x, lo.y, hi.x, hi.y));
+    }
+    static __device__ __forceinline__ int col_of(int t, int lane) { return 32 * (t >> 1) + 8 * (lane & 3) + 4 * (t & 1); }
+    static __device__ __forceinline__ int narrow_col_of(int lane) { return 4 * (lane & 3); }
+    // results of two tiles (rows 4 g .. 4 g + 3 of either) as an operand
+    static __device__ __forceinline__ Frag pack_scores(floatx4 a, floatx4 b) {
+        return __builtin_bit_cast(Frag, make_uint4(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])));
+    }
     // Parts whose sum is f times w: bfloat16 numbers w[i] f[i] rounded, what that left over rounded, and so on; 8 bits each.
     static constexpr int kStateParts = 2;
     static __device__ __forceinline__ void scaled(Frag f, const float* w, Frag* parts, int n) {
@@ -134,6 +147,13 @@ struct Mma<float> {
         const float* q = p + 4 * (lane >> 4) * stride + 16 * t + (lane & 15);
         return Frag{q[0], q[stride], q[2 * stride], q[3 * stride]};
     }
+    static __device__ __forceinline__ Frag col_frag_of_scores(const float* p, int stride, int col, int lane) {
+        const float* q = p + 4 * (lane >> 4) * stride + col;
+        return Frag{q[0], q[stride], q[2 * stride], q[3 * stride]};
+    }
+    static __device__ __forceinline__ int col_of(int t, int lane) { return 16 * t + (lane & 15); }
+    static __device__ __forceinline__ int narrow_col_of(int lane) { return lane & 15; }
+    static __device__ __forceinline__ Frag pack_scores(floatx4 a, floatx4) { return a; }
     static constexpr int kStateParts = 1;
     static __device__ __forceinline__ void scaled(Frag f, const float* w, Frag* parts, int) { parts[0] = Frag{f[0] * w[0], f[1] * w[1], f[2] * w[2], f[3] * w[3]}; }
     static __device__ __forceinline__ void pack(const floatx4* x, Frag* parts) { parts[0] = x[0]; }
@@ -210,13 +230,13 @@ struct Problem {
     long long b, p;
     int h, len;         // head, tokens
 };
-__device__ __forceinline__ Problem problem_of(const MixArgs& a, long long index) {
+__device__ __forceinline__ Problem problem_of(const MixArgs& a, long long index) {   // there are fewer than 2^31
     Problem r;
     r.index = index;
-    r.h = (int)(index % a.H);
-    const long long rest = index / a.H;
-    r.p = rest % a.P;
-    r.b = rest / a.P;
+    const unsigned i = (unsigned)index, rest = i / (unsigned)a.H, b = rest / (unsigned)a.P;
+    r.h = (int)(i - rest * (unsigned)a.H);
+    r.p = rest - b * (unsigned)a.P;
+    r.b = b;
     r.len = (int)a.T;
     if (a.lengths) {
         const int l = a.lengths[r.b];
@@ -510,6 +530,161 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs
         });
 }
 
+// ------------------------------------------------------------------ short sequences of narrow heads
+// At most 64 tokens of at most 32 values without a state, as the frames of a series at one pixel: a wave has a whole problem, all
+// three gradients of it in the backward pass, and there are no barriers.  An operand whose rows are tokens is loaded straight from memory in
+// the layout of the product; LDS only turns over those whose contracted index is the token.  Scores go from the result of one product
+// to the operand of the next in registers: the contracted tokens may come in any order that both operands have.
+// TT: tiles of 16 tokens.  U: tiles of 16 columns.
+constexpr int kShortTokens = 64, kShortWidth = 32, kShortWaves = 4;
+
+template <class T, int TT, int U, bool BWD>
+__global__ __launch_bounds__(64 * kShortWaves) void mix_short_kernel(MixArgs args) {
+    typedef Mma<T> M;
+    typedef typename M::Frag Frag;
+    constexpr int VE = M::kVec, KB = M::kBlock, KS = (16 * U + KB - 1) / KB, kPair = KB / 16, TS = (TT + kPair - 1) / kPair;
+    constexpr int kRow = 32 + VE, kTurned = BWD ? 3 : 1;
+    __shared__ __attribute__((aligned(16))) T lds[kShortWaves][kTurned][TS * KB * kRow];
+    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4, slot = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long long index = (long long)blockIdx.x * kShortWaves + slot;
+    if (index >= args.B * args.P * args.H) return;
+    const Problem r = problem_of(args, index);
+    const float decay = args.log_decay[r.h];
+
+    // rows of tokens in the layout of an operand: token 16 t + m, values s KB + g VE on
+    auto rows = [&](const MixTensor& x, Frag(&f)[TT][KS]) {
+        const T* base = base_of<T>(x, r);
+        Pack<T, VE> n[TT][KS];
+        if (x.d >= VE) {
+#pragma unroll
+            for (int t = 0; t < TT; ++t)
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    const int at = 16 * t + m < r.len ? 16 * t + m : r.len - 1;
+                    n[t][s].load(base + at * x.s.t + Edge<T>(s * KB + g * VE, x.d).at);
+                }
+        }
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const bool there = 16 * t + m < r.len;
+                const Edge<T> e(s * KB + g * VE, x.d);
+                if (x.d < VE) {                       // rows shorter than a vector
+                    float v[VE];
+#pragma unroll
+                    for (int i = 0; i < VE; ++i) v[i] = there && s * KB + g * VE + i < x.d ? to_f32(base[(16 * t + m) * x.s.t + g * VE + i]) : 0.f;
+                    n[t][s].set(v);
+                } else {
+                    n[t][s] = e.settle(n[t][s], there);
+                }
+                f[t][s] = __builtin_bit_cast(Frag, n[t][s]);
+            }
+    };
+    auto turn = [&](const Frag(&f)[TT][KS], int which) {
+#pragma unroll
+        for (int t = 0; t < TS * kPair; ++t)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) *(Frag*)(lds[slot][which] + (16 * t + m) * kRow + s * KB + g * VE) = t < TT ? f[t < TT ? t : 0][s] : Frag{};
+    };
+    auto turned = [&](int which, int s, int u) {     // column block u, tokens of block s
+        return M::col_frag_of_scores(lds[slot][which] + s * KB * kRow, kRow, U == 1 ? M::narrow_col_of(lane) : M::col_of(u, lane), lane);
+    };
+    auto store = [&](const MixRole& ro, int t, const floatx4(&o)[U]) {
+        if (16 * t + m >= args.T) return;
+        const long long at = r.b * ro.o.s.b + (16 * t + m) * ro.o.s.t + r.p * ro.o.s.p + (long long)(r.h / ro.o.share) * ro.o.s.h;
+        if constexpr (U == 1) {
+            const float v[4] = {o[0][0], o[0][1], o[0][2], o[0][3]};
+            if (ro.out_f32) store_part<float, 4>((float*)ro.out + at + 4 * g, ro.o.d - 4 * g, v);
+            else store_part<T, 4>((T*)ro.out + at + 4 * g, ro.o.d - 4 * g, v);
+        } else {
+            if (ro.out_f32) M::store((float*)ro.out + at, ro.o.d, g, o);
+            else M::store((T*)ro.out + at, ro.o.d, g, o);
+        }
+    };
+    if (r.len == 0) {
+        const floatx4 zero[U] = {};
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+#pragma unroll
+            for (int i = 0; i < (BWD ? 3 : 1); ++i) store(args.role[i], t, zero);
+        return;
+    }
+    const float scale = args.role[0].in_scale * args.role[0].out_scale;
+    // scores of the tiles of one output row tile as operands: columns of the product are the output's tokens, which are the later
+    // (UP: the earlier) ones of the two; tiles that the mask leaves out are zero
+    auto scores = [&](const Frag(&contracted)[TT][KS], const Frag(&output)[TT][KS], int t, bool up, Frag(&p)[TS]) {
+        floatx4 tile[2 * TS];
+#pragma unroll
+        for (int j = 0; j < 2 * TS; ++j) {
+            tile[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+            const int n = up ? j - t : t - j;        // tiles apart
+            if (j >= TT || n < 0) continue;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) tile[j] = M::mma(contracted[j][s], output[t][s], tile[j]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int apart = 16 * n + (up ? 4 * g + i - m : m - 4 * g - i);
+                tile[j][i] = apart >= 0 ? tile[j][i] * (scale * decay_of(decay, apart)) : 0.f;
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < TS; ++s) p[s] = M::pack_scores(tile[kPair * s], tile[kPair * s + kPair - 1]);
+    };
+    auto product = [&](int which, const Frag(&p)[TS], int t, bool up, floatx4(&o)[U]) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) o[u] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < TS; ++s) {
+            if (up ? (s + 1) * kPair <= t : s * kPair > t) continue;
+#pragma unroll
+            for (int u = 0; u < U; ++u) o[u] = M::mma(turned(which, s, u), p[s], o[u]);
+        }
+    };
+    if constexpr (!BWD) {
+        const MixRole& ro = args.role[0];
+        Frag q[TT][KS], k[TT][KS], v[TT][KS];
+        rows(ro.q, q);
+        rows(ro.k, k);
+        rows(ro.v, v);
+        turn(v, 0);
+        exchange<1>();
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+            Frag p[TS];
+            floatx4 o[U];
+            scores(k, q, t, false, p);
+            product(0, p, t, false, o);
+            store(ro, t, o);
+        }
+    } else {
+        const MixRole &rq = args.role[0], &rk = args.role[1], &rv = args.role[2];
+        Frag q[TT][KS], k[TT][KS], v[TT][KS], go[TT][KS];
+        rows(rv.k, q);
+        rows(rv.q, k);
+        rows(rq.k, v);
+        rows(rq.q, go);
+        turn(k, 0);
+        turn(q, 1);
+        turn(go, 2);
+        exchange<1>();
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+            Frag p[TS];
+            floatx4 o[U];
+            scores(v, go, t, false, p);              // g_q of token t: earlier tokens' keys
+            product(0, p, t, false, o);
+            store(rq, t, o);
+            scores(go, v, t, true, p);               // g_k: later tokens' queries
+            product(1, p, t, true, o);
+            store(rk, t, o);
+            scores(q, k, t, true, p);                // g_v: later tokens' gradients
+            product(2, p, t, true, o);
+            store(rv, t, o);
+        }
+    }
+}
+
 // States at the start of every segment from the sums of the segments: X_{s+1} = e^{a n} X_s + sum_s, n tokens a segment.  A thread
 // has four elements; slot 0 is the state that comes in.
 template <int D>
@@ -649,6 +824,26 @@ hipError_t mix_any(const MixArgs& a, int roles, const MixArgs& states, int n_sta
     }
 }
 
+// Rule for the kernel of short sequences.  It reads and writes every array once, in the backward pass as well, and a problem is one wave;
+// it has no state, and beyond these sizes the operands do not fit its registers.
+bool is_short(const gleam_linattn_desc& d, bool state) { return !state && d.T <= kShortTokens && d.dk <= kShortWidth && d.dv <= kShortWidth; }
+template <class T, int TT, bool BWD>
+void launch_short(const MixArgs& a, unsigned groups, hipStream_t st) {
+    if (a.dk <= 16 && a.dv <= 16) hipLaunchKernelGGL((mix_short_kernel<T, TT, 1, BWD>), dim3(groups), dim3(64 * kShortWaves), 0, st, a);
+    else hipLaunchKernelGGL((mix_short_kernel<T, TT, 2, BWD>), dim3(groups), dim3(64 * kShortWaves), 0, st, a);
+}
+template <class T, bool BWD>
+hipError_t mix_short(const MixArgs& a, const char* name, hipStream_t st) {
+    const long long problems = a.B * a.P * a.H;
+    const unsigned groups = (unsigned)((problems + kShortWaves - 1) / kShortWaves);
+    const double tokens = (double)problems * a.T;
+    KernelScope ks(name, (BWD ? 10.0 : 4.0) * tokens * a.dk * a.dv, (BWD ? 3.5 : 2.0) * tokens * sizeof(T) * (a.dk + a.dv), st);
+    if (a.T <= 16) launch_short<T, 1, BWD>(a, groups, st);
+    else if (a.T <= 32) launch_short<T, 2, BWD>(a, groups, st);
+    else launch_short<T, 4, BWD>(a, groups, st);
+    return hipGetLastError();
+}
+
 gleam_seq_strides row_major(const gleam_linattn_desc& d, int heads, int width) {
     return {d.T * d.P * heads * width, d.P * heads * width, (int64_t)heads * width, width};
 }
@@ -706,6 +901,8 @@ hipError_t linattn_forward(const gleam_linattn_desc& d, const void* q, const voi
         else hipLaunchKernelGGL(mix_step_kernel<float>, grid, dim3(kStepThreads), 0, st, a);
         return hipGetLastError();
     }
+    if (is_short(d, state_in || state_out))
+        return d.dtype ? mix_short<unsigned short, false>(a, "linattn_fwd_short", st) : mix_short<float, false>(a, "linattn_fwd_short", st);
     states.role[0] = role_of(tq, tv, tk, 1, 0, 1.f, 1.f, state_in, seg);
     return d.dtype ? mix_any<unsigned short>(a, 1, states, 1, state_out, "linattn_fwd", st)
                    : mix_any<float>(a, 1, states, 1, state_out, "linattn_fwd", st);
@@ -743,8 +940,12 @@ hipError_t linattn_backward(const gleam_linattn_desc& d, const void* q, const vo
             a.role[i].out_f32 = 1;
         }
     }
-    hipError_t e = d.dtype ? mix_any<unsigned short>(a, 3, states, 2, g_state_in, "linattn_bwd", st)
-                           : mix_any<float>(a, 3, states, 2, g_state_in, "linattn_bwd", st);
+    hipError_t e;
+    if (is_short(d, state_in || g_state_out || g_state_in))
+        e = d.dtype ? mix_short<unsigned short, true>(a, "linattn_bwd_short", st) : mix_short<float, true>(a, "linattn_bwd_short", st);
+    else
+        e = d.dtype ? mix_any<unsigned short>(a, 3, states, 2, g_state_in, "linattn_bwd", st)
+                    : mix_any<float>(a, 3, states, 2, g_state_in, "linattn_bwd", st);
     for (int i = 0; i < 3 && e == hipSuccess; ++i) {
         if (!part[i]) continue;
         const MixTensor& x = *of[i];

@@ -243,17 +243,17 @@ class Mix:
         o = self.new("g")
         d = gb.make_linattn(self.arrays["q"], self.arrays["k"], self.arrays["v"], o, self.scale)
         n = gb.gleam_linattn_workspace_bytes(d)[0]
-        out = torch.full(self.state_shape, POISON, device="cuda") if state_out else None
+        out = torch.full(self.state_shape, POISON, device="cuda") if state_out else None   # None: not wanted
         gb.gleam_linattn_fwd(d, self.arrays["q"], self.arrays["k"], self.arrays["v"], self.log_decay, self.lengths, self.state, o, out,
                              torch.full((n,), 255, dtype=torch.uint8, device="cuda"))
         return o, out
 
-    def bwd(self):
+    def bwd(self, g_state=True):
         a = self.arrays
         d = gb.make_linattn(a["q"], a["k"], a["v"], a["g"], self.scale)
         n = gb.gleam_linattn_workspace_bytes(d)[1]
         grads = [self.new(x) for x in "qkv"]
-        gs = torch.full(self.state_shape, POISON, device="cuda")
+        gs = torch.full(self.state_shape, POISON, device="cuda") if g_state else None
         gb.gleam_linattn_bwd(d, a["q"], a["k"], a["v"], self.log_decay, self.lengths, self.state, a["g"], self.gstate, *grads, gs,
                              torch.full((n,), 255, dtype=torch.uint8, device="cuda"))
         return grads, gs
@@ -261,15 +261,18 @@ class Mix:
     def check(self):
         tol = BF16 if self.low else F32
         h = self.host
-        o, S = self.fwd()
+        states = self.state is not None
+        o, S = self.fwd(states)
         ro, rS = lo.linattn(h["q"], h["k"], h["v"], self.ha, self.scale, self.hl, self.hs)
         assert_close(host(o), ro, tol, "o")
-        assert_close(host(S), rS, F32, "state")
-        grads, gS = self.bwd()
+        if states:
+            assert_close(host(S), rS, F32, "state")
+        grads, gS = self.bwd(states)
         ref = lo.linattn_bwd(h["q"], h["k"], h["v"], self.ha, self.scale, h["g"], self.hl, self.hs, self.hgs)
         for name, got, want in zip(("g_q", "g_k", "g_v"), grads, ref):
             assert_close(host(got), want, tol, name)
-        assert_close(host(gS), ref[3], F32, "g_state")
+        if states:
+            assert_close(host(gS), ref[3], F32, "g_state")
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -308,6 +311,21 @@ def test_linattn_ragged(T, lengths, state, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("layout", ["tokens", "gaps"])
+@pytest.mark.parametrize("dk,dv", [(16, 16), (8, 8), (5, 3), (25, 25), (12, 30), (32, 32)])
+def test_linattn_short_sequences_of_narrow_heads(dk, dv, layout, dtype):
+    """Few tokens at many pixels, no state: the tokens of one, two and four tiles, and their ends."""
+    for T in (2, 7, 16, 17, 20, 32, 33, 50, 64):
+        print("case linattn short", dk, dv, layout, T, dtype, flush=True)
+        Mix(1, T, 5, (3, 3, 3, 3), dk, dv, dtype, layout, state=False).check()
+        Mix(3, T, 3, (4, 2, 1, 4), dk, dv, dtype, layout, lengths=[T, 0, T // 2], state=False).check()
+
+
+def test_linattn_short_sequences_without_memory():
+    Mix(1, 20, 2, (3, 3, 3, 3), 16, 16, "f32", state=False, decays=[-np.inf, -300.0, 0.0]).check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("d", [32, 64, 128])
 def test_linattn_long(d, dtype):
     """Few problems of many chunks: the split into segments; a state in and out, heads shared, one sequence shorter."""
@@ -339,6 +357,16 @@ def test_linattn_pieces_are_the_whole(dtype):
         gb.gleam_linattn_fwd(d, *x, m.log_decay, None, run, part[:, lo_:hi], run, torch.empty(gb.gleam_linattn_workspace_bytes(d)[0], dtype=torch.uint8, device="cuda"))
     assert_close(host(part), host(o), BF16 if m.low else F32, "o")
     assert_close(host(run), host(S), F32, "state")
+
+
+def test_linattn_state_out_of_nothing():
+    """A state behind the last token is wanted, none comes in."""
+    for dtype in ("f32", "bf16"):
+        m = Mix(2, 90, 1, (2, 2, 2, 2), 24, 16, dtype, lengths=[90, 0], state=False)
+        _, S = m.fwd()
+        assert_close(host(S), lo.linattn(m.host["q"], m.host["k"], m.host["v"], m.ha, m.scale, m.hl)[1], F32, "state")
+        gS = m.bwd()[1]
+        assert_close(host(gS), lo.linattn_bwd(m.host["q"], m.host["k"], m.host["v"], m.ha, m.scale, m.host["g"], m.hl)[3], F32, "g_state")
 
 
 def test_linattn_gradients_against_differences():
