@@ -128,6 +128,13 @@ struct Mma<unsigned short> {
         for (int i = 0; i < 8; ++i) v[i] = o[i >> 2][i & 3];
         store_part<O, 8>(p + 8 * g, left - 8 * g, v);
     }
+    // the same into LDS, where width and address are multiples of 16 bytes
+    static __device__ __forceinline__ void keep(unsigned short* p, int width, int g, const floatx4* o) {
+        if (8 * g < width) {
+            put4(p + 8 * g, o[0]);
+            put4(p + 8 * g + 4, o[1]);
+        }
+    }
     static __device__ __forceinline__ void put4(unsigned short* p, floatx4 v) {
         *(uint2*)p = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
     }
@@ -165,11 +172,16 @@ struct Mma<float> {
             store_part<O, 4>(p + 16 * u + 4 * g, left - 16 * u - 4 * g, v);
         }
     }
+    static __device__ __forceinline__ void keep(float* p, int width, int g, const floatx4* o) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            if (16 * u + 4 * g < width) put4(p + 16 * u + 4 * g, o[u]);
+    }
     static __device__ __forceinline__ void put4(float* p, floatx4 v) { *(floatx4*)p = v; }
 };
 
 // e^{a n}; 1 for n = 0 whatever a is.
-__device__ __forceinline__ float decay_of(float a, int n) { return n == 0 ? 1.f : exp2f(a * kLog2e * (float)n); }
+__device__ __forceinline__ float decay_of(float a, int n) { return n == 0 ? 1.f : __builtin_amdgcn_exp2f(a * kLog2e * (float)n); }
 
 // Tokens a chunk has, and waves and problems of a workgroup.
 template <class T, int D>
@@ -206,8 +218,7 @@ struct Edge {
         back = live && col + VE > d && !narrow ? col + VE - d : 0;
         at = live ? col - back : 0;
     }
-    // zeros where nothing exists, the rest in its place
-    __device__ __forceinline__ Pack<T, VE> settle(Pack<T, VE> x, bool there) const {
+    __device__ __forceinline__ Pack<T, VE> in_place(Pack<T, VE> x) const {
         if (d % VE) {
             unsigned long long lo = x.w[0] | (unsigned long long)x.w[1] << 32, hi = x.w[2] | (unsigned long long)x.w[3] << 32;
             const int bits = 8 * (int)sizeof(T) * back, b = bits & 63;
@@ -219,6 +230,11 @@ struct Edge {
             x.w[2] = (unsigned)hi;
             x.w[3] = (unsigned)(hi >> 32);
         }
+        return x;
+    }
+    // zeros where nothing exists, the rest in its place
+    __device__ __forceinline__ Pack<T, VE> settle(Pack<T, VE> x, bool there) const {
+        x = in_place(x);
 #pragma unroll
         for (int i = 0; i < 4; ++i) x.w[i] = there && live ? x.w[i] : 0;
         return x;
@@ -532,155 +548,252 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs
 
 // ------------------------------------------------------------------ short sequences of narrow heads
 // At most 64 tokens of at most 32 values without a state, as the frames of a series at one pixel: a wave has a whole problem, all
-// three gradients of it in the backward pass, and there are no barriers.  An operand whose rows are tokens is loaded straight from memory in
-// the layout of the product; LDS only turns over those whose contracted index is the token.  Scores go from the result of one product
-// to the operand of the next in registers: the contracted tokens may come in any order that both operands have.
+// three gradients of it in the backward pass.  Scores go from the result of one product to the operand of the next in registers: the
+// contracted tokens may come in any order that both operands have.
 // TT: tiles of 16 tokens.  U: tiles of 16 columns.
+// ROWS: the four problems of a workgroup are neighbouring heads of a pixel, whose values lie side by side; the workgroup moves whole
+// rows of the four through LDS.  Otherwise an operand whose rows are tokens is loaded straight from memory in the layout of the product,
+// and LDS only turns over those whose contracted index is the token; there are no barriers then.
 constexpr int kShortTokens = 64, kShortWidth = 32, kShortWaves = 4;
 
-template <class T, int TT, int U, bool BWD>
+template <class T, int TT, int U, bool BWD, bool ROWS>
 __global__ __launch_bounds__(64 * kShortWaves) void mix_short_kernel(MixArgs args) {
     typedef Mma<T> M;
     typedef typename M::Frag Frag;
     constexpr int VE = M::kVec, KB = M::kBlock, KS = (16 * U + KB - 1) / KB, kPair = KB / 16, TS = (TT + kPair - 1) / kPair;
-    constexpr int kRow = 32 + VE, kTurned = BWD ? 3 : 1;
-    __shared__ __attribute__((aligned(16))) T lds[kShortWaves][kTurned][TS * KB * kRow];
+    constexpr int kArrays = ROWS ? (BWD ? 4 : 3) : (BWD ? 3 : 1), kTokens = TS * KB;
+    // between tokens in LDS: a wave's own columns, or those of four heads
+    constexpr int kRow = ROWS ? 4 * 16 * U + VE : 32 + VE;
+    __shared__ __attribute__((aligned(16))) T lds[ROWS ? 1 : kShortWaves][kArrays][kTokens * kRow];
+    __shared__ float weights[kShortWaves][16 + kShortTokens];
     const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4, slot = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const long long index = (long long)blockIdx.x * kShortWaves + slot;
-    if (index >= args.B * args.P * args.H) return;
+    if (index >= args.B * args.P * args.H) return;   // not where ROWS: a multiple of four heads
     const Problem r = problem_of(args, index);
     const float decay = args.log_decay[r.h];
+    auto own = [&](int which, int width) { return lds[ROWS ? 0 : slot][which] + (ROWS ? slot * width : 0); };
 
+    // ROWS: tokens of the four heads to LDS and back, 16 bytes a lane, zeros behind the sequence's end.  f(token, first value)
+    // of the vectors of this lane; the products fit 24 bits by the rule that chooses ROWS.
+    auto vectors = [&](int width, int tokens, auto&& f) {
+        const int per = 4 * width / VE, n = tokens * per;
+        const float share = 1.f / (float)per;
+        for (int v = threadIdx.x; v < n; v += 64 * kShortWaves) {
+            const int t = (int)(((float)v + 0.5f) * share);
+            f(t, (v - t * per) * VE);
+        }
+    };
+    auto take = [&](const MixTensor& x, int which) {
+        const T* base = (const T*)x.p + r.b * x.s.b + r.p * x.s.p + (long long)(r.h - slot) * x.s.h;
+        vectors(x.d, kTokens, [&](int t, int c) {
+            Pack<T, VE> n{};
+            if (t < r.len) n.load(base + (unsigned)(__umul24(t, (unsigned)x.s.t) + c));
+            n.store_lds(lds[0][which] + t * kRow + c);
+        });
+    };
+    auto give = [&](const MixRole& ro, int which) {
+        T* base = (T*)ro.out + r.b * ro.o.s.b + r.p * ro.o.s.p + (long long)(r.h - slot) * ro.o.s.h;
+        vectors(ro.o.d, (int)args.T, [&](int t, int c) {
+            const uint4 n = *(const uint4*)(lds[0][which] + t * kRow + c);
+            __builtin_memcpy(base + (unsigned)(__umul24(t, (unsigned)ro.o.s.t) + c), &n, 16);
+        });
+    };
     // rows of tokens in the layout of an operand: token 16 t + m, values s KB + g VE on
-    auto rows = [&](const MixTensor& x, Frag(&f)[TT][KS]) {
-        const T* base = base_of<T>(x, r);
-        Pack<T, VE> n[TT][KS];
-        if (x.d >= VE) {
+    auto rows = [&](const MixTensor& x, int which, Frag(&f)[TT][KS]) {
+        if constexpr (ROWS) {
 #pragma unroll
             for (int t = 0; t < TT; ++t)
 #pragma unroll
                 for (int s = 0; s < KS; ++s) {
-                    const int at = 16 * t + m < r.len ? 16 * t + m : r.len - 1;
-                    n[t][s].load(base + at * x.s.t + Edge<T>(s * KB + g * VE, x.d).at);
+                    const int c = s * KB + g * VE;
+                    f[t][s] = c < x.d ? M::row_frag(own(which, x.d) + (16 * t + m) * kRow + c) : Frag{};
                 }
+            return;
         }
+        // lanes without values load nothing: addresses are what bounds this, one a lane (20 x 192 x 160 pixels, 4 heads of 16:
+        // 124 us where all lanes load, 110 so)
+        const T* base = base_of<T>(x, r);
+        Pack<T, VE> n[TT][KS];
 #pragma unroll
         for (int t = 0; t < TT; ++t)
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
-                const bool there = 16 * t + m < r.len;
                 const Edge<T> e(s * KB + g * VE, x.d);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) n[t][s].w[i] = 0;
+                if (16 * t + m < r.len && e.live && !e.narrow) n[t][s].load(base + (16 * t + m) * x.s.t + e.at);
+            }
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
                 if (x.d < VE) {                       // rows shorter than a vector
                     float v[VE];
 #pragma unroll
-                    for (int i = 0; i < VE; ++i) v[i] = there && s * KB + g * VE + i < x.d ? to_f32(base[(16 * t + m) * x.s.t + g * VE + i]) : 0.f;
+                    for (int i = 0; i < VE; ++i) v[i] = 16 * t + m < r.len && s * KB + g * VE + i < x.d ? to_f32(base[(16 * t + m) * x.s.t + g * VE + i]) : 0.f;
                     n[t][s].set(v);
                 } else {
-                    n[t][s] = e.settle(n[t][s], there);
+                    n[t][s] = Edge<T>(s * KB + g * VE, x.d).in_place(n[t][s]);
                 }
                 f[t][s] = __builtin_bit_cast(Frag, n[t][s]);
             }
     };
     auto turn = [&](const Frag(&f)[TT][KS], int which) {
+        if constexpr (!ROWS) {
 #pragma unroll
-        for (int t = 0; t < TS * kPair; ++t)
+            for (int t = 0; t < TS * kPair; ++t)
 #pragma unroll
-            for (int s = 0; s < KS; ++s) *(Frag*)(lds[slot][which] + (16 * t + m) * kRow + s * KB + g * VE) = t < TT ? f[t < TT ? t : 0][s] : Frag{};
+                for (int s = 0; s < KS; ++s) *(Frag*)(lds[slot][which] + (16 * t + m) * kRow + s * KB + g * VE) = t < TT ? f[t < TT ? t : 0][s] : Frag{};
+        }
     };
-    auto turned = [&](int which, int s, int u) {     // column block u, tokens of block s
-        return M::col_frag_of_scores(lds[slot][which] + s * KB * kRow, kRow, U == 1 ? M::narrow_col_of(lane) : M::col_of(u, lane), lane);
+    // tokens of block s of the columns of tile u; columns that do not exist only reach results that are not stored
+    auto turned = [&](int which, int width, int s, int u) {
+        return M::col_frag_of_scores(own(which, width) + s * KB * kRow, kRow, U == 1 ? M::narrow_col_of(lane) : M::col_of(u, lane), lane);
     };
-    auto store = [&](const MixRole& ro, int t, const floatx4(&o)[U]) {
-        if (16 * t + m >= args.T) return;
+    auto store = [&](const MixRole& ro, int which, int t, const floatx4(&o)[U]) {
+        T* keep = own(which, ro.o.d) + (16 * t + m) * kRow;       // ROWS: in the place of the wave's own columns of an input
+        if (!ROWS && 16 * t + m >= args.T) return;
         const long long at = r.b * ro.o.s.b + (16 * t + m) * ro.o.s.t + r.p * ro.o.s.p + (long long)(r.h / ro.o.share) * ro.o.s.h;
         if constexpr (U == 1) {
             const float v[4] = {o[0][0], o[0][1], o[0][2], o[0][3]};
-            if (ro.out_f32) store_part<float, 4>((float*)ro.out + at + 4 * g, ro.o.d - 4 * g, v);
-            else store_part<T, 4>((T*)ro.out + at + 4 * g, ro.o.d - 4 * g, v);
+            if constexpr (ROWS) {
+                if (4 * g < ro.o.d) M::put4(keep + 4 * g, o[0]);
+            } else if (ro.out_f32) {
+                store_part<float, 4>((float*)ro.out + at + 4 * g, ro.o.d - 4 * g, v);
+            } else {
+                store_part<T, 4>((T*)ro.out + at + 4 * g, ro.o.d - 4 * g, v);
+            }
         } else {
-            if (ro.out_f32) M::store((float*)ro.out + at, ro.o.d, g, o);
+            if constexpr (ROWS) M::keep(keep, ro.o.d, g, o);
+            else if (ro.out_f32) M::store((float*)ro.out + at, ro.o.d, g, o);
             else M::store((T*)ro.out + at, ro.o.d, g, o);
         }
     };
-    if (r.len == 0) {
+    if (!ROWS && r.len == 0) {
         const floatx4 zero[U] = {};
 #pragma unroll
         for (int t = 0; t < TT; ++t)
 #pragma unroll
-            for (int i = 0; i < (BWD ? 3 : 1); ++i) store(args.role[i], t, zero);
+            for (int i = 0; i < (BWD ? 3 : 1); ++i) store(args.role[i], 0, t, zero);
         return;
     }
+    // decays of scores whose tiles are n apart, with scale: the later token's row m, or (up) the earlier one's
     const float scale = args.role[0].in_scale * args.role[0].out_scale;
+    float* table = weights[slot];
+    if (lane < 16) table[lane] = 0.f;
+    table[16 + lane] = scale * decay_of(decay, lane);
+    exchange<1>();
+    floatx4 down[TT], up[BWD ? TT : 1];
+#pragma unroll
+    for (int n = 0; n < TT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            down[n][i] = table[16 + m - 4 * g + 16 * n - i];
+            if constexpr (BWD) up[n][i] = table[16 + 4 * g - m + 16 * n + i];
+        }
     // scores of the tiles of one output row tile as operands: columns of the product are the output's tokens, which are the later
     // (UP: the earlier) ones of the two; tiles that the mask leaves out are zero
-    auto scores = [&](const Frag(&contracted)[TT][KS], const Frag(&output)[TT][KS], int t, bool up, Frag(&p)[TS]) {
+    auto scores = [&](const Frag(&contracted)[TT][KS], const Frag(&output)[TT][KS], int t, const floatx4* w, bool is_up, Frag(&p)[TS]) {
         floatx4 tile[2 * TS];
 #pragma unroll
         for (int j = 0; j < 2 * TS; ++j) {
             tile[j] = floatx4{0.f, 0.f, 0.f, 0.f};
-            const int n = up ? j - t : t - j;        // tiles apart
+            const int n = is_up ? j - t : t - j;     // tiles apart
             if (j >= TT || n < 0) continue;
 #pragma unroll
             for (int s = 0; s < KS; ++s) tile[j] = M::mma(contracted[j][s], output[t][s], tile[j]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int apart = 16 * n + (up ? 4 * g + i - m : m - 4 * g - i);
-                tile[j][i] = apart >= 0 ? tile[j][i] * (scale * decay_of(decay, apart)) : 0.f;
+                const bool masked = n == 0 && (is_up ? 4 * g + i < m : m < 4 * g + i);
+                tile[j][i] = masked ? 0.f : tile[j][i] * w[n][i];
             }
         }
 #pragma unroll
         for (int s = 0; s < TS; ++s) p[s] = M::pack_scores(tile[kPair * s], tile[kPair * s + kPair - 1]);
     };
-    auto product = [&](int which, const Frag(&p)[TS], int t, bool up, floatx4(&o)[U]) {
+    auto product = [&](int which, int width, const Frag(&p)[TS], int t, bool is_up, floatx4(&o)[U]) {
 #pragma unroll
         for (int u = 0; u < U; ++u) o[u] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < TS; ++s) {
-            if (up ? (s + 1) * kPair <= t : s * kPair > t) continue;
+            if (is_up ? (s + 1) * kPair <= t : s * kPair > t) continue;
 #pragma unroll
-            for (int u = 0; u < U; ++u) o[u] = M::mma(turned(which, s, u), p[s], o[u]);
+            for (int u = 0; u < U; ++u) o[u] = M::mma(turned(which, width, s, u), p[s], o[u]);
         }
     };
     if constexpr (!BWD) {
         const MixRole& ro = args.role[0];
         Frag q[TT][KS], k[TT][KS], v[TT][KS];
-        rows(ro.q, q);
-        rows(ro.k, k);
-        rows(ro.v, v);
+        if constexpr (ROWS) {
+            take(ro.v, 0);
+            take(ro.q, 1);
+            take(ro.k, 2);
+            __syncthreads();
+        }
+        rows(ro.q, 1, q);
+        rows(ro.k, 2, k);
+        if constexpr (!ROWS) rows(ro.v, 0, v);
         turn(v, 0);
-        exchange<1>();
+        if constexpr (!ROWS) exchange<1>();
+        floatx4 o[TT][U];
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
             Frag p[TS];
-            floatx4 o[U];
-            scores(k, q, t, false, p);
-            product(0, p, t, false, o);
-            store(ro, t, o);
+            scores(k, q, t, down, false, p);
+            product(0, ro.v.d, p, t, false, o[t]);
+            if constexpr (!ROWS) store(ro, 0, t, o[t]);
+        }
+        if constexpr (ROWS) {
+            exchange<1>();                           // the wave is done with its own columns of v
+#pragma unroll
+            for (int t = 0; t < TT; ++t) store(ro, 0, t, o[t]);
+            __syncthreads();
+            give(ro, 0);
         }
     } else {
         const MixRole &rq = args.role[0], &rk = args.role[1], &rv = args.role[2];
         Frag q[TT][KS], k[TT][KS], v[TT][KS], go[TT][KS];
-        rows(rv.k, q);
-        rows(rv.q, k);
-        rows(rq.k, v);
-        rows(rq.q, go);
+        if constexpr (ROWS) {
+            take(rv.q, 0);
+            take(rv.k, 1);
+            take(rq.q, 2);
+            take(rq.k, 3);
+            __syncthreads();
+        }
+        rows(rv.k, 1, q);
+        rows(rv.q, 0, k);
+        rows(rq.k, 3, v);
+        rows(rq.q, 2, go);
         turn(k, 0);
         turn(q, 1);
         turn(go, 2);
-        exchange<1>();
+        if constexpr (!ROWS) exchange<1>();
+        floatx4 oq[TT][U], ok[TT][U], ov[TT][U];
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
             Frag p[TS];
-            floatx4 o[U];
-            scores(v, go, t, false, p);              // g_q of token t: earlier tokens' keys
-            product(0, p, t, false, o);
-            store(rq, t, o);
-            scores(go, v, t, true, p);               // g_k: later tokens' queries
-            product(1, p, t, true, o);
-            store(rk, t, o);
-            scores(q, k, t, true, p);                // g_v: later tokens' gradients
-            product(2, p, t, true, o);
-            store(rv, t, o);
+            scores(v, go, t, down, false, p);        // g_q of token t: earlier tokens' keys
+            product(0, rv.q.d, p, t, false, oq[t]);
+            if constexpr (!ROWS) store(rq, 0, t, oq[t]);
+            scores(go, v, t, up, true, p);           // g_k: later tokens' queries
+            product(1, rv.k.d, p, t, true, ok[t]);
+            if constexpr (!ROWS) store(rk, 0, t, ok[t]);
+            scores(q, k, t, up, true, p);            // g_v: later tokens' gradients
+            product(2, rq.q.d, p, t, true, ov[t]);
+            if constexpr (!ROWS) store(rv, 0, t, ov[t]);
+        }
+        if constexpr (ROWS) {
+            exchange<1>();
+#pragma unroll
+            for (int t = 0; t < TT; ++t) {
+                store(rq, 1, t, oq[t]);
+                store(rk, 0, t, ok[t]);
+                store(rv, 3, t, ov[t]);
+            }
+            __syncthreads();
+            give(rq, 1);
+            give(rk, 0);
+            give(rv, 3);
         }
     }
 }
@@ -827,10 +940,22 @@ hipError_t mix_any(const MixArgs& a, int roles, const MixArgs& states, int n_sta
 // Rule for the kernel of short sequences.  It reads and writes every array once, in the backward pass as well, and a problem is one wave;
 // it has no state, and beyond these sizes the operands do not fit its registers.
 bool is_short(const gleam_linattn_desc& d, bool state) { return !state && d.T <= kShortTokens && d.dk <= kShortWidth && d.dv <= kShortWidth; }
+// Whether four neighbouring heads lie side by side in an array, in whole 16 bytes (so that they are aligned in LDS), and tokens no further
+// apart than the kernel's 24-bit products allow.
+bool side_by_side(const MixTensor& x, int elements16) { return x.share == 1 && x.s.h == x.d && x.d % elements16 == 0 && x.s.t < 1 << 24; }
+template <class T, int TT, int U, bool BWD>
+void launch_short(const MixArgs& a, unsigned groups, hipStream_t st) {
+    const int e = 16 / (int)sizeof(T);
+    const MixRole& r = a.role[BWD ? 2 : 0];           // q and k in any case
+    bool whole = a.H % kShortWaves == 0 && side_by_side(r.q, e) && side_by_side(r.k, e) && side_by_side(a.role[0].k, e) && side_by_side(r.v, e);
+    for (int i = 0; i < (BWD ? 3 : 1); ++i) whole = whole && !a.role[i].out_f32 && side_by_side(a.role[i].o, e);
+    if (whole) hipLaunchKernelGGL((mix_short_kernel<T, TT, U, BWD, true>), dim3(groups), dim3(64 * kShortWaves), 0, st, a);
+    else hipLaunchKernelGGL((mix_short_kernel<T, TT, U, BWD, false>), dim3(groups), dim3(64 * kShortWaves), 0, st, a);
+}
 template <class T, int TT, bool BWD>
 void launch_short(const MixArgs& a, unsigned groups, hipStream_t st) {
-    if (a.dk <= 16 && a.dv <= 16) hipLaunchKernelGGL((mix_short_kernel<T, TT, 1, BWD>), dim3(groups), dim3(64 * kShortWaves), 0, st, a);
-    else hipLaunchKernelGGL((mix_short_kernel<T, TT, 2, BWD>), dim3(groups), dim3(64 * kShortWaves), 0, st, a);
+    if (a.dk <= 16 && a.dv <= 16) launch_short<T, TT, 1, BWD>(a, groups, st);
+    else launch_short<T, TT, 2, BWD>(a, groups, st);
 }
 template <class T, bool BWD>
 hipError_t mix_short(const MixArgs& a, const char* name, hipStream_t st) {

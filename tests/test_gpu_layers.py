@@ -312,13 +312,14 @@ def test_linattn_ragged(T, lengths, state, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("layout", ["tokens", "gaps"])
-@pytest.mark.parametrize("dk,dv", [(16, 16), (8, 8), (5, 3), (25, 25), (12, 30), (32, 32)])
+@pytest.mark.parametrize("dk,dv", [(16, 16), (8, 8), (5, 3), (25, 25), (24, 8), (12, 30), (32, 32)])
 def test_linattn_short_sequences_of_narrow_heads(dk, dv, layout, dtype):
     """Few tokens at many pixels, no state: the tokens of one, two and four tiles, and their ends."""
     for T in (2, 7, 16, 17, 20, 32, 33, 50, 64):
         print("case linattn short", dk, dv, layout, T, dtype, flush=True)
         Mix(1, T, 5, (3, 3, 3, 3), dk, dv, dtype, layout, state=False).check()
         Mix(3, T, 3, (4, 2, 1, 4), dk, dv, dtype, layout, lengths=[T, 0, T // 2], state=False).check()
+        Mix(3, T, 2, (8, 8, 8, 8), dk, dv, dtype, layout, lengths=[T, 0, T // 2], state=False).check()
 
 
 def test_linattn_short_sequences_without_memory():
