@@ -339,33 +339,35 @@ def _dtype_code(dtype) -> int:
 _DTYPES = []
 
 
-def _array(t, code: int, count: int, what: str) -> Optional[int]:
-    """Address of a device array of `count` elements of type code 0 / 1 (2: int32, 3: int64 words); strides are the description's."""
-    if t is None or isinstance(t, int):
-        return t
+def _types():
+    """torch types of the codes 0, 1 (activations), 2 (lengths), 3 (counters)."""
     if not _DTYPES:
         import torch
         _DTYPES.extend((torch.float32, torch.bfloat16, torch.int32, torch.int64))
-    if t.dtype is not _DTYPES[code] or t.numel() != count or not t.is_cuda:
-        raise ValueError(f"{what}: {t.numel()} elements of {t.dtype} on {t.device}, the description has {count} of {_DTYPES[code]} on the GPU")
-    return t.data_ptr()
+    return _DTYPES
 
 
 def _flat(t, code: int, count: int, what: str) -> Optional[int]:
-    if t is not None and not isinstance(t, int) and not t.is_contiguous():
-        raise ValueError(f"{what} must be contiguous")
-    return _array(t, code, count, what)
+    """Address of a contiguous device array of `count` elements of type code 0 / 1 (2: int32, 3: int64 words)."""
+    if t is None or type(t) is int:
+        return t
+    if t.dtype is not _types()[code] or t.numel() != count or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what}: {t.numel()} elements of {t.dtype} on {t.device} with strides {t.stride()}, {count} contiguous ones of "
+                         f"{_types()[code]} on the GPU expected")
+    return t.data_ptr()
 
 
 def _rows(t, code: int, rows: int, n: int, ld: int, what: str) -> Optional[int]:
     """A rows x n array with `ld` elements from row to row: contiguous (ld = n) of any shape, or two-dimensional with that stride."""
-    if t is not None and not isinstance(t, int):
-        if t.is_contiguous():
-            if ld != n and rows > 1:
-                raise ValueError(f"{what} is contiguous, the description has {ld} elements from row to row of {n}")
-        elif t.shape != (rows, n) or (n > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) != ld):
-            raise ValueError(f"{what}: shape {tuple(t.shape)} with strides {t.stride()}, the description has {rows} rows of {n}, {ld} apart")
-    return _array(t, code, rows * n, what)
+    if t is None or type(t) is int:
+        return t
+    if ld == n and t.is_contiguous():
+        return _flat(t, code, rows * n, what)
+    if (t.shape != (rows, n) or (n > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) != ld) or t.dtype is not _types()[code] or
+            not t.is_cuda):
+        raise ValueError(f"{what}: shape {tuple(t.shape)} with strides {t.stride()} of {t.dtype} on {t.device}, the description has {rows} rows "
+                         f"of {n}, {ld} apart, of {_types()[code]} on the GPU")
+    return t.data_ptr()
 
 
 def make_layer_norm(dtype, rows, n, eps=1e-5, ld=None, ld_out=None) -> gleam_layer_norm_desc:
@@ -434,15 +436,28 @@ def make_linattn(q, k, v, o, scale=1.0) -> gleam_linattn_desc:
                               *(gleam_seq_strides(*t.stride()[:4]) for t in (q, k, v, o)))
 
 
-def _seq(t, desc, s: gleam_seq_strides, heads: int, width: int, what: str) -> Optional[int]:
-    if t is not None and not isinstance(t, int):
-        if t.shape != (desc.B, desc.T, desc.P, heads, width):
-            raise ValueError(f"{what}: shape {tuple(t.shape)}, the description has {(desc.B, desc.T, desc.P, heads, width)}")
-        got = t.stride()
-        if got != (s.b, s.t, s.p, s.h, 1) and any(n > 1 and x != y for n, x, y in zip(t.shape, got, (s.b, s.t, s.p, s.h, 1))):
-            raise ValueError(f"{what}: strides {got}, the description has {(s.b, s.t, s.p, s.h, 1)}")
-        return _array(t, desc.dtype, t.numel(), what)
-    return t
+def _want(desc):
+    """What the arrays of a call have to be: {name: (shape, strides, type)} of q, k, v and o, kept with the description."""
+    want = getattr(desc, "_want", None)
+    if want is None:
+        want = {}
+        for name, heads, width in (("q", desc.q_heads, desc.dk), ("k", desc.k_heads, desc.dk), ("v", desc.v_heads, desc.dv), ("o", desc.heads, desc.dv)):
+            s = getattr(desc, name)
+            want[name] = ((desc.B, desc.T, desc.P, heads, width), (s.b, s.t, s.p, s.h, 1), _types()[desc.dtype])
+        desc._want = want
+    return want
+
+
+def _seq(t, want, what: str) -> Optional[int]:
+    if t is None or type(t) is int:
+        return t
+    shape, strides, dtype = want
+    got = t.stride()
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or (
+            got != strides and any(n > 1 and x != y for n, x, y in zip(shape, got, strides))):
+        raise ValueError(f"{what}: shape {tuple(t.shape)} with strides {got} of {t.dtype} on {t.device}, the description has {shape} with strides "
+                         f"{strides} of {dtype} on the GPU")
+    return t.data_ptr()
 
 
 def gleam_linattn_workspace_bytes(desc):
@@ -453,25 +468,23 @@ def gleam_linattn_workspace_bytes(desc):
 
 
 def gleam_linattn_fwd(desc, q, k, v, log_decay, lengths, state_in, o, state_out, ws, stream=None):
-    H, dk, dv = desc.heads, desc.dk, desc.dv
-    state = desc.B * desc.P * H * dk * dv
-    _check(lib().gleam_linattn_fwd(C.byref(desc), _seq(q, desc, desc.q, desc.q_heads, dk, "q"), _seq(k, desc, desc.k, desc.k_heads, dk, "k"),
-                                   _seq(v, desc, desc.v, desc.v_heads, dv, "v"), _flat(log_decay, 0, H, "log_decay"),
-                                   _flat(lengths, 2, desc.B, "lengths"), _flat(state_in, 0, state, "state_in"),
-                                   _seq(o, desc, desc.o, H, dv, "o"), _flat(state_out, 0, state, "state_out"), _ptr(ws), _nbytes(ws),
-                                   _stream(stream)), "gleam_linattn_fwd")
+    H, want = desc.heads, _want(desc)
+    state = desc.B * desc.P * H * desc.dk * desc.dv
+    _check(lib().gleam_linattn_fwd(C.byref(desc), _seq(q, want["q"], "q"), _seq(k, want["k"], "k"), _seq(v, want["v"], "v"),
+                                   _flat(log_decay, 0, H, "log_decay"), _flat(lengths, 2, desc.B, "lengths"),
+                                   _flat(state_in, 0, state, "state_in"), _seq(o, want["o"], "o"), _flat(state_out, 0, state, "state_out"),
+                                   _ptr(ws), _nbytes(ws), _stream(stream)), "gleam_linattn_fwd")
 
 
 def gleam_linattn_bwd(desc, q, k, v, log_decay, lengths, state_in, g_o, g_state_out, g_q, g_k, g_v, g_state_in, ws, stream=None):
-    H, dk, dv = desc.heads, desc.dk, desc.dv
-    state = desc.B * desc.P * H * dk * dv
-    _check(lib().gleam_linattn_bwd(C.byref(desc), _seq(q, desc, desc.q, desc.q_heads, dk, "q"), _seq(k, desc, desc.k, desc.k_heads, dk, "k"),
-                                   _seq(v, desc, desc.v, desc.v_heads, dv, "v"), _flat(log_decay, 0, H, "log_decay"),
-                                   _flat(lengths, 2, desc.B, "lengths"), _flat(state_in, 0, state, "state_in"),
-                                   _seq(g_o, desc, desc.o, H, dv, "g_o"), _flat(g_state_out, 0, state, "g_state_out"),
-                                   _seq(g_q, desc, desc.q, desc.q_heads, dk, "g_q"), _seq(g_k, desc, desc.k, desc.k_heads, dk, "g_k"),
-                                   _seq(g_v, desc, desc.v, desc.v_heads, dv, "g_v"), _flat(g_state_in, 0, state, "g_state_in"),
-                                   _ptr(ws), _nbytes(ws), _stream(stream)), "gleam_linattn_bwd")
+    H, want = desc.heads, _want(desc)
+    state = desc.B * desc.P * H * desc.dk * desc.dv
+    _check(lib().gleam_linattn_bwd(C.byref(desc), _seq(q, want["q"], "q"), _seq(k, want["k"], "k"), _seq(v, want["v"], "v"),
+                                   _flat(log_decay, 0, H, "log_decay"), _flat(lengths, 2, desc.B, "lengths"),
+                                   _flat(state_in, 0, state, "state_in"), _seq(g_o, want["o"], "g_o"),
+                                   _flat(g_state_out, 0, state, "g_state_out"), _seq(g_q, want["q"], "g_q"), _seq(g_k, want["k"], "g_k"),
+                                   _seq(g_v, want["v"], "g_v"), _flat(g_state_in, 0, state, "g_state_in"), _ptr(ws), _nbytes(ws),
+                                   _stream(stream)), "gleam_linattn_bwd")
 
 
 def gleam_profile_begin():

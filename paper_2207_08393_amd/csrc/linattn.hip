@@ -840,36 +840,84 @@ __global__ __launch_bounds__(256) void mix_share_kernel(const float* __restrict_
     put_f32((T*)out + b * x.s.b + t * x.s.t + p * x.s.p + h * x.s.h + c, s);
 }
 
-// One token: S' = e^a S + k v^T, o = scale q S'.  A workgroup has a problem; a thread has column c of dv and every R-th row.
-constexpr int kStepThreads = 256;
+// One token: S' = e^a S + k v^T, o = scale q S'.  Bound by the state, read once and written once.  A workgroup has a problem; a thread
+// has four columns of dv and every R-th row of dk, kStepRows of them on their way at a time, the first before it waits for q, k and v.
+constexpr int kStepThreads = 256, kStepRows = 8;
 template <class T>
 __global__ __launch_bounds__(kStepThreads) void mix_step_kernel(MixArgs args) {
     const MixRole& a = args.role[0];
-    __shared__ float sq[128], sk[128], red[kStepThreads];
+    __shared__ float sq[128], sk[128];
+    __shared__ floatx4 red[kStepThreads];
     const Problem r = problem_of(args, blockIdx.x);
     const T *gq = base_of<T>(a.q, r), *gk = base_of<T>(a.k, r), *gv = base_of<T>(a.v, r);
     const int tid = threadIdx.x, dk = a.k.d, dv = a.v.d;
     const bool live = r.len > 0;
+    const int quads = (dv + 3) / 4, log_w = quads <= 1 ? 0 : 32 - __clz(quads - 1), row0 = tid >> log_w, rows = kStepThreads >> log_w;
+    const int c = 4 * (tid & ((1 << log_w) - 1)), width = dv - c < 4 ? dv - c : 4;   // columns that exist, none or fewer: <= 0
+    const long long base = r.index * dk * dv + c;
+    const float* in = a.state_in ? a.state_in + base : nullptr;
+    floatx4 s[kStepRows];
+    auto fetch = [&](int first) {
+#pragma unroll
+        for (int k = 0; k < kStepRows; ++k) {
+            const int row = first + k * rows;
+            s[k] = floatx4{0.f, 0.f, 0.f, 0.f};
+            if (!in || row >= dk) continue;
+            if (width == 4) {
+                __builtin_memcpy(&s[k], in + row * dv, 16);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+                    if (i < width) s[k][i] = in[row * dv + i];
+            }
+        }
+    };
+    fetch(row0);
     if (tid < dk) {
         sq[tid] = live ? to_f32(gq[tid]) : 0.f;
         sk[tid] = live ? to_f32(gk[tid]) : 0.f;
     }
+    floatx4 v{0.f, 0.f, 0.f, 0.f}, o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < width && live) v[i] = to_f32(gv[c + i]);
+    const float whole = live ? decay_of(args.log_decay[r.h], 1) : 1.f;
     __syncthreads();
-    const int width = dv <= 32 ? 32 : dv <= 64 ? 64 : 128, c = tid % width, rows = kStepThreads / width;
-    const float whole = live ? decay_of(args.log_decay[r.h], 1) : 1.f, v = c < dv && live ? to_f32(gv[c]) : 0.f;
-    const long long base = r.index * dk * dv;
-    float o = 0.f;
-    if (c < dv)
-        for (int row = tid / width; row < dk; row += rows) {
-            const float s = (a.state_in ? a.state_in[base + (long long)row * dv + c] : 0.f) * whole + sk[row] * v;
-            o += sq[row] * s;
-            if (a.state_out) a.state_out[base + (long long)row * dv + c] = s;
+    for (int first = row0; first < dk; first += kStepRows * rows) {
+        if (first != row0) fetch(first);
+#pragma unroll
+        for (int k = 0; k < kStepRows; ++k) {
+            const int row = first + k * rows;
+            if (row >= dk) break;
+            s[k] = s[k] * whole + v * sk[row];
+            o += s[k] * sq[row];
+            if (!a.state_out) continue;
+            float* out = a.state_out + base + row * dv;
+            if (width == 4) {
+                __builtin_memcpy(out, &s[k], 16);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+                    if (i < width) out[i] = s[k][i];
+            }
         }
+    }
     red[tid] = o;
     __syncthreads();
+    // the sum over the threads of a column quad in two steps, then one thread an element
+    const int w = 1 << log_w;
+    if (tid < 4 * w && rows >= 4) {
+        o = red[tid];
+        for (int k = tid + 4 * w; k < kStepThreads; k += 4 * w) o += red[k];
+    }
+    __syncthreads();
+    if (tid < 4 * w) red[tid] = o;
+    __syncthreads();
     if (tid < dv) {
-        for (int k = 1; k < rows; ++k) o += red[k * width + tid];
-        put_f32((T*)a.out + r.b * a.o.s.b + r.p * a.o.s.p + r.h * a.o.s.h + tid, live ? o * a.out_scale : 0.f);
+        const int quad = tid >> 2, i = tid & 3;
+        float e = red[quad][i];
+        for (int k = 1; k < 4 && k < rows; ++k) e += red[k * w + quad][i];
+        put_f32((T*)a.out + r.b * a.o.s.b + r.p * a.o.s.p + r.h * a.o.s.h + tid, live ? e * a.out_scale : 0.f);
     }
 }
 

@@ -16,7 +16,6 @@ namespace gleam {
 namespace {
 
 constexpr int kNormThreads = 256;
-constexpr int kNormGrid = 2048;   // workgroups at most: every one walks rows and keeps gamma, beta and its sums
 
 template <class T>
 constexpr int vec_of() { return 16 / (int)sizeof(T); }
@@ -24,58 +23,63 @@ constexpr int vec_of() { return 16 / (int)sizeof(T); }
 template <int LANES>
 constexpr int threads_of() { return LANES > 64 ? LANES : kNormThreads; }
 
-// Sum over a team of LANES lanes, the same value in all of them.  A team wider than a wave is the workgroup; `red` is then LDS for
-// one float2 a wave, and the barrier in front makes its last use over.
-template <int LANES>
-__device__ __forceinline__ float2 team_sum(float2 v, float2* red) {
+// Sums over a team of LANES lanes, the same values in all of them.  A team wider than a wave is the workgroup; `red` is then LDS for
+// N floats a wave, and the barrier in front makes its last use over.
+template <int LANES, int N>
+__device__ __forceinline__ void team_sum(float (&v)[N], float* red) {
 #pragma unroll
-    for (int o = (LANES < 64 ? LANES : 64) / 2; o > 0; o >>= 1) {
-        v.x += __shfl_xor(v.x, o);
-        v.y += __shfl_xor(v.y, o);
-    }
+    for (int o = (LANES < 64 ? LANES : 64) / 2; o > 0; o >>= 1)
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], o);
     if constexpr (LANES > 64) {
+        constexpr int W = LANES / 64;
         __syncthreads();
-        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = red[0];
+        if ((threadIdx.x & 63) == 0)
 #pragma unroll
-        for (int w = 1; w < LANES / 64; ++w) {
-            v.x += red[w].x;
-            v.y += red[w].y;
+            for (int k = 0; k < N; ++k) red[k * W + (threadIdx.x >> 6)] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            v[k] = red[k * W];
+#pragma unroll
+            for (int w = 1; w < W; ++w) v[k] += red[k * W + w];
         }
     }
-    return v;
 }
 
-// The columns of a lane's vectors: vector j begins at column (lane + j LANES) VE.  The row's last vector is moved back to end at n;
-// its first elements, [0, lo), are then the vector's before it and stay out of sums (their results are written twice, the same
-// bits).  Rows shorter than a vector: hi < VE, element by element.
+// The columns of one of a lane's vectors, the same in every row.  The row's last vector is moved back to end with the row; its first
+// elements are then those of the vector before it and stay out of sums (keep = 0; their results are written twice, the same bits).
+// Rows shorter than a vector: hi < VE, element by element.
 template <int VE>
 struct Columns {
-    long long col;
-    int lo, hi;
-    __device__ __forceinline__ Columns(long long unit, long long n) {
+    int col, hi;
+    float keep[VE];
+    __device__ __forceinline__ void set(int unit, int n) {
         col = unit * VE;
-        lo = 0;
         hi = col < n ? VE : 0;
+        int lo = 0;
         if (hi && col + VE > n) {
             if (n >= VE) {
-                lo = (int)(col + VE - n);
+                lo = col + VE - n;
                 col = n - VE;
             } else {
-                hi = (int)n;
+                hi = n;
             }
         }
+        if (!hi) col = 0;
+#pragma unroll
+        for (int i = 0; i < VE; ++i) keep[i] = i >= lo && i < hi ? 1.f : 0.f;
     }
 };
+// Lanes without columns read the row's first elements, or nothing where a row is shorter than a vector; they count for nothing.
 template <class T, int VE>
-__device__ __forceinline__ void load_cols(const T* row, const Columns<VE>& c, Pack<T, VE>& p) {
-    if (c.hi == VE) {
+__device__ __forceinline__ void load_cols(const T* row, const Columns<VE>& c, bool narrow, Pack<T, VE>& p) {
+    if (!narrow) {
         p.load(row + c.col);
     } else {
         float v[VE];
 #pragma unroll
-        for (int i = 0; i < VE; ++i) v[i] = i < c.hi ? to_f32(row[c.col + i]) : 0.f;
+        for (int i = 0; i < VE; ++i) v[i] = i < c.hi ? to_f32(row[i]) : 0.f;
         p.set(v);
     }
 }
@@ -94,7 +98,16 @@ __device__ __forceinline__ void store_cols(T* row, const Columns<VE>& c, const f
 template <int VE>
 __device__ __forceinline__ void load_param(const float* p, const Columns<VE>& c, float fallback, float* v) {
 #pragma unroll
-    for (int i = 0; i < VE; ++i) v[i] = p && i < c.hi ? p[c.col + i] : fallback;
+    for (int i = 0; i < VE; ++i) v[i] = fallback;
+    if (!p) return;
+    if (c.hi == VE) {
+#pragma unroll
+        for (int i = 0; i < VE; i += 4) __builtin_memcpy(v + i, p + c.col + i, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VE; ++i)
+            if (i < c.hi) v[i] = p[c.col + i];
+    }
 }
 
 struct NormArgs {
@@ -107,60 +120,79 @@ struct NormArgs {
     float eps;
 };
 
+// A workgroup walks rows.  The next row is on its way while one is computed on, where registers allow it, and the parameters
+// stay in registers up to kKept of them a lane (more are read again from the cache for every row).
+constexpr int kKept = 16;
+
 template <class T, int LANES, int NV>
 __global__ __launch_bounds__(threads_of<LANES>()) void norm_fwd_kernel(NormArgs a) {
     constexpr int VE = vec_of<T>(), TEAMS = threads_of<LANES>() / LANES;
-    __shared__ float2 red[LANES > 64 ? LANES / 64 : 1];
-    const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
-    const float inv_n = 1.f / (float)a.n;
+    constexpr bool kKeep = NV * VE <= kKept;
+    __shared__ float red[LANES > 64 ? LANES / 64 : 1];
+    const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES, n = (int)a.n;
+    const bool narrow = n < VE;
+    const float inv_n = 1.f / (float)n;
     const T* x = (const T*)a.x;
     T* y = (T*)a.out;
-    // a row beyond the last is computed on zeros and not written, so that every lane of a wave takes part in the sums
-    for (long long r0 = (long long)blockIdx.x * TEAMS; r0 < a.rows; r0 += (long long)gridDim.x * TEAMS) {
-        const long long row = r0 + team;
-        const bool there = row < a.rows;
-        const float pivot = there ? to_f32(x[row * a.ld_x]) : 0.f;
-        float v[NV][VE];
-        float2 s = {0.f, 0.f};
+    Columns<VE> cols[NV];
+    float gm[NV][VE], bt[NV][VE];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const Columns<VE> c(lane + j * LANES, a.n);
-            if (there && c.hi) {
-                Pack<T, VE> p;
-                load_cols(x + row * a.ld_x, c, p);
-#pragma unroll
-                for (int i = 0; i < VE; ++i) {
-                    v[j][i] = p.get(i);
-                    s.x += i >= c.lo && i < c.hi ? v[j][i] - pivot : 0.f;
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < VE; ++i) v[j][i] = 0.f;
-            }
+    for (int j = 0; j < NV; ++j) {
+        cols[j].set(lane + j * LANES, n);
+        if (kKeep) {
+            load_param(a.gamma, cols[j], 1.f, gm[j]);
+            load_param(a.beta, cols[j], 0.f, bt[j]);
         }
-        const float mean = pivot + team_sum<LANES>(s, red).x * inv_n;
-        s.x = 0.f;
+    }
+    const long long step = (long long)gridDim.x * TEAMS;
+    // a row beyond the last is read as the last and not written, so that every lane of a wave takes part in the sums
+    auto there = [&](long long row) { return row < a.rows ? row : a.rows - 1; };
+    long long row = (long long)blockIdx.x * TEAMS + team;
+    Pack<T, VE> next[NV];
+    T next_pivot = x[there(row) * a.ld_x];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const Columns<VE> c(lane + j * LANES, a.n);
+    for (int j = 0; j < NV; ++j) load_cols(x + there(row) * a.ld_x, cols[j], narrow, next[j]);
+    for (long long first = (long long)blockIdx.x * TEAMS; first < a.rows; first += step, row += step) {
+        const float pivot = to_f32(next_pivot);
+        float v[NV][VE], s[1] = {0.f};
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VE; ++i) v[j][i] = next[j].get(i);
+        if (first + step < a.rows) {
+            const T* p = x + there(row + step) * a.ld_x;
+            next_pivot = p[0];
+#pragma unroll
+            for (int j = 0; j < NV; ++j) load_cols(p, cols[j], narrow, next[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VE; ++i) s[0] += (v[j][i] - pivot) * cols[j].keep[i];
+        team_sum<LANES>(s, red);
+        const float mean = pivot + s[0] * inv_n;
+        s[0] = 0.f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int i = 0; i < VE; ++i) {
                 v[j][i] -= mean;
-                s.x += i >= c.lo && i < c.hi ? v[j][i] * v[j][i] : 0.f;
+                s[0] += v[j][i] * v[j][i] * cols[j].keep[i];
             }
-        }
-        const float rstd = 1.f / sqrtf(team_sum<LANES>(s, red).x * inv_n + a.eps);
-        if (!there) continue;
+        team_sum<LANES>(s, red);
+        const float rstd = 1.f / sqrtf(s[0] * inv_n + a.eps);
+        if (row >= a.rows) continue;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const Columns<VE> c(lane + j * LANES, a.n);
-            if (!c.hi) continue;
-            float gm[VE], bt[VE], o[VE];
-            load_param(a.gamma, c, 1.f, gm);
-            load_param(a.beta, c, 0.f, bt);
+            if (!cols[j].hi) continue;
+            if (!kKeep) {
+                load_param(a.gamma, cols[j], 1.f, gm[j]);
+                load_param(a.beta, cols[j], 0.f, bt[j]);
+            }
+            float o[VE];
 #pragma unroll
-            for (int i = 0; i < VE; ++i) o[i] = v[j][i] * rstd * gm[i] + bt[i];
-            store_cols(y + row * a.ld_y, c, o);
+            for (int i = 0; i < VE; ++i) o[i] = v[j][i] * rstd * gm[j][i] + bt[j][i];
+            store_cols(y + row * a.ld_y, cols[j], o);
         }
         if (lane == 0) {
             if (a.mean) a.mean[row] = mean;
@@ -172,54 +204,73 @@ __global__ __launch_bounds__(threads_of<LANES>()) void norm_fwd_kernel(NormArgs 
 template <class T, int LANES, int NV>
 __global__ __launch_bounds__(threads_of<LANES>()) void norm_bwd_kernel(NormArgs a) {
     constexpr int VE = vec_of<T>(), TEAMS = threads_of<LANES>() / LANES;
-    __shared__ float2 red[LANES > 64 ? LANES / 64 : 1];
+    constexpr bool kKeep = NV * VE <= kKept, kAhead = NV * VE <= (LANES == 1024 ? 8 : kKept);
+    __shared__ float red[LANES > 64 ? 2 * LANES / 64 : 1];
     __shared__ float fold[TEAMS > 1 ? TEAMS : 1][TEAMS > 1 ? LANES * VE : 1];
-    const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
-    const float inv_n = 1.f / (float)a.n;
+    const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES, n = (int)a.n;
+    const bool narrow = n < VE;
+    const float inv_n = 1.f / (float)n;
     const T *x = (const T*)a.x, *g = (const T*)a.g;
     T* gx = (T*)a.out;
-    float dg[NV][VE] = {}, db[NV][VE] = {};
-    for (long long r0 = (long long)blockIdx.x * TEAMS; r0 < a.rows; r0 += (long long)gridDim.x * TEAMS) {
-        const long long row = r0 + team;
-        const bool there = row < a.rows;
-        const float mean = there ? a.mean_in[row] : 0.f, rstd = there ? a.rstd_in[row] : 0.f;
-        float xh[NV][VE], gg[NV][VE];
-        float2 s = {0.f, 0.f};
+    Columns<VE> cols[NV];
+    float gm[NV][VE], dg[NV][VE] = {}, db[NV][VE] = {};
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        cols[j].set(lane + j * LANES, n);
+        if (kKeep) load_param(a.gamma, cols[j], 1.f, gm[j]);
+    }
+    const long long step = (long long)gridDim.x * TEAMS;
+    auto there = [&](long long row) { return row < a.rows ? row : a.rows - 1; };
+    long long row = (long long)blockIdx.x * TEAMS + team;
+    Pack<T, VE> nx[NV], ng[NV];
+    float next_mean, next_rstd;
+    auto fetch = [&](long long at) {
+        next_mean = a.mean_in[at];
+        next_rstd = a.rstd_in[at];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const Columns<VE> c(lane + j * LANES, a.n);
-            if (there && c.hi) {
-                Pack<T, VE> px, pg;
-                load_cols(x + row * a.ld_x, c, px);
-                load_cols(g + row * a.ld_y, c, pg);
-                float gm[VE];
-                load_param(a.gamma, c, 1.f, gm);
+            load_cols(x + at * a.ld_x, cols[j], narrow, nx[j]);
+            load_cols(g + at * a.ld_y, cols[j], narrow, ng[j]);
+        }
+    };
+    if (kAhead) fetch(there(row));
+    for (long long first = (long long)blockIdx.x * TEAMS; first < a.rows; first += step, row += step) {
+        if (!kAhead) fetch(there(row));
+        const float mean = next_mean, rstd = next_rstd, counts = row < a.rows ? 1.f : 0.f;
+        float xh[NV][VE], gg[NV][VE], s[2] = {0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < VE; ++i) {
-                    const bool mine = i >= c.lo && i < c.hi;
-                    xh[j][i] = (px.get(i) - mean) * rstd;
-                    const float gy = pg.get(i);
-                    gg[j][i] = gy * gm[i];
-                    dg[j][i] += mine ? gy * xh[j][i] : 0.f;
-                    db[j][i] += mine ? gy : 0.f;
-                    s.x += mine ? gg[j][i] : 0.f;
-                    s.y += mine ? gg[j][i] * xh[j][i] : 0.f;
-                }
-            } else {
+        for (int j = 0; j < NV; ++j)
 #pragma unroll
-                for (int i = 0; i < VE; ++i) xh[j][i] = gg[j][i] = 0.f;
+            for (int i = 0; i < VE; ++i) {
+                xh[j][i] = nx[j].get(i);
+                gg[j][i] = ng[j].get(i);
+            }
+        if (kAhead && first + step < a.rows) fetch(there(row + step));
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (!kKeep) load_param(a.gamma, cols[j], 1.f, gm[j]);
+#pragma unroll
+            for (int i = 0; i < VE; ++i) {
+                xh[j][i] = (xh[j][i] - mean) * rstd;
+                const float gy = gg[j][i] * (cols[j].keep[i] * counts);
+                dg[j][i] += gy * xh[j][i];
+                db[j][i] += gy;
+                gg[j][i] *= gm[j][i];
+                const float kept = gy * gm[j][i];
+                s[0] += kept;
+                s[1] += kept * xh[j][i];
             }
         }
-        s = team_sum<LANES>(s, red);
-        if (!there) continue;
+        team_sum<LANES>(s, red);
+        if (row >= a.rows) continue;
+        const float s0 = s[0] * inv_n, s1 = s[1] * inv_n;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const Columns<VE> c(lane + j * LANES, a.n);
-            if (!c.hi) continue;
+            if (!cols[j].hi) continue;
             float o[VE];
 #pragma unroll
-            for (int i = 0; i < VE; ++i) o[i] = rstd * (gg[j][i] - s.x * inv_n - xh[j][i] * (s.y * inv_n));
-            store_cols(gx + row * a.ld_x, c, o);
+            for (int i = 0; i < VE; ++i) o[i] = rstd * (gg[j][i] - s0 - xh[j][i] * s1);
+            store_cols(gx + row * a.ld_x, cols[j], o);
         }
     }
     if (!a.part) return;
@@ -228,7 +279,6 @@ __global__ __launch_bounds__(threads_of<LANES>()) void norm_bwd_kernel(NormArgs 
     for (int k = 0; k < 2; ++k) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const Columns<VE> c(lane + j * LANES, a.n);
             float v[VE];
 #pragma unroll
             for (int i = 0; i < VE; ++i) v[i] = k ? db[j][i] : dg[j][i];
@@ -246,7 +296,7 @@ __global__ __launch_bounds__(threads_of<LANES>()) void norm_bwd_kernel(NormArgs 
             if (team == 0) {
 #pragma unroll
                 for (int i = 0; i < VE; ++i)
-                    if (i >= c.lo && i < c.hi) part[k * a.n + c.col + i] = v[i];
+                    if (cols[j].keep[i] != 0.f) part[k * a.n + cols[j].col + i] = v[i];
             }
         }
     }
@@ -260,6 +310,7 @@ __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float* __restri
     const long long col = (long long)blockIdx.x * 32 + tx;
     float s = 0.f;
     if (col < 2 * n)
+#pragma unroll 8
         for (int w = ty; w < n_part; w += 32) s += part[(long long)w * 2 * n + col];
     red[ty][tx] = s;
     __syncthreads();
@@ -279,21 +330,23 @@ constexpr int kLongThreads = 1024;
 // One workgroup a row, the row read three times (from the cache after the first, up to its size).
 template <class T>
 __global__ __launch_bounds__(kLongThreads) void norm_fwd_long_kernel(NormArgs a) {
-    __shared__ float2 red[kLongThreads / 64];
+    __shared__ float red[kLongThreads / 64];
     const long long row = blockIdx.x;
     const T* x = (const T*)a.x + row * a.ld_x;
     T* y = (T*)a.out + row * a.ld_y;
     const float inv_n = 1.f / (float)a.n;
-    float2 s = {0.f, 0.f};
+    float s[1] = {0.f};
     const float pivot = to_f32(x[0]);
-    for (long long c = threadIdx.x; c < a.n; c += kLongThreads) s.x += to_f32(x[c]) - pivot;
-    const float mean = pivot + team_sum<kLongThreads>(s, red).x * inv_n;
-    s.x = 0.f;
+    for (long long c = threadIdx.x; c < a.n; c += kLongThreads) s[0] += to_f32(x[c]) - pivot;
+    team_sum<kLongThreads>(s, red);
+    const float mean = pivot + s[0] * inv_n;
+    s[0] = 0.f;
     for (long long c = threadIdx.x; c < a.n; c += kLongThreads) {
         const float d = to_f32(x[c]) - mean;
-        s.x += d * d;
+        s[0] += d * d;
     }
-    const float rstd = 1.f / sqrtf(team_sum<kLongThreads>(s, red).x * inv_n + a.eps);
+    team_sum<kLongThreads>(s, red);
+    const float rstd = 1.f / sqrtf(s[0] * inv_n + a.eps);
     for (long long c = threadIdx.x; c < a.n; c += kLongThreads)
         put_f32(y + c, (to_f32(x[c]) - mean) * rstd * (a.gamma ? a.gamma[c] : 1.f) + (a.beta ? a.beta[c] : 0.f));
     if (threadIdx.x == 0) {
@@ -304,21 +357,21 @@ __global__ __launch_bounds__(kLongThreads) void norm_fwd_long_kernel(NormArgs a)
 
 template <class T>
 __global__ __launch_bounds__(kLongThreads) void norm_bwd_long_kernel(NormArgs a) {
-    __shared__ float2 red[kLongThreads / 64];
+    __shared__ float red[2 * kLongThreads / 64];
     const long long row = blockIdx.x;
     const T *x = (const T*)a.x + row * a.ld_x, *g = (const T*)a.g + row * a.ld_y;
     T* gx = (T*)a.out + row * a.ld_x;
     const float inv_n = 1.f / (float)a.n, mean = a.mean_in[row], rstd = a.rstd_in[row];
-    float2 s = {0.f, 0.f};
+    float s[2] = {0.f, 0.f};
     for (long long c = threadIdx.x; c < a.n; c += kLongThreads) {
         const float gg = to_f32(g[c]) * (a.gamma ? a.gamma[c] : 1.f);
-        s.x += gg;
-        s.y += gg * ((to_f32(x[c]) - mean) * rstd);
+        s[0] += gg;
+        s[1] += gg * ((to_f32(x[c]) - mean) * rstd);
     }
-    s = team_sum<kLongThreads>(s, red);
+    team_sum<kLongThreads>(s, red);
     for (long long c = threadIdx.x; c < a.n; c += kLongThreads) {
         const float gg = to_f32(g[c]) * (a.gamma ? a.gamma[c] : 1.f), xh = (to_f32(x[c]) - mean) * rstd;
-        put_f32(gx + c, rstd * (gg - s.x * inv_n - xh * (s.y * inv_n)));
+        put_f32(gx + c, rstd * (gg - s[0] * inv_n - xh * (s[1] * inv_n)));
     }
 }
 
@@ -347,13 +400,15 @@ struct Team {
 Team team_for(const gleam_layer_norm_desc& d) {
     const long long units = (d.n * (d.dtype ? 2 : 4) + 15) / 16;
     for (Team t : {Team{4, 1}, Team{8, 1}, Team{16, 1}, Team{32, 1}, Team{64, 1}, Team{64, 2}, Team{64, 4}, Team{256, 2}, Team{256, 4},
-                   Team{1024, 2}})
+                   Team{512, 3}, Team{1024, 2}})
         if (units <= (long long)t.lanes * t.nv) return t;
     return Team{0, 0};
 }
-int grid_for(const gleam_layer_norm_desc& d, Team t) {
+// Workgroups that walk the rows.  Backward: every one leaves 2 n partial sums, so that there are no more than fill the chip.
+int grid_for(const gleam_layer_norm_desc& d, Team t, bool backward) {
     const long long teams = t.lanes > 64 ? 1 : kNormThreads / t.lanes, wgs = (d.rows + teams - 1) / teams;
-    return (int)(wgs < kNormGrid ? wgs : kNormGrid);
+    const int most = backward ? (t.lanes >= 512 ? 512 : 1024) : 2048;
+    return (int)(wgs < most ? wgs : most);
 }
 int long_parts(const gleam_layer_norm_desc& d) { return (int)(d.rows < 64 ? d.rows : 64); }
 
@@ -370,6 +425,7 @@ void with_team(Team t, F&& f) {
     GLEAM_TEAM(64, 4);
     GLEAM_TEAM(256, 2);
     GLEAM_TEAM(256, 4);
+    GLEAM_TEAM(512, 3);
     GLEAM_TEAM(1024, 2);
 #undef GLEAM_TEAM
 }
@@ -383,7 +439,7 @@ hipError_t forward(const gleam_layer_norm_desc& d, const NormArgs& a, hipStream_
         return hipGetLastError();
     }
     with_team<T>(t, [&](auto L, auto N) {
-        hipLaunchKernelGGL((norm_fwd_kernel<T, L(), N()>), dim3(grid_for(d, t)), dim3(threads_of<L()>()), 0, st, a);
+        hipLaunchKernelGGL((norm_fwd_kernel<T, L(), N()>), dim3(grid_for(d, t, false)), dim3(threads_of<L()>()), 0, st, a);
     });
     return hipGetLastError();
 }
@@ -401,7 +457,7 @@ hipError_t backward(const gleam_layer_norm_desc& d, const NormArgs& a, float* g_
         KernelScope ks("layer_norm_bwd", 8.0 * d.rows * d.n, 3.0 * sizeof(T) * d.rows * d.n, st);
         hipLaunchKernelGGL(norm_bwd_long_kernel<T>, dim3((unsigned)d.rows), dim3(kLongThreads), 0, st, a);
     } else {
-        parts = grid_for(d, t);
+        parts = grid_for(d, t, true);
         KernelScope ks("layer_norm_bwd", 12.0 * d.rows * d.n, 3.0 * sizeof(T) * d.rows * d.n, st);
         with_team<T>(t, [&](auto L, auto N) {
             hipLaunchKernelGGL((norm_bwd_kernel<T, L(), N()>), dim3(parts), dim3(threads_of<L()>()), 0, st, a);
@@ -436,7 +492,7 @@ hipError_t layer_norm_forward(const gleam_layer_norm_desc& d, const void* x, con
 
 size_t layer_norm_ws_bytes(const gleam_layer_norm_desc& d) {
     const Team t = team_for(d);
-    return (size_t)(t.lanes ? grid_for(d, t) : long_parts(d)) * 2 * (size_t)d.n * sizeof(float);
+    return (size_t)(t.lanes ? grid_for(d, t, true) : long_parts(d)) * 2 * (size_t)d.n * sizeof(float);
 }
 
 hipError_t layer_norm_backward(const gleam_layer_norm_desc& d, const void* x, const float* gamma, const float* mean, const float* rstd,
