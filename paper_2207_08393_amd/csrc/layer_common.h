@@ -15,6 +15,7 @@ __device__ __forceinline__ void put_f32(unsigned short* p, float v) { *p = (unsi
 template <class T, int N>
 struct Pack {
     static constexpr int kWords = N * (int)sizeof(T) / 4;
+    static_assert(kWords * 4 == N * (int)sizeof(T), "whole words");
     unsigned w[kWords];
     __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(w, p, sizeof(w)); }
     __device__ __forceinline__ void store(T* p) const { __builtin_memcpy(p, w, sizeof(w)); }

@@ -52,6 +52,7 @@ struct MixArgs {
     const float* log_decay;             // [H]
     const int* lengths;                 // [B] or null
     int n_seg, seg_chunks;
+    unsigned groups, roles, near_groups;   // of a launch: workgroups of problems, passes, groups that stand next to each other
 };
 size_t linattn_fwd_ws_bytes(const gleam_linattn_desc& d);
 size_t linattn_bwd_ws_bytes(const gleam_linattn_desc& d);

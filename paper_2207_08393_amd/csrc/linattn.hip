@@ -265,12 +265,31 @@ __device__ __forceinline__ const T* base_of(const MixTensor& x, const Problem& r
     return (const T*)x.p + r.b * x.s.b + r.p * x.s.p + (long long)(r.h / x.share) * x.s.h;
 }
 
-// STATES: only the sum of k (x) v over segment blockIdx.y, for the scan over segments; seg_state slot blockIdx.y + 1.
+// What a workgroup works on.  Workgroups are dealt to the 8 XCDs by their number, and each XCD has its own L2, so an XCD gets a
+// contiguous range of the work: heads that share keys, and the passes of a backward call over the same tokens, run next to each other on
+// one XCD and read from its L2 what the first of them fetched.
+struct Work {
+    long long group;    // of S::kProblems problems
+    int seg, role;
+    bool none;
+};
+__device__ __forceinline__ Work work_of(const MixArgs& a, unsigned groups, unsigned segs, unsigned roles) {
+    const unsigned total = groups * segs * roles, per = (total + 7) / 8, i = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    Work w;
+    w.none = blockIdx.x >> 3 >= per || i >= total;
+    const unsigned inner = a.near_groups, outer = i / (inner * segs * roles), in = i - outer * (inner * segs * roles);
+    const unsigned in_seg = in / (inner * roles), rest = in - in_seg * (inner * roles);
+    w.role = rest / inner;
+    w.group = (long long)outer * inner + (rest - w.role * inner);
+    w.seg = in_seg;
+    return w;
+}
+
+// STATES: only the sum of k (x) v over a segment, for the scan over segments; slot seg + 1 of seg_state.
 // PARTS: numbers a decayed value is the sum of on its way into the state (bfloat16: 3 give 24 bits, for a state that is handed out; 2
 // where the state only feeds outputs, which are rounded to 8 bits).
 template <class T, int D, bool STATES, int PARTS>
 __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs args) {
-    const MixRole& a = args.role[blockIdx.z];
     typedef Shape<T, D> S;
     typedef Mma<T> M;
     typedef typename M::Frag Frag;
@@ -288,10 +307,14 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs
     const int tid = S::kProblems == 1 ? threadIdx.x : threadIdx.x & 63;
     const int lane = tid & 63, m = lane & 15, g = lane >> 4;
     const int wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
-    const long long index = (long long)blockIdx.x * S::kProblems + slot;
-    if (index >= args.B * args.P * args.H) return;             // several problems a workgroup: a wave each, and no barriers
+    const Work work = work_of(args, args.groups, STATES ? args.n_seg - 1 : args.n_seg, args.roles);
+    if (work.none) return;
+    const MixRole& a = args.role[work.role];
+    const long long index = work.group * S::kProblems + slot;
+    if (index >= args.B * args.P * args.H) return;    // several problems a workgroup: a wave each, and no barriers
     const Problem r = problem_of(args, index);
-    const int seg = blockIdx.y;
+    // passes in reverse count segments from the end: those over the same tokens stand next to each other
+    const int seg = a.reverse ? (STATES ? args.n_seg - 2 : args.n_seg - 1) - work.seg : work.seg;
     const int c_begin = seg * args.seg_chunks;
     int c_end = (r.len + L - 1) / L;
     if (c_end > c_begin + args.seg_chunks) c_end = c_begin + args.seg_chunks;
@@ -823,21 +846,27 @@ __global__ __launch_bounds__(256) void mix_scan_kernel(MixArgs args, int chunk) 
     }
 }
 
-// Sum over the output heads that share a head: float32 [B][T][P][H][d] to x.  One thread an element.
-template <class T>
-__global__ __launch_bounds__(256) void mix_share_kernel(const float* __restrict__ part, MixTensor x, void* out, long long T_, long long P, int H,
+// Sum over the output heads that share a head: float32 [B][T][P][H][d] to x.  A thread has N neighbouring elements.
+template <class T, int N>
+__global__ __launch_bounds__(256) void mix_share_kernel(const float* __restrict__ part, MixTensor x, void* out, unsigned T_, unsigned P, unsigned H,
                                                         long long n) {
     const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
     if (at >= n) return;
-    const int c = (int)(at % x.d);
-    long long rest = at / x.d;
-    const int heads = H / x.share, h = (int)(rest % heads);
-    rest /= heads;
-    const long long p = rest % P, bt = rest / P, t = bt % T_, b = bt / T_;
-    const float* src = part + ((bt * P + p) * H + (long long)h * x.share) * x.d + c;
-    float s = src[0];
-    for (int k = 1; k < x.share; ++k) s += src[(long long)k * x.d];
-    put_f32((T*)out + b * x.s.b + t * x.s.t + p * x.s.p + h * x.s.h + c, s);
+    const unsigned per = x.d / N, heads = H / x.share;
+    const long long row = at / (per * heads);         // (b T + t) P + p
+    const unsigned in = (unsigned)(at - row * (per * heads)), h = in / per, c = (in - h * per) * N;
+    const long long bt = P == 1 ? row : row / P, b = bt / T_;
+    const float* src = part + (row * H + (long long)h * x.share) * x.d + c;
+    float s[N], v[N];
+    __builtin_memcpy(s, src, sizeof(s));
+    for (int k = 1; k < x.share; ++k) {
+        __builtin_memcpy(v, src + (long long)k * x.d, sizeof(v));
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] += v[i];
+    }
+    T* dst = (T*)out + b * x.s.b + (bt - b * T_) * x.s.t + (row - bt * P) * x.s.p + h * x.s.h + c;
+    if constexpr (N == 1) put_f32(dst, s[0]);
+    else store_part<T, N>(dst, N, s);
 }
 
 // One token: S' = e^a S + k v^T, o = scale q S'.  Bound by the state, read once and written once.  A workgroup has a problem; a thread
@@ -950,17 +979,27 @@ size_t share_bytes(const gleam_linattn_desc& d, int heads, int width) {
     return heads == d.heads ? 0 : align_up((size_t)(d.B * d.T * d.P * d.heads) * width * sizeof(float));
 }
 
+// Workgroups of a launch: the ranges of the 8 XCDs are of one length.
+unsigned blocks_of(unsigned groups, unsigned segs, unsigned roles) { return (groups * segs * roles + 7) / 8 * 8; }
+
 // `roles` passes side by side; `states` of them first, over segments, where there are several.
 template <class T, int D, int PARTS>
-hipError_t mix_passes(const MixArgs& a, int roles, const MixArgs& states, int n_states, const char* name, hipStream_t st) {
+hipError_t mix_passes(MixArgs a, int roles, MixArgs states, int n_states, const char* name, hipStream_t st) {
     typedef Shape<T, D> S;
     const long long problems = a.B * a.P * a.H;
     const unsigned groups = (unsigned)((problems + S::kProblems - 1) / S::kProblems);
+    a.groups = states.groups = groups;
+    a.roles = roles;
+    states.roles = n_states;
+    // workgroups that share keys or values stand next to each other
+    int share = 1;
+    for (int i = 0; i < roles; ++i) share = share > a.role[i].k.share ? share : a.role[i].k.share;
+    a.near_groups = states.near_groups = S::kProblems == 1 && groups % share == 0 ? share : 1;
     const double tokens = (double)problems * a.T, flops = 2.0 * tokens * a.dk * a.dv, bytes = tokens * sizeof(T) * (a.dk + a.dv);
     if (a.n_seg > 1) {
         {
             KernelScope ks("linattn_segments", n_states * flops, n_states * bytes, st);
-            hipLaunchKernelGGL((mix_kernel<T, D, true, PARTS>), dim3(groups, a.n_seg - 1, n_states), dim3(S::kThreads), 0, st, states);
+            hipLaunchKernelGGL((mix_kernel<T, D, true, PARTS>), dim3(blocks_of(groups, a.n_seg - 1, n_states)), dim3(S::kThreads), 0, st, states);
         }
         const double floats = (double)n_states * problems * a.n_seg * S::kStateFloats;
         KernelScope ks("linattn_scan", 2.0 * floats, 8.0 * floats, st);
@@ -968,7 +1007,7 @@ hipError_t mix_passes(const MixArgs& a, int roles, const MixArgs& states, int n_
         hipLaunchKernelGGL(mix_scan_kernel<D>, dim3(blocks, 1, n_states), dim3(256), 0, st, states, S::kL);
     }
     KernelScope ks(name, roles * 2.0 * flops, roles * 2.0 * bytes, st);
-    hipLaunchKernelGGL((mix_kernel<T, D, false, PARTS>), dim3(groups, a.n_seg, roles), dim3(S::kThreads), 0, st, a);
+    hipLaunchKernelGGL((mix_kernel<T, D, false, PARTS>), dim3(blocks_of(groups, a.n_seg, roles)), dim3(S::kThreads), 0, st, a);
     return hipGetLastError();
 }
 template <class T, int D>
@@ -1014,6 +1053,13 @@ hipError_t mix_short(const MixArgs& a, const char* name, hipStream_t st) {
     if (a.T <= 16) launch_short<T, 1, BWD>(a, groups, st);
     else if (a.T <= 32) launch_short<T, 2, BWD>(a, groups, st);
     else launch_short<T, 4, BWD>(a, groups, st);
+    return hipGetLastError();
+}
+
+template <class T, int N>
+hipError_t share_sum(const gleam_linattn_desc& d, const float* part, const MixTensor& x, void* out, long long n, hipStream_t st) {
+    hipLaunchKernelGGL((mix_share_kernel<T, N>), dim3((unsigned)((n / N + 255) / 256)), dim3(256), 0, st, part, x, out, (unsigned)d.T, (unsigned)d.P,
+                       (unsigned)d.heads, n / N);
     return hipGetLastError();
 }
 
@@ -1124,10 +1170,8 @@ hipError_t linattn_backward(const gleam_linattn_desc& d, const void* q, const vo
         const MixTensor& x = *of[i];
         const long long n = d.B * d.T * d.P * (d.heads / x.share) * x.d;
         KernelScope ks("linattn_share", (double)n * x.share, 4.0 * n * x.share + (d.dtype ? 2.0 : 4.0) * n, st);
-        const dim3 grid((unsigned)((n + 255) / 256));
-        if (d.dtype) hipLaunchKernelGGL(mix_share_kernel<unsigned short>, grid, dim3(256), 0, st, (const float*)part[i], x, out[i], d.T, d.P, d.heads, n);
-        else hipLaunchKernelGGL(mix_share_kernel<float>, grid, dim3(256), 0, st, (const float*)part[i], x, out[i], d.T, d.P, d.heads, n);
-        e = hipGetLastError();
+        e = x.d % 4 ? (d.dtype ? share_sum<unsigned short, 1>(d, part[i], x, out[i], n, st) : share_sum<float, 1>(d, part[i], x, out[i], n, st))
+                    : (d.dtype ? share_sum<unsigned short, 4>(d, part[i], x, out[i], n, st) : share_sum<float, 4>(d, part[i], x, out[i], n, st));
     }
     return e;
 }
