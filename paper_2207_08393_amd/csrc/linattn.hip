@@ -27,7 +27,7 @@ namespace {
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef short short4v __attribute__((ext_vector_type(4)));
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr int kNear = 1 << 26;   // elements between tokens whose offsets within 16 rows fit 32 bits
+constexpr long long kFarBytes = 0x7fffffff / 64 - 128;   // between tokens: 64 of them and a row fit 31 bits
 
 // Within each group of 16 lanes, lane s passes the address of 4 consecutive 16-bit values of row s/4; lane j gets column j of the
 // 4 x 16 block, rows 0..3.
@@ -63,12 +63,14 @@ struct Mma<unsigned short> {
     static constexpr int kBlock = 32, kVec = 8;
     typedef bf16x8 Frag;
     static __device__ __forceinline__ int tile(int t, int m) { return 32 * (t >> 1) + 8 * (m >> 2) + 4 * (t & 1) + (m & 3); }
+    static __device__ __forceinline__ int tile4(int t, int g) { return 32 * (t >> 1) + 8 * g + 4 * (t & 1); }   // of results 4 g .. 4 g + 3
     static __device__ __forceinline__ floatx4 mma(Frag a, Frag b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ Frag row_frag(const unsigned short* p) { return *(const Frag*)p; }
-    // rows 8 g .. 8 g + 7 of the block that begins at p, column tile(t, m)
+    // rows 8 g .. 8 g + 7 of the block that begins at p, column tile(t, m), or 16 t + m (PLAIN)
+    template <bool PLAIN = false>
     static __device__ __forceinline__ Frag col_frag(const unsigned short* p, int stride, int t, int lane) {
         const int g = lane >> 4, s = lane & 15;
-        const unsigned short* q = p + (8 * g + (s >> 2)) * stride + 32 * (t >> 1) + 8 * (s & 3) + 4 * (t & 1);
+        const unsigned short* q = p + (8 * g + (s >> 2)) * stride + (PLAIN ? 16 * t + 4 * (s & 3) : 32 * (t >> 1) + 8 * (s & 3) + 4 * (t & 1));
         const uint2 lo = read_tr16(q), hi = read_tr16(q + 4 * stride);
         return __builtin_bit_cast(Frag, make_uint4(lo.x, lo.y, hi.x, hi.y));
     }
@@ -144,12 +146,14 @@ struct Mma<float> {
     static constexpr int kBlock = 16, kVec = 4;
     typedef floatx4 Frag;
     static __device__ __forceinline__ int tile(int t, int m) { return 16 * t + m; }
+    static __device__ __forceinline__ int tile4(int t, int g) { return 16 * t + 4 * g; }
     static __device__ __forceinline__ floatx4 mma(Frag a, Frag b, floatx4 c) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
         return c;
     }
     static __device__ __forceinline__ Frag row_frag(const float* p) { return *(const Frag*)p; }
+    template <bool PLAIN = false>
     static __device__ __forceinline__ Frag col_frag(const float* p, int stride, int t, int lane) {
         const float* q = p + 4 * (lane >> 4) * stride + 16 * t + (lane & 15);
         return Frag{q[0], q[stride], q[2 * stride], q[3 * stride]};
@@ -179,6 +183,17 @@ struct Mma<float> {
     }
     static __device__ __forceinline__ void put4(float* p, floatx4 v) { *(floatx4*)p = v; }
 };
+
+// 16 bytes from byte `at` of a buffer; zeros beyond its end (also for a negative `at`).  A plain function: the host pass drops the
+// stub of a kernel template whose own body makes this call.
+__device__ __forceinline__ void load_buffer(__amdgpu_buffer_rsrc_t rs, int at, unsigned* w) {
+    typedef unsigned uint4v __attribute__((ext_vector_type(4)));
+    const uint4v v = __builtin_amdgcn_raw_buffer_load_b128(rs, at, 0, 0);
+    w[0] = v[0];
+    w[1] = v[1];
+    w[2] = v[2];
+    w[3] = v[3];
+}
 
 // e^{a n}; 1 for n = 0 whatever a is.
 __device__ __forceinline__ float decay_of(float a, int n) { return n == 0 ? 1.f : __builtin_amdgcn_exp2f(a * kLog2e * (float)n); }
@@ -288,8 +303,11 @@ __device__ __forceinline__ Work work_of(const MixArgs& a, unsigned groups, unsig
 // STATES: only the sum of k (x) v over a segment, for the scan over segments; slot seg + 1 of seg_state.
 // PARTS: numbers a decayed value is the sum of on its way into the state (bfloat16: 3 give 24 bits, for a state that is handed out; 2
 // where the state only feeds outputs, which are rounded to 8 bits).
-template <class T, int D, bool STATES, int PARTS>
-__global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs args) {
+// NARROW: rows shorter than a vector, and tokens so far apart that a chunk's offsets pass 31 bits, go element by element, nothing
+// ahead of time.  (A kernel of its own: where one kernel has both ways the compiler waits for loads in flight when it reuses their
+// registers, since it cannot see that they have arrived.)
+template <class T, int D, bool STATES, int PARTS, bool NARROW>
+__global__ __launch_bounds__((Shape<T, D>::kThreads), (STATES ? 3 : 2)) void mix_kernel(MixArgs args) {
     typedef Shape<T, D> S;
     typedef Mma<T> M;
     typedef typename M::Frag Frag;
@@ -303,7 +321,7 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs
     __shared__ __attribute__((aligned(16))) T lds_p[STATES ? 1 : S::kProblems][STATES ? 8 : L * S::kScoreRow];
     __shared__ __attribute__((aligned(16))) float lds_w[S::kProblems][L + 4];   // decay over n tokens
     __shared__ __attribute__((aligned(16))) float lds_e[S::kProblems][L];       // from token j to the end of a whole chunk, with scale
-    const int slot = S::kProblems == 1 ? 0 : threadIdx.x >> 6;
+    const int slot = S::kProblems == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int tid = S::kProblems == 1 ? threadIdx.x : threadIdx.x & 63;
     const int lane = tid & 63, m = lane & 15, g = lane >> 4;
     const int wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -328,45 +346,31 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs
 
     // tokens of the chunk from the first one on (or, in reverse, from the last one down)
     const long long way = a.reverse ? -1 : 1, start = a.reverse ? r.len - 1 : 0;
-    // staging: vectors tid + i NT of the chunk's rows
+    // Staging: vectors tid + i NT of the chunk's rows, read a chunk ahead from a buffer that holds the chunk's tokens and ends with the
+    // last of them: rows behind the sequence's end are out of its range, so they need no branch and touch no memory, and become zero on the
+    // way into LDS.  A row's last vector ends with the row and is moved into place there.
     const int col = tid % (D / VE) * VE, row0 = tid / (D / VE);
     constexpr int kRowStep = NT / (D / VE);
-    const T *gq = base_of<T>(a.q, r), *gk = base_of<T>(a.k, r), *gv = base_of<T>(a.v, r);
-    // A whole chunk is read at a scalar address plus a lane's own offset.  In a chunk that ends early, and where tokens are too far
-    // apart for 32 bits, every load goes to a token that exists, and what does not belong to the chunk becomes zero on the way into
-    // LDS, so that nothing waits for a load before it has to.  A row's last vector ends with the row and is moved into place there.
-    Pack<T, VE> nq[NV], nk[NV], nv[NV];
     const Edge<T> ek(col, a.k.d), ev(col, a.v.d);
-    const bool narrow = ek.narrow || ev.narrow;
-    const bool near = a.q.s.t < kNear && a.k.s.t < kNear && a.v.s.t < kNear;
-    const int lane_row = a.reverse ? kRowStep - 1 - row0 : row0;
-    auto fetch_array = [&](int c, bool whole, const T* base, long long t, const Edge<T>& e, Pack<T, VE>(&n)[NV]) {
-        if (whole) {
-            const unsigned off = (unsigned)(lane_row * (int)t + e.at);
+    const T *gq = base_of<T>(a.q, r), *gk = base_of<T>(a.k, r), *gv = base_of<T>(a.v, r);
+    Pack<T, VE> nq[NV], nk[NV], nv[NV];
+    auto fetch_array = [&](int c, int count, const T* base, long long t, const Edge<T>& e, Pack<T, VE>(&n)[NV]) {
+        const T* low = base + (start + way * (c * L + (a.reverse ? count - 1 : 0))) * t;
+        const int token = (int)(t * (long long)sizeof(T));
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)low, 0, (count - 1) * token + e.d * (int)sizeof(T), 0x00027000);
+        const int first = (a.reverse ? count - 1 - row0 : row0) * token + e.at * (int)sizeof(T), step = (a.reverse ? -kRowStep : kRowStep) * token;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int first = c * L + i * kRowStep;
-                const T* p = base + (a.reverse ? (long long)(r.len - kRowStep - first) : (long long)first) * t;
-                n[i].load(p + off);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                int at = c * L + row0 + i * kRowStep;
-                at = at < r.len ? at : r.len - 1;
-                n[i].load(base + (a.reverse ? r.len - 1 - at : at) * t + e.at);
-            }
-        }
+        for (int i = 0; i < NV; ++i) load_buffer(rs, first + i * step, n[i].w);
     };
     auto fetch = [&](int c) {
-        if (narrow) return;
-        const bool whole = near && (c + 1) * L <= r.len;
-        if constexpr (!STATES) fetch_array(c, whole, gq, a.q.s.t, ek, nq);
-        fetch_array(c, whole, gk, a.k.s.t, ek, nk);
-        fetch_array(c, whole, gv, a.v.s.t, ev, nv);
+        if (NARROW) return;
+        const int left = r.len - c * L, count = left < L ? left : L;
+        if constexpr (!STATES) fetch_array(c, count, gq, a.q.s.t, ek, nq);
+        fetch_array(c, count, gk, a.k.s.t, ek, nk);
+        fetch_array(c, count, gv, a.v.s.t, ev, nv);
     };
     auto stage = [&](int c, int count) {
-        if (narrow) {                                 // rows shorter than a vector: element by element, nothing ahead of time
+        if (NARROW) {
             for (int e = tid; e < L * S::kRow; e += NT) {
                 const int row = e / S::kRow, cc = e % S::kRow, at = c * L + row;
                 const long long token = a.reverse ? r.len - 1 - at : at;
@@ -396,17 +400,16 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs
     bool have = false;                                // it is not zero
 #pragma unroll
     for (int t = 0; t < S::kTiles; ++t) x[t][0] = x[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
-    // f(tile t, u, number i, offset in the layer's [rows dk][columns dv]) of every element of the lane; pitch: elements of a row
+    // f(tile t, u, values there are, offset of the first and between them in the layer's [rows dk][columns dv]) of every four elements
+    // of the lane; pitch: elements of a row.  STATES: the tiles' rows and columns in their own order, for whole 64 bytes a row.
     auto for_state = [&](int pitch, auto&& f) {
 #pragma unroll
         for (int t = 0; t < S::kTiles; ++t)
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int row = M::tile(t, 4 * g + i), c = 32 * wave + M::tile(u, m);
-                    f(t, u, i, row < a.k.d && c < a.v.d, a.state_t ? c * pitch + row : row * pitch + c);
-                }
+            for (int u = 0; u < 2; ++u) {
+                const int row = STATES ? 16 * t + 4 * g : M::tile4(t, g), c = 32 * wave + (STATES ? 16 * u + m : M::tile(u, m));
+                f(t, u, c < a.v.d ? a.k.d - row : 0, a.state_t ? c * pitch + row : row * pitch + c, a.state_t ? 1 : pitch);
+            }
     };
     const long long state_base = r.index * args.dk * args.dv;
     auto segment = [&](int s) { return a.seg_state + (r.index * args.n_seg + s) * S::kStateFloats; };
@@ -414,11 +417,16 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs
     if constexpr (!STATES) {
         if (a.seg_state) {
             const float* s = segment(seg);
-            for_state(D, [&](int t, int u, int i, bool, int at) { x[t][u][i] = s[at]; });
+            for_state(D, [&](int t, int u, int, int at, int step) {
+                if (a.state_t) x[t][u] = *(const floatx4*)(s + at);
+                else x[t][u] = floatx4{s[at], s[at + step], s[at + 2 * step], s[at + 3 * step]};
+            });
             have = seg > 0 || a.state_in;
         } else if (a.state_in) {
-            for_state(args.dv, [&](int t, int u, int i, bool there, int at) {
-                if (there) x[t][u][i] = a.state_in[state_base + at];
+            for_state(args.dv, [&](int t, int u, int left, int at, int step) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i < left) x[t][u][i] = a.state_in[state_base + at + i * step];
             });
             have = true;
         }
@@ -434,6 +442,7 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs
                 wt[n][i] = apart < 0 ? 0.f : a.in_scale * a.out_scale * decay_of(decay, apart);
             }
     }
+    long long out_at = r.b * a.o.s.b + r.p * a.o.s.p + (long long)(r.h / a.o.share) * a.o.s.h + (start + way * ((long long)c_begin * L + m)) * a.o.s.t + 32 * wave;
     for (int c = c_begin; c < c_end; ++c) {
         const int left = r.len - c * L, count = left < L ? left : L;
         exchange<W>();                                // everyone is done with the chunk before
@@ -444,7 +453,7 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs
 #pragma unroll
         for (int s = 0; s < L / KB; ++s)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) vf[s][u] = M::col_frag(sv + s * KB * S::kRow, S::kRow, 2 * wave + u, lane);
+            for (int u = 0; u < 2; ++u) vf[s][u] = M::template col_frag<STATES>(sv + s * KB * S::kRow, S::kRow, 2 * wave + u, lane);
         if constexpr (!STATES) {
             // scores of rows `it`: the lane has four consecutive columns of row m of the tile
 #pragma unroll
@@ -496,9 +505,9 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs
                 }
             }
             exchange<W>();
-            long long at = r.b * a.o.s.b + r.p * a.o.s.p + (long long)(r.h / a.o.share) * a.o.s.h + (start + way * ((long long)c * L + m)) * a.o.s.t + 32 * wave;
+            const long long out_step = way * 16 * a.o.s.t;
 #pragma unroll
-            for (int it = 0; it < kRows; ++it, at += way * 16 * a.o.s.t) {
+            for (int it = 0; it < kRows; ++it) {
                 if (it * 16 >= count) break;
 #pragma unroll
                 for (int s = 0; s <= it * 16 / KB; ++s) {
@@ -507,10 +516,11 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs
                     for (int u = 0; u < 2; ++u) o[it][u] = M::mma(vf[s][u], pf, o[it][u]);
                 }
                 if (16 * it + m < count) {
-                    if (a.out_f32) M::store((float*)a.out + at, a.o.d - 32 * wave, g, o[it]);
-                    else M::store((T*)a.out + at, a.o.d - 32 * wave, g, o[it]);
+                    if (a.out_f32) M::store((float*)a.out + out_at + it * out_step, a.o.d - 32 * wave, g, o[it]);
+                    else M::store((T*)a.out + out_at + it * out_step, a.o.d - 32 * wave, g, o[it]);
                 }
             }
+            out_at += kRows * out_step;
         }
         // the state: decay over the chunk, then k (x) v with each token's decay to its end; not where nothing reads it
         if (!STATES && c + 1 == c_end && !(a.state_out && last_seg)) break;
@@ -539,7 +549,7 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs
             for (int u = 0; u < 2; ++u) M::scaled(vf[s][u], w, part[u], PARTS);
 #pragma unroll
             for (int t = 0; t < S::kTiles; ++t) {
-                const Frag kf = M::col_frag(sk + s * KB * S::kRow, S::kRow, t, lane);
+                const Frag kf = M::template col_frag<STATES>(sk + s * KB * S::kRow, S::kRow, t, lane);
 #pragma unroll
                 for (int n = 0; n < PARTS; ++n)
 #pragma unroll
@@ -550,7 +560,7 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs
     }
     if constexpr (STATES) {
         float* s = segment(seg + 1);
-        for_state(D, [&](int t, int u, int i, bool, int at) { s[at] = x[t][u][i]; });
+        for_state(D, [&](int t, int u, int, int at, int) { *(floatx4*)(s + at) = x[t][u]; });   // these passes have state_t
         return;
     }
     // zeros behind the end of the sequence, in this segment's range of tokens
@@ -564,8 +574,10 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), 2) void mix_kernel(MixArgs
         else put_f32((T*)a.out + at, 0.f);
     }
     if (a.state_out && last_seg)
-        for_state(args.dv, [&](int t, int u, int i, bool there, int at) {
-            if (there) a.state_out[state_base + at] = x[t][u][i];
+        for_state(args.dv, [&](int t, int u, int left, int at, int step) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < left) a.state_out[state_base + at + i * step] = x[t][u][i];
         });
 }
 
@@ -983,7 +995,7 @@ size_t share_bytes(const gleam_linattn_desc& d, int heads, int width) {
 unsigned blocks_of(unsigned groups, unsigned segs, unsigned roles) { return (groups * segs * roles + 7) / 8 * 8; }
 
 // `roles` passes side by side; `states` of them first, over segments, where there are several.
-template <class T, int D, int PARTS>
+template <class T, int D, int PARTS, bool NARROW>
 hipError_t mix_passes(MixArgs a, int roles, MixArgs states, int n_states, const char* name, hipStream_t st) {
     typedef Shape<T, D> S;
     const long long problems = a.B * a.P * a.H;
@@ -999,7 +1011,7 @@ hipError_t mix_passes(MixArgs a, int roles, MixArgs states, int n_states, const 
     if (a.n_seg > 1) {
         {
             KernelScope ks("linattn_segments", n_states * flops, n_states * bytes, st);
-            hipLaunchKernelGGL((mix_kernel<T, D, true, PARTS>), dim3(blocks_of(groups, a.n_seg - 1, n_states)), dim3(S::kThreads), 0, st, states);
+            hipLaunchKernelGGL((mix_kernel<T, D, true, PARTS, NARROW>), dim3(blocks_of(groups, a.n_seg - 1, n_states)), dim3(S::kThreads), 0, st, states);
         }
         const double floats = (double)n_states * problems * a.n_seg * S::kStateFloats;
         KernelScope ks("linattn_scan", 2.0 * floats, 8.0 * floats, st);
@@ -1007,13 +1019,19 @@ hipError_t mix_passes(MixArgs a, int roles, MixArgs states, int n_states, const 
         hipLaunchKernelGGL(mix_scan_kernel<D>, dim3(blocks, 1, n_states), dim3(256), 0, st, states, S::kL);
     }
     KernelScope ks(name, roles * 2.0 * flops, roles * 2.0 * bytes, st);
-    hipLaunchKernelGGL((mix_kernel<T, D, false, PARTS>), dim3(blocks_of(groups, a.n_seg, roles)), dim3(S::kThreads), 0, st, a);
+    hipLaunchKernelGGL((mix_kernel<T, D, false, PARTS, NARROW>), dim3(blocks_of(groups, a.n_seg, roles)), dim3(S::kThreads), 0, st, a);
     return hipGetLastError();
 }
 template <class T, int D>
 hipError_t mix_parts(const MixArgs& a, int roles, const MixArgs& states, int n_states, bool state_out, const char* name, hipStream_t st) {
-    if constexpr (sizeof(T) == 4) return mix_passes<T, D, 1>(a, roles, states, n_states, name, st);
-    else return state_out ? mix_passes<T, D, 3>(a, roles, states, n_states, name, st) : mix_passes<T, D, 2>(a, roles, states, n_states, name, st);
+    constexpr int kMost = sizeof(T) == 4 ? 1 : 3;
+    const int vec = 16 / (int)sizeof(T);
+    bool narrow = a.dk < vec || a.dv < vec;
+    for (int i = 0; i < roles; ++i)
+        for (const MixTensor* x : {&a.role[i].q, &a.role[i].k, &a.role[i].v}) narrow = narrow || x->s.t > kFarBytes / (long long)sizeof(T);
+    if (narrow) return mix_passes<T, D, kMost, true>(a, roles, states, n_states, name, st);
+    if (state_out) return mix_passes<T, D, kMost, false>(a, roles, states, n_states, name, st);
+    return mix_passes<T, D, (kMost < 2 ? kMost : 2), false>(a, roles, states, n_states, name, st);
 }
 template <class T>
 hipError_t mix_any(const MixArgs& a, int roles, const MixArgs& states, int n_states, bool state_out, const char* name, hipStream_t st) {
