@@ -12,7 +12,7 @@
 // Backwards the decay of the state is applied after a token has read it (dL/dv_s = .. + e^{a(T-1-s)} k_s . dS_T): the
 // exponents i+1 and L-1-j above become i and L-j ("shift" in the code).
 //
-// One problem is one sequence, pixel and head.  D is dk and dv rounded up to 32, 64 or 128; a problem is worked on by D/32 waves, and
+// One problem is one sequence, pixel and head.  D is dk and dv rounded up to 32, 64, 96 or 128; a problem is worked on by D/32 waves, and
 // a wave owns 32 columns (dv) of the state, in registers in the layout of a 16x16 product's result: the lane holds
 // column l % 16 and four rows.  That is also an operand's layout, so the state enters the next product without a trip through LDS.
 // Scores are formed by all waves, each for its rows of the chunk, and exchanged through LDS.
@@ -966,7 +966,7 @@ __global__ __launch_bounds__(kStepThreads) void mix_step_kernel(MixArgs args) {
 inline size_t align_up(size_t v) { return (v + 255) / 256 * 256; }
 int width_of(int dk, int dv) {
     const int d = dk > dv ? dk : dv;
-    return d <= 32 ? 32 : d <= 64 ? 64 : 128;
+    return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : 128;
 }
 // Segments of a call of `roles` passes: enough workgroups to fill the chip where there are few problems.
 struct Split {
@@ -1038,6 +1038,7 @@ hipError_t mix_any(const MixArgs& a, int roles, const MixArgs& states, int n_sta
     switch (width_of(a.dk, a.dv)) {
         case 32: return mix_parts<T, 32>(a, roles, states, n_states, state_out, name, st);
         case 64: return mix_parts<T, 64>(a, roles, states, n_states, state_out, name, st);
+        case 96: return mix_parts<T, 96>(a, roles, states, n_states, state_out, name, st);
         default: return mix_parts<T, 128>(a, roles, states, n_states, state_out, name, st);
     }
 }

@@ -284,7 +284,7 @@ def test_linattn_lengths(T, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("dk,dv", [(1, 1), (3, 2), (8, 8), (16, 16), (25, 25), (33, 7), (7, 33), (40, 72), (64, 64), (65, 128), (128, 64), (127, 127), (128, 128)])
+@pytest.mark.parametrize("dk,dv", [(1, 1), (3, 2), (8, 8), (16, 16), (25, 25), (33, 7), (7, 33), (40, 72), (64, 64), (96, 80), (65, 128), (128, 64), (127, 127), (128, 128)])
 def test_linattn_widths(dk, dv, dtype):
     print("case linattn widths", dk, dv, dtype, flush=True)
     Mix(1, 70, 2, (3, 3, 3, 3), dk, dv, dtype).check()
@@ -327,7 +327,7 @@ def test_linattn_short_sequences_without_memory():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("d", [32, 64, 96, 128])
 def test_linattn_long(d, dtype):
     """Few problems of many chunks: the split into segments; a state in and out, heads shared, one sequence shorter."""
     print("case linattn long", d, dtype, flush=True)
