@@ -1,0 +1,127 @@
+"""A causal temporal layer for feature maps of a dynamic series: every pixel's frames are mixed by linear attention whose heads forget at
+rates of their own.
+
+    y = layer_norm(x);  q, k, v = y W_qkv^T;  h = x + dropout(linear_attention(q, k, v) W_o^T)
+
+x, h: [B][T][P][C], P pixels of T frames, channels last, as the prox networks hold them.  A recorded series goes through `forward` (and
+`backward` in training), a running one through `frame`, which takes the next frame of every pixel and keeps a state of fixed size instead
+of the frames before.  Both give the same result.  The projections are plain library products; everything else is
+the framework's own kernels through `binding`.  `python -m paper_2207_08393_amd.temporal` trains such a layer on a synthetic series and then
+streams it."""
+from __future__ import annotations
+
+import math
+
+import torch
+
+from . import binding as gb
+from .runner import byte_buffer
+
+
+class TemporalLayer:
+    """Parameters, gradients and Adam moments are flat float32 arrays: gamma [C], beta [C], W_qkv [3C][C], W_o [C][C]."""
+
+    def __init__(self, B, T, P, C, heads, dtype=torch.bfloat16, dropout=0.1, seed=0, eps=1e-5, longest=64.0):
+        if C % heads:
+            raise ValueError("channels are split evenly over the heads")
+        self.shape, self.C, self.H, self.d, self.dtype = (B, T, P, C), C, heads, C // heads, dtype
+        sizes = (C, C, 3 * C * C, C * C)
+        gen = torch.Generator().manual_seed(seed)
+        parts = [torch.ones(C), torch.zeros(C), torch.randn(3 * C * C, generator=gen) / math.sqrt(C), 0.1 * torch.randn(C * C, generator=gen) / math.sqrt(C)]
+        self.theta = torch.cat(parts).cuda()
+        self.grad, self.m, self.v = (torch.zeros_like(self.theta) for _ in range(3))
+        self.gamma, self.beta, self.w_qkv, self.w_o = self._views(self.theta, sizes)
+        self.g_gamma, self.g_beta, self.g_qkv_w, self.g_o_w = self._views(self.grad, sizes)
+        # from a memory of one frame to one of `longest` frames, in equal ratios
+        frames = longest ** torch.linspace(0.0, 1.0, heads)
+        self.log_decay = (-1.0 / frames).cuda()
+        rows, scale = B * T * P, self.d ** -0.5
+        new = lambda *s: torch.empty(*s, dtype=dtype, device="cuda")  # noqa: E731
+        self.y, self.qkv, self.o, self.z, self.h = new(B, T, P, C), new(B, T, P, 3 * C), new(B, T, P, heads, self.d), new(rows, C), new(B, T, P, C)
+        self.mean, self.rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        self.step = torch.zeros(1, dtype=torch.int64, device="cuda")       # counts training steps: a new mask for each
+        self.norm = gb.make_layer_norm(dtype, rows, C, eps)
+        self.drop = gb.make_dropout(dtype, rows, C, dropout, seed)
+        self.keep = gb.make_dropout(dtype, rows, C, 0.0, seed)
+        self.mix = gb.make_linattn(*self._heads(self.qkv), self.o, scale)
+        self.ws = byte_buffer(max(*gb.gleam_linattn_workspace_bytes(self.mix), gb.gleam_layer_norm_workspace_bytes(self.norm)))
+        # one frame of every pixel
+        self.state = torch.zeros(B, P, heads, self.d, self.d, device="cuda")
+        self.frame_qkv, self.frame_o, self.frame_y, self.frame_h = new(B, 1, P, 3 * C), new(B, 1, P, heads, self.d), new(B, P, C), new(B, P, C)
+        self.frame_norm = gb.make_layer_norm(dtype, B * P, C, eps)
+        self.frame_keep = gb.make_dropout(dtype, B * P, C, 0.0, seed)
+        self.frame_mix = gb.make_linattn(*self._heads(self.frame_qkv), self.frame_o, scale)
+
+    def _views(self, flat, sizes):
+        a, b, c, d = flat.split(sizes)
+        return a, b, c.view(3 * self.C, self.C), d.view(self.C, self.C)
+
+    def _heads(self, qkv):
+        return [x.unflatten(3, (self.H, self.d)) for x in qkv.split(self.C, 3)]
+
+    def forward(self, x, lengths=None, training=True):
+        """x: [B][T][P][C]; lengths: int32 [B], frames that are there, or None.  Keeps what `backward` needs."""
+        self.x, self.lengths = x, lengths
+        gb.gleam_layer_norm_fwd(self.norm, x, self.gamma, self.beta, self.y, self.mean, self.rstd)
+        torch.mm(self.y.view(-1, self.C), self.w_qkv.to(self.dtype).t(), out=self.qkv.view(-1, 3 * self.C))
+        gb.gleam_linattn_fwd(self.mix, *self._heads(self.qkv), self.log_decay, lengths, None, self.o, None, self.ws)
+        torch.mm(self.o.view(-1, self.C), self.w_o.to(self.dtype).t(), out=self.z)
+        self.drop_now = self.drop if training else self.keep
+        gb.gleam_dropout_fwd(self.drop_now, self.z, x, self.h, self.step)
+        return self.h
+
+    def backward(self, g_h):
+        """dL/dx from dL/dh; the parameters' gradients are left in `grad`."""
+        g_z, g_qkv, g_x = torch.empty_like(self.z), torch.empty_like(self.qkv), torch.empty_like(self.y)
+        gb.gleam_dropout_bwd(self.drop_now, g_h, g_z, self.step)
+        torch.mm(g_z.float().t(), self.o.view(-1, self.C).float(), out=self.g_o_w)
+        g_o = (g_z @ self.w_o.to(self.dtype)).view_as(self.o)
+        gb.gleam_linattn_bwd(self.mix, *self._heads(self.qkv), self.log_decay, self.lengths, None, g_o, None, *self._heads(g_qkv), None, self.ws)
+        rows = g_qkv.view(-1, 3 * self.C)
+        torch.mm(rows.float().t(), self.y.view(-1, self.C).float(), out=self.g_qkv_w)
+        g_y = rows @ self.w_qkv.to(self.dtype)
+        gb.gleam_layer_norm_bwd(self.norm, self.x, self.gamma, self.mean, self.rstd, g_y, g_x, self.g_gamma, self.g_beta, self.ws)
+        return g_x.add_(g_h)
+
+    def update(self, hyper, t):
+        """One Adam step with the gradients of the last backward pass, and the next step's mask."""
+        gb.gleam_adam_step(hyper, t, self.theta, self.grad, self.m, self.v)
+        self.step += 1
+
+    def restart(self):
+        """Before the first frame of a new series."""
+        self.state.zero_()
+
+    def frame(self, x):
+        """The next frame [B][P][C] of every pixel; no dropout."""
+        gb.gleam_layer_norm_fwd(self.frame_norm, x, self.gamma, self.beta, self.frame_y)
+        torch.mm(self.frame_y.view(-1, self.C), self.w_qkv.to(self.dtype).t(), out=self.frame_qkv.view(-1, 3 * self.C))
+        gb.gleam_linattn_fwd(self.frame_mix, *self._heads(self.frame_qkv), self.log_decay, None, self.state, self.frame_o, self.state, None)
+        z = self.frame_o.view(-1, self.C) @ self.w_o.to(self.dtype).t()
+        gb.gleam_dropout_fwd(self.frame_keep, z, x, self.frame_h)
+        return self.frame_h
+
+
+def main(steps=200, B=1, T=20, P=96 * 80, C=64, heads=4):
+    """Learns to take noise off a slowly changing series from its past frames, then runs it frame by frame."""
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    t = torch.arange(T, device="cuda")[None, :, None, None] / T
+    phase, amount = torch.rand(B, 1, P, C, device="cuda", generator=gen), torch.randn(B, 1, P, C, device="cuda", generator=gen)
+    clean = amount * torch.cos(2 * math.pi * (0.5 * t + phase))
+    layer = TemporalLayer(B, T, P, C, heads)
+    hyper = gb.make_adam(2e-3)
+    for k in range(1, steps + 1):
+        x = (clean + 0.5 * torch.randn(clean.shape, device="cuda", generator=gen)).to(layer.dtype)
+        d = layer.forward(x).float() - clean
+        layer.backward((2.0 / d.numel() * d).to(layer.dtype))
+        layer.update(hyper, k)
+        if k == 1 or k % 40 == 0:
+            print(f"step {k}: mean squared error {float((d * d).mean()):.4f} (noise alone: 0.25)", flush=True)
+    whole = layer.forward(x, training=False).clone()
+    layer.restart()
+    one_by_one = torch.stack([layer.frame(x[:, i].contiguous()).clone() for i in range(T)], 1)
+    print(f"frame by frame: differs from the whole series by {float((one_by_one - whole).float().norm() / whole.float().norm()):.1e} of its norm")
+
+
+if __name__ == "__main__":
+    main()
