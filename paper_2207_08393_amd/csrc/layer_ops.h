@@ -43,7 +43,8 @@ struct MixRole {
     float in_scale, out_scale;          // on k (x) v, and on what a query reads
     const float* state_in;              // natural layout [B][P][H][dk][dv] of the layer, or null: zero
     float* state_out;                   // or null
-    float* seg_state;                   // [problem][segment][D][D], rows dk: states at the segments' starts; or null for one segment
+    float* seg_state;                   // [problem][segment][D][D]: states at the segments' starts, or null for one segment
+    int seg_t;                          // they come from a pass with the roles of dk and dv exchanged against this one's
 };
 struct MixArgs {
     MixRole role[3];

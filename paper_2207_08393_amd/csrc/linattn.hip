@@ -400,14 +400,13 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), (STATES ? 3 : 2)) void mix
     bool have = false;                                // it is not zero
 #pragma unroll
     for (int t = 0; t < S::kTiles; ++t) x[t][0] = x[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
-    // f(tile t, u, values there are, offset of the first and between them in the layer's [rows dk][columns dv]) of every four elements
-    // of the lane; pitch: elements of a row.  STATES: the tiles' rows and columns in their own order, for whole 64 bytes a row.
-    auto for_state = [&](int pitch, auto&& f) {
+    // f(tile t, u, values there are, offset of the first and between them in the layer's [dk][dv]) of every four elements of the lane
+    auto for_state = [&](auto&& f) {
 #pragma unroll
         for (int t = 0; t < S::kTiles; ++t)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const int row = STATES ? 16 * t + 4 * g : M::tile4(t, g), c = 32 * wave + (STATES ? 16 * u + m : M::tile(u, m));
+                const int row = M::tile4(t, g), c = 32 * wave + M::tile(u, m), pitch = args.dv;
                 f(t, u, c < a.v.d ? a.k.d - row : 0, a.state_t ? c * pitch + row : row * pitch + c, a.state_t ? 1 : pitch);
             }
     };
@@ -417,13 +416,18 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), (STATES ? 3 : 2)) void mix
     if constexpr (!STATES) {
         if (a.seg_state) {
             const float* s = segment(seg);
-            for_state(D, [&](int t, int u, int, int at, int step) {
-                if (a.state_t) x[t][u] = *(const floatx4*)(s + at);
-                else x[t][u] = floatx4{s[at], s[at + step], s[at + 2 * step], s[at + 3 * step]};
-            });
+            // [column][row] of the pass over segments, whose roles are this pass's or (seg_t) exchanged
+#pragma unroll
+            for (int t = 0; t < S::kTiles; ++t)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int row = M::tile4(t, g), c = 32 * wave + M::tile(u, m);
+                    if (!a.seg_t) x[t][u] = *(const floatx4*)(s + c * D + row);
+                    else x[t][u] = floatx4{s[row * D + c], s[(row + 1) * D + c], s[(row + 2) * D + c], s[(row + 3) * D + c]};
+                }
             have = seg > 0 || a.state_in;
         } else if (a.state_in) {
-            for_state(args.dv, [&](int t, int u, int left, int at, int step) {
+            for_state([&](int t, int u, int left, int at, int step) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (i < left) x[t][u][i] = a.state_in[state_base + at + i * step];
@@ -443,6 +447,79 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), (STATES ? 3 : 2)) void mix
             }
     }
     long long out_at = r.b * a.o.s.b + r.p * a.o.s.p + (long long)(r.h / a.o.share) * a.o.s.h + (start + way * ((long long)c_begin * L + m)) * a.o.s.t + 32 * wave;
+    const long long out_step = way * 16 * a.o.s.t;
+    // Scores into LDS, rows `it`: the lane has four consecutive columns of row m of the tile.
+    auto scores = [&](int count) {
+#pragma unroll
+        for (int rr = 0; rr < (kRows + W - 1) / W; ++rr) {
+            const int it = wave + rr * W;
+            if (it < kRows && it * 16 < count) {
+                Frag qf[D / KB];
+#pragma unroll
+                for (int s = 0; s < D / KB; ++s) qf[s] = M::row_frag(sq + (16 * it + m) * S::kRow + s * KB + g * VE);
+#pragma unroll
+                for (int n = 0; n < kRows; ++n) {
+                    if (n >= rr * W + W) continue;            // n <= it, whatever the wave
+                    // a tile beyond the first column: zeros into tile n, right of the diagonal
+                    const int jt = it >= n ? it - n : n;
+                    floatx4 p{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int s = 0; s < D / KB; ++s) p = M::mma(M::row_frag(sk + (16 * jt + m) * S::kRow + s * KB + g * VE), qf[s], p);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p[i] = (n > 0 || m >= 4 * g + i) && it >= n ? p[i] * wt[n][i] : 0.f;
+                    M::put4(sp + (16 * it + m) * S::kScoreRow + 16 * jt + 4 * g, p);
+                }
+                // the tile right of the diagonal, where it shares an operand with it and is not among those
+                if (kPair == 2 && W % 2 && !(it & 1)) M::put4(sp + (16 * it + m) * S::kScoreRow + 16 * (it + 1) + 4 * g, floatx4{0.f, 0.f, 0.f, 0.f});
+            }
+        }
+    };
+    // What the queries read of the state.
+    auto from_state = [&](floatx4(&o)[kRows][2]) {
+#pragma unroll
+        for (int s = 0; s < D / KB; ++s) {
+            Frag xf[2][M::kStateParts];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const floatx4 both[2] = {x[kPair * s][u], x[kPair * s + kPair - 1][u]};
+                M::pack(both, xf[u]);
+            }
+#pragma unroll
+            for (int it = 0; it < kRows; ++it) {
+                const Frag qf = M::row_frag(sq + (16 * it + m) * S::kRow + s * KB + g * VE);
+#pragma unroll
+                for (int n = 0; n < M::kStateParts; ++n)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) o[it][u] = M::mma(xf[u][n], qf, o[it][u]);
+            }
+        }
+#pragma unroll
+        for (int it = 0; it < kRows; ++it) {
+            const float f = a.out_scale * sw[16 * it + m + 1 - shift];
+            o[it][0] *= f;
+            o[it][1] *= f;
+        }
+    };
+    auto from_chunk = [&](int count, const Frag(&vf)[L / KB][2], floatx4(&o)[kRows][2]) {
+#pragma unroll
+        for (int it = 0; it < kRows; ++it) {
+            if (it * 16 >= count) break;
+#pragma unroll
+            for (int s = 0; s <= it * 16 / KB; ++s) {
+                const Frag pf = M::row_frag(sp + (16 * it + m) * S::kScoreRow + s * KB + g * VE);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) o[it][u] = M::mma(vf[s][u], pf, o[it][u]);
+            }
+        }
+        auto put = [&](auto* out) {
+#pragma unroll
+            for (int it = 0; it < kRows; ++it)
+                if (16 * it + m < count) M::store(out + out_at + it * out_step, a.o.d - 32 * wave, g, o[it]);
+        };
+        if (a.out_f32) put((float*)a.out);
+        else put((T*)a.out);
+        out_at += kRows * out_step;
+    };
     for (int c = c_begin; c < c_end; ++c) {
         const int left = r.len - c * L, count = left < L ? left : L;
         exchange<W>();                                // everyone is done with the chunk before
@@ -455,72 +532,11 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), (STATES ? 3 : 2)) void mix
 #pragma unroll
             for (int u = 0; u < 2; ++u) vf[s][u] = M::template col_frag<STATES>(sv + s * KB * S::kRow, S::kRow, 2 * wave + u, lane);
         if constexpr (!STATES) {
-            // scores of rows `it`: the lane has four consecutive columns of row m of the tile
-#pragma unroll
-            for (int rr = 0; rr < (kRows + W - 1) / W; ++rr) {
-                const int it = wave + rr * W;
-                if (it < kRows && it * 16 < count) {
-                    Frag qf[D / KB];
-#pragma unroll
-                    for (int s = 0; s < D / KB; ++s) qf[s] = M::row_frag(sq + (16 * it + m) * S::kRow + s * KB + g * VE);
-#pragma unroll
-                    for (int n = 0; n < kRows; ++n) {
-                        if (n >= rr * W + W) continue;            // n <= it, whatever the wave
-                        const int jt = it > n ? it - n : 0;
-                        floatx4 p{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int s = 0; s < D / KB; ++s) p = M::mma(M::row_frag(sk + (16 * jt + m) * S::kRow + s * KB + g * VE), qf[s], p);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) p[i] = n > 0 || m >= 4 * g + i ? p[i] * wt[n][i] : 0.f;
-                        if (n <= it) M::put4(sp + (16 * it + m) * S::kScoreRow + 16 * jt + 4 * g, p);
-                    }
-                    if (kPair == 2 && !(it & 1)) M::put4(sp + (16 * it + m) * S::kScoreRow + 16 * (it + 1) + 4 * g, floatx4{0.f, 0.f, 0.f, 0.f});
-                }
-            }
-            // what the queries read of the state; needs no scores, so it stands in front of their exchange
             floatx4 o[kRows][2] = {};
-            if (have) {
-#pragma unroll
-                for (int s = 0; s < D / KB; ++s) {
-                    Frag xf[2][M::kStateParts];
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const floatx4 both[2] = {x[kPair * s][u], x[kPair * s + kPair - 1][u]};
-                        M::pack(both, xf[u]);
-                    }
-#pragma unroll
-                    for (int it = 0; it < kRows; ++it) {
-                        const Frag qf = M::row_frag(sq + (16 * it + m) * S::kRow + s * KB + g * VE);
-#pragma unroll
-                        for (int n = 0; n < M::kStateParts; ++n)
-#pragma unroll
-                            for (int u = 0; u < 2; ++u) o[it][u] = M::mma(xf[u][n], qf, o[it][u]);
-                    }
-                }
-#pragma unroll
-                for (int it = 0; it < kRows; ++it) {
-                    const float f = a.out_scale * sw[16 * it + m + 1 - shift];
-                    o[it][0] *= f;
-                    o[it][1] *= f;
-                }
-            }
+            scores(count);
+            if (have) from_state(o);                  // needs no scores, so it stands in front of their exchange
             exchange<W>();
-            const long long out_step = way * 16 * a.o.s.t;
-#pragma unroll
-            for (int it = 0; it < kRows; ++it) {
-                if (it * 16 >= count) break;
-#pragma unroll
-                for (int s = 0; s <= it * 16 / KB; ++s) {
-                    const Frag pf = M::row_frag(sp + (16 * it + m) * S::kScoreRow + s * KB + g * VE);
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) o[it][u] = M::mma(vf[s][u], pf, o[it][u]);
-                }
-                if (16 * it + m < count) {
-                    if (a.out_f32) M::store((float*)a.out + out_at + it * out_step, a.o.d - 32 * wave, g, o[it]);
-                    else M::store((T*)a.out + out_at + it * out_step, a.o.d - 32 * wave, g, o[it]);
-                }
-            }
-            out_at += kRows * out_step;
+            from_chunk(count, vf, o);
         }
         // the state: decay over the chunk, then k (x) v with each token's decay to its end; not where nothing reads it
         if (!STATES && c + 1 == c_end && !(a.state_out && last_seg)) break;
@@ -531,8 +547,7 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), (STATES ? 3 : 2)) void mix
             x[t][1] *= whole;
         }
 #pragma unroll
-        for (int s = 0; s < L / KB; ++s) {
-            if (s * KB >= count) break;
+        for (int s = 0; s < L / KB; ++s) {            // tokens behind the end are zeros: their weights only have to be finite
             float w[VE];
             if (count == L) {
 #pragma unroll
@@ -560,7 +575,10 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), (STATES ? 3 : 2)) void mix
     }
     if constexpr (STATES) {
         float* s = segment(seg + 1);
-        for_state(D, [&](int t, int u, int, int at, int) { *(floatx4*)(s + at) = x[t][u]; });   // these passes have state_t
+#pragma unroll
+        for (int t = 0; t < S::kTiles; ++t)           // tiles in their own order here: whole 64 bytes of a column
+#pragma unroll
+            for (int u = 0; u < 2; ++u) *(floatx4*)(s + (32 * wave + 16 * u + m) * D + 16 * t + 4 * g) = x[t][u];
         return;
     }
     // zeros behind the end of the sequence, in this segment's range of tokens
@@ -574,7 +592,7 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), (STATES ? 3 : 2)) void mix
         else put_f32((T*)a.out + at, 0.f);
     }
     if (a.state_out && last_seg)
-        for_state(args.dv, [&](int t, int u, int left, int at, int step) {
+        for_state([&](int t, int u, int left, int at, int step) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (i < left) a.state_out[state_base + at + i * step] = x[t][u][i];
@@ -845,8 +863,10 @@ __global__ __launch_bounds__(256) void mix_scan_kernel(MixArgs args, int chunk) 
     floatx4 x{0.f, 0.f, 0.f, 0.f};
     if (a.state_in) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (row < args.dk && col + i < args.dv) x[i] = a.state_in[(index * args.dk + row) * args.dv + col + i];
+        for (int i = 0; i < 4; ++i) {                 // row: of the pass's columns; col: of its rows
+            const int at_k = a.state_t ? row : col + i, at_v = a.state_t ? col + i : row;
+            if (at_k < args.dk && at_v < args.dv) x[i] = a.state_in[(index * args.dk + at_k) * args.dv + at_v];
+        }
     }
     const float whole = decay_of(args.log_decay[index % args.H], args.seg_chunks * chunk);
     floatx4* s = (floatx4*)a.seg_state + index * args.n_seg * kQuads + e;
@@ -1141,7 +1161,7 @@ hipError_t linattn_forward(const gleam_linattn_desc& d, const void* q, const voi
     }
     if (is_short(d, state_in || state_out))
         return d.dtype ? mix_short<unsigned short, false>(a, "linattn_fwd_short", st) : mix_short<float, false>(a, "linattn_fwd_short", st);
-    states.role[0] = role_of(tq, tv, tk, 1, 0, 1.f, 1.f, state_in, seg);
+    states.role[0] = role_of(tq, tk, tv, 0, 0, 1.f, 1.f, state_in, seg);
     return d.dtype ? mix_any<unsigned short>(a, 1, states, 1, state_out, "linattn_fwd", st)
                    : mix_any<float>(a, 1, states, 1, state_out, "linattn_fwd", st);
 }
@@ -1161,6 +1181,7 @@ hipError_t linattn_backward(const gleam_linattn_desc& d, const void* q, const vo
     a.role[1] = role_of(tv, tg, tq, 1, 1, d.scale, 1.f, g_state_out, seg_g);
     a.role[2] = role_of(tk, tq, tg, 0, 1, d.scale, 1.f, g_state_out, seg_g);
     a.role[2].state_out = g_state_in;
+    a.role[2].seg_t = 1;
     states.role[0] = role_of(tg, tv, tk, 1, 0, 1.f, 1.f, state_in, seg_s);
     states.role[1] = role_of(tv, tg, tq, 1, 1, d.scale, 1.f, g_state_out, seg_g);
     const MixTensor* of[3] = {&tq, &tk, &tv};

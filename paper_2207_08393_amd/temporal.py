@@ -27,7 +27,7 @@ class TemporalLayer:
         self.shape, self.C, self.H, self.d, self.dtype = (B, T, P, C), C, heads, C // heads, dtype
         sizes = (C, C, 3 * C * C, C * C)
         gen = torch.Generator().manual_seed(seed)
-        parts = [torch.ones(C), torch.zeros(C), torch.randn(3 * C * C, generator=gen) / math.sqrt(C), 0.1 * torch.randn(C * C, generator=gen) / math.sqrt(C)]
+        parts = [torch.ones(C), torch.zeros(C), torch.randn(3 * C * C, generator=gen) / math.sqrt(C), torch.randn(C * C, generator=gen) / math.sqrt(C)]
         self.theta = torch.cat(parts).cuda()
         self.grad, self.m, self.v = (torch.zeros_like(self.theta) for _ in range(3))
         self.gamma, self.beta, self.w_qkv, self.w_o = self._views(self.theta, sizes)
