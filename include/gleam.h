@@ -381,7 +381,7 @@ int gleam_linattn_fwd(const gleam_linattn_desc* desc, const void* q, const void*
                       void* stream);
 /* Gradients of the same call from g_o = dL/do (strides of o) and g_state_out = dL/d state_out (or NULL: zero).  g_q, g_k, g_v have the
  * strides of q, k, v; heads that are shared receive the sum over the output heads that use them, in a fixed order.  g_state_in
- * (or NULL) = dL/d state_in, may be g_state_out.  No gradient may overlap an input. */
+ * (or NULL) = dL/d state_in.  No gradient may overlap an input, the states' among them. */
 int gleam_linattn_bwd(const gleam_linattn_desc* desc, const void* q, const void* k, const void* v, const float* log_decay,
                       const int32_t* lengths, const float* state_in, const void* g_o, const float* g_state_out, void* g_q,
                       void* g_k, void* g_v, float* g_state_in, void* ws, size_t ws_bytes, void* stream);

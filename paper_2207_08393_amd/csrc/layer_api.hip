@@ -13,6 +13,8 @@ namespace {
 
 constexpr long long kMostElements = 1LL << 40;   // keeps every byte offset far inside int64
 
+constexpr long long kMostProblems = 1LL << 29;    // sequences x pixels x heads: three workgroups each fit a launch
+
 inline bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) % 256) == 0; }
 
 // a * b, or -1 beyond kMostElements; both at least 1
@@ -30,6 +32,7 @@ int check_norm(const gleam_layer_norm_desc* d) {
     if (!d) return GLEAM_E_NULL;
     const int rc = check_rows(d->dtype, d->rows, d->n, {d->ld_in, d->ld_out});
     if (rc) return rc;
+    if (d->n > 0x7fffffffLL) return GLEAM_E_DIMS;
     return d->eps > 0.f && std::isfinite(d->eps) ? GLEAM_OK : GLEAM_E_DESC;
 }
 
@@ -88,7 +91,7 @@ int check_linattn(const gleam_linattn_desc* d, bool gradients) {
         if (h < 1 || d->heads < h || d->heads % h) return GLEAM_E_DIMS;
     if (d->B < 1 || d->T < 1 || d->P < 1 || d->T > (1 << 30)) return GLEAM_E_DIMS;
     const long long problems = product(product(d->B, d->P), d->heads);
-    if (problems < 0 || problems > 0x7fffffffLL || product(problems, d->T) < 0) return GLEAM_E_DIMS;
+    if (problems < 0 || problems > kMostProblems || product(problems, d->T) < 0) return GLEAM_E_DIMS;
     if (product(problems * d->T, std::max(d->dk, d->dv)) < 0 || product(problems, d->dk * d->dv) < 0) return GLEAM_E_DIMS;
     int rc = check_strides(*d, d->q, d->q_heads, d->dk, gradients);
     if (!rc) rc = check_strides(*d, d->k, d->k_heads, d->dk, gradients);
@@ -192,6 +195,7 @@ int gleam_linattn_bwd(const gleam_linattn_desc* desc, const void* q, const void*
         for (const void* x : {q, k, v, g_o})
             if (g == x) return GLEAM_E_DIMS;
     if (g_q == g_k || g_q == g_v || g_k == g_v) return GLEAM_E_DIMS;
+    if (g_state_in && (g_state_in == g_state_out || g_state_in == state_in)) return GLEAM_E_DIMS;   // read and written side by side
     rc = check_ws(ws, ws_bytes, linattn_bwd_ws_bytes(*desc));
     if (rc) return rc;
     return status_of(linattn_backward(*desc, q, k, v, log_decay, lengths, state_in, g_o, g_state_out, g_q, g_k, g_v, g_state_in, ws,

@@ -307,7 +307,7 @@ __device__ __forceinline__ Work work_of(const MixArgs& a, unsigned groups, unsig
 // ahead of time.  (A kernel of its own: where one kernel has both ways the compiler waits for loads in flight when it reuses their
 // registers, since it cannot see that they have arrived.)
 template <class T, int D, bool STATES, int PARTS, bool NARROW>
-__global__ __launch_bounds__((Shape<T, D>::kThreads), (STATES ? 3 : 2)) void mix_kernel(MixArgs args) {
+__global__ __launch_bounds__((Shape<T, D>::kThreads), (STATES && PARTS < 3 ? 3 : 2)) void mix_kernel(MixArgs args) {
     typedef Shape<T, D> S;
     typedef Mma<T> M;
     typedef typename M::Frag Frag;
@@ -965,9 +965,9 @@ __global__ __launch_bounds__(kStepThreads) void mix_step_kernel(MixArgs args) {
     }
     red[tid] = o;
     __syncthreads();
-    // the sum over the threads of a column quad in two steps, then one thread an element
+    // the sum over the threads of a column quad, eight or more, in two steps, then one thread an element
     const int w = 1 << log_w;
-    if (tid < 4 * w && rows >= 4) {
+    if (tid < 4 * w) {
         o = red[tid];
         for (int k = tid + 4 * w; k < kStepThreads; k += 4 * w) o += red[k];
     }
@@ -977,7 +977,7 @@ __global__ __launch_bounds__(kStepThreads) void mix_step_kernel(MixArgs args) {
     if (tid < dv) {
         const int quad = tid >> 2, i = tid & 3;
         float e = red[quad][i];
-        for (int k = 1; k < 4 && k < rows; ++k) e += red[k * w + quad][i];
+        for (int k = 1; k < 4; ++k) e += red[k * w + quad][i];
         put_f32((T*)a.out + r.b * a.o.s.b + r.p * a.o.s.p + r.h * a.o.s.h + tid, live ? e * a.out_scale : 0.f);
     }
 }

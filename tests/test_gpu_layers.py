@@ -416,3 +416,47 @@ def test_linattn_offsets_past_32_bits():
     desc = gb.make_linattn(q, k, v, o, 1.0)
     gb.gleam_linattn_fwd(desc, q, k, v, a, None, None, o, None, None)
     assert_close(host(o), lo.linattn(host(q), host(k), host(v), host(a), 1.0)[0], BF16, "o")
+
+
+def test_captured_calls_replay_as_the_eager_ones():
+    """Layer norm, linear attention in segments, its gradients and dropout in one graph, replayed with other inputs and another step each
+    time, eager work in between."""
+    B, T, P, H, d = 1, 700, 1, 2, 32
+    rows, C = B * T * P, H * d
+    x = torch.randn(rows, C, device="cuda").bfloat16()
+    gamma, beta, a = torch.ones(C, device="cuda"), torch.zeros(C, device="cuda"), torch.tensor([-0.1, -0.01], device="cuda")
+    step = torch.zeros(1, dtype=torch.int64, device="cuda")
+    norm, drop = gb.make_layer_norm(torch.bfloat16, rows, C), gb.make_dropout(torch.bfloat16, rows, C, 0.3, 5)
+    y, o, h = torch.empty_like(x), torch.empty_like(x).view(B, T, P, H, d), torch.empty_like(x)
+    q = y.view(B, T, P, H, d)
+    grads = [torch.empty_like(q) for _ in range(3)]
+    mix = gb.make_linattn(q, q, q, o, 0.2)
+    fwd, bwd = gb.gleam_linattn_workspace_bytes(mix)
+    assert fwd > 0
+    ws = torch.empty(max(fwd, bwd), dtype=torch.uint8, device="cuda")
+
+    def calls():
+        gb.gleam_layer_norm_fwd(norm, x, gamma, beta, y)
+        gb.gleam_linattn_fwd(mix, q, q, q, a, None, None, o, None, ws)
+        gb.gleam_linattn_bwd(mix, q, q, q, a, None, None, o, None, *grads, None, ws)
+        gb.gleam_dropout_fwd(drop, o.view(rows, C), x, h, step)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    masks = []
+    for k in range(4):
+        x.copy_(torch.randn(rows, C, device="cuda"))
+        step.fill_(k)
+        graph.replay()
+        got = [t.clone() for t in (y, o, h, *grads)]
+        torch.cuda.synchronize()
+        calls()
+        assert all(torch.equal(g, t) for g, t in zip(got, (y, o, h, *grads)))
+        masks.append((h - x == 0).sum().item())
+    assert len(set(masks)) > 1                                                     # another mask at every step

@@ -71,7 +71,7 @@ def test_linattn_refusals():
     S = gb.gleam_seq_strides
     bad = [(0, None, gb.GLEAM_E_NULL), (0, changed(d, dtype=2), gb.GLEAM_E_DESC), (0, changed(d, scale=float("inf")), gb.GLEAM_E_DESC)]
     bad += [(0, changed(d, **{f: v}), gb.GLEAM_E_DIMS) for f, v in (("dk", 0), ("dk", 129), ("dv", 0), ("dv", 129), ("heads", 0), ("q_heads", 3), ("k_heads", 0),
-                                                                  ("v_heads", 8), ("B", 0), ("T", 0), ("P", -1), ("T", (1 << 30) + 1), ("B", 1 << 31), ("P", 1 << 45),
+                                                                  ("v_heads", 8), ("B", 0), ("T", 0), ("P", -1), ("T", (1 << 30) + 1), ("B", 1 << 31), ("P", 1 << 28), ("P", 1 << 45),
                                                                   ("q", S(-1, 1, 1, 1)), ("k", S(1 << 45, 1, 1, 1)))]
     args = [C.byref(d), *FAKE[:3], FAKE[3], FAKE[4], FAKE[5], FAKE[6], FAKE[7], FAKE[8], 1 << 40, None]
     o = d.o
@@ -82,7 +82,7 @@ def test_linattn_refusals():
     q = d.q
     refused(L.gleam_linattn_bwd, args, bad + [(i, None, gb.GLEAM_E_NULL) for i in (1, 2, 3, 4, 7, 9, 10, 11, 13)] +
             [(9, FAKE[0], gb.GLEAM_E_DIMS), (10, FAKE[6], gb.GLEAM_E_DIMS), (11, FAKE[9], gb.GLEAM_E_DIMS), (14, bwd - 256, gb.GLEAM_E_WORKSPACE),
-             (13, FAKE[12] + 64, gb.GLEAM_E_WORKSPACE), (0, changed(d, q=S(q.b, 0, q.p, q.h)), gb.GLEAM_E_DIMS)])
+             (13, FAKE[12] + 64, gb.GLEAM_E_WORKSPACE), (12, FAKE[7], gb.GLEAM_E_DIMS), (12, FAKE[5], gb.GLEAM_E_DIMS), (0, changed(d, q=S(q.b, 0, q.p, q.h)), gb.GLEAM_E_DIMS)])
     n = C.c_size_t(0)
     assert L.gleam_linattn_workspace_bytes(C.byref(d), C.byref(n), None) == gb.GLEAM_E_NULL
     assert L.gleam_linattn_workspace_bytes(changed(d, T=0), C.byref(n), C.byref(n)) == gb.GLEAM_E_DIMS
