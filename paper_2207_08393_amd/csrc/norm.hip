@@ -202,11 +202,11 @@ __global__ __launch_bounds__(threads_of<LANES>()) void norm_fwd_kernel(NormArgs 
 }
 
 template <class T, int LANES, int NV>
-__global__ __launch_bounds__(threads_of<LANES>()) void norm_bwd_kernel(NormArgs a) {
+__global__ __launch_bounds__(threads_of<LANES>(), (NV * vec_of<T>() <= 8 && LANES <= 64 ? 4 : 1)) void norm_bwd_kernel(NormArgs a) {
     constexpr int VE = vec_of<T>(), TEAMS = threads_of<LANES>() / LANES;
     constexpr bool kKeep = NV * VE <= kKept, kAhead = NV * VE <= (LANES == 1024 ? 8 : kKept);
     __shared__ float red[LANES > 64 ? 2 * LANES / 64 : 1];
-    __shared__ float fold[TEAMS > 1 ? TEAMS : 1][TEAMS > 1 ? LANES * VE : 1];
+    __shared__ float fold[TEAMS > 1 ? kNormThreads / 64 : 1][TEAMS > 1 ? LANES * VE : 1];
     const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES, n = (int)a.n;
     const bool narrow = n < VE;
     const float inv_n = 1.f / (float)n;
@@ -282,15 +282,21 @@ __global__ __launch_bounds__(threads_of<LANES>()) void norm_bwd_kernel(NormArgs 
             float v[VE];
 #pragma unroll
             for (int i = 0; i < VE; ++i) v[i] = k ? db[j][i] : dg[j][i];
-            if constexpr (TEAMS > 1) {
-                __syncthreads();
+            if constexpr (TEAMS > 1) {                // the teams of a wave, then the waves
 #pragma unroll
-                for (int i = 0; i < VE; ++i) fold[team][lane * VE + i] = v[i];
+                for (int o = LANES; o < 64; o *= 2)
+#pragma unroll
+                    for (int i = 0; i < VE; ++i) v[i] += __shfl_xor(v[i], o);
+                __syncthreads();
+                if ((threadIdx.x & 63) < LANES)
+#pragma unroll
+                    for (int i = 0; i < VE; ++i) fold[threadIdx.x >> 6][lane * VE + i] = v[i];
                 __syncthreads();
                 if (team == 0) {
 #pragma unroll
                     for (int i = 0; i < VE; ++i)
-                        for (int t = 1; t < TEAMS; ++t) v[i] += fold[t][lane * VE + i];
+#pragma unroll
+                        for (int w = 1; w < kNormThreads / 64; ++w) v[i] += fold[w][lane * VE + i];
                 }
             }
             if (team == 0) {
@@ -327,28 +333,72 @@ __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float* __restri
 // ------------------------------------------------------------------ rows longer than the registers of a workgroup
 constexpr int kLongThreads = 1024;
 
+// f(first column, columns) of the vectors of a row that are this thread's.
+template <class T, class F>
+__device__ __forceinline__ void each_vector(long long n, F&& f) {
+    constexpr int VE = vec_of<T>();
+    for (long long c = (long long)threadIdx.x * VE; c < n; c += (long long)kLongThreads * VE) f(c, n - c < VE ? (int)(n - c) : VE);
+}
+template <class T>
+__device__ __forceinline__ void load_some(const T* p, int left, float* v) {
+    constexpr int VE = vec_of<T>();
+    if (left == VE) {
+        Pack<T, VE> x;
+        x.load(p);
+#pragma unroll
+        for (int i = 0; i < VE; ++i) v[i] = x.get(i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VE; ++i) v[i] = i < left ? to_f32(p[i]) : 0.f;
+    }
+}
+template <class T>
+__device__ __forceinline__ void store_some(T* p, int left, const float* v) {
+    constexpr int VE = vec_of<T>();
+    if (left == VE) {
+        Pack<T, VE> x;
+        x.set(v);
+        x.store(p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VE; ++i)
+            if (i < left) put_f32(p + i, v[i]);
+    }
+}
+
 // One workgroup a row, the row read three times (from the cache after the first, up to its size).
 template <class T>
 __global__ __launch_bounds__(kLongThreads) void norm_fwd_long_kernel(NormArgs a) {
+    constexpr int VE = vec_of<T>();
     __shared__ float red[kLongThreads / 64];
     const long long row = blockIdx.x;
     const T* x = (const T*)a.x + row * a.ld_x;
     T* y = (T*)a.out + row * a.ld_y;
     const float inv_n = 1.f / (float)a.n;
-    float s[1] = {0.f};
+    float s[1] = {0.f}, v[VE];
     const float pivot = to_f32(x[0]);
-    for (long long c = threadIdx.x; c < a.n; c += kLongThreads) s[0] += to_f32(x[c]) - pivot;
+    each_vector<T>(a.n, [&](long long c, int left) {
+        load_some(x + c, left, v);
+#pragma unroll
+        for (int i = 0; i < VE; ++i) s[0] += i < left ? v[i] - pivot : 0.f;
+    });
     team_sum<kLongThreads>(s, red);
     const float mean = pivot + s[0] * inv_n;
     s[0] = 0.f;
-    for (long long c = threadIdx.x; c < a.n; c += kLongThreads) {
-        const float d = to_f32(x[c]) - mean;
-        s[0] += d * d;
-    }
+    each_vector<T>(a.n, [&](long long c, int left) {
+        load_some(x + c, left, v);
+#pragma unroll
+        for (int i = 0; i < VE; ++i) s[0] += i < left ? (v[i] - mean) * (v[i] - mean) : 0.f;
+    });
     team_sum<kLongThreads>(s, red);
     const float rstd = 1.f / sqrtf(s[0] * inv_n + a.eps);
-    for (long long c = threadIdx.x; c < a.n; c += kLongThreads)
-        put_f32(y + c, (to_f32(x[c]) - mean) * rstd * (a.gamma ? a.gamma[c] : 1.f) + (a.beta ? a.beta[c] : 0.f));
+    each_vector<T>(a.n, [&](long long c, int left) {
+        load_some(x + c, left, v);
+#pragma unroll
+        for (int i = 0; i < VE; ++i)
+            if (i < left) v[i] = (v[i] - mean) * rstd * (a.gamma ? a.gamma[c + i] : 1.f) + (a.beta ? a.beta[c + i] : 0.f);
+        store_some(y + c, left, v);
+    });
     if (threadIdx.x == 0) {
         if (a.mean) a.mean[row] = mean;
         if (a.rstd) a.rstd[row] = rstd;
@@ -357,22 +407,37 @@ __global__ __launch_bounds__(kLongThreads) void norm_fwd_long_kernel(NormArgs a)
 
 template <class T>
 __global__ __launch_bounds__(kLongThreads) void norm_bwd_long_kernel(NormArgs a) {
+    constexpr int VE = vec_of<T>();
     __shared__ float red[2 * kLongThreads / 64];
     const long long row = blockIdx.x;
     const T *x = (const T*)a.x + row * a.ld_x, *g = (const T*)a.g + row * a.ld_y;
     T* gx = (T*)a.out + row * a.ld_x;
     const float inv_n = 1.f / (float)a.n, mean = a.mean_in[row], rstd = a.rstd_in[row];
-    float s[2] = {0.f, 0.f};
-    for (long long c = threadIdx.x; c < a.n; c += kLongThreads) {
-        const float gg = to_f32(g[c]) * (a.gamma ? a.gamma[c] : 1.f);
-        s[0] += gg;
-        s[1] += gg * ((to_f32(x[c]) - mean) * rstd);
-    }
+    float s[2] = {0.f, 0.f}, v[VE], w[VE];
+    auto load = [&](long long c, int left) {          // normalised values and g gamma
+        load_some(x + c, left, v);
+        load_some(g + c, left, w);
+#pragma unroll
+        for (int i = 0; i < VE; ++i) {
+            v[i] = (v[i] - mean) * rstd;
+            if (i < left && a.gamma) w[i] *= a.gamma[c + i];
+        }
+    };
+    each_vector<T>(a.n, [&](long long c, int left) {
+        load(c, left);
+#pragma unroll
+        for (int i = 0; i < VE; ++i) {
+            s[0] += i < left ? w[i] : 0.f;
+            s[1] += i < left ? w[i] * v[i] : 0.f;
+        }
+    });
     team_sum<kLongThreads>(s, red);
-    for (long long c = threadIdx.x; c < a.n; c += kLongThreads) {
-        const float gg = to_f32(g[c]) * (a.gamma ? a.gamma[c] : 1.f), xh = (to_f32(x[c]) - mean) * rstd;
-        put_f32(gx + c, rstd * (gg - s[0] * inv_n - xh * (s[1] * inv_n)));
-    }
+    each_vector<T>(a.n, [&](long long c, int left) {
+        load(c, left);
+#pragma unroll
+        for (int i = 0; i < VE; ++i) w[i] = rstd * (w[i] - s[0] * inv_n - v[i] * (s[1] * inv_n));
+        store_some(gx + c, left, w);
+    });
 }
 
 // Partial sums over rows blockIdx.y, + gridDim.y, ...: one column a thread.  Runs before norm_bwd_long_kernel, whose output may
@@ -400,14 +465,15 @@ struct Team {
 Team team_for(const gleam_layer_norm_desc& d) {
     const long long units = (d.n * (d.dtype ? 2 : 4) + 15) / 16;
     for (Team t : {Team{4, 1}, Team{8, 1}, Team{16, 1}, Team{32, 1}, Team{64, 1}, Team{64, 2}, Team{64, 4}, Team{256, 2}, Team{256, 4},
-                   Team{512, 3}, Team{1024, 2}})
+                   Team{512, 3}, Team{1024, 2}, Team{1024, d.dtype ? 0 : 4}})
         if (units <= (long long)t.lanes * t.nv) return t;
     return Team{0, 0};
 }
-// Workgroups that walk the rows.  Backward: every one leaves 2 n partial sums, so that there are no more than fill the chip.
+// Workgroups that walk the rows.  Backward: every one leaves 2 n partial sums, so there are no more than keep the chip busy (2000 rows
+// of 5001 float32, 512 lanes: 51 us with 512 workgroups, 45 with 256).
 int grid_for(const gleam_layer_norm_desc& d, Team t, bool backward) {
     const long long teams = t.lanes > 64 ? 1 : kNormThreads / t.lanes, wgs = (d.rows + teams - 1) / teams;
-    const int most = backward ? (t.lanes >= 512 ? 512 : 1024) : 2048;
+    const int most = backward ? (t.lanes >= 512 ? 256 : 1024) : 2048;
     return (int)(wgs < most ? wgs : most);
 }
 int long_parts(const gleam_layer_norm_desc& d) { return (int)(d.rows < 64 ? d.rows : 64); }
@@ -427,6 +493,7 @@ void with_team(Team t, F&& f) {
     GLEAM_TEAM(256, 4);
     GLEAM_TEAM(512, 3);
     GLEAM_TEAM(1024, 2);
+    if constexpr (sizeof(T) == 4) GLEAM_TEAM(1024, 4);
 #undef GLEAM_TEAM
 }
 

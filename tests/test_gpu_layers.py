@@ -39,7 +39,7 @@ def rows_array(rows, n, ld, dtype, fill=POISON, offset=0):
 
 # ------------------------------------------------------------------------------------------------------------ layer norm
 NORM = [(1, 1, 0, 0), (3, 1, 2, 1), (1, 7, 0, 0), (5, 2, 0, 0), (9, 8, 0, 0), (4, 13, 0, 1), (70, 16, 0, 0), (65, 17, 3, 3), (33, 64, 0, 0), (130, 100, 0, 0),
-        (17, 129, 0, 0), (16, 250, 6, 0), (7, 511, 0, 0), (9, 1001, 0, 2), (5, 2048, 0, 0), (3, 4100, 4, 0), (4, 5001, 7, 0), (3, 8192, 0, 0), (2, 16384, 0, 0),
+        (17, 129, 0, 0), (16, 250, 6, 0), (7, 511, 0, 0), (9, 1001, 0, 2), (5, 2048, 0, 0), (3, 4100, 4, 0), (4, 5001, 7, 0), (3, 8192, 0, 0), (2, 16384, 0, 0), (700, 12000, 0, 0), (5, 9001, 0, 1),
         (3, 16391, 1, 0), (2, 40003, 0, 1)]
 
 
