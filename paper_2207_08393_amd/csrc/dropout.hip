@@ -44,7 +44,8 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(DropoutArgs a) {
     if (first >= size) return;
     const T *x = (const T*)a.x, *res = (const T*)a.res;
     T* out = (T*)a.out;
-    const long long row = a.rows == 1 ? 0 : first / a.n, col = first - row * a.n;
+    const bool few = size <= 0x7fffffff;   // a division of 32 bits does
+    const long long row = a.rows == 1 ? 0 : few ? (long long)((unsigned)first / (unsigned)a.n) : first / a.n, col = first - row * a.n;
     if (col + 8 <= a.n) {
         Pack<T, 8> px, pr;
         px.load(x + row * a.ld_x + col);
@@ -60,16 +61,33 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(DropoutArgs a) {
         px.store(out + row * a.ld_out + col);
         return;
     }
-    const uint4 r = draws_of(a, (unsigned long long)blk);
-    long long rr = row, cc = col;
-    for (int i = 0; i < 8 && first + i < size; ++i) {
-        float v = draw16(r, i) < a.kept ? to_f32(x[rr * a.ld_x + cc]) * a.scale : 0.f;
-        if (res) v += to_f32(res[rr * a.ld_res + cc]);
-        put_f32(out + rr * a.ld_out + cc, v);
-        if (++cc == a.n) {
-            cc = 0;
-            ++rr;
+    // places of the eight elements, then all loads, then the rest
+    const int there = size - first < 8 ? (int)(size - first) : 8;
+    const T *px = x + row * a.ld_x + col, *pr = res ? res + row * a.ld_res + col : nullptr;
+    T* po = out + row * a.ld_out + col;
+    T vx[8], vr[8];
+    T* to[8];
+    long long cc = col;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        to[i] = po;
+        vx[i] = vr[i] = (T)0;
+        if (i < there) {
+            vx[i] = *px;
+            if (res) vr[i] = *pr;
         }
+        const bool end = ++cc == a.n;
+        px += end ? a.ld_x - a.n + 1 : 1;
+        pr += end ? a.ld_res - a.n + 1 : 1;
+        po += end ? a.ld_out - a.n + 1 : 1;
+        cc = end ? 0 : cc;
+    }
+    const uint4 r = draws_of(a, (unsigned long long)blk);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float v = draw16(r, i) < a.kept ? to_f32(vx[i]) * a.scale : 0.f;
+        if (res) v += to_f32(vr[i]);
+        if (i < there) put_f32(to[i], v);
     }
 }
 
