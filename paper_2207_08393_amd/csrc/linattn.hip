@@ -17,8 +17,8 @@
 //
 // Measured (listed calls; copy rate of the card 5.2 TB/s, bfloat16 matrix products 1212 TFLOP/s):
 //   4 x 2048 tokens, 16 heads of 64, bfloat16               39 us   (14 segments, 10 states, 23 outputs; all read once and written once: 13)
-//   16384 tokens, 16 heads of 128, 4 of k and v, gradients 310 us   (65, 16, 192, and 31 for the sum over shared heads; 52)
-//   3 x 1001 tokens, 6 heads of 40 and 72, float32, gradients 68 us (19, 10, 46; 5)
+//   16384 tokens, 16 heads of 128, 4 of k and v, gradients 320 us   (64, 16, 194, and 31 for the sum over shared heads; 52)
+//   3 x 1001 tokens, 6 heads of 40 and 72, float32, gradients 65 us (17, 8, 47; 5)
 // What bounds the chunk loop at a width of 128 is no single unit: vector instructions 39 %, matrix instructions 32 %, LDS 45 % of the
 // time busy, at the two workgroups of 256 registers a lane that a compute unit holds.  Tried without gain: other paddings of the LDS rows
 // (0 to +3 % time), chunks without branches where they are whole, half or twice as many segments.
@@ -1007,14 +1007,18 @@ int width_of(int dk, int dv) {
     const int d = dk > dv ? dk : dv;
     return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : 128;
 }
-// Segments of a call of `roles` passes: enough workgroups to fill the chip where there are few problems.
+// Segments of a call of `roles` passes, where there are few problems: as many workgroups as run at once (256 compute units hold two of
+// them each, four at a width of 64), or twice as many where they have eight chunks each all the same, for the pass over segments, which has
+// fewer.  (16384 tokens, 16 heads of 128, gradients: 296 us with one round, 288 with two, 302 with three; 3 x 1001 tokens, 6 heads of 40
+// and 72, float32, gradients: 67 with one round of four chunks each, 71 with two of two.)
 struct Split {
     int n_seg, chunks;
 };
 Split split_of(const gleam_linattn_desc& d, int roles) {
     const int D = width_of(d.dk, d.dv), L = d.dtype && D > 32 ? 64 : 32;
     const long long problems = d.B * d.P * d.heads, groups = D == 32 ? (problems + 3) / 4 : problems, chunks = (d.T + L - 1) / L;
-    long long n = 1024 / (groups * roles);
+    const long long once = (D == 64 ? 1024 : 512) / (groups * roles);
+    long long n = 2 * once * 8 <= chunks ? 2 * once : once;
     if (n > chunks / 2) n = chunks / 2;
     if (n < 2) return {1, (int)chunks};
     const long long per = (chunks + n - 1) / n;
