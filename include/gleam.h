@@ -362,7 +362,7 @@ int gleam_dropout_bwd(const gleam_dropout_desc* desc, const void* g_out, void* g
  * lengths: device int32 [B] or NULL (all T), tokens of each sequence that are there; others are not read, their outputs and
  * gradients are written as zeros; values outside 0..T count as the nearest of them.  A sequence of length 0 leaves its state as it is.
  * A token that is not finite can reach the outputs of up to 63 tokens before it (and in the gradients behind it) as NaN: they share a
- * matrix product.
+ * matrix product.  Infinities, and with bfloat16 arrays states beyond 3.39e38, come out as infinity or NaN.
  * 1 <= dk, dv <= 128.  One token (T = 1) takes the recurrent form: every state is read once and written once. */
 typedef struct { int64_t b, t, p, h; } gleam_seq_strides;
 typedef struct {
