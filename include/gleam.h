@@ -309,7 +309,8 @@ int gleam_unrolled_infer(const gleam_geom* geom, const gleam_prox_desc* prox, in
 
 /* Layer norm over the last dimension of `rows` rows of n elements: mean m and variance s^2 (over n) of the row,
  *     y = (x - m) * r * gamma + beta,   r = 1 / sqrt(s^2 + eps)
- * ld_in, ld_out: elements between the starts of neighbouring rows of x and g_x, and of y and g_y (>= n).  eps > 0. */
+ * ld_in, ld_out: elements between the starts of neighbouring rows of x and g_x, and of y and g_y (>= n).  eps > 0.  Where s^2 passes the
+ * range of a float32, r = 0.  A row that holds an infinity or NaN becomes NaN. */
 typedef struct {
     int32_t dtype;
     float eps;

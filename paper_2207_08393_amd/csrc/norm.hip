@@ -1,8 +1,10 @@
 // Layer norm over rows of n elements, forward and backward (gfx950).
 //
 // Forward: one read and one write of the row.  A team of lanes holds a whole row in registers, so the variance is the mean of the
-// squared distances from the mean (no cancellation where the mean is large) without a second read; the mean is the row's first element
-// plus the mean distance from it, so that a row of equal numbers has exactly that mean and becomes zeros.  Backward: one read of x and g_y,
+// squared distances from the mean (no cancellation where the mean is large) without a second read.  The mean is a sum of x / n (which stays
+// in range) and then the mean of what the elements are away from that, which takes out what the first sum was rounded by: it is
+// good to its last bits whatever the row's order and size, and a row of equal numbers has exactly that mean and becomes zeros.  Where the
+// variance passes the range of a float32, r = 0 and outputs are beta.  Backward: one read of x and g_y,
 // one write of g_x; every lane keeps its columns from row to row and sums g_gamma and g_beta in registers, a workgroup writes one
 // partial sum per column and a second launch adds them up in a fixed order.  Both are bound by HBM.
 // Measured: forward 4 x 320 x 256 pixels of 100 channels, float32, 60 us (4.4 TB/s); backward 4 x 640 x 320 of 128 channels, bfloat16, 123 us
@@ -10,6 +12,8 @@
 //
 // Rows too long for the registers of a workgroup are read three times (forward) or twice (backward), see the streaming kernels.
 #include <hip/hip_runtime.h>
+
+#include <cfloat>
 
 #include "layer_common.h"
 #include "layer_ops.h"
@@ -25,14 +29,27 @@ constexpr int vec_of() { return 16 / (int)sizeof(T); }
 template <int LANES>
 constexpr int threads_of() { return LANES > 64 ? LANES : kNormThreads; }
 
+// Another lane's value, by a DPP pattern.
+template <int PATTERN>
+__device__ __forceinline__ float dpp(float v) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), PATTERN, 0xf, 0xf, false));
+}
+template <class V>
+__device__ __forceinline__ float sum_of_pair(V r) { return __uint_as_float(r[0]) + __uint_as_float(r[1]); }
+
 // Sums over a team of LANES lanes, the same values in all of them.  A team wider than a wave is the workgroup; `red` is then LDS for
 // N floats a wave, and the barrier in front makes its last use over.
 template <int LANES, int N>
 __device__ __forceinline__ void team_sum(float (&v)[N], float* red) {
 #pragma unroll
-    for (int o = (LANES < 64 ? LANES : 64) / 2; o > 0; o >>= 1)
-#pragma unroll
-        for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], o);
+    for (int k = 0; k < N; ++k) {
+        v[k] += dpp<0xB1>(v[k]);                      // lane i and i ^ 1
+        v[k] += dpp<0x4E>(v[k]);                      // i ^ 2
+        if (LANES >= 8) v[k] += dpp<0x141>(v[k]);     // 7 - i of eight lanes, which are equal in fours
+        if (LANES >= 16) v[k] += dpp<0x140>(v[k]);    // 15 - i of sixteen
+        if (LANES >= 32) v[k] = sum_of_pair(__builtin_amdgcn_permlane16_swap(__float_as_uint(v[k]), __float_as_uint(v[k]), false, false));
+        if (LANES >= 64) v[k] = sum_of_pair(__builtin_amdgcn_permlane32_swap(__float_as_uint(v[k]), __float_as_uint(v[k]), false, false));
+    }
     if constexpr (LANES > 64) {
         constexpr int W = LANES / 64;
         __syncthreads();
@@ -50,12 +67,14 @@ __device__ __forceinline__ void team_sum(float (&v)[N], float* red) {
 }
 
 // The columns of one of a lane's vectors, the same in every row.  The row's last vector is moved back to end with the row; its first
-// elements are then those of the vector before it and stay out of sums (keep = 0; their results are written twice, the same bits).
+// elements are then those of the vector before it and stay out of sums (their results are written twice, the same bits).  What stays out
+// is masked and not multiplied by zero, which would make NaN of an infinity or a square that overflows.
 // Rows shorter than a vector: hi < VE, element by element.
 template <int VE>
 struct Columns {
     int col, hi;
-    float keep[VE];
+    unsigned counts[VE];      // all bits where the element is one of the vector's own
+    __device__ __forceinline__ float own(int i, float v) const { return __uint_as_float(__float_as_uint(v) & counts[i]); }
     __device__ __forceinline__ void set(int unit, int n) {
         col = unit * VE;
         hi = col < n ? VE : 0;
@@ -70,7 +89,10 @@ struct Columns {
         }
         if (!hi) col = 0;
 #pragma unroll
-        for (int i = 0; i < VE; ++i) keep[i] = i >= lo && i < hi ? 1.f : 0.f;
+        for (int i = 0; i < VE; ++i) {
+            counts[i] = i >= lo && i < hi ? ~0u : 0u;
+            asm("" : "+v"(counts[i]));   // stays a number: as conditions they would be pairs of scalar registers, more than there are
+        }
     }
 };
 // Lanes without columns read the row's first elements, or nothing where a row is shorter than a vector; they count for nothing.
@@ -112,6 +134,18 @@ __device__ __forceinline__ void load_param(const float* p, const Columns<VE>& c,
     }
 }
 
+// The first mean and the mean of the distances from it.  The latter is out of range only where the row holds infinities or NaN (then the
+// first mean is one of them), or numbers of both signs near the end of the range.
+__device__ __forceinline__ float mean_of(float first, float rest) { return fabsf(rest) <= FLT_MAX ? first + rest : first; }
+// The variance from the mean distance d[0] and the sum d[1] of squared distances from the first mean.  False where it would be lost in the
+// difference (the spread is of the size of the first mean's rounding, as in a row of equal numbers) or is out of range: then the squared
+// distances from the mean itself are summed.
+__device__ __forceinline__ bool variance_of(const float (&d)[2], float inv_n, float& var) {
+    const float about = d[1] * inv_n, off = d[0] * d[0];
+    var = about - off;
+    return d[1] <= FLT_MAX && off <= 0.0625f * about;
+}
+
 struct NormArgs {
     const void *x, *g;
     const float *gamma, *beta, *mean_in, *rstd_in;
@@ -130,7 +164,7 @@ template <class T, int LANES, int NV>
 __global__ __launch_bounds__(threads_of<LANES>()) void norm_fwd_kernel(NormArgs a) {
     constexpr int VE = vec_of<T>(), TEAMS = threads_of<LANES>() / LANES;
     constexpr bool kKeep = NV * VE <= kKept;
-    __shared__ float red[LANES > 64 ? LANES / 64 : 1];
+    __shared__ float red[LANES > 64 ? 2 * LANES / 64 : 1];
     const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES, n = (int)a.n;
     const bool narrow = n < VE;
     const float inv_n = 1.f / (float)n;
@@ -151,11 +185,9 @@ __global__ __launch_bounds__(threads_of<LANES>()) void norm_fwd_kernel(NormArgs 
     auto there = [&](long long row) { return row < a.rows ? row : a.rows - 1; };
     long long row = (long long)blockIdx.x * TEAMS + team;
     Pack<T, VE> next[NV];
-    T next_pivot = x[there(row) * a.ld_x];
 #pragma unroll
     for (int j = 0; j < NV; ++j) load_cols(x + there(row) * a.ld_x, cols[j], narrow, next[j]);
     for (long long first = (long long)blockIdx.x * TEAMS; first < a.rows; first += step, row += step) {
-        const float pivot = to_f32(next_pivot);
         float v[NV][VE], s[1] = {0.f};
 #pragma unroll
         for (int j = 0; j < NV; ++j)
@@ -163,26 +195,44 @@ __global__ __launch_bounds__(threads_of<LANES>()) void norm_fwd_kernel(NormArgs 
             for (int i = 0; i < VE; ++i) v[j][i] = next[j].get(i);
         if (first + step < a.rows) {
             const T* p = x + there(row + step) * a.ld_x;
-            next_pivot = p[0];
 #pragma unroll
             for (int j = 0; j < NV; ++j) load_cols(p, cols[j], narrow, next[j]);
         }
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int i = 0; i < VE; ++i) s[0] += (v[j][i] - pivot) * cols[j].keep[i];
+            for (int i = 0; i < VE; ++i) s[0] += cols[j].own(i, v[j][i]) * inv_n;
         team_sum<LANES>(s, red);
-        const float mean = pivot + s[0] * inv_n;
-        s[0] = 0.f;
+        const float first_mean = s[0];
+        float t[2] = {0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int i = 0; i < VE; ++i) {
-                v[j][i] -= mean;
-                s[0] += v[j][i] * v[j][i] * cols[j].keep[i];
+                const float d = cols[j].own(i, v[j][i] - first_mean);
+                t[0] += d * inv_n;
+                t[1] += d * d;
             }
-        team_sum<LANES>(s, red);
-        const float rstd = 1.f / sqrtf(s[0] * inv_n + a.eps);
+        team_sum<LANES>(t, red);
+        const float mean = mean_of(first_mean, t[0]);
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VE; ++i) v[j][i] -= mean;
+        float var;
+        if (!variance_of(t, inv_n, var)) {
+            s[0] = 0.f;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int i = 0; i < VE; ++i) {
+                    const float d = cols[j].own(i, v[j][i]);
+                    s[0] += d * d;
+                }
+            team_sum<LANES>(s, red);
+            var = s[0] * inv_n;
+        }
+        const float rstd = 1.f / sqrtf(var + a.eps);
         if (row >= a.rows) continue;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -254,7 +304,7 @@ __global__ __launch_bounds__(threads_of<LANES>(), (NV * vec_of<T>() <= 8 && LANE
 #pragma unroll
             for (int i = 0; i < VE; ++i) {
                 xh[j][i] = (xh[j][i] - mean) * rstd;
-                const float gy = gg[j][i] * (cols[j].keep[i] * counts);
+                const float gy = cols[j].own(i, gg[j][i]) * counts;
                 dg[j][i] += gy * xh[j][i];
                 db[j][i] += gy;
                 gg[j][i] *= gm[j][i];
@@ -304,7 +354,7 @@ __global__ __launch_bounds__(threads_of<LANES>(), (NV * vec_of<T>() <= 8 && LANE
             if (team == 0) {
 #pragma unroll
                 for (int i = 0; i < VE; ++i)
-                    if (cols[j].keep[i] != 0.f) part[k * a.n + cols[j].col + i] = v[i];
+                    if (cols[j].counts[i]) part[k * a.n + cols[j].col + i] = v[i];
             }
         }
     }
@@ -372,28 +422,43 @@ __device__ __forceinline__ void store_some(T* p, int left, const float* v) {
 template <class T>
 __global__ __launch_bounds__(kLongThreads) void norm_fwd_long_kernel(NormArgs a) {
     constexpr int VE = vec_of<T>();
-    __shared__ float red[kLongThreads / 64];
+    __shared__ float red[2 * kLongThreads / 64];
     const long long row = blockIdx.x;
     const T* x = (const T*)a.x + row * a.ld_x;
     T* y = (T*)a.out + row * a.ld_y;
     const float inv_n = 1.f / (float)a.n;
     float s[1] = {0.f}, v[VE];
-    const float pivot = to_f32(x[0]);
     each_vector<T>(a.n, [&](long long c, int left) {
         load_some(x + c, left, v);
 #pragma unroll
-        for (int i = 0; i < VE; ++i) s[0] += i < left ? v[i] - pivot : 0.f;
+        for (int i = 0; i < VE; ++i) s[0] += i < left ? v[i] * inv_n : 0.f;
     });
     team_sum<kLongThreads>(s, red);
-    const float mean = pivot + s[0] * inv_n;
-    s[0] = 0.f;
+    const float first_mean = s[0];
+    float t[2] = {0.f, 0.f};
     each_vector<T>(a.n, [&](long long c, int left) {
         load_some(x + c, left, v);
 #pragma unroll
-        for (int i = 0; i < VE; ++i) s[0] += i < left ? (v[i] - mean) * (v[i] - mean) : 0.f;
+        for (int i = 0; i < VE; ++i) {
+            const float d = i < left ? v[i] - first_mean : 0.f;
+            t[0] += d * inv_n;
+            t[1] += d * d;
+        }
     });
-    team_sum<kLongThreads>(s, red);
-    const float rstd = 1.f / sqrtf(s[0] * inv_n + a.eps);
+    team_sum<kLongThreads>(t, red);
+    const float mean = mean_of(first_mean, t[0]);
+    float var;
+    if (!variance_of(t, inv_n, var)) {
+        s[0] = 0.f;
+        each_vector<T>(a.n, [&](long long c, int left) {
+            load_some(x + c, left, v);
+#pragma unroll
+            for (int i = 0; i < VE; ++i) s[0] += i < left ? (v[i] - mean) * (v[i] - mean) : 0.f;
+        });
+        team_sum<kLongThreads>(s, red);
+        var = s[0] * inv_n;
+    }
+    const float rstd = 1.f / sqrtf(var + a.eps);
     each_vector<T>(a.n, [&](long long c, int left) {
         load_some(x + c, left, v);
 #pragma unroll
@@ -472,10 +537,11 @@ Team team_for(const gleam_layer_norm_desc& d) {
     return Team{0, 0};
 }
 // Workgroups that walk the rows.  Backward: every one leaves 2 n partial sums, so there are no more than keep the chip busy (2000 rows
-// of 5001 float32, 512 lanes: 51 us with 512 workgroups, 45 with 256).
+// of 5001 float32, 512 lanes: 51 us with 512 workgroups, 45 with 256).  Forward: 327680 rows of 100 float32 65 us with 2048 workgroups, 62
+// with 8192, 69 with one for every eight rows; 60000 of 512 bfloat16 21.8, 21.5, 23.5.
 int grid_for(const gleam_layer_norm_desc& d, Team t, bool backward) {
     const long long teams = t.lanes > 64 ? 1 : kNormThreads / t.lanes, wgs = (d.rows + teams - 1) / teams;
-    const int most = backward ? (t.lanes >= 512 ? 256 : 1024) : 2048;
+    const int most = backward ? (t.lanes >= 512 ? 256 : 1024) : 8192;
     return (int)(wgs < most ? wgs : most);
 }
 int long_parts(const gleam_layer_norm_desc& d) { return (int)(d.rows < 64 ? d.rows : 64); }

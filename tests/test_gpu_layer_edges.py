@@ -1,0 +1,98 @@
+"""Rows, tokens and sizes at which the sequence-layer operators could go wrong: against the float64 oracle, or exactly.
+
+Tolerances are those of the operators' other parity tests, derived the same way.  Layer norm: the mean is a sum of n terms x / n
+and a second one of what that left over; with at most 38 additions in a row (16 a lane, 6 in a wave, 16 waves) each within 2^-24 of
+the sum of magnitudes, itself at most twice the mean of |x| here, its error is below 38 x 2^-23 = 4.5e-6 of that; F32 = 1e-5."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import layer_oracle as lo
+from paper_2207_08393_amd import binding as gb
+from tests.gpu_util import assert_close
+
+pytestmark = pytest.mark.gpu
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+F32, ONCE = 1e-5, 2.0 ** -8
+POISON = float("nan")
+
+
+def dev(a, dtype):
+    """numpy -> device, and the values that the device has."""
+    t = torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).cuda().to(dtype)
+    return t, t.double().cpu().numpy()
+
+
+def host(t):
+    torch.cuda.synchronize()
+    return t.double().cpu().numpy()
+
+
+# ------------------------------------------------------------------------------------------------------------ layer norm
+def norm_fwd(x, gamma=None, beta=None, eps=1e-5):
+    rows, n = x.shape
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    gb.gleam_layer_norm_fwd(gb.make_layer_norm(x.dtype, rows, n, eps), x, gamma, beta, y, mean, rstd)
+    return y, mean, rstd
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,size", [(13, 1e3), (100, 1e3), (129, 1e3), (1024, 1e3), (4096, 1e4), (5001, 1e4), (16384, 1e4), (20011, 1e4)])
+def test_layer_norm_of_rows_whose_first_element_is_unlike_the_others(n, size, dtype):
+    """One channel much larger than the others, the first one or the last: the others' outputs and the mean are as good as elsewhere."""
+    print("case norm outlier", n, size, dtype, flush=True)
+    rng = np.random.default_rng(n)
+    a = rng.normal(0.3, 1.0, (6, n))
+    a[:3, 0] = size * np.array([1.0, -1.0, 3.0])
+    a[3:, -1] = size * np.array([1.0, -1.0, 3.0])
+    x, hx = dev(a, TYPES[dtype])
+    y, mean, rstd = norm_fwd(x)
+    ry, rmean, rrstd = lo.layer_norm(hx, None, None, np.float32(1e-5))
+    once = ONCE if dtype == "bf16" else 0.0
+    for r in range(6):
+        assert abs(host(mean)[r] - rmean[r]) <= F32 * np.abs(hx[r]).mean(), (r, host(mean)[r], rmean[r])
+        others = slice(1, n) if r < 3 else slice(0, n - 1)
+        assert_close(host(y)[r, others], ry[r, others], F32 + once, f"row {r}")
+    assert_close(host(rstd), rrstd, F32, "rstd")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [2, 13, 100, 129, 1024, 5001, 9001, 20011])
+def test_layer_norm_of_rows_that_begin_with_the_lowest_value(n, dtype):
+    """The variance passes the range of a float32: r = 0 and outputs are beta, as 32-bit arithmetic has it, and not NaN."""
+    print("case norm lowest", n, dtype, flush=True)
+    rng = np.random.default_rng(n)
+    x = torch.from_numpy(rng.normal(size=(5, n)).astype(np.float32)).cuda().to(TYPES[dtype])
+    low = torch.finfo(TYPES[dtype]).min
+    x[0, 0], x[1, -1], x[2, n // 2], x[3, 0] = low, low, low, -low
+    beta, hbeta = dev(rng.normal(size=n), torch.float32)
+    y, mean, rstd = norm_fwd(x, None, beta)
+    want = hbeta if dtype == "f32" else host(beta.bfloat16())
+    for r in range(4):
+        assert np.array_equal(host(y)[r], want), r
+    assert_close(host(mean)[:4], host(x)[:4].mean(1), F32, "mean")
+    assert not host(rstd)[:4].any()
+    assert_close(host(y)[4:], lo.layer_norm(host(x)[4:], None, hbeta, 1e-5)[0], F32 + (ONCE if dtype == "bf16" else 0.0), "y")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [3, 13, 100, 300, 1001, 5001, 12000, 20011])
+def test_layer_norm_of_constant_rows(n, dtype):
+    """The mean of equal numbers is that number, bit by bit."""
+    a = torch.tensor([7.0, 0.1, -3.3e4, 1e-20, 1e30, 0.0, -3e38], device="cuda")
+    x = a[:, None].repeat(1, n).to(TYPES[dtype])
+    y, mean, rstd = norm_fwd(x)
+    assert not host(y).any()
+    assert np.array_equal(host(mean), host(x)[:, 0])
+    assert_close(host(rstd), np.full(len(a), 1e-5 ** -0.5), F32, "rstd")
+
+
+@pytest.mark.parametrize("n", [13, 100, 5001, 20011])
+def test_layer_norm_of_rows_with_infinities_and_nan(n):
+    """A row that holds an infinity or NaN becomes NaN; its neighbours stay as they are."""
+    x, hx = dev(np.random.default_rng(n).normal(size=(7, n)), torch.float32)
+    y0 = norm_fwd(x)[0]
+    x[1, 0], x[3, -1], x[5, n // 2] = float("inf"), POISON, -float("inf")
+    y, mean, _ = norm_fwd(x)
+    assert np.isnan(host(y)[1::2]).all() and torch.equal(y[::2], y0[::2])
+    assert host(mean)[1] == np.inf and np.isnan(host(mean)[3]) and host(mean)[5] == -np.inf
