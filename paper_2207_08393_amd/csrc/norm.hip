@@ -95,6 +95,9 @@ struct Columns {
         }
     }
 };
+// A team is as small as the row allows, so that the first half of every lane's vectors (rounded up, of more than one) is whole: no mask.
+template <int NV, int VE>
+__device__ __forceinline__ float own(const Columns<VE>& c, int j, int i, float v) { return NV > 1 && j < (NV + 1) / 2 ? v : c.own(i, v); }
 // Lanes without columns read the row's first elements, or nothing where a row is shorter than a vector; they count for nothing.
 template <class T, int VE>
 __device__ __forceinline__ void load_cols(const T* row, const Columns<VE>& c, bool narrow, Pack<T, VE>& p) {
@@ -201,7 +204,7 @@ __global__ __launch_bounds__(threads_of<LANES>()) void norm_fwd_kernel(NormArgs 
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int i = 0; i < VE; ++i) s[0] += cols[j].own(i, v[j][i]) * inv_n;
+            for (int i = 0; i < VE; ++i) s[0] += own<NV>(cols[j], j, i, v[j][i]) * inv_n;
         team_sum<LANES>(s, red);
         const float first_mean = s[0];
         float t[2] = {0.f, 0.f};
@@ -209,7 +212,7 @@ __global__ __launch_bounds__(threads_of<LANES>()) void norm_fwd_kernel(NormArgs 
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int i = 0; i < VE; ++i) {
-                const float d = cols[j].own(i, v[j][i] - first_mean);
+                const float d = own<NV>(cols[j], j, i, v[j][i] - first_mean);
                 t[0] += d * inv_n;
                 t[1] += d * d;
             }
@@ -226,7 +229,7 @@ __global__ __launch_bounds__(threads_of<LANES>()) void norm_fwd_kernel(NormArgs 
             for (int j = 0; j < NV; ++j)
 #pragma unroll
                 for (int i = 0; i < VE; ++i) {
-                    const float d = cols[j].own(i, v[j][i]);
+                    const float d = own<NV>(cols[j], j, i, v[j][i]);
                     s[0] += d * d;
                 }
             team_sum<LANES>(s, red);
@@ -259,7 +262,8 @@ __global__ __launch_bounds__(threads_of<LANES>(), (NV * vec_of<T>() <= 8 && LANE
     constexpr bool kKeep = NV * VE <= kKept, kAhead = NV * VE <= (LANES == 1024 ? 8 : kKept);
     __shared__ float red[LANES > 64 ? 2 * LANES / 64 : 1];
     __shared__ float fold[TEAMS > 1 ? kNormThreads / 64 : 1][TEAMS > 1 ? LANES * VE : 1];
-    const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES, n = (int)a.n;
+    const int lane = TEAMS == 1 ? threadIdx.x : threadIdx.x % LANES, n = (int)a.n;
+    const int team = TEAMS == 1 ? 0 : LANES == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : threadIdx.x / LANES;
     const bool narrow = n < VE;
     const float inv_n = 1.f / (float)n;
     const T *x = (const T*)a.x, *g = (const T*)a.g;
@@ -272,7 +276,6 @@ __global__ __launch_bounds__(threads_of<LANES>(), (NV * vec_of<T>() <= 8 && LANE
         if (kKeep) load_param(a.gamma, cols[j], 1.f, gm[j]);
     }
     const long long step = (long long)gridDim.x * TEAMS;
-    auto there = [&](long long row) { return row < a.rows ? row : a.rows - 1; };
     long long row = (long long)blockIdx.x * TEAMS + team;
     Pack<T, VE> nx[NV], ng[NV];
     float next_mean, next_rstd;
@@ -285,10 +288,12 @@ __global__ __launch_bounds__(threads_of<LANES>(), (NV * vec_of<T>() <= 8 && LANE
             load_cols(g + at * a.ld_y, cols[j], narrow, ng[j]);
         }
     };
-    if (kAhead) fetch(there(row));
-    for (long long first = (long long)blockIdx.x * TEAMS; first < a.rows; first += step, row += step) {
-        if (!kAhead) fetch(there(row));
-        const float mean = next_mean, rstd = next_rstd, counts = row < a.rows ? 1.f : 0.f;
+    if (kAhead) fetch(row < a.rows ? row : a.rows - 1);
+    // teams end at different rows: their sums need no other lanes, or (a team that is the workgroup) all end alike
+    for (; row < a.rows; row += step) {
+        if constexpr (LANES >= 64) asm("" : "+s"(row));   // addresses from the row's number every time: kept from row to row they are spilled
+        if (!kAhead) fetch(row);
+        const float mean = next_mean, rstd = next_rstd;
         float xh[NV][VE], gg[NV][VE], s[2] = {0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < NV; ++j)
@@ -297,24 +302,23 @@ __global__ __launch_bounds__(threads_of<LANES>(), (NV * vec_of<T>() <= 8 && LANE
                 xh[j][i] = nx[j].get(i);
                 gg[j][i] = ng[j].get(i);
             }
-        if (kAhead && first + step < a.rows) fetch(there(row + step));
+        if (kAhead && row + step < a.rows) fetch(row + step);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             if (!kKeep) load_param(a.gamma, cols[j], 1.f, gm[j]);
 #pragma unroll
             for (int i = 0; i < VE; ++i) {
                 xh[j][i] = (xh[j][i] - mean) * rstd;
-                const float gy = cols[j].own(i, gg[j][i]) * counts;
+                const float gy = own<NV>(cols[j], j, i, gg[j][i]);
                 dg[j][i] += gy * xh[j][i];
                 db[j][i] += gy;
                 gg[j][i] *= gm[j][i];
-                const float kept = gy * gm[j][i];
+                const float kept = own<NV>(cols[j], j, i, gg[j][i]);
                 s[0] += kept;
                 s[1] += kept * xh[j][i];
             }
         }
         team_sum<LANES>(s, red);
-        if (row >= a.rows) continue;
         const float s0 = s[0] * inv_n, s1 = s[1] * inv_n;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {

@@ -96,3 +96,30 @@ def test_layer_norm_of_rows_with_infinities_and_nan(n):
     y, mean, _ = norm_fwd(x)
     assert np.isnan(host(y)[1::2]).all() and torch.equal(y[::2], y0[::2])
     assert host(mean)[1] == np.inf and np.isnan(host(mean)[3]) and host(mean)[5] == -np.inf
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,n", [(1, 13), (5, 16), (37, 100), (3, 129), (1030, 64), (5, 5001), (3, 20011)])
+def test_layer_norm_gradients_of_infinities(rows, n, dtype):
+    """An infinite gradient, in the last row too (where lanes without a row of their own must not count): sums over rows are infinite in
+    its column and as they were in the others; the gradients of other rows are what they were."""
+    print("case norm gradient infinity", rows, n, dtype, flush=True)
+    T, rng = TYPES[dtype], np.random.default_rng(rows + n)
+    x, hx = dev(rng.normal(size=(rows, n)), T)
+    g, hg = dev(rng.normal(size=(rows, n)), T)
+    d = gb.make_layer_norm(T, rows, n, 1e-5)
+    _, mean, rstd = norm_fwd(x)
+    ws = torch.empty(gb.gleam_layer_norm_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+
+    def gradients(g):
+        gx, gg, gbt = torch.empty_like(x), torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+        gb.gleam_layer_norm_bwd(d, x, None, mean, rstd, g, gx, gg, gbt, ws)
+        return gx, gg, gbt
+
+    gx0, gg0, gb0 = gradients(g)
+    g[-1, n - 1] = float("inf")
+    gx, gg, gbt = gradients(g)
+    xh = (hx[-1, n - 1] - host(mean)[-1]) * host(rstd)[-1]
+    assert host(gbt)[-1] == np.inf and host(gg)[-1] == np.sign(xh) * np.inf
+    assert torch.equal(gbt[:-1], gb0[:-1]) and torch.equal(gg[:-1], gg0[:-1]) and torch.equal(gx[:-1], gx0[:-1])
+    assert not np.isfinite(host(gx)[-1]).any()
