@@ -660,7 +660,8 @@ __global__ __launch_bounds__(64 * kShortWaves) void mix_short_kernel(MixArgs arg
     auto give = [&](const MixRole& ro, int which) {
         T* base = (T*)ro.out + r.b * ro.o.s.b + r.p * ro.o.s.p + (long long)(r.h - slot) * ro.o.s.h;
         vectors(ro.o.d, (int)args.T, [&](int t, int c) {
-            const uint4 n = *(const uint4*)(lds[0][which] + t * kRow + c);
+            uint4 n = *(const uint4*)(lds[0][which] + t * kRow + c);
+            if (t >= r.len) n = make_uint4(0, 0, 0, 0);           // behind the end, also where a token before it is not finite
             __builtin_memcpy(base + (unsigned)(__umul24(t, (unsigned)ro.o.s.t) + c), &n, 16);
         });
     };
@@ -718,7 +719,7 @@ __global__ __launch_bounds__(64 * kShortWaves) void mix_short_kernel(MixArgs arg
     };
     auto store = [&](const MixRole& ro, int which, int t, const floatx4(&o)[U]) {
         T* keep = own(which, ro.o.d) + (16 * t + m) * kRow;       // ROWS: in the place of the wave's own columns of an input
-        if (!ROWS && 16 * t + m >= args.T) return;
+        if (!ROWS && 16 * t + m >= r.len) return;
         const long long at = r.b * ro.o.s.b + (16 * t + m) * ro.o.s.t + r.p * ro.o.s.p + (long long)(r.h / ro.o.share) * ro.o.s.h;
         if constexpr (U == 1) {
             const float v[4] = {o[0][0], o[0][1], o[0][2], o[0][3]};
@@ -735,13 +736,20 @@ __global__ __launch_bounds__(64 * kShortWaves) void mix_short_kernel(MixArgs arg
             else M::store((T*)ro.out + at, ro.o.d, g, o);
         }
     };
-    if (!ROWS && r.len == 0) {
-        const floatx4 zero[U] = {};
+    if constexpr (!ROWS) {                           // zeros behind the end, whatever the tokens before it hold
+        if (r.len < args.T) {
 #pragma unroll
-        for (int t = 0; t < TT; ++t)
-#pragma unroll
-            for (int i = 0; i < (BWD ? 3 : 1); ++i) store(args.role[i], 0, t, zero);
-        return;
+            for (int i = 0; i < (BWD ? 3 : 1); ++i) {
+                const MixRole& ro = args.role[i];
+                const int c = lane & 31;
+                for (int t = r.len + (lane >> 5); t < args.T && c < ro.o.d; t += 2) {
+                    const long long at = r.b * ro.o.s.b + t * ro.o.s.t + r.p * ro.o.s.p + (long long)(r.h / ro.o.share) * ro.o.s.h + c;
+                    if (ro.out_f32) ((float*)ro.out)[at] = 0.f;
+                    else put_f32((T*)ro.out + at, 0.f);
+                }
+            }
+        }
+        if (r.len == 0) return;
     }
     // decays of scores whose tiles are n apart, with scale: the later token's row m, or (up) the earlier one's
     const float scale = args.role[0].in_scale * args.role[0].out_scale;

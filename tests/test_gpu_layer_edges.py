@@ -123,3 +123,36 @@ def test_layer_norm_gradients_of_infinities(rows, n, dtype):
     assert host(gbt)[-1] == np.inf and host(gg)[-1] == np.sign(xh) * np.inf
     assert torch.equal(gbt[:-1], gb0[:-1]) and torch.equal(gg[:-1], gg0[:-1]) and torch.equal(gx[:-1], gx0[:-1])
     assert not np.isfinite(host(gx)[-1]).any()
+
+
+# ------------------------------------------------------------------------------------------------------ linear attention
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads", [(4, 4, 4, 4), (3, 3, 3, 3), (4, 2, 1, 4)])
+@pytest.mark.parametrize("dk,dv", [(16, 16), (5, 3), (25, 25), (32, 24), (40, 40)])
+@pytest.mark.parametrize("T", [1, 2, 17, 40, 64, 100])
+def test_linattn_zeros_behind_the_ends_whatever_the_tokens_hold(T, dk, dv, heads, dtype):
+    """Infinities and NaN in tokens that are there: outputs and gradients behind the sequences' ends are zeros all the same, with a state
+    and without one."""
+    print("case linattn dead tokens", T, dk, dv, heads, dtype, flush=True)
+    H, Hq, Hk, Hv = heads
+    B, P, rng = 4, 2, np.random.default_rng(T + dk)
+    lengths = [T, T // 2, 0, max(T - 1, 0)]
+    live = np.arange(T)[None, :] < np.array(lengths)[:, None]
+    T_ = TYPES[dtype]
+    arrays = {}
+    for name, h, d in (("q", Hq, dk), ("k", Hk, dk), ("v", Hv, dv), ("g", H, dv)):
+        a = rng.normal(size=(B, T, P, h, d))
+        bad = rng.random(size=a.shape) < 0.2
+        a[bad] = rng.choice([np.nan, np.inf, -np.inf], size=int(bad.sum()))
+        arrays[name] = dev(a, T_)[0]
+    log_decay = torch.full((H,), -0.1, device="cuda")
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    desc = gb.make_linattn(arrays["q"], arrays["k"], arrays["v"], arrays["g"], 1.0)
+    ws = torch.empty(max(gb.gleam_linattn_workspace_bytes(desc)), dtype=torch.uint8, device="cuda")
+    for state in (None, torch.zeros(B, P, H, dk, dv, device="cuda")):
+        o = torch.full_like(arrays["g"], POISON)
+        gb.gleam_linattn_fwd(desc, arrays["q"], arrays["k"], arrays["v"], log_decay, n, state, o, None, ws)
+        grads = [torch.full_like(arrays[x], POISON) for x in "qkv"]
+        gb.gleam_linattn_bwd(desc, arrays["q"], arrays["k"], arrays["v"], log_decay, n, state, arrays["g"], None, *grads, None, ws)
+        for name, t in zip(("o", "g_q", "g_k", "g_v"), (o, *grads)):
+            assert not host(t)[~live].any(), name
