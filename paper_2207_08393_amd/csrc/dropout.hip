@@ -40,7 +40,7 @@ __device__ __forceinline__ uint4 draws_of(const DropoutArgs& a, unsigned long lo
 // One thread, one block of eight elements; a block that crosses rows, or the end, goes element by element.
 template <class T>
 __global__ __launch_bounds__(kDropThreads) void dropout_kernel(DropoutArgs a) {
-    const long long blk = (long long)blockIdx.x * kDropThreads + threadIdx.x;
+    const long long blk = group_of_grid() * kDropThreads + threadIdx.x;
     const long long first = blk * 8, size = a.rows * a.n;
     if (first >= size) return;
     const T *x = (const T*)a.x, *res = (const T*)a.res;
@@ -95,9 +95,8 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(DropoutArgs a) {
 template <class T>
 hipError_t launch(const DropoutArgs& a, hipStream_t st) {
     const long long blocks = (a.rows * a.n + 7) / 8;
-    const dim3 grid((unsigned)((blocks + kDropThreads - 1) / kDropThreads));
     KernelScope ks("dropout", 2.0 * a.rows * a.n, (a.res ? 3.0 : 2.0) * sizeof(T) * a.rows * a.n, st);
-    hipLaunchKernelGGL(dropout_kernel<T>, grid, dim3(kDropThreads), 0, st, a);
+    hipLaunchKernelGGL(dropout_kernel<T>, grid_of((blocks + kDropThreads - 1) / kDropThreads), dim3(kDropThreads), 0, st, a);
     return hipGetLastError();
 }
 

@@ -10,6 +10,14 @@ __device__ __forceinline__ float to_f32(unsigned short v) { return bf16_to_f32(v
 __device__ __forceinline__ void put_f32(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put_f32(unsigned short* p, float v) { *p = (unsigned short)pack_bf16x2(v, v); }
 
+// Workgroups of a launch.  A grid's dimension holds fewer than 2^32 work-items (2^22 workgroups of 1024), so workgroups past the first
+// kGridX go on in the second dimension; there may be up to 2^37 of them, and some more than asked for, which have nothing to do.
+constexpr unsigned kGridX = 1u << 21;
+inline dim3 grid_of(long long groups) {
+    return dim3((unsigned)(groups < kGridX ? groups : kGridX), (unsigned)((groups + kGridX - 1) / kGridX));
+}
+__device__ __forceinline__ long long group_of_grid() { return (long long)blockIdx.y * kGridX + blockIdx.x; }
+
 // N elements of type T; 16 bytes, or two times 16 for eight float32.  Global addresses need the alignment of an element only: the
 // memory unit takes 16 bytes from any address (an access that crosses a cache line costs two).
 template <class T, int N>

@@ -156,3 +156,27 @@ def test_linattn_zeros_behind_the_ends_whatever_the_tokens_hold(T, dk, dv, heads
         gb.gleam_linattn_bwd(desc, arrays["q"], arrays["k"], arrays["v"], log_decay, n, state, arrays["g"], None, *grads, None, ws)
         for name, t in zip(("o", "g_q", "g_k", "g_v"), (o, *grads)):
             assert not host(t)[~live].any(), name
+
+
+# ------------------------------------------------------------- calls of more work-items than a grid's dimension holds (2^32)
+def room_for(gigabytes):
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < (gigabytes + 8) * 2 ** 30:
+        pytest.skip(f"{gigabytes} GiB of GPU memory are not free")
+
+
+def test_dropout_of_more_than_2_35_elements():
+    """Eight elements a work-item: 33 x 2^30 of them, bfloat16 in place; 64 elements are looked at where the mask's counters, the grid's
+    dimensions and the array begin and end."""
+    room_for(67)
+    rows, n = 33, 2 ** 30
+    x = torch.ones(rows, n, dtype=torch.bfloat16, device="cuda")
+    gb.gleam_dropout_fwd(gb.make_dropout(torch.bfloat16, rows, n, 0.5, 11, 1), x, None, x)
+    for e in (0, 2 ** 32 - 32, 2 ** 35 - 32, 2 ** 35, rows * n - 64):
+        mask, factor = lo.dropout_mask(1, 64, 0.5, 11, 1, first_row=e // 64) if e % 64 == 0 else (None, None)
+        if mask is None:                              # half of it before the border
+            both = [lo.dropout_mask(1, 64, 0.5, 11, 1, first_row=(e - 32) // 64 + i) for i in range(2)]
+            mask, factor = np.concatenate([both[0][0][:, 32:], both[1][0][:, :32]], 1), both[0][1]
+        assert np.array_equal(host(x.view(-1)[e:e + 64]), np.where(mask, factor, 0.0)[0]), e
+    del x
+    torch.cuda.empty_cache()
