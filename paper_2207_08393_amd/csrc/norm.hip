@@ -369,7 +369,7 @@ __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float* __restri
                                                            float* g_beta) {
     __shared__ float red[32][33];
     const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-    const long long col = (long long)blockIdx.x * 32 + tx;
+    const long long col = group_of_grid() * 32 + tx;
     float s = 0.f;
     if (col < 2 * n)
 #pragma unroll 8
@@ -427,7 +427,8 @@ template <class T>
 __global__ __launch_bounds__(kLongThreads) void norm_fwd_long_kernel(NormArgs a) {
     constexpr int VE = vec_of<T>();
     __shared__ float red[2 * kLongThreads / 64];
-    const long long row = blockIdx.x;
+    const long long row = group_of_grid();
+    if (row >= a.rows) return;
     const T* x = (const T*)a.x + row * a.ld_x;
     T* y = (T*)a.out + row * a.ld_y;
     const float inv_n = 1.f / (float)a.n;
@@ -480,7 +481,8 @@ template <class T>
 __global__ __launch_bounds__(kLongThreads) void norm_bwd_long_kernel(NormArgs a) {
     constexpr int VE = vec_of<T>();
     __shared__ float red[2 * kLongThreads / 64];
-    const long long row = blockIdx.x;
+    const long long row = group_of_grid();
+    if (row >= a.rows) return;
     const T *x = (const T*)a.x + row * a.ld_x, *g = (const T*)a.g + row * a.ld_y;
     T* gx = (T*)a.out + row * a.ld_x;
     const float inv_n = 1.f / (float)a.n, mean = a.mean_in[row], rstd = a.rstd_in[row];
@@ -574,7 +576,7 @@ hipError_t forward(const gleam_layer_norm_desc& d, const NormArgs& a, hipStream_
     const Team t = team_for(d);
     KernelScope ks("layer_norm_fwd", 7.0 * d.rows * d.n, 2.0 * sizeof(T) * d.rows * d.n, st);
     if (!t.lanes) {
-        hipLaunchKernelGGL(norm_fwd_long_kernel<T>, dim3((unsigned)d.rows), dim3(kLongThreads), 0, st, a);
+        hipLaunchKernelGGL(norm_fwd_long_kernel<T>, grid_of(d.rows), dim3(kLongThreads), 0, st, a);
         return hipGetLastError();
     }
     with_team<T>(t, [&](auto L, auto N) {
@@ -594,7 +596,7 @@ hipError_t backward(const gleam_layer_norm_desc& d, const NormArgs& a, float* g_
             hipLaunchKernelGGL(norm_cols_kernel<T>, dim3((unsigned)((d.n + kNormThreads - 1) / kNormThreads), parts), dim3(kNormThreads), 0, st, a);
         }
         KernelScope ks("layer_norm_bwd", 8.0 * d.rows * d.n, 3.0 * sizeof(T) * d.rows * d.n, st);
-        hipLaunchKernelGGL(norm_bwd_long_kernel<T>, dim3((unsigned)d.rows), dim3(kLongThreads), 0, st, a);
+        hipLaunchKernelGGL(norm_bwd_long_kernel<T>, grid_of(d.rows), dim3(kLongThreads), 0, st, a);
     } else {
         parts = grid_for(d, t, true);
         KernelScope ks("layer_norm_bwd", 12.0 * d.rows * d.n, 3.0 * sizeof(T) * d.rows * d.n, st);
@@ -604,7 +606,7 @@ hipError_t backward(const gleam_layer_norm_desc& d, const NormArgs& a, float* g_
     }
     if (a.part) {
         KernelScope ks("layer_norm_reduce", 2.0 * parts * d.n, 8.0 * parts * d.n, st);
-        hipLaunchKernelGGL(norm_reduce_kernel, dim3((unsigned)((2 * d.n + 31) / 32)), dim3(1024), 0, st, (const float*)a.part, parts,
+        hipLaunchKernelGGL(norm_reduce_kernel, grid_of((2 * d.n + 31) / 32), dim3(1024), 0, st, (const float*)a.part, parts,
                            (long long)d.n, g_gamma, g_beta);
     }
     return hipGetLastError();

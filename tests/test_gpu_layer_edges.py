@@ -180,3 +180,50 @@ def test_dropout_of_more_than_2_35_elements():
         assert np.array_equal(host(x.view(-1)[e:e + 64]), np.where(mask, factor, 0.0)[0]), e
     del x
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype,rows", [("bf16", 2 ** 22 + 5)])
+def test_layer_norm_of_more_than_2_22_long_rows(dtype, rows):
+    """A workgroup of 1024 for each row, in place; every row is the same, so every result has to be."""
+    n = 16385
+    room_for(rows * n * 2 / 2 ** 30)
+    base = torch.randn(n, generator=torch.Generator().manual_seed(1)).cuda().to(TYPES[dtype])
+    want = norm_fwd(base[None])[0][0]
+    x = base.expand(rows, n).contiguous()
+    gb.gleam_layer_norm_fwd(gb.make_layer_norm(x.dtype, rows, n, 1e-5), x, None, None, x)
+    for r in (0, 2 ** 21 - 3, 2 ** 21, 2 ** 22 - 3, 2 ** 22, rows - 3, *np.random.default_rng(0).integers(0, rows - 3, 50).tolist()):
+        assert bool((x[r:r + 3] == want).all()), r
+    del x
+    torch.cuda.empty_cache()
+
+
+def test_layer_norm_gradients_of_more_than_2_21_long_rows():
+    rows, n = 2 ** 21 + 5, 16385
+    room_for(2 * rows * n * 2 / 2 ** 30)
+    gen = torch.Generator().manual_seed(1)
+    base, gbase = (torch.randn(n, generator=gen).cuda().bfloat16() for _ in range(2))
+    _, m, r = norm_fwd(base[None])
+    want = torch.empty(1, n, dtype=torch.bfloat16, device="cuda")
+    gb.gleam_layer_norm_bwd(gb.make_layer_norm(torch.bfloat16, 1, n, 1e-5), base[None], None, m, r, gbase[None], want, None, None, None)
+    x, g = base.expand(rows, n).contiguous(), gbase.expand(rows, n).contiguous()
+    gb.gleam_layer_norm_bwd(gb.make_layer_norm(torch.bfloat16, rows, n, 1e-5), x, None, m.repeat(rows), r.repeat(rows), g, g, None, None, None)
+    for k in (0, 2 ** 21 - 3, 2 ** 21, rows - 3, *np.random.default_rng(0).integers(0, rows - 3, 50).tolist()):
+        assert bool((g[k:k + 3] == want).all()), k
+    del x, g
+    torch.cuda.empty_cache()
+
+
+def test_layer_norm_parameter_gradients_of_rows_of_more_than_2_26():
+    """The sum over rows, 1024 work-items for 32 columns of both gradients."""
+    rows, n = 2, 2 ** 26 + 35
+    room_for(8)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    x, g = (torch.randn(rows, n, device="cuda", generator=gen) for _ in range(2))
+    mean, rstd = torch.tensor([0.1, -0.2], device="cuda"), torch.tensor([1.3, 0.7], device="cuda")
+    d = gb.make_layer_norm(torch.float32, rows, n, 1e-5)
+    gx, gg, gbt = torch.empty_like(x), torch.full((n,), POISON, device="cuda"), torch.full((n,), POISON, device="cuda")
+    gb.gleam_layer_norm_bwd(d, x, None, mean, rstd, g, gx, gg, gbt, torch.empty(gb.gleam_layer_norm_workspace_bytes(d), dtype=torch.uint8, device="cuda"))
+    assert torch.equal(gbt, g[0] + g[1])                                           # one rounding, and that is the same one
+    for c in (slice(0, 4096), slice(2 ** 25 - 4096, 2 ** 25 + 4096), slice(n - 4096, n)):
+        xh = (host(x[:, c]) - host(mean)[:, None]) * host(rstd)[:, None]
+        assert_close(host(gg[c]), (host(g[:, c]) * xh).sum(0), F32, "g_gamma")
