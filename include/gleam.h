@@ -304,7 +304,7 @@ int gleam_unrolled_infer(const gleam_geom* geom, const gleam_prox_desc* prox, in
  * dynamic series, or the tokens of any sequence: y = layer_norm(x); q, k, v = projections of y; h = x + dropout(projection of
  * linear_attention(q, k, v)).  Activations are float32 (dtype 0) or bfloat16 (dtype 1) and are computed on in float32 (products of
  * bfloat16 arrays on the bfloat16 matrix cores with float32 sums); scales, shifts, statistics, decays and states are float32.
- * Conventions are those above, except that arrays may have strides.  Pointers need the alignment of their element type; accesses are
+ * Conventions are those above, except that arrays may have strides (rows: fewer than 2^31, arrays of at most 2^40 elements).  Pointers need the alignment of their element type; accesses are
  * fastest where base addresses and strides are multiples of 16 bytes. */
 
 /* Layer norm over the last dimension of `rows` rows of n elements: mean m and variance s^2 (over n) of the row,
@@ -364,7 +364,8 @@ int gleam_dropout_bwd(const gleam_dropout_desc* desc, const void* g_out, void* g
  * gradients are written as zeros; values outside 0..T count as the nearest of them.  A sequence of length 0 leaves its state as it is.
  * A token that is not finite can reach the outputs of up to 63 tokens before it (and in the gradients behind it) as NaN: they share a
  * matrix product.  Infinities, and with bfloat16 arrays states beyond 3.39e38, come out as infinity or NaN.
- * 1 <= dk, dv <= 128.  One token (T = 1) takes the recurrent form: every state is read once and written once. */
+ * 1 <= dk, dv <= 128, T <= 2^30, B P heads <= 2^29, no array reaches over more than 2^40 elements (GLEAM_E_DIMS otherwise).  One token
+ * (T = 1) takes the recurrent form: every state is read once and written once. */
 typedef struct { int64_t b, t, p, h; } gleam_seq_strides;
 typedef struct {
     int32_t dtype, heads, q_heads, k_heads, v_heads, dk, dv;

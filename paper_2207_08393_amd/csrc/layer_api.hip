@@ -13,7 +13,7 @@ namespace {
 
 constexpr long long kMostElements = 1LL << 40;   // keeps every byte offset far inside int64
 
-constexpr long long kMostProblems = 1LL << 29;    // sequences x pixels x heads: three workgroups each fit a launch
+constexpr long long kMostProblems = 1LL << 29;   // sequences x pixels x heads: the numbers of three workgroups for each fit 32 bits
 
 inline bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) % 256) == 0; }
 

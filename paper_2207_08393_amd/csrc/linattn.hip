@@ -300,9 +300,9 @@ struct Work {
     bool none;
 };
 __device__ __forceinline__ Work work_of(const MixArgs& a, unsigned groups, unsigned segs, unsigned roles) {
-    const unsigned total = groups * segs * roles, per = (total + 7) / 8, i = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    const unsigned total = groups * segs * roles, per = (total + 7) / 8, n = (unsigned)group_of_grid(), i = (n & 7) * per + (n >> 3);
     Work w;
-    w.none = blockIdx.x >> 3 >= per || i >= total;
+    w.none = n >> 3 >= per || i >= total;
     const unsigned inner = a.near_groups, outer = i / (inner * segs * roles), in = i - outer * (inner * segs * roles);
     const unsigned in_seg = in / (inner * roles), rest = in - in_seg * (inner * roles);
     w.role = rest / inner;
@@ -633,7 +633,7 @@ __global__ __launch_bounds__(64 * kShortWaves) void mix_short_kernel(MixArgs arg
     __shared__ __attribute__((aligned(16))) T lds[ROWS ? 1 : kShortWaves][kArrays][kTokens * kRow];
     __shared__ float weights[kShortWaves][16 + kShortTokens];
     const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4, slot = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const long long index = (long long)blockIdx.x * kShortWaves + slot;
+    const long long index = group_of_grid() * kShortWaves + slot;
     if (index >= args.B * args.P * args.H) return;   // not where ROWS: a multiple of four heads
     const Problem r = problem_of(args, index);
     const float decay = args.log_decay[r.h];
@@ -903,7 +903,7 @@ __global__ __launch_bounds__(256) void mix_scan_kernel(MixArgs args, int chunk) 
 template <class T, int N>
 __global__ __launch_bounds__(256) void mix_share_kernel(const float* __restrict__ part, MixTensor x, void* out, unsigned T_, unsigned P, unsigned H,
                                                         long long n) {
-    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+    const long long at = group_of_grid() * 256 + threadIdx.x;
     if (at >= n) return;
     const unsigned per = x.d / N, heads = H / x.share;
     const long long row = at / (per * heads);         // (b T + t) P + p
@@ -934,7 +934,7 @@ __global__ __launch_bounds__(kStepThreads) void mix_step_kernel(MixArgs args) {
     __shared__ float lds_q[kSlots][128], lds_k[kSlots][128];
     __shared__ floatx4 red[kWaves][64];
     const int slot = kSlots == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / TP), tid = threadIdx.x % TP;
-    const long long index = (long long)blockIdx.x * kSlots + slot;
+    const long long index = group_of_grid() * kSlots + slot;
     if (index >= args.B * args.P * args.H) return;    // a wave each: no barriers
     const Problem r = problem_of(args, index);
     const T *gq = base_of<T>(a.q, r), *gk = base_of<T>(a.k, r), *gv = base_of<T>(a.v, r);
@@ -1043,7 +1043,7 @@ size_t share_bytes(const gleam_linattn_desc& d, int heads, int width) {
 }
 
 // Workgroups of a launch: the ranges of the 8 XCDs are of one length.
-unsigned blocks_of(unsigned groups, unsigned segs, unsigned roles) { return (groups * segs * roles + 7) / 8 * 8; }
+dim3 blocks_of(unsigned groups, unsigned segs, unsigned roles) { return grid_of((groups * segs * roles + 7) / 8 * 8); }
 
 // `roles` passes side by side; `states` of them first, over segments, where there are several.
 template <class T, int D, int PARTS, bool NARROW>
@@ -1062,7 +1062,7 @@ hipError_t mix_passes(MixArgs a, int roles, MixArgs states, int n_states, const 
     if (a.n_seg > 1) {
         {
             KernelScope ks("linattn_segments", n_states * flops, n_states * bytes, st);
-            hipLaunchKernelGGL((mix_kernel<T, D, true, PARTS, NARROW>), dim3(blocks_of(groups, a.n_seg - 1, n_states)), dim3(S::kThreads), 0, st, states);
+            hipLaunchKernelGGL((mix_kernel<T, D, true, PARTS, NARROW>), blocks_of(groups, a.n_seg - 1, n_states), dim3(S::kThreads), 0, st, states);
         }
         const double floats = (double)n_states * problems * a.n_seg * S::kStateFloats;
         KernelScope ks("linattn_scan", 2.0 * floats, 8.0 * floats, st);
@@ -1070,7 +1070,7 @@ hipError_t mix_passes(MixArgs a, int roles, MixArgs states, int n_states, const 
         hipLaunchKernelGGL(mix_scan_kernel<D>, dim3(blocks, 1, n_states), dim3(256), 0, st, states, S::kL);
     }
     KernelScope ks(name, roles * 2.0 * flops, roles * 2.0 * bytes, st);
-    hipLaunchKernelGGL((mix_kernel<T, D, false, PARTS, NARROW>), dim3(blocks_of(groups, a.n_seg, roles)), dim3(S::kThreads), 0, st, a);
+    hipLaunchKernelGGL((mix_kernel<T, D, false, PARTS, NARROW>), blocks_of(groups, a.n_seg, roles), dim3(S::kThreads), 0, st, a);
     return hipGetLastError();
 }
 template <class T, int D>
@@ -1106,8 +1106,8 @@ void launch_short(const MixArgs& a, unsigned groups, hipStream_t st) {
     const MixRole& r = a.role[BWD ? 2 : 0];           // q and k in any case
     bool whole = a.H % kShortWaves == 0 && side_by_side(r.q, e) && side_by_side(r.k, e) && side_by_side(a.role[0].k, e) && side_by_side(r.v, e);
     for (int i = 0; i < (BWD ? 3 : 1); ++i) whole = whole && !a.role[i].out_f32 && side_by_side(a.role[i].o, e);
-    if (whole) hipLaunchKernelGGL((mix_short_kernel<T, TT, U, BWD, true>), dim3(groups), dim3(64 * kShortWaves), 0, st, a);
-    else hipLaunchKernelGGL((mix_short_kernel<T, TT, U, BWD, false>), dim3(groups), dim3(64 * kShortWaves), 0, st, a);
+    if (whole) hipLaunchKernelGGL((mix_short_kernel<T, TT, U, BWD, true>), grid_of(groups), dim3(64 * kShortWaves), 0, st, a);
+    else hipLaunchKernelGGL((mix_short_kernel<T, TT, U, BWD, false>), grid_of(groups), dim3(64 * kShortWaves), 0, st, a);
 }
 template <class T, int TT, bool BWD>
 void launch_short(const MixArgs& a, unsigned groups, hipStream_t st) {
@@ -1128,7 +1128,7 @@ hipError_t mix_short(const MixArgs& a, const char* name, hipStream_t st) {
 
 template <class T, int N>
 hipError_t share_sum(const gleam_linattn_desc& d, const float* part, const MixTensor& x, void* out, long long n, hipStream_t st) {
-    hipLaunchKernelGGL((mix_share_kernel<T, N>), dim3((unsigned)((n / N + 255) / 256)), dim3(256), 0, st, part, x, out, (unsigned)d.T, (unsigned)d.P,
+    hipLaunchKernelGGL((mix_share_kernel<T, N>), grid_of((n / N + 255) / 256), dim3(256), 0, st, part, x, out, (unsigned)d.T, (unsigned)d.P,
                        (unsigned)d.heads, n / N);
     return hipGetLastError();
 }
@@ -1137,9 +1137,9 @@ template <class T>
 hipError_t mix_step(const MixArgs& a, hipStream_t st) {
     const long long problems = a.B * a.P * a.H;
     if (a.dk * ((a.dv + 3) / 4) <= 64 * kStepRows)    // a wave has the whole state on its way at once
-        hipLaunchKernelGGL((mix_step_kernel<T, 64>), dim3((unsigned)((problems + 3) / 4)), dim3(kStepThreads), 0, st, a);
+        hipLaunchKernelGGL((mix_step_kernel<T, 64>), grid_of((problems + 3) / 4), dim3(kStepThreads), 0, st, a);
     else
-        hipLaunchKernelGGL((mix_step_kernel<T, kStepThreads>), dim3((unsigned)problems), dim3(kStepThreads), 0, st, a);
+        hipLaunchKernelGGL((mix_step_kernel<T, kStepThreads>), grid_of(problems), dim3(kStepThreads), 0, st, a);
     return hipGetLastError();
 }
 

@@ -227,3 +227,82 @@ def test_layer_norm_parameter_gradients_of_rows_of_more_than_2_26():
     for c in (slice(0, 4096), slice(2 ** 25 - 4096, 2 ** 25 + 4096), slice(n - 4096, n)):
         xh = (host(x[:, c]) - host(mean)[:, None]) * host(rstd)[:, None]
         assert_close(host(gg[c]), (host(g[:, c]) * xh).sum(0), F32, "g_gamma")
+
+
+class ManyProblems:
+    """B = 1 sequence of T tokens at P pixels; results are compared with the oracle at pixels where the grid's dimensions, and the arrays,
+    begin and end, and everything has to be written."""
+
+    def __init__(self, T, P, heads, dk, dv, dtype, state=False, most=0):
+        print("case linattn many problems", T, P, heads, dk, dv, dtype, state, flush=True)
+        H, Hq, Hk, Hv = heads
+        assert P * H > most
+        gen = torch.Generator(device="cuda").manual_seed(T + dk)
+        make = lambda h, d: torch.empty(1, T, P, h, d, dtype=TYPES[dtype], device="cuda").normal_(generator=gen)  # noqa: E731
+        self.a = {"q": make(Hq, dk), "k": make(Hk, dk), "v": make(Hv, dv), "g": make(H, dv)}
+        self.log_decay = torch.linspace(-0.5, -0.1, H, device="cuda")
+        self.state, self.g_state = (torch.empty(1, P, H, dk, dv, device="cuda").normal_(generator=gen) if state else None for _ in range(2))
+        self.P, self.low = P, dtype == "bf16"
+        self.desc = gb.make_linattn(*(self.a[n] for n in "qkvg"), 0.5)
+        self.ws = gb.gleam_linattn_workspace_bytes(self.desc)
+
+    def check(self, ref, got, names):
+        edges = sorted({0, self.P - 40, *(min(e, self.P - 40) for e in (2 ** 20 - 20, 2 ** 21 - 20, 2 ** 22 - 20, 2 ** 23 - 20, 2 ** 24 - 20, 2 ** 27 - 20))})
+        for e in edges:
+            s = slice(e, e + 40)
+            want = ref(*(host(self.a[n][:, :, s]) for n in "qkvg"), *(None if x is None else host(x[:, s]) for x in (self.state, self.g_state)))
+            for name, t, w in zip(names, got, want):
+                if t is not None:
+                    states = name.endswith("state")
+                    assert_close(host(t[:, s] if states else t[:, :, s]), w, F32 if states or not self.low else 2.0 ** -7, (name, e))
+        assert not any(bool(torch.isnan(t).any()) for t in got if t is not None)
+
+    def fwd(self):
+        o = torch.full_like(self.a["g"], POISON)
+        S = None if self.state is None else torch.full_like(self.state, POISON)
+        gb.gleam_linattn_fwd(self.desc, *(self.a[n] for n in "qkv"), self.log_decay, None, self.state, o, S,
+                             torch.empty(self.ws[0], dtype=torch.uint8, device="cuda"))
+        self.check(lambda q, k, v, g, S0, gS: lo.linattn(q, k, v, host(self.log_decay), 0.5, None, S0), (o, S), ("o", "state"))
+
+    def bwd(self):
+        grads = [torch.full_like(self.a[n], POISON) for n in "qkv"]
+        gS = None if self.state is None else torch.full_like(self.state, POISON)
+        gb.gleam_linattn_bwd(self.desc, *(self.a[n] for n in "qkv"), self.log_decay, None, self.state, self.a["g"], self.g_state, *grads, gS,
+                             torch.empty(self.ws[1], dtype=torch.uint8, device="cuda"))
+        self.check(lambda q, k, v, g, S0, gS: lo.linattn_bwd(q, k, v, host(self.log_decay), 0.5, g, None, S0, gS), (*grads, gS), ("g_q", "g_k", "g_v", "g_state"))
+
+
+def test_linattn_single_tokens_of_more_than_2_26_problems():
+    """A wave each; and of 2^24, a workgroup each."""
+    room_for(14)
+    ManyProblems(1, 2 ** 24 + 50, (4, 4, 4, 4), 1, 1, "bf16", state=True, most=2 ** 26).fwd()
+    ManyProblems(1, 2 ** 22 + 50, (4, 4, 4, 4), 128, 20, "bf16", most=2 ** 24).fwd()
+    torch.cuda.empty_cache()
+
+
+def test_linattn_short_sequences_of_more_than_2_26_problems():
+    room_for(32)
+    m = ManyProblems(2, 2 ** 24 + 50, (4, 4, 4, 4), 8, 8, "bf16", most=2 ** 26)       # four heads as whole rows
+    m.fwd()
+    m.bwd()
+    del m
+    m = ManyProblems(2, 2 ** 24 + 50, (4, 4, 4, 4), 1, 1, "f32", most=2 ** 26)
+    m.fwd()
+    m.bwd()
+    torch.cuda.empty_cache()
+
+
+def test_linattn_chunks_of_more_problems_than_one_launch_dimension_holds():
+    """Four waves for four problems, three passes in the backward call: 2^32 work-items at 22.4 million problems."""
+    room_for(8)
+    m = ManyProblems(2, 2 ** 24 + 50, (4, 4, 4, 4), 1, 1, "bf16", state=True, most=2 ** 26)
+    m.fwd()
+    m.bwd()
+    torch.cuda.empty_cache()
+
+
+def test_linattn_gradients_of_more_than_2_29_shared_values():
+    """The sum over shared heads, a value a work-item."""
+    room_for(40)
+    ManyProblems(4, 2 ** 27 + 50, (2, 2, 1, 2), 1, 1, "bf16", most=2 ** 28).bwd()
+    torch.cuda.empty_cache()
