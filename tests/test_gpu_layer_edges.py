@@ -306,3 +306,55 @@ def test_linattn_gradients_of_more_than_2_29_shared_values():
     room_for(40)
     ManyProblems(4, 2 ** 27 + 50, (2, 2, 1, 2), 1, 1, "bf16", most=2 ** 28).bwd()
     torch.cuda.empty_cache()
+
+
+# ------------------------------------------------------------------------------------------- walks over more rows than teams
+def norm64(x, gamma, beta, eps):
+    """The same in 64 bits on the device, row by row in blocks."""
+    x = x.double()
+    mean = x.mean(1)
+    rstd = 1.0 / torch.sqrt(((x - mean[:, None]) ** 2).mean(1) + eps)
+    return (x - mean[:, None]) * rstd[:, None] * gamma.double() + beta.double(), mean, rstd
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,n", [(2 * 524288 + 37, 8), (524288 + 37, 16), (2 * 65536 + 5, 100), (65536 + 3, 250), (32768 + 3, 512), (2 * 32768 + 1, 700), (16384 + 7, 1000),
+                                    (8192 + 3, 1500), (2 * 8192 + 1, 4000), (8192 + 5, 5001), (8192 + 1, 8000), (8192 + 3, 12000), (8192 + 1, 16001)])
+def test_layer_norm_of_more_rows_than_teams(rows, n, dtype):
+    """Rows behind the first of a team, with a remainder: the row on its way, the sums over rows, in place.  Sums over rows are of at most 80
+    partial sums in a row, each rounded by 2^-24 of it: F32."""
+    print("case norm rows", rows, n, dtype, flush=True)
+    T, gen, eps = TYPES[dtype], torch.Generator(device="cuda").manual_seed(n), 1e-3
+    make = lambda *s: torch.empty(*s, device="cuda").normal_(0.2, 1.3, generator=gen)  # noqa: E731
+    x, g, gamma, beta = make(rows, n).to(T), make(rows, n).to(T), make(n), make(n)
+    d = gb.make_layer_norm(T, rows, n, eps)
+    y, mean, rstd = torch.full_like(x, POISON), torch.full((rows,), POISON, device="cuda"), torch.full((rows,), POISON, device="cuda")
+    gb.gleam_layer_norm_fwd(d, x, gamma, beta, y, mean, rstd)
+    ry, rmean, rrstd = norm64(x, gamma, beta, float(np.float32(eps)))
+    once = ONCE if dtype == "bf16" else 0.0
+
+    def close(got, want, tol, what):
+        diff = (got.double() - want).abs_()
+        assert float(diff.norm() / want.norm()) <= tol, what
+        assert float(diff.max() / want.abs().max()) <= tol * (2 * np.log(2 * got.numel())) ** 0.5, what
+
+    close(y, ry, F32 + once, "y")
+    close(mean, rmean, F32, "mean")
+    close(rstd, rrstd, F32, "rstd")
+    del ry
+    again = x.clone()
+    gb.gleam_layer_norm_fwd(d, again, gamma, beta, again)
+    assert torch.equal(again, y)
+    del again, y
+    gx, gg, gbt = torch.full_like(x, POISON), torch.full((n,), POISON, device="cuda"), torch.full((n,), POISON, device="cuda")
+    ws = torch.empty(gb.gleam_layer_norm_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    gb.gleam_layer_norm_bwd(d, x, gamma, mean, rstd, g, gx, gg, gbt, ws)
+    xh = (x.double() - mean.double()[:, None]) * rstd.double()[:, None]
+    gd = g.double()
+    close(gg, (gd * xh).sum(0), F32, "g_gamma")
+    close(gbt, gd.sum(0), F32, "g_beta")
+    gd *= gamma.double()
+    want = rstd.double()[:, None] * (gd - gd.mean(1, keepdim=True) - xh * (gd * xh).mean(1, keepdim=True))
+    close(gx, want, 4 * F32 + once, "g_x")
+    gb.gleam_layer_norm_bwd(d, x, gamma, mean, rstd, g, g, None, None, None)
+    assert torch.equal(g, gx)
