@@ -358,3 +358,54 @@ def test_layer_norm_of_more_rows_than_teams(rows, n, dtype):
     close(gx, want, 4 * F32 + once, "g_x")
     gb.gleam_layer_norm_bwd(d, x, gamma, mean, rstd, g, g, None, None, None)
     assert torch.equal(g, gx)
+
+
+# ------------------------------------------------------------------------------------- how far bfloat16 results are from exact ones
+def relative(got, want):
+    return float(np.linalg.norm((got - want).ravel()) / np.linalg.norm(want.ravel()))
+
+
+def rounded(a):
+    """An exact result as a bfloat16 array holds it."""
+    return torch.from_numpy(a).bfloat16().double().numpy()
+
+
+def bf16_mix(B, T, P, heads, dk, dv, log_decay, seed):
+    """Outputs and gradients without a state, and the exact ones: [(name, result, exact)]."""
+    H, Hq, Hk, Hv = heads
+    rng = np.random.default_rng(seed)
+    arrays, h = {}, {}
+    for name, n, d in (("q", Hq, dk), ("k", Hk, dk), ("v", Hv, dv), ("g", H, dv)):
+        arrays[name], h[name] = dev(rng.normal(size=(B, T, P, n, d)), torch.bfloat16)
+    a, ha = dev(np.asarray(log_decay), torch.float32)
+    desc = gb.make_linattn(*(arrays[n] for n in "qkvg"), dk ** -0.5)
+    ws = torch.empty(max(gb.gleam_linattn_workspace_bytes(desc)), dtype=torch.uint8, device="cuda")
+    o, grads = torch.full_like(arrays["g"], POISON), [torch.full_like(arrays[n], POISON) for n in "qkv"]
+    gb.gleam_linattn_fwd(desc, *(arrays[n] for n in "qkv"), a, None, None, o, None, ws)
+    gb.gleam_linattn_bwd(desc, *(arrays[n] for n in "qkv"), a, None, None, arrays["g"], None, *grads, None, ws)
+    exact = [lo.linattn(h["q"], h["k"], h["v"], ha, dk ** -0.5)[0], *lo.linattn_bwd(h["q"], h["k"], h["v"], ha, dk ** -0.5, h["g"])[:3]]
+    return [(name, host(t), e) for name, t, e in zip(("o", "g_q", "g_k", "g_v"), (o, *grads), exact)]
+
+
+@pytest.mark.parametrize("T,P,heads,dk,dv", [(20, 50, (4, 4, 4, 4), 16, 16), (64, 20, (3, 3, 3, 3), 25, 25), (40, 20, (4, 4, 2, 2), 32, 24), (300, 2, (2, 2, 2, 2), 64, 64),
+                                             (1500, 1, (2, 2, 2, 2), 128, 128), (200, 3, (4, 4, 1, 1), 40, 72)])
+def test_linattn_bf16_error_is_that_of_two_roundings(T, P, heads, dk, dv):
+    """Scores and outputs are rounded to bfloat16, each by a relative error of the same distribution, and independent of the other; what
+    else is rounded has 16 bits or more.  So the error is sqrt 2 = 1.41 times that of the exact results rounded once, with as many
+    values as here within some per cent of it: 1.6."""
+    print("case linattn bf16 error", T, P, heads, dk, dv, flush=True)
+    for name, got, exact in bf16_mix(1, T, P, heads, dk, dv, np.linspace(-0.3, -0.01, heads[0]), T):
+        assert relative(got, exact) <= 1.6 * relative(rounded(exact), exact), (name, relative(got, exact), relative(rounded(exact), exact))
+
+
+def test_linattn_bf16_error_where_the_state_carries_the_result():
+    """Hardly any decay: from the 1250th token on at most 64 of 1250 tokens reach an output by way of rounded scores, 5 % of its mean square, and
+    the rest by the state, in 16 bits or more: the error is sqrt(1.05) = 1.03 times that of one rounding, 1.2 asked for.  One part less of the
+    state, or of the values on their way into it, would make that sqrt 2."""
+    T = 2500
+    for d in (32, 64, 128):
+        print("case linattn bf16 state", d, flush=True)
+        for name, got, exact in bf16_mix(1, T, 1, (2, 2, 2, 2), d, d, [-1e-5, -1e-6], d):
+            far = slice(T // 2, T) if name in ("o", "g_q") else slice(0, T // 2)
+            got, exact = got[:, far], exact[:, far]
+            assert relative(got, exact) <= 1.2 * relative(rounded(exact), exact), (name, relative(got, exact), relative(rounded(exact), exact))
