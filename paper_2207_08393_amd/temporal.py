@@ -19,7 +19,8 @@ from .runner import byte_buffer
 
 
 class TemporalLayer:
-    """Parameters, gradients and Adam moments are flat float32 arrays: gamma [C], beta [C], W_qkv [3C][C], W_o [C][C]."""
+    """Parameters, gradients and Adam moments are flat float32 arrays: gamma [C], beta [C], W_qkv [3C][C], W_o [C][C].  Layers of one network
+    take a seed each: with the same one they start alike and drop the same elements."""
 
     def __init__(self, B, T, P, C, heads, dtype=torch.bfloat16, dropout=0.1, seed=0, eps=1e-5, longest=64.0):
         if C % heads:
@@ -60,7 +61,10 @@ class TemporalLayer:
         return [x.unflatten(3, (self.H, self.d)) for x in qkv.split(self.C, 3)]
 
     def forward(self, x, lengths=None, training=True):
-        """x: [B][T][P][C]; lengths: int32 [B], frames that are there, or None.  Keeps what `backward` needs."""
+        """h from x: [B][T][P][C]; lengths: int32 [B], frames that are there, or None.  h is the layer's own buffer, which the next call
+        overwrites.  For `backward` the layer keeps x and lengths themselves, which have to stay as they are until then.  Frames behind a
+        sequence's end come out as they went in and take no part in anything else, but they have to be finite: layer norm and the
+        products with the weights run over them, and their gradients are zero times what is there."""
         self.x, self.lengths = x, lengths
         gb.gleam_layer_norm_fwd(self.norm, x, self.gamma, self.beta, self.y, self.mean, self.rstd)
         torch.mm(self.y.view(-1, self.C), self.w_qkv.to(self.dtype).t(), out=self.qkv.view(-1, 3 * self.C))
@@ -71,7 +75,7 @@ class TemporalLayer:
         return self.h
 
     def backward(self, g_h):
-        """dL/dx from dL/dh; the parameters' gradients are left in `grad`."""
+        """dL/dx, a new array, from dL/dh of the last forward call; the parameters' gradients are left in `grad`."""
         g_z, g_qkv, g_x = torch.empty_like(self.z), torch.empty_like(self.qkv), torch.empty_like(self.y)
         gb.gleam_dropout_bwd(self.drop_now, g_h, g_z, self.step)
         torch.mm(g_z.float().t(), self.o.view(-1, self.C).float(), out=self.g_o_w)
@@ -93,7 +97,7 @@ class TemporalLayer:
         self.state.zero_()
 
     def frame(self, x):
-        """The next frame [B][P][C] of every pixel; no dropout."""
+        """The next frame [B][P][C] of every pixel; no dropout.  The result is the layer's own buffer, which the next frame overwrites."""
         gb.gleam_layer_norm_fwd(self.frame_norm, x, self.gamma, self.beta, self.frame_y)
         torch.mm(self.frame_y.view(-1, self.C), self.w_qkv.to(self.dtype).t(), out=self.frame_qkv.view(-1, 3 * self.C))
         gb.gleam_linattn_fwd(self.frame_mix, *self._heads(self.frame_qkv), self.log_decay, None, self.state, self.frame_o, self.state, None)

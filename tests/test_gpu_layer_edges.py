@@ -409,3 +409,25 @@ def test_linattn_bf16_error_where_the_state_carries_the_result():
             far = slice(T // 2, T) if name in ("o", "g_q") else slice(0, T // 2)
             got, exact = got[:, far], exact[:, far]
             assert relative(got, exact) <= 1.2 * relative(rounded(exact), exact), (name, relative(got, exact), relative(rounded(exact), exact))
+
+
+# ------------------------------------------------------------------------------------------------------------- temporal layer
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T", [20, 100])
+def test_temporal_layer_frames_behind_the_end_take_no_part(T, dtype):
+    """Whatever finite numbers stand there: they come out as they went in, their gradient goes through, and nothing else changes."""
+    from paper_2207_08393_amd.temporal import TemporalLayer
+    B, P, C = 2, 5, 32
+    layer = TemporalLayer(B, T, P, C, 4, dtype=dtype, dropout=0.2, seed=3)
+    gen = torch.Generator().manual_seed(T)
+    x, g = (torch.randn(B, T, P, C, generator=gen).cuda().to(dtype) for _ in range(2))
+    lengths = torch.tensor([T, T // 3], dtype=torch.int32, device="cuda")
+    live = torch.arange(T, device="cuda")[None] < lengths[:, None]
+    results = []
+    for filling in (0.0, 1e3):
+        x[~live] = filling * torch.randn(int((~live).sum()), P, C, generator=gen).cuda().to(dtype)
+        h = layer.forward(x, lengths).clone()
+        gx = layer.backward(g)
+        assert torch.equal(h[~live], x[~live]) and torch.equal(gx[~live], g[~live])
+        results.append((h[live], gx[live], layer.grad.clone()))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
