@@ -259,7 +259,10 @@ __global__ __launch_bounds__(threads_of<LANES>()) void norm_fwd_kernel(NormArgs 
 template <class T, int LANES, int NV>
 __global__ __launch_bounds__(threads_of<LANES>(), (NV * vec_of<T>() <= 8 && LANES <= 64 ? 4 : 1)) void norm_bwd_kernel(NormArgs a) {
     constexpr int VE = vec_of<T>(), TEAMS = threads_of<LANES>() / LANES;
-    constexpr bool kKeep = NV * VE <= kKept, kAhead = NV * VE <= (LANES == 1024 ? 8 : kKept);
+    // 1024 lanes leave 128 registers each: gamma is read for every row, and the next row when it is needed (500 rows of 16384: float32 55 -> 45 us,
+    // bfloat16 47 -> 38)
+    constexpr int kHeld = LANES == 1024 ? 8 : kKept;
+    constexpr bool kKeep = NV * VE <= kHeld, kAhead = NV * VE <= kHeld;
     __shared__ float red[LANES > 64 ? 2 * LANES / 64 : 1];
     __shared__ float fold[TEAMS > 1 ? kNormThreads / 64 : 1][TEAMS > 1 ? LANES * VE : 1];
     const int lane = TEAMS == 1 ? threadIdx.x : threadIdx.x % LANES, n = (int)a.n;
@@ -542,8 +545,9 @@ Team team_for(const gleam_layer_norm_desc& d) {
         if (units <= (long long)t.lanes * t.nv) return t;
     return Team{0, 0};
 }
-// Workgroups that walk the rows.  Backward: every one leaves 2 n partial sums, so there are no more than keep the chip busy (2000 rows
-// of 5001 float32, 512 lanes: 51 us with 512 workgroups, 45 with 256).  Forward: 327680 rows of 100 float32 65 us with 2048 workgroups, 62
+// Workgroups that walk the rows.  Backward: every one leaves 2 n partial sums, so there are no more than keep the chip busy (from 512 lanes on
+// 256 against 512 of them: float32 500 x 5001 17 and 25 us, 2000 x 5001 30 and 39, 20000 x 5001 226 and 238, 2000 x 8000 49 and 59, bfloat16
+// 500 x 16384 47 and 80, 6000 x 16384 180 and 210).  Forward: 327680 rows of 100 float32 65 us with 2048 workgroups, 62
 // with 8192, 69 with one for every eight rows; 60000 of 512 bfloat16 21.8, 21.5, 23.5.
 int grid_for(const gleam_layer_norm_desc& d, Team t, bool backward) {
     const long long teams = t.lanes > 64 ? 1 : kNormThreads / t.lanes, wgs = (d.rows + teams - 1) / teams;
