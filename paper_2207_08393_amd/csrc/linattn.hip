@@ -1018,17 +1018,17 @@ int width_of(int dk, int dv) {
     return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : 128;
 }
 // Segments of a call of `roles` passes, where there are few problems: as many workgroups as run at once (256 compute units hold two of
-// them each, four at a width of 64), or twice as many where they have eight chunks each all the same, for the pass over segments, which has
-// fewer.  (16384 tokens, 16 heads of 128, gradients: 296 us with one round, 288 with two, 302 with three; 3 x 1001 tokens, 6 heads of 40
-// and 72, float32, gradients: 67 with one round of four chunks each, 71 with two of two.)
+// them each, four at a width of 64), of two chunks at least.  Against twice as many where they have eight chunks each all the same:
+// 16384 tokens, 16 heads of 128, bfloat16 gradients 251 and 267 us (318 and 321 with 4 heads of keys and values), 50000 of them forward 303 and
+// 334, 100000 tokens, 4 heads of 32, gradients 88 and 105, 8192 x 4, 8 heads of 96, gradients 240 and 247; float32 the same within 1 %.
+// Against half as many: 419 us for the 318, and 3 x 1001 tokens, 6 heads of 40 and 72, float32, gradients 82 for 65.
 struct Split {
     int n_seg, chunks;
 };
 Split split_of(const gleam_linattn_desc& d, int roles) {
     const int D = width_of(d.dk, d.dv), L = d.dtype && D > 32 ? 64 : 32;
     const long long problems = d.B * d.P * d.heads, groups = D == 32 ? (problems + 3) / 4 : problems, chunks = (d.T + L - 1) / L;
-    const long long once = (D == 64 ? 1024 : 512) / (groups * roles);
-    long long n = 2 * once * 8 <= chunks ? 2 * once : once;
+    long long n = (D == 64 ? 1024 : 512) / (groups * roles);
     if (n > chunks / 2) n = chunks / 2;
     if (n < 2) return {1, (int)chunks};
     const long long per = (chunks + n - 1) / n;
