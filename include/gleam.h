@@ -363,11 +363,11 @@ int gleam_dropout_bwd(const gleam_dropout_desc* desc, const void* g_out, void* g
  * lengths: device int32 [B] or NULL (all T), tokens of each sequence that are there; others are not read, their outputs and
  * gradients are written as zeros; values outside 0..T count as the nearest of them.  A sequence of length 0 leaves its state as it is.
  * A token that is not finite can reach the outputs of up to 63 tokens before it (and in the gradients behind it) as NaN: they share a
- * matrix product.  Infinities, and with bfloat16 arrays states beyond 3.39e38, come out as infinity or NaN.
- * With bfloat16 arrays and T > 1, numbers on their way from one product to the next are rounded as follows (sums and states themselves are
- * float32): scores - the products of queries and keys, with their decay and scale - once, to bfloat16, so that an output from tokens up to 63
- * before it is sqrt 2 times as far from exact as its own rounding alone; values with their decay, on their way into a state, to 24 bits
- * (16 where that state only feeds outputs); the state that a query reads to 16 bits.  The same holds for the gradients.
+ * matrix product.  Infinities, and with bfloat16 arrays states and scores beyond 3.39e38, come out as infinity or NaN.
+ * With bfloat16 arrays and T > 1, numbers on their way from one product to the next are held in parts of 8 bits (sums and states themselves
+ * are float32): scores - the products of queries and keys, with their decay and scale - and the state that a query reads in 16 bits, values
+ * with their decay, on their way into a state, in 24 (16 where that state only feeds outputs).  So outputs and gradients are as far from
+ * exact as their own rounding to bfloat16.
  * 1 <= dk, dv <= 128, T <= 2^30, B P heads <= 2^29, no array reaches over more than 2^40 elements (GLEAM_E_DIMS otherwise).  One token
  * (T = 1) takes the recurrent form: every state is read once and written once. */
 typedef struct { int64_t b, t, p, h; } gleam_seq_strides;

@@ -85,7 +85,7 @@ struct Mma<unsigned short> {
         const uint2 lo = read_tr16(q), hi = read_tr16(q + 4 * stride);
         return __builtin_bit_cast(Frag, make_uint4(lo.x, lo.y, hi.x, hi.y));
     }
-    // the same with the block's rows in the order in which pack_scores has them
+    // the same with the block's rows in the order in which score_parts has them
     static __device__ __forceinline__ Frag col_frag_of_scores(const unsigned short* p, int stride, int col, int lane) {
         const int g = lane >> 4, s = lane & 15;
         const unsigned short* q = p + (4 * g + (s >> 2)) * stride + col;
@@ -94,11 +94,15 @@ struct Mma<unsigned short> {
     }
     static __device__ __forceinline__ int col_of(int t, int lane) { return 32 * (t >> 1) + 8 * (lane & 3) + 4 * (t & 1); }
     static __device__ __forceinline__ int narrow_col_of(int lane) { return 4 * (lane & 3); }
-    // results of two tiles (rows 4 g .. 4 g + 3 of either) as an operand.  Scores are rounded to 8 bits here and in put4, once: a second part
-    // takes the outputs' error from sqrt 2 times that of their own rounding to that alone, and the short kernel 4 to 7 % more time (20 x 192 x
-    // 160 pixels, 4 heads of 16: 78 -> 81 us forward, 197 -> 210 the gradients).
-    static __device__ __forceinline__ Frag pack_scores(floatx4 a, floatx4 b) {
-        return __builtin_bit_cast(Frag, make_uint4(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])));
+    // results of two tiles (rows 4 g .. 4 g + 3 of either) as an operand.  Scores are two bfloat16 numbers each, here and in put_score: with one an
+    // output is sqrt 2 times as far from exact as its own rounding, with two that alone, for 2 to 6 % more time (20 x 192 x 160 pixels, 4 heads
+    // of 16: 75 -> 78 us; 4 x 2048 tokens, 16 heads of 64: 39.3 -> 40.5; 16384 tokens, 16 heads of 128, gradients: 310 -> 319).
+    static constexpr int kScoreParts = 2;
+    static __device__ __forceinline__ void score_parts(floatx4 a, floatx4 b, Frag* parts) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < 4 ? a[i] : b[i & 3];
+        split(v, parts, kScoreParts);
     }
     // Parts whose sum is f times w: bfloat16 numbers w[i] f[i] rounded, what that left over rounded, and so on; 8 bits each.
     static constexpr int kStateParts = 2;
@@ -153,6 +157,13 @@ struct Mma<unsigned short> {
     static __device__ __forceinline__ void put4(unsigned short* p, floatx4 v) {
         *(uint2*)p = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
     }
+    // the same as two parts, each into an array of its own
+    static __device__ __forceinline__ void put_score(unsigned short* p, unsigned short* rest, floatx4 v) {
+        const unsigned a = pack_bf16x2(v[0], v[1]), b = pack_bf16x2(v[2], v[3]);
+        *(uint2*)p = make_uint2(a, b);
+        *(uint2*)rest = make_uint2(pack_bf16x2(v[0] - __uint_as_float(a << 16), v[1] - __uint_as_float(a & 0xffff0000u)),
+                                   pack_bf16x2(v[2] - __uint_as_float(b << 16), v[3] - __uint_as_float(b & 0xffff0000u)));
+    }
 };
 template <>
 struct Mma<float> {
@@ -177,7 +188,8 @@ struct Mma<float> {
     }
     static __device__ __forceinline__ int col_of(int t, int lane) { return 16 * t + (lane & 15); }
     static __device__ __forceinline__ int narrow_col_of(int lane) { return lane & 15; }
-    static __device__ __forceinline__ Frag pack_scores(floatx4 a, floatx4) { return a; }
+    static constexpr int kScoreParts = 1;
+    static __device__ __forceinline__ void score_parts(floatx4 a, floatx4, Frag* parts) { parts[0] = a; }
     static constexpr int kStateParts = 1;
     static __device__ __forceinline__ void scaled(Frag f, const float* w, Frag* parts, int) { parts[0] = Frag{f[0] * w[0], f[1] * w[1], f[2] * w[2], f[3] * w[3]}; }
     static __device__ __forceinline__ void pack(const floatx4* x, Frag* parts) { parts[0] = x[0]; }
@@ -195,6 +207,7 @@ struct Mma<float> {
             if (16 * u + 4 * g < width) put4(p + 16 * u + 4 * g, o[u]);
     }
     static __device__ __forceinline__ void put4(float* p, floatx4 v) { *(floatx4*)p = v; }
+    static __device__ __forceinline__ void put_score(float* p, float*, floatx4 v) { put4(p, v); }
 };
 
 // 16 bytes from byte `at` of a buffer; zeros beyond its end (also for a negative `at`).  A plain function: the host pass drops the
@@ -461,7 +474,8 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), (STATES && PARTS < 3 ? 3 :
     }
     long long out_at = r.b * a.o.s.b + r.p * a.o.s.p + (long long)(r.h / a.o.share) * a.o.s.h + (start + way * ((long long)c_begin * L + m)) * a.o.s.t + 32 * wave;
     const long long out_step = way * 16 * a.o.s.t;
-    // Scores into LDS, rows `it`: the lane has four consecutive columns of row m of the tile.
+    // Scores into LDS, rows `it`: the lane has four consecutive columns of row m of the tile.  Their second parts take the place of the
+    // values, which are in registers by then.
     auto scores = [&](int count) {
 #pragma unroll
         for (int rr = 0; rr < (kRows + W - 1) / W; ++rr) {
@@ -480,10 +494,14 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), (STATES && PARTS < 3 ? 3 :
                     for (int s = 0; s < D / KB; ++s) p = M::mma(M::row_frag(sk + (16 * jt + m) * S::kRow + s * KB + g * VE), qf[s], p);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) p[i] = (n > 0 || m >= 4 * g + i) && it >= n ? p[i] * wt[n][i] : 0.f;
-                    M::put4(sp + (16 * it + m) * S::kScoreRow + 16 * jt + 4 * g, p);
+                    const int at = (16 * it + m) * S::kScoreRow + 16 * jt + 4 * g;
+                    M::put_score(sp + at, sv + at, p);
                 }
                 // the tile right of the diagonal, where it shares an operand with it and is not among those
-                if (kPair == 2 && W % 2 && !(it & 1)) M::put4(sp + (16 * it + m) * S::kScoreRow + 16 * (it + 1) + 4 * g, floatx4{0.f, 0.f, 0.f, 0.f});
+                if (kPair == 2 && W % 2 && !(it & 1)) {
+                    const int at = (16 * it + m) * S::kScoreRow + 16 * (it + 1) + 4 * g;
+                    M::put_score(sp + at, sv + at, floatx4{0.f, 0.f, 0.f, 0.f});
+                }
             }
         }
     };
@@ -519,9 +537,12 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), (STATES && PARTS < 3 ? 3 :
             if (it * 16 >= count) break;
 #pragma unroll
             for (int s = 0; s <= it * 16 / KB; ++s) {
-                const Frag pf = M::row_frag(sp + (16 * it + m) * S::kScoreRow + s * KB + g * VE);
 #pragma unroll
-                for (int u = 0; u < 2; ++u) o[it][u] = M::mma(vf[s][u], pf, o[it][u]);
+                for (int n = 0; n < M::kScoreParts; ++n) {
+                    const Frag pf = M::row_frag((n ? sv : sp) + (16 * it + m) * S::kScoreRow + s * KB + g * VE);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) o[it][u] = M::mma(vf[s][u], pf, o[it][u]);
+                }
             }
         }
         auto put = [&](auto* out) {
@@ -546,6 +567,7 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), (STATES && PARTS < 3 ? 3 :
             for (int u = 0; u < 2; ++u) vf[s][u] = M::template col_frag<STATES>(sv + s * KB * S::kRow, S::kRow, 2 * wave + u, lane);
         if constexpr (!STATES) {
             floatx4 o[kRows][2] = {};
+            if constexpr (M::kScoreParts > 1) exchange<W>();          // everyone has its values
             scores(count);
             if (have) from_state(o);                  // needs no scores, so it stands in front of their exchange
             exchange<W>();
@@ -769,7 +791,7 @@ __global__ __launch_bounds__(64 * kShortWaves) void mix_short_kernel(MixArgs arg
         }
     // scores of the tiles of one output row tile as operands: columns of the product are the output's tokens, which are the later
     // (UP: the earlier) ones of the two; tiles that the mask leaves out are zero
-    auto scores = [&](const Frag(&contracted)[TT][KS], const Frag(&output)[TT][KS], int t, const floatx4* w, bool is_up, Frag(&p)[TS]) {
+    auto scores = [&](const Frag(&contracted)[TT][KS], const Frag(&output)[TT][KS], int t, const floatx4* w, bool is_up, Frag(&p)[TS][M::kScoreParts]) {
         floatx4 tile[2 * TS];
 #pragma unroll
         for (int j = 0; j < 2 * TS; ++j) {
@@ -785,16 +807,20 @@ __global__ __launch_bounds__(64 * kShortWaves) void mix_short_kernel(MixArgs arg
             }
         }
 #pragma unroll
-        for (int s = 0; s < TS; ++s) p[s] = M::pack_scores(tile[kPair * s], tile[kPair * s + kPair - 1]);
+        for (int s = 0; s < TS; ++s) M::score_parts(tile[kPair * s], tile[kPair * s + kPair - 1], p[s]);
     };
-    auto product = [&](int which, int width, const Frag(&p)[TS], int t, bool is_up, floatx4(&o)[U]) {
+    auto product = [&](int which, int width, const Frag(&p)[TS][M::kScoreParts], int t, bool is_up, floatx4(&o)[U]) {
 #pragma unroll
         for (int u = 0; u < U; ++u) o[u] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < TS; ++s) {
             if (is_up ? (s + 1) * kPair <= t : s * kPair > t) continue;
 #pragma unroll
-            for (int u = 0; u < U; ++u) o[u] = M::mma(turned(which, width, s, u), p[s], o[u]);
+            for (int u = 0; u < U; ++u) {
+                const Frag f = turned(which, width, s, u);
+#pragma unroll
+                for (int n = 0; n < M::kScoreParts; ++n) o[u] = M::mma(f, p[s][n], o[u]);
+            }
         }
     };
     if constexpr (!BWD) {
@@ -814,7 +840,7 @@ __global__ __launch_bounds__(64 * kShortWaves) void mix_short_kernel(MixArgs arg
         floatx4 o[TT][U];
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
-            Frag p[TS];
+            Frag p[TS][M::kScoreParts];
             scores(k, q, t, down, false, p);
             product(0, ro.v.d, p, t, false, o[t]);
             if constexpr (!ROWS) store(ro, 0, t, o[t]);
@@ -847,7 +873,7 @@ __global__ __launch_bounds__(64 * kShortWaves) void mix_short_kernel(MixArgs arg
         floatx4 oq[TT][U], ok[TT][U], ov[TT][U];
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
-            Frag p[TS];
+            Frag p[TS][M::kScoreParts];
             scores(v, go, t, down, false, p);        // g_q of token t: earlier tokens' keys
             product(0, rv.q.d, p, t, false, oq[t]);
             if constexpr (!ROWS) store(rq, 0, t, oq[t]);
