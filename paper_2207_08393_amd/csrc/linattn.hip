@@ -16,12 +16,14 @@
 // states from segment to segment, the third has all segments side by side; the three passes of a backward call share each of the launches.
 //
 // Measured (listed calls; copy rate of the card 5.2 TB/s, bfloat16 matrix products 1212 TFLOP/s):
-//   4 x 2048 tokens, 16 heads of 64, bfloat16               39 us   (14 segments, 10 states, 23 outputs; all read once and written once: 13)
-//   16384 tokens, 16 heads of 128, 4 of k and v, gradients 320 us   (64, 16, 194, and 31 for the sum over shared heads; 52)
-//   3 x 1001 tokens, 6 heads of 40 and 72, float32, gradients 65 us (17, 8, 47; 5)
-// What bounds the chunk loop at a width of 128 is no single unit: vector instructions 39 %, matrix instructions 32 %, LDS 45 % of the
+//   4 x 2048 tokens, 16 heads of 64, bfloat16                 40 us (all read once and written once: 13)
+//   16384 tokens, 16 heads of 128, 4 of k and v, gradients    320   (52)
+//   3 x 1001 tokens, 6 heads of 40 and 72, float32, gradients 65    (5)
+// Under a profiler, which makes them a tenth longer, segments, states and outputs take 13 + 8 + 23, 79 + 8 + 214 and 16 + 6 + 46 us, and the
+// sums over the heads that share keys and values 2 x 27 in the second.
+// What bounds the chunk loop at a width of 128 is no single unit: vector instructions 40 %, matrix instructions 33 %, LDS 47 % of the
 // time busy, at the two workgroups of 256 registers a lane that a compute unit holds.  Tried without gain: other paddings of the LDS rows
-// (0 to +3 % time), chunks without branches where they are whole, half or twice as many segments.
+// (0 to +3 % time), chunks without branches where they are whole.
 //
 // One problem is one sequence, pixel and head.  D is dk and dv rounded up to 32, 64, 96 or 128; a problem is worked on by D/32 waves, and
 // a wave owns 32 columns (dv) of the state, in registers in the layout of a 16x16 product's result: the lane holds
@@ -638,8 +640,8 @@ __global__ __launch_bounds__((Shape<T, D>::kThreads), (STATES && PARTS < 3 ? 3 :
 // At most 64 tokens of at most 32 values without a state, as the frames of a series at one pixel: a wave has a whole problem, all
 // three gradients of it in the backward pass.  Scores go from the result of one product to the operand of the next in registers: the
 // contracted tokens may come in any order that both operands have.
-// 20 x 192 x 160 pixels, 4 heads of 16, bfloat16: 75 us, 4.2 TB/s, bound by vector instructions and memory about alike (275 us by the
-// kernel above).
+// 20 x 192 x 160 pixels, 4 heads of 16, bfloat16: 78 us, 4.0 TB/s, bound by vector instructions (85 % of the time busy) and memory (275 us by
+// the kernel above); gradients 210 us, 2.6 TB/s.
 // TT: tiles of 16 tokens.  U: tiles of 16 columns.
 // ROWS: the four problems of a workgroup are neighbouring heads of a pixel, whose values lie side by side; the workgroup moves whole
 // rows of the four through LDS.  Otherwise an operand whose rows are tokens is loaded straight from memory in the layout of the product,
@@ -1045,9 +1047,9 @@ int width_of(int dk, int dv) {
 }
 // Segments of a call of `roles` passes, where there are few problems: as many workgroups as run at once (256 compute units hold two of
 // them each, four at a width of 64), of two chunks at least.  Against twice as many where they have eight chunks each all the same:
-// 16384 tokens, 16 heads of 128, bfloat16 gradients 251 and 267 us (318 and 321 with 4 heads of keys and values), 50000 of them forward 303 and
-// 334, 100000 tokens, 4 heads of 32, gradients 88 and 105, 8192 x 4, 8 heads of 96, gradients 240 and 247; float32 the same within 1 %.
-// Against half as many: 419 us for the 318, and 3 x 1001 tokens, 6 heads of 40 and 72, float32, gradients 82 for 65.
+// 16384 tokens, 16 heads of 128, bfloat16 gradients 259 and 274 us (322 and 326 with 4 heads of keys and values), 50000 of them forward 305 and
+// 337, 100000 tokens, 4 heads of 32, gradients 90 and 105, 8192 x 4, 8 heads of 96, gradients 255 and 264; float32 the same within 1 %.
+// Against half as many: 431 us for the 322, 459 for the 255, and 3 x 1001 tokens, 6 heads of 40 and 72, float32, gradients 82 for 65.
 struct Split {
     int n_seg, chunks;
 };
@@ -1164,7 +1166,8 @@ hipError_t share_sum(const gleam_linattn_desc& d, const float* part, const MixTe
 template <class T>
 hipError_t mix_step(const MixArgs& a, hipStream_t st) {
     const long long problems = a.B * a.P * a.H;
-    if (a.dk * ((a.dv + 3) / 4) <= 64 * kStepRows)    // a wave has the whole state on its way at once
+    // the whole state is on its way to a wave at once, or in two turns where the columns' fours are not a power of two
+    if (a.dk * ((a.dv + 3) / 4) <= 64 * kStepRows)
         hipLaunchKernelGGL((mix_step_kernel<T, 64>), grid_of((problems + 3) / 4), dim3(kStepThreads), 0, st, a);
     else
         hipLaunchKernelGGL((mix_step_kernel<T, kStepThreads>), grid_of(problems), dim3(kStepThreads), 0, st, a);

@@ -7,8 +7,8 @@
 // variance passes the range of a float32, r = 0 and outputs are beta.  Backward: one read of x and g_y,
 // one write of g_x; every lane keeps its columns from row to row and sums g_gamma and g_beta in registers, a workgroup writes one
 // partial sum per column and a second launch adds them up in a fixed order.  Both are bound by HBM.
-// Measured: forward 4 x 320 x 256 pixels of 100 channels, float32, 60 us (4.4 TB/s); backward 4 x 640 x 320 of 128 channels, bfloat16, 123 us
-// (5.2 TB/s, the rate of a copy), 2000 rows of 5001 float32 40 us (3.0 TB/s; 8 us of it the sum of the partial sums).
+// Measured: forward 4 x 320 x 256 pixels of 100 channels, float32, 60 us (4.4 TB/s); backward 4 x 640 x 320 of 128 channels, bfloat16, 121 us
+// (5.2 TB/s, the rate of a copy), 2000 rows of 5001 float32 34 us (3.5 TB/s; some 6 us of it the sum of the partial sums).
 //
 // Rows too long for the registers of a workgroup are read three times (forward) or twice (backward), see the streaming kernels.
 #include <hip/hip_runtime.h>
