@@ -302,10 +302,11 @@ int gleam_unrolled_infer(const gleam_geom* geom, const gleam_prox_desc* prox, in
 /* ---- Sequence layers: layer norm, dropout, linear attention along the frames -----------------------------------------
  * Operators of their own: a prox network (gleam_prox_desc) has convolutions only and does not call them.  They take feature maps
  * [..][channels], channels last, and mix the frames of a dynamic series, or the tokens of any sequence: y = layer_norm(x); q, k, v =
- * projections of y; h = x + dropout(projection of linear_attention(q, k, v)).  Activations are float32 (dtype 0) or bfloat16 (dtype 1) and are computed on in float32 (products of
- * bfloat16 arrays on the bfloat16 matrix cores with float32 sums); scales, shifts, statistics, decays and states are float32.
- * Conventions are those above, except that arrays may have strides (rows: fewer than 2^31, arrays of at most 2^40 elements).  Pointers need the alignment of their element type; accesses are
- * fastest where base addresses and strides are multiples of 16 bytes. */
+ * projections of y; h = x + dropout(projection of linear_attention(q, k, v)).  Activations are float32 (dtype 0) or bfloat16 (dtype 1) and
+ * are computed on in float32 (products of bfloat16 arrays on the bfloat16 matrix cores with float32 sums); scales, shifts, statistics,
+ * decays and states are float32.  Conventions are those above, except that arrays may have strides (rows: fewer than 2^31, arrays of at
+ * most 2^40 elements).  Pointers need the alignment of their element type; accesses are fastest where base addresses and strides are
+ * multiples of 16 bytes. */
 
 /* Layer norm over the last dimension of `rows` rows of n elements: mean m and variance s^2 (over n) of the row,
  *     y = (x - m) * r * gamma + beta,   r = 1 / sqrt(s^2 + eps)
@@ -359,7 +360,8 @@ int gleam_dropout_bwd(const gleam_dropout_desc* desc, const void* g_out, void* g
  * layer and has no gradient.  Heads: `heads` of the output and the states; q, k and v have heads of their own number, each a
  * divisor of `heads`, and output head h uses head h / (heads / their number).
  * Arrays: element [b][t][p][head][c] of an activation lies at b*s.b + t*s.t + p*s.p + head*s.h + c (strides in elements, >= 0).  Strides
- * of arrays that are written - o, and in the backward pass those of q, k and v - must not let elements overlap.  States are [B][P][heads][dk][dv] float32, row-major.
+ * of arrays that are written - o, and in the backward pass those of q, k and v - must not let elements overlap.  States are
+ * [B][P][heads][dk][dv] float32, row-major.
  * lengths: device int32 [B] or NULL (all T), tokens of each sequence that are there; others are not read, their outputs and
  * gradients are written as zeros; values outside 0..T count as the nearest of them.  A sequence of length 0 leaves its state as it is.
  * A token that is not finite can reach the outputs of up to 63 tokens before it (and in the gradients behind it) as NaN: they share a
