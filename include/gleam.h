@@ -394,6 +394,91 @@ int gleam_linattn_bwd(const gleam_linattn_desc* desc, const void* q, const void*
                       const int32_t* lengths, const float* state_in, const void* g_o, const float* g_state_out, void* g_q,
                       void* g_k, void* g_v, float* g_state_in, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- Norm and rotation of queries and keys ----------------------------------------------------------------------------------
+ * Each head of q and k, a row x of d values, is divided by its root mean square, scaled, and its first `rot` values are turned in pairs
+ * by angles that grow with the token's position, so that products of queries and keys depend on how far apart they are:
+ *     r = 1 / sqrt(mean(x^2) + eps),   y = x r gamma,   (y_a, y_b) <- (y_a cos f - y_b sin f, y_b cos f + y_a sin f),   f = pos * freq[j]
+ * for pairs j < rot/2.  pairs 0: a = j, b = j + rot/2 (halves); 1: a = 2j, b = 2j + 1 (neighbours).  Values from `rot` on are normed and
+ * scaled only.  Arithmetic is float32 whatever the type, angles are formed and reduced in 64 bits: they are right to float32 for every int32
+ * position.  Where the mean square passes the range of a float32, r = 0; infinities and NaN stay in their head.
+ * gamma_q, gamma_k: [d] float32, shared by the heads of a tensor, or NULL (1).  freq: [rot/2] float32, radians a position (NULL where rot is 0).
+ * positions: device int32, [B] (each = 0: token t of sequence b is at positions[b] + t) or [B][T] (each = 1), or NULL: token t is at t.
+ * lengths: device int32 [B] or NULL, tokens of each sequence that are there, as for linear attention: others are not read, their results
+ * are written as zeros, and they take no part in the gradients of gamma.
+ * Arrays [B][T][P][heads][d] with strides as for linear attention (q_out, k_out: of results, and of their gradients); those of arrays that
+ * are written must keep elements apart.  k_heads = 0: no k, all its pointers are ignored.  1 <= d <= 256, rot even, 0 <= rot <= d, eps > 0, T <= 2^30,
+ * P (q_heads + k_heads) < 2^31, B T P heads <= 2^40. */
+typedef struct {
+    int32_t dtype, q_heads, k_heads, d, rot, pairs, each;
+    float eps;
+    int64_t B, T, P;
+    gleam_seq_strides q, k, q_out, k_out;
+} gleam_qknorm_desc;
+
+/* q_out may be q where their strides are equal, k_out may be k; nothing else that is written may overlap what is read. */
+int gleam_qknorm_fwd(const gleam_qknorm_desc* desc, const void* q, const void* k, const float* gamma_q, const float* gamma_k,
+                     const float* freq, const int32_t* positions, const int32_t* lengths, void* q_out, void* k_out, void* stream);
+
+/* Gradients of the same call from g_q_out = dL/d q_out and g_k_out (strides of q_out, k_out).  With g the gradient turned back and
+ * gg = g gamma:   g_x = r (gg - x r^2 mean(gg x)),   g_gamma = sum over rows of g x r.
+ * g_q, g_k: strides of q and k; g_q may be g_q_out where those are equal, g_k may be g_k_out; neither may be q or k.  g_gamma_q,
+ * g_gamma_k: [d], overwritten, either may be NULL (not wanted); sums are formed in a fixed order.  ws: gleam_qknorm_workspace_bytes,
+ * 256-byte aligned, not read where neither is wanted. */
+int gleam_qknorm_workspace_bytes(const gleam_qknorm_desc* desc, size_t* ws_bytes);
+int gleam_qknorm_bwd(const gleam_qknorm_desc* desc, const void* q, const void* k, const float* gamma_q, const float* gamma_k,
+                     const float* freq, const int32_t* positions, const int32_t* lengths, const void* g_q_out, const void* g_k_out,
+                     void* g_q, void* g_k, float* g_gamma_q, float* g_gamma_k, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- Gated scan -------------------------------------------------------------------------------------------------------------
+ * A linear recurrence along the tokens whose memory the input itself opens and closes, channel by channel:
+ *     s_t = sigmoid(r_t),   a_t = exp(-kappa softplus(lambda[c]) s_t),   h_t = a_t h_(t-1) + sqrt(1 - a_t^2) sigmoid(i_t) x_t
+ * with x, r, i, h [B][T][P][C] and lambda [C] float32 (a parameter, with a gradient).  Its state is C numbers for each sequence and pixel.
+ * Element [b][t][p][c] of an array lies at b*s.b + t*s.t + p*s.p + c (strides in elements, >= 0); arrays that are written - h, and in the
+ * backward pass those of x, r and i - must keep elements apart.  States are [B][P][C] float32.
+ * lengths: as for linear attention; a sequence of length 0 leaves its state as it is.
+ * Arithmetic is float32; 1 - a_t is formed without cancellation, so a memory of many thousand tokens decays at its own rate.  Long sequences
+ * are scanned in stretches whose carries are joined in a fixed order.  A token that is not finite reaches h of later tokens, and gradients of
+ * tokens before it, of its own channel only, as infinity or NaN.
+ * kappa >= 0.  T <= 2^30, C < 2^31, B T P C <= 2^40, no array reaches over more than 2^40 elements. */
+typedef struct { int64_t b, t, p; } gleam_scan_strides;
+typedef struct {
+    int32_t dtype;
+    float kappa;
+    int64_t B, T, P, C;
+    gleam_scan_strides x, r, i, h;
+} gleam_gatedscan_desc;
+
+/* Scratch of either direction; 0 where none is needed (then ws may be NULL). */
+int gleam_gatedscan_workspace_bytes(const gleam_gatedscan_desc* desc, size_t* fwd_bytes, size_t* bwd_bytes);
+/* state_in: state before the first token, or NULL (zero).  state_out: state behind the last token, or NULL (not wanted); may be
+ * state_in.  h may not overlap x, r or i. */
+int gleam_gatedscan_fwd(const gleam_gatedscan_desc* desc, const void* x, const void* r, const void* i, const float* lambda,
+                        const int32_t* lengths, const float* state_in, void* h, float* state_out, void* ws, size_t ws_bytes, void* stream);
+/* Gradients of the same call from g_h = dL/dh (strides of h) and g_state_out = dL/d state_out (or NULL: zero).  g_x, g_r, g_i have the
+ * strides of x, r, i; g_lambda: [C], overwritten; g_state_in (or NULL) = dL/d state_in.  h is formed again in float32 and not read.
+ * No gradient may overlap an input. */
+int gleam_gatedscan_bwd(const gleam_gatedscan_desc* desc, const void* x, const void* r, const void* i, const float* lambda,
+                        const int32_t* lengths, const float* state_in, const void* g_h, const float* g_state_out, void* g_x, void* g_r,
+                        void* g_i, float* g_lambda, float* g_state_in, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- Orthogonalised update ----------------------------------------------------------------------------------------------------
+ * One step for `count` weight matrices of rows x cols, beside gleam_adam_step for everything that is no matrix (Jordan et al., "Muon", 2024):
+ *     m <- momentum m + g,   u = g + momentum m (nesterov) or m,   X = u / (|u|_F + eps)
+ *     `steps` times:  A = X X^T,  X <- (a I + b A + c A^2) X      (of X^T where rows > cols: the smaller Gram matrix)
+ *     theta <- (1 - lr weight_decay) theta - lr sqrt(max(1, rows / cols)) X
+ * theta, grad, m: device float32, matrix k at k * stride elements, rows x cols row-major there; theta and m are updated in place and may
+ * not overlap each other or grad; m is zero before the first step.  |u| is summed in 64 bits.  Products are of float32 numbers in three bfloat16 parts on the
+ * matrix cores with float32 sums: as good as float32 products.  A matrix whose update is zero keeps X = 0; one that holds an infinity or NaN
+ * becomes NaN, the others do not.  rows, cols <= 65536, count rows cols <= 2^40. */
+typedef struct {
+    float lr, momentum, weight_decay, eps, a, b, c;   /* eps > 0, 0 <= momentum < 1 */
+    int32_t nesterov, steps;                          /* 1 <= steps <= 100 */
+} gleam_muon;
+int gleam_muon_workspace_bytes(int64_t count, int64_t rows, int64_t cols, size_t* ws_bytes);
+/* ws: at least gleam_muon_workspace_bytes, 256-byte aligned.  stride >= rows * cols (any value >= 0 where count is 1). */
+int gleam_muon_step(const gleam_muon* hyper, int64_t count, int64_t rows, int64_t cols, int64_t stride, float* theta,
+                    const float* grad, float* m, void* ws, size_t ws_bytes, void* stream);
+
 /* Measurement aid (not part of the method): between gleam_profile_begin and gleam_profile_end every kernel
  * this library launches is bracketed by HIP events on the caller's stream.  gleam_profile_end synchronises
  * the device and copies up to `capacity` per-launch records (launch order) to the HOST array `out`;

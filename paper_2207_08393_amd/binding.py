@@ -65,6 +65,24 @@ class gleam_linattn_desc(C.Structure):
                 [(n, C.c_int64) for n in ("B", "T", "P")] + [(n, gleam_seq_strides) for n in ("q", "k", "v", "o")])
 
 
+class gleam_qknorm_desc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("dtype", "q_heads", "k_heads", "d", "rot", "pairs", "each")] + [("eps", C.c_float)] +
+                [(n, C.c_int64) for n in ("B", "T", "P")] + [(n, gleam_seq_strides) for n in ("q", "k", "q_out", "k_out")])
+
+
+class gleam_scan_strides(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("b", "t", "p")]
+
+
+class gleam_gatedscan_desc(C.Structure):
+    _fields_ = ([("dtype", C.c_int32), ("kappa", C.c_float)] + [(n, C.c_int64) for n in ("B", "T", "P", "C")] +
+                [(n, gleam_scan_strides) for n in ("x", "r", "i", "h")])
+
+
+class gleam_muon(C.Structure):
+    _fields_ = [(n, C.c_float) for n in ("lr", "momentum", "weight_decay", "eps", "a", "b", "c")] + [("nesterov", C.c_int32), ("steps", C.c_int32)]
+
+
 class GleamError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -119,6 +137,15 @@ def lib() -> C.CDLL:
         L.gleam_linattn_workspace_bytes.argtypes = [pl, C.POINTER(sz), C.POINTER(sz)]
         L.gleam_linattn_fwd.argtypes = [pl, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.gleam_linattn_bwd.argtypes = [pl, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        pq, pg2, pm = C.POINTER(gleam_qknorm_desc), C.POINTER(gleam_gatedscan_desc), C.POINTER(gleam_muon)
+        L.gleam_qknorm_fwd.argtypes = [pq] + [vp] * 10
+        L.gleam_qknorm_workspace_bytes.argtypes = [pq, C.POINTER(sz)]
+        L.gleam_qknorm_bwd.argtypes = [pq] + [vp] * 14 + [sz, vp]
+        L.gleam_gatedscan_workspace_bytes.argtypes = [pg2, C.POINTER(sz), C.POINTER(sz)]
+        L.gleam_gatedscan_fwd.argtypes = [pg2] + [vp] * 9 + [sz, vp]
+        L.gleam_gatedscan_bwd.argtypes = [pg2] + [vp] * 14 + [sz, vp]
+        L.gleam_muon_workspace_bytes.argtypes = [C.c_int64] * 3 + [C.POINTER(sz)]
+        L.gleam_muon_step.argtypes = [pm] + [C.c_int64] * 4 + [vp] * 4 + [sz, vp]
         L.gleam_profile_begin.argtypes = []
         L.gleam_profile_end.argtypes = [C.POINTER(gleam_kernel_record), C.c_int, C.POINTER(C.c_int)]
         _lib = L
@@ -132,6 +159,8 @@ EXPORTS = ("gleam_strerror", "gleam_fft_size_supported", "gleam_set_kernel_polic
            "gleam_modl_module_fwd", "gleam_modl_module_bwd", "gleam_adam_step",
            "gleam_greedy_iteration", "gleam_unrolled_infer", "gleam_layer_norm_fwd", "gleam_layer_norm_workspace_bytes", "gleam_layer_norm_bwd",
            "gleam_dropout_fwd", "gleam_dropout_bwd", "gleam_linattn_workspace_bytes", "gleam_linattn_fwd", "gleam_linattn_bwd",
+           "gleam_qknorm_fwd", "gleam_qknorm_workspace_bytes", "gleam_qknorm_bwd", "gleam_gatedscan_workspace_bytes", "gleam_gatedscan_fwd",
+           "gleam_gatedscan_bwd", "gleam_muon_workspace_bytes", "gleam_muon_step",
            "gleam_profile_begin", "gleam_profile_end")
 
 
@@ -485,6 +514,138 @@ def gleam_linattn_bwd(desc, q, k, v, log_decay, lengths, state_in, g_o, g_state_
                                    _flat(g_state_out, 0, state, "g_state_out"), _seq(g_q, want["q"], "g_q"), _seq(g_k, want["k"], "g_k"),
                                    _seq(g_v, want["v"], "g_v"), _flat(g_state_in, 0, state, "g_state_in"), _ptr(ws), _nbytes(ws),
                                    _stream(stream)), "gleam_linattn_bwd")
+
+
+# ---- norm and rotation of queries and keys, gated scan, orthogonalised update
+def _apart(t, dims: int, like, what: str):
+    """A description's array: so many dimensions, the type and leading sizes of the others, contiguous along the last."""
+    if t.dim() != dims or t.dtype is not like.dtype or t.shape[:3] != like.shape[:3] or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{what}: {dims} dimensions [B][T][P].. of one type with a contiguous last one expected, got {tuple(t.shape)} with strides "
+                         f"{t.stride()} of {t.dtype}")
+
+
+def make_qknorm(q, k, q_out, k_out, rot, eps=1e-6, pairs="halves", positions="start") -> gleam_qknorm_desc:
+    """From the arrays of a call, or others of their shapes and strides: [B][T][P][heads][d] with any strides but the last; k and k_out may be
+    None.  Gradients have the strides of the arrays they belong to.  pairs: 'halves' or 'neighbours'; positions: 'start', one for each
+    sequence, or 'each', one for each token."""
+    if pairs not in ("halves", "neighbours") or positions not in ("start", "each"):
+        raise ValueError(f"pairs {pairs!r}: 'halves' or 'neighbours'; positions {positions!r}: 'start' or 'each'")
+    if (k is None) != (k_out is None):
+        raise ValueError("k and k_out belong together")
+    for name, t in (("q", q), ("q_out", q_out), ("k", k), ("k_out", k_out)):
+        if t is not None:
+            _apart(t, 5, q, name)
+            if t.shape[4] != q.shape[4] or t.shape[3] != (q if name[0] == "q" else k).shape[3]:
+                raise ValueError(f"{name}: {tuple(t.shape)}: results have the heads of their source, and all heads one width")
+    B, T, P, heads, d = q.shape
+    return gleam_qknorm_desc(_dtype_code(q.dtype), heads, 0 if k is None else k.shape[3], d, int(rot), int(pairs == "neighbours"), int(positions == "each"),
+                             float(eps), B, T, P, *(gleam_seq_strides(*(t.stride()[:4] if t is not None else (0,) * 4)) for t in (q, k, q_out, k_out)))
+
+
+def _want_qk(desc):
+    key, (made_for, want) = bytes(desc), getattr(desc, "_want", (None, None))
+    if made_for != key:
+        want = {}
+        for name, heads in (("q", desc.q_heads), ("k", desc.k_heads), ("q_out", desc.q_heads), ("k_out", desc.k_heads)):
+            s = getattr(desc, name)
+            want[name] = ((desc.B, desc.T, desc.P, heads, desc.d), (s.b, s.t, s.p, s.h, 1), _types()[desc.dtype])
+        desc._want = key, want
+    return want
+
+
+def gleam_qknorm_fwd(desc, q, k, gamma_q, gamma_k, freq, positions, lengths, q_out, k_out, stream=None):
+    want, d = _want_qk(desc), desc.d
+    _check(lib().gleam_qknorm_fwd(C.byref(desc), _seq(q, want["q"], "q"), _seq(k, want["k"], "k"), _flat(gamma_q, 0, d, "gamma_q"),
+                                  _flat(gamma_k, 0, d, "gamma_k"), _flat(freq, 0, desc.rot // 2, "freq"),
+                                  _flat(positions, 2, desc.B * (desc.T if desc.each else 1), "positions"), _flat(lengths, 2, desc.B, "lengths"),
+                                  _seq(q_out, want["q_out"], "q_out"), _seq(k_out, want["k_out"], "k_out"), _stream(stream)), "gleam_qknorm_fwd")
+
+
+def gleam_qknorm_workspace_bytes(desc) -> int:
+    n = C.c_size_t(0)
+    _check(lib().gleam_qknorm_workspace_bytes(C.byref(desc), C.byref(n)), "gleam_qknorm_workspace_bytes")
+    return n.value
+
+
+def gleam_qknorm_bwd(desc, q, k, gamma_q, gamma_k, freq, positions, lengths, g_q_out, g_k_out, g_q, g_k, g_gamma_q, g_gamma_k, ws, stream=None):
+    want, d = _want_qk(desc), desc.d
+    _check(lib().gleam_qknorm_bwd(C.byref(desc), _seq(q, want["q"], "q"), _seq(k, want["k"], "k"), _flat(gamma_q, 0, d, "gamma_q"),
+                                  _flat(gamma_k, 0, d, "gamma_k"), _flat(freq, 0, desc.rot // 2, "freq"),
+                                  _flat(positions, 2, desc.B * (desc.T if desc.each else 1), "positions"), _flat(lengths, 2, desc.B, "lengths"),
+                                  _seq(g_q_out, want["q_out"], "g_q_out"), _seq(g_k_out, want["k_out"], "g_k_out"), _seq(g_q, want["q"], "g_q"),
+                                  _seq(g_k, want["k"], "g_k"), _flat(g_gamma_q, 0, d, "g_gamma_q"), _flat(g_gamma_k, 0, d, "g_gamma_k"), _ptr(ws),
+                                  _nbytes(ws), _stream(stream)), "gleam_qknorm_bwd")
+
+
+def make_gatedscan(x, r, i, h, kappa=8.0) -> gleam_gatedscan_desc:
+    """From the arrays of a call, or others of their shapes and strides: [B][T][P][C] with any strides but the last."""
+    for name, t in (("x", x), ("r", r), ("i", i), ("h", h)):
+        _apart(t, 4, h, name)
+        if t.shape != h.shape:
+            raise ValueError(f"{name}: {tuple(t.shape)}, {tuple(h.shape)} expected")
+    return gleam_gatedscan_desc(_dtype_code(h.dtype), float(kappa), *h.shape, *(gleam_scan_strides(*t.stride()[:3]) for t in (x, r, i, h)))
+
+
+def _want_scan(desc):
+    key, (made_for, want) = bytes(desc), getattr(desc, "_want", (None, None))
+    if made_for != key:
+        shape = (desc.B, desc.T, desc.P, desc.C)
+        want = {n: (shape, (s.b, s.t, s.p, 1), _types()[desc.dtype]) for n, s in ((n, getattr(desc, n)) for n in "xrih")}
+        desc._want = key, want
+    return want
+
+
+def gleam_gatedscan_workspace_bytes(desc):
+    """(forward, backward) bytes; 0: no workspace needed."""
+    fwd, bwd = C.c_size_t(0), C.c_size_t(0)
+    _check(lib().gleam_gatedscan_workspace_bytes(C.byref(desc), C.byref(fwd), C.byref(bwd)), "gleam_gatedscan_workspace_bytes")
+    return fwd.value, bwd.value
+
+
+def gleam_gatedscan_fwd(desc, x, r, i, lam, lengths, state_in, h, state_out, ws, stream=None):
+    want, state = _want_scan(desc), desc.B * desc.P * desc.C
+    _check(lib().gleam_gatedscan_fwd(C.byref(desc), _seq(x, want["x"], "x"), _seq(r, want["r"], "r"), _seq(i, want["i"], "i"),
+                                     _flat(lam, 0, desc.C, "lambda"), _flat(lengths, 2, desc.B, "lengths"), _flat(state_in, 0, state, "state_in"),
+                                     _seq(h, want["h"], "h"), _flat(state_out, 0, state, "state_out"), _ptr(ws), _nbytes(ws), _stream(stream)),
+           "gleam_gatedscan_fwd")
+
+
+def gleam_gatedscan_bwd(desc, x, r, i, lam, lengths, state_in, g_h, g_state_out, g_x, g_r, g_i, g_lam, g_state_in, ws, stream=None):
+    want, state = _want_scan(desc), desc.B * desc.P * desc.C
+    _check(lib().gleam_gatedscan_bwd(C.byref(desc), _seq(x, want["x"], "x"), _seq(r, want["r"], "r"), _seq(i, want["i"], "i"),
+                                     _flat(lam, 0, desc.C, "lambda"), _flat(lengths, 2, desc.B, "lengths"), _flat(state_in, 0, state, "state_in"),
+                                     _seq(g_h, want["h"], "g_h"), _flat(g_state_out, 0, state, "g_state_out"), _seq(g_x, want["x"], "g_x"),
+                                     _seq(g_r, want["r"], "g_r"), _seq(g_i, want["i"], "g_i"), _flat(g_lam, 0, desc.C, "g_lambda"),
+                                     _flat(g_state_in, 0, state, "g_state_in"), _ptr(ws), _nbytes(ws), _stream(stream)), "gleam_gatedscan_bwd")
+
+
+def make_muon(lr, momentum=0.95, weight_decay=0.0, nesterov=True, steps=5, eps=1e-7, a=3.4445, b=-4.7750, c=2.0315) -> gleam_muon:
+    """a, b, c: coefficients of a step's polynomial; the defaults carry singular values from 0.004 to 1 to between 0.68 and 1.21 in five steps."""
+    return gleam_muon(float(lr), float(momentum), float(weight_decay), float(eps), float(a), float(b), float(c), int(nesterov), int(steps))
+
+
+def gleam_muon_workspace_bytes(count, rows, cols) -> int:
+    n = C.c_size_t(0)
+    _check(lib().gleam_muon_workspace_bytes(int(count), int(rows), int(cols), C.byref(n)), "gleam_muon_workspace_bytes")
+    return n.value
+
+
+def _matrices(t, like, what: str):
+    """Address of float32 matrices [rows][cols] or [count][rows][cols] on the device, contiguous each, at equal distances as in `like`."""
+    import torch
+    if (t.dtype is not torch.float32 or not t.is_cuda or t.shape != like.shape or t.stride() != like.stride() or t.dim() not in (2, 3) or
+            (t.shape[-1] > 1 and t.stride(-1) != 1) or (t.shape[-2] > 1 and t.stride(-2) != t.shape[-1])):
+        raise ValueError(f"{what}: shape {tuple(t.shape)} with strides {t.stride()} of {t.dtype} on {t.device}: float32 matrices on the GPU, contiguous "
+                         f"each, of the shape and strides of theta, {tuple(like.shape)} and {like.stride()}, expected")
+    return t.data_ptr()
+
+
+def gleam_muon_step(hyper, theta, grad, m, ws, stream=None):
+    """theta, grad, m: [rows][cols], or [count][rows][cols] with matrices any distance apart."""
+    at = [_matrices(t, theta, name) for name, t in (("theta", theta), ("grad", grad), ("m", m))]
+    count, stride = (1, 0) if theta.dim() == 2 else (theta.shape[0], theta.stride(0))
+    _check(lib().gleam_muon_step(C.byref(hyper), count, theta.shape[-2], theta.shape[-1], stride, *at, _ptr(ws), _nbytes(ws), _stream(stream)),
+           "gleam_muon_step")
 
 
 def gleam_profile_begin():

@@ -1,0 +1,582 @@
+// Gated scan along the tokens and its gradients (gfx950):
+//     s = sigmoid(r),  a = exp(-c s),  h <- a h + sqrt(1 - a^2) sigmoid(i) x      c = kappa softplus(lambda), channel by channel
+//
+// Numbers.  Where a > e^-1/2, what is kept of it is -d, d = 1 - a = -expm1(-c s), good to float32 however near to 1 a is: h <- h - (d h - b)
+// forgets at the right rate over thousands of tokens, where a rounded to float32 would be off by 2^-25 / d of it.  Smaller ones are kept as they
+// are, so that little is left of a state to its last bits too; the sign tells which.  sqrt(1 - a^2) = sqrt(d (2 - d)).  Over a
+// stretch of tokens, a state passes as exp(-sum c s) h + (what the stretch adds), with the sum in the exponent.
+//
+// Gradients.  With E_t = a_t G_t what token t hands back to the one before it and G_t = g_t + E_(t+1):
+//     dL/d log a = G (a h_(t-1) - (a^2 / m) u),   m = sqrt(1 - a^2), u = sigmoid(i) x
+// and log a = -c s, so W = (dL/d log a) log a = G a (a u (c s / m) - h_(t-1) c s) has no pole where the gate closes (m -> 0 as sqrt(2 c s)):
+// g_r = W (1 - s), and g_lambda = sigmoid(lambda) / softplus(lambda) sum W.  h_(t-1) is formed again from x, r and i in float32.
+//
+// Layout.  A lane owns V neighbouring channels of a pixel; a wave L tokens of 64 such columns, in registers; the waves of a workgroup
+// stand one behind the other along the tokens and hand their carries over through LDS.  A sequence longer than a workgroup's tokens
+// (a chunk) takes two more launches: what every chunk does to a state, and the carries at the chunks' starts from that, in order.
+#include <hip/hip_runtime.h>
+
+#include "layer_common.h"
+#include "layer_ops.h"
+
+namespace gleam {
+namespace {
+
+constexpr int kScanTokens = 8;     // of a wave
+constexpr int kScanWaves = 16;     // of a workgroup, at most
+
+struct ScanArgs {
+    const void *x, *r, *i, *g;
+    void *out, *out_r, *out_i;            // h; or the gradients of x, r and i
+    gleam_scan_strides sx, sr, si, sh;
+    const float *lambda, *state_in, *state_end;   // state_end: gradient of the last state
+    const int* lengths;
+    float *state_out, *g_state_in;
+    float *log_a, *add_h, *add_e;         // [b][chunk][p][c]: sum of log a, what a chunk adds to h and to E; then h and E that enter it
+    float* part;                          // [b][chunk][p][c]: sums of W
+    long long B, T, P, C, chunks, groups; // groups of 64 columns
+    float kappa;
+    int tokens;                           // of a wave
+};
+
+// e^x for x <= 0: the product with log2 e in two parts.  From -200 on it is 0 in float32.
+__device__ __forceinline__ float exp_neg(float x) {
+    x = x < -200.f ? -200.f : x;
+    const float hi = x * 1.44269502f, lo = __builtin_fmaf(x, 1.44269502f, -hi) + x * 1.92596299e-8f;
+    const float e = __builtin_amdgcn_exp2f(hi);
+    return __builtin_fmaf(e, lo * 0.693147181f, e);
+}
+// e^-y of y >= 0 as it is kept, w: e^-y - 1 (negative, or -0) below 1/2, by the series to y^8 / 8! (what is left out is 1e-8 of it), e^-y above.
+__device__ __forceinline__ float kept_of(float y) {
+    float p = 1.f / 40320.f;
+    p = __builtin_fmaf(p, y, -1.f / 5040.f);
+    p = __builtin_fmaf(p, y, 1.f / 720.f);
+    p = __builtin_fmaf(p, y, -1.f / 120.f);
+    p = __builtin_fmaf(p, y, 1.f / 24.f);
+    p = __builtin_fmaf(p, y, -1.f / 6.f);
+    p = __builtin_fmaf(p, y, 0.5f);
+    p = __builtin_fmaf(p, y, -1.f);
+    return y < 0.5f ? p * y : exp_neg(-y);
+}
+__device__ __forceinline__ bool near_one(float w) { return __float_as_int(w) < 0; }
+__device__ __forceinline__ float a_of(float w) { return near_one(w) ? 1.f + w : w; }
+__device__ __forceinline__ float lost_of(float w) { return near_one(w) ? -w : 1.f - w; }      // 1 - a
+__device__ __forceinline__ float level_of(float w) {                                        // sqrt(1 - a^2)
+    const float d = lost_of(w);
+    return __builtin_amdgcn_sqrtf(d * (2.f - d));
+}
+__device__ __forceinline__ float step_h(float h, float w, float b) { return __builtin_fmaf(w, h, b) + (near_one(w) ? h : 0.f); }   // a h + b
+// sigmoid(v) and 1 - sigmoid(v), both to their last bits
+__device__ __forceinline__ void sigmoids(float v, float& s, float& rest) {
+    const float t = exp_neg(-fabsf(v)), p = __builtin_amdgcn_rcpf(1.f + t), q = t * p;
+    s = v < 0.f ? q : p;
+    rest = v < 0.f ? p : q;
+}
+__device__ __forceinline__ float softplus(float v) { return fmaxf(v, 0.f) + log1pf(expf(-fabsf(v))); }
+
+// The token's gates of one channel: c s, a as it is kept, and b = sqrt(1 - a^2) u.
+struct Gate {
+    float cs, w, b;
+};
+__device__ __forceinline__ Gate gate_of(float x, float r, float i, float c) {
+    float s, si, rest;
+    sigmoids(r, s, rest);
+    sigmoids(i, si, rest);
+    Gate g;
+    g.cs = c * s;
+    g.w = kept_of(g.cs);
+    g.b = level_of(g.w) * (si * x);
+    return g;
+}
+
+// Where a workgroup and a lane are.
+template <int V>
+struct Spot {
+    long long b, k, col;       // sequence, chunk, p * C + first channel
+    long long p;
+    int c, back;               // first channel; 1: the vector's second channel does not exist, and it is read from the one before on
+    bool live;                 // lanes past the last column do the last one's work too, and write nothing
+    int t0, t1, t2;            // tokens of the wave: from t0, those before t1 are there, those before t2 in the array
+    __device__ __forceinline__ bool set(const ScanArgs& a) {
+        const long long id = group_of_grid(), rest = id / a.groups;
+        b = rest / a.chunks;
+        k = rest - b * a.chunks;
+        if (b >= a.B) return false;
+        const long long vecs = (a.C + V - 1) / V, all = vecs * a.P, mine = (id - rest * a.groups) * 64 + (threadIdx.x & 63);
+        live = mine < all;
+        const long long n = live ? mine : all - 1;
+        p = all < 0x7fffffff ? (long long)((unsigned)n / (unsigned)vecs) : n / vecs;
+        const long long v = n - p * vecs;
+        c = (int)(v * V);
+        back = V > 1 && c + V > a.C;
+        col = p * a.C + c;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+        const long long first = (k * waves + wave) * a.tokens;
+        int len = (int)a.T;
+        if (a.lengths) {
+            len = a.lengths[b];
+            len = len < 0 ? 0 : len > a.T ? (int)a.T : len;
+        }
+        const long long end = first + a.tokens;
+        t0 = (int)(first < a.T ? first : a.T);
+        t2 = (int)(end < a.T ? end : a.T);
+        t1 = t2 < len ? t2 : len > t0 ? len : t0;
+        return true;
+    }
+    __device__ __forceinline__ long long at(const gleam_scan_strides& s) const { return b * s.b + p * s.p + c; }
+    template <class T>
+    __device__ __forceinline__ void load(const T* p, float* v) const {   // p: of the first channel
+        load_vec<T, V>(p - back, v);
+        if (V > 1) v[0] = back ? v[V - 1] : v[0];
+    }
+    template <class T>
+    __device__ __forceinline__ void store(T* p, const float* v) const {
+        if (!live) return;
+        if (back) put_f32(p, v[0]);
+        else store_vec<T, V>(p, v);
+    }
+    __device__ __forceinline__ void load_state(const float* p, float* v) const {   // null: zeros
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = p ? p[e && back ? 0 : e] : 0.f;
+    }
+    __device__ __forceinline__ void store_state(float* p, const float* v) const {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            if (live && !(e && back)) p[e] = v[e];
+    }
+    __device__ __forceinline__ long long slot(const ScanArgs& a) const { return (b * a.chunks + k) * a.P * a.C + col; }
+    __device__ __forceinline__ long long state(const ScanArgs& a) const { return b * a.P * a.C + col; }
+};
+
+// A wave's tokens as it reads them.
+template <class T, int V, bool WITH_G>
+struct Tokens {
+    static constexpr int L = kScanTokens;
+    float x[L][V], r[L][V], i[L][V], g[WITH_G ? L : 1][V];
+    __device__ __forceinline__ void load(const ScanArgs& a, const Spot<V>& s) {
+        const T *px = (const T*)a.x + s.at(a.sx) + s.t0 * a.sx.t, *pr = (const T*)a.r + s.at(a.sr) + s.t0 * a.sr.t;
+        const T *pi = (const T*)a.i + s.at(a.si) + s.t0 * a.si.t, *pg = WITH_G ? (const T*)a.g + s.at(a.sh) + s.t0 * a.sh.t : nullptr;
+#pragma unroll
+        for (int j = 0; j < L; ++j)
+            if (s.t0 + j < s.t1) {
+                s.load(px + j * a.sx.t, x[j]);
+                s.load(pr + j * a.sr.t, r[j]);
+                s.load(pi + j * a.si.t, i[j]);
+                if (WITH_G) s.load(pg + j * a.sh.t, g[j]);
+            }
+    }
+};
+
+template <int V>
+__device__ __forceinline__ void rates(const ScanArgs& a, const Spot<V>& s, float* c) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) c[e] = a.kappa * softplus(a.lambda[s.c + (e && s.back ? 0 : e)]);
+}
+
+// What the chunk does to a state: h' = exp(log_a) h + add_h, and backwards E' = exp(log_a) E + add_e.
+template <class T, int V, bool BWD>
+__global__ __launch_bounds__(64 * kScanWaves) void scan_chunk_kernel(ScanArgs a) {
+    constexpr int L = kScanTokens;
+    __shared__ float ends[kScanWaves][BWD ? 3 : 2][V][64];
+    Spot<V> s;
+    if (!s.set(a)) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    float c[V], sum[V], h[V], e_add[V];
+    rates(a, s, c);
+#pragma unroll
+    for (int e = 0; e < V; ++e) sum[e] = h[e] = e_add[e] = 0.f;
+    Tokens<T, V, BWD> tok;
+    tok.load(a, s);
+    float w[L][V];
+#pragma unroll
+    for (int j = 0; j < L; ++j)
+        if (s.t0 + j < s.t1)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const Gate g = gate_of(tok.x[j][e], tok.r[j][e], tok.i[j][e], c[e]);
+                w[j][e] = g.w;
+                sum[e] -= g.cs;
+                h[e] = step_h(h[e], g.w, g.b);
+            }
+    if (BWD)
+#pragma unroll
+        for (int j = L - 1; j >= 0; --j)
+            if (s.t0 + j < s.t1)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    e_add[e] = step_h(tok.g[j][e] + e_add[e], w[j][e], 0.f);
+                }
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        ends[wave][0][e][lane] = sum[e];
+        ends[wave][1][e][lane] = h[e];
+        if (BWD) ends[wave][2][e][lane] = e_add[e];
+    }
+    __syncthreads();
+    if (wave) return;
+    for (int v = 1; v < waves; ++v)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const float more = ends[v][0][e][lane];
+            if (BWD) e_add[e] += exp_neg(sum[e]) * ends[v][2][e][lane];
+            h[e] = __builtin_fmaf(exp_neg(more), h[e], ends[v][1][e][lane]);
+            sum[e] += more;
+        }
+    const long long at = s.slot(a);
+    s.store_state(a.log_a + at, sum);
+    s.store_state(a.add_h + at, h);
+    if (BWD) s.store_state(a.add_e + at, e_add);
+}
+
+// Carries at the chunks' starts (and ends, backwards), in the place of what the chunks add.
+template <bool BWD>
+__global__ __launch_bounds__(256) void scan_carry_kernel(ScanArgs a) {
+    const long long n = group_of_grid() * 256 + threadIdx.x, pc = a.P * a.C;
+    if (n >= a.B * pc) return;
+    const long long b = n / pc, col = n - b * pc, base = b * a.chunks * pc + col;
+    float h = a.state_in ? a.state_in[n] : 0.f;
+    for (long long k = 0; k < a.chunks; ++k) {
+        const long long at = base + k * pc;
+        const float add = a.add_h[at];
+        a.add_h[at] = h;
+        h = __builtin_fmaf(exp_neg(a.log_a[at]), h, add);
+    }
+    if (!BWD) return;
+    float e = a.state_end ? a.state_end[n] : 0.f;
+    for (long long k = a.chunks - 1; k >= 0; --k) {
+        const long long at = base + k * pc;
+        const float add = a.add_e[at];
+        a.add_e[at] = e;
+        e = __builtin_fmaf(exp_neg(a.log_a[at]), e, add);
+    }
+}
+
+template <class T, int V>
+__global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs a) {
+    constexpr int L = kScanTokens;
+    __shared__ float ends[kScanWaves][2][V][64];
+    Spot<V> s;
+    if (!s.set(a)) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    float c[V], sum[V], h[V], w[L][V], b[L][V];
+    rates(a, s, c);
+    Tokens<T, V, false> tok;
+    tok.load(a, s);
+    const float* from = a.chunks > 1 ? a.add_h + s.slot(a) : a.state_in ? a.state_in + s.state(a) : nullptr;
+    float carry[V];
+    s.load_state(from, carry);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        sum[e] = h[e] = 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < L; ++j)
+        if (s.t0 + j < s.t1)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const Gate g = gate_of(tok.x[j][e], tok.r[j][e], tok.i[j][e], c[e]);
+                w[j][e] = g.w;
+                b[j][e] = g.b;
+                sum[e] -= g.cs;
+                h[e] = step_h(h[e], g.w, g.b);
+            }
+    if (waves > 1) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            ends[wave][0][e][lane] = sum[e];
+            ends[wave][1][e][lane] = h[e];
+        }
+        __syncthreads();
+        for (int v = 0; v < wave; ++v)
+#pragma unroll
+            for (int e = 0; e < V; ++e) carry[e] = __builtin_fmaf(exp_neg(ends[v][0][e][lane]), carry[e], ends[v][1][e][lane]);
+    }
+    T* out = (T*)a.out + s.at(a.sh) + s.t0 * a.sh.t;
+#pragma unroll
+    for (int j = 0; j < L; ++j) {
+        if (s.t0 + j < s.t1) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) carry[e] = step_h(carry[e], w[j][e], b[j][e]);
+            s.store(out + j * a.sh.t, carry);
+        } else if (s.t0 + j < s.t2) {
+            const float none[V] = {};
+            s.store(out + j * a.sh.t, none);
+        }
+    }
+    if (a.state_out && s.k == a.chunks - 1 && wave == waves - 1) s.store_state(a.state_out + s.state(a), carry);
+}
+
+template <class T, int V>
+__global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs a) {
+    constexpr int L = kScanTokens;
+    __shared__ float ends[kScanWaves][3][V][64];
+    Spot<V> s;
+    if (!s.set(a)) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    float c[V], sum[V], h[V], e_add[V], w[L][V], b[L][V], w_sum[V];
+    rates(a, s, c);
+    Tokens<T, V, true> tok;
+    tok.load(a, s);
+    const bool split = a.chunks > 1;
+    const float* from = split ? a.add_h + s.slot(a) : a.state_in ? a.state_in + s.state(a) : nullptr;
+    const float* back = split ? a.add_e + s.slot(a) : a.state_end ? a.state_end + s.state(a) : nullptr;
+    float carry[V], ahead[V];
+    s.load_state(from, carry);
+    s.load_state(back, ahead);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        sum[e] = h[e] = e_add[e] = w_sum[e] = 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < L; ++j)
+        if (s.t0 + j < s.t1)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const Gate g = gate_of(tok.x[j][e], tok.r[j][e], tok.i[j][e], c[e]);
+                w[j][e] = g.w;
+                b[j][e] = g.b;
+                sum[e] -= g.cs;
+                h[e] = step_h(h[e], g.w, g.b);
+            }
+    if (waves > 1) {
+#pragma unroll
+        for (int j = L - 1; j >= 0; --j)
+            if (s.t0 + j < s.t1)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    e_add[e] = step_h(tok.g[j][e] + e_add[e], w[j][e], 0.f);
+                }
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            ends[wave][0][e][lane] = sum[e];
+            ends[wave][1][e][lane] = h[e];
+            ends[wave][2][e][lane] = e_add[e];
+        }
+        __syncthreads();
+        for (int v = 0; v < wave; ++v)
+#pragma unroll
+            for (int e = 0; e < V; ++e) carry[e] = __builtin_fmaf(exp_neg(ends[v][0][e][lane]), carry[e], ends[v][1][e][lane]);
+        for (int v = waves - 1; v > wave; --v)
+#pragma unroll
+            for (int e = 0; e < V; ++e) ahead[e] = __builtin_fmaf(exp_neg(ends[v][0][e][lane]), ahead[e], ends[v][2][e][lane]);
+    }
+    // h before each token, in the place of b
+#pragma unroll
+    for (int j = 0; j < L; ++j)
+        if (s.t0 + j < s.t1)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float next = step_h(carry[e], w[j][e], b[j][e]);
+                b[j][e] = carry[e];
+                carry[e] = next;
+            }
+    T *gx = (T*)a.out + s.at(a.sx) + s.t0 * a.sx.t, *gr = (T*)a.out_r + s.at(a.sr) + s.t0 * a.sr.t, *gi = (T*)a.out_i + s.at(a.si) + s.t0 * a.si.t;
+#pragma unroll
+    for (int j = L - 1; j >= 0; --j) {
+        float ox[V] = {}, orr[V] = {}, oi[V] = {};
+        if (s.t0 + j < s.t1) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                float sr, rest, si, rest_i;
+                sigmoids(tok.r[j][e], sr, rest);
+                sigmoids(tok.i[j][e], si, rest_i);
+                const float G = tok.g[j][e] + ahead[e], wj = w[j][e], x = tok.x[j][e], cs = c[e] * sr;
+                const float m = level_of(wj), gu = G * m, al = a_of(wj);
+                const float q = m > 0.f ? cs * __builtin_amdgcn_rcpf(m) : 0.f;
+                const float W = G * al * (al * (si * x) * q - b[j][e] * cs);
+                ox[e] = gu * si;
+                oi[e] = gu * x * (si * rest_i);
+                orr[e] = W * rest;
+                w_sum[e] += W;
+                ahead[e] = step_h(G, wj, 0.f);
+            }
+        }
+        if (s.t0 + j < s.t2) {
+            s.store(gx + j * a.sx.t, ox);
+            s.store(gr + j * a.sr.t, orr);
+            s.store(gi + j * a.si.t, oi);
+        }
+    }
+    if (a.g_state_in && s.k == 0 && wave == 0) s.store_state(a.g_state_in + s.state(a), ahead);
+    if (waves > 1) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < V; ++e) ends[wave][0][e][lane] = w_sum[e];
+        __syncthreads();
+        if (wave) return;
+        for (int v = 1; v < waves; ++v)
+#pragma unroll
+            for (int e = 0; e < V; ++e) w_sum[e] += ends[v][0][e][lane];
+    }
+    s.store_state(a.part + s.slot(a), w_sum);
+}
+
+// Sums over rows of C columns: 64 columns and a slab of rows a workgroup.  lambda not null: the last sum, out = g_lambda.
+__global__ __launch_bounds__(256) void scan_sums_kernel(const float* part, long long rows, long long C, long long slab, const float* lambda, float* out) {
+    __shared__ float red[4][64];
+    const long long col_groups = (C + 63) / 64, id = group_of_grid(), s = id / col_groups;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long c = (id - s * col_groups) * 64 + lane, end = (s + 1) * slab < rows ? (s + 1) * slab : rows;
+    float v = 0.f;
+    if (c < C)
+        for (long long r = s * slab + wave; r < end; r += 4) v += part[r * C + c];
+    red[wave][lane] = v;
+    __syncthreads();
+    if (wave || c >= C || s * slab >= rows) return;
+    v = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
+    if (lambda) {
+        // d softplus / softplus: goes to 1 where both vanish
+        const float l = lambda[c];
+        v *= l < -20.f ? 1.f : 1.f / ((1.f + expf(-l)) * softplus(l));
+    }
+    out[s * C + c] = v;
+}
+
+struct ScanPlan {
+    int waves, tokens, vec;
+    long long chunks, groups, slots;     // slots: states of all chunks
+    long long rows, slabs, slab;         // of the sums of W
+};
+ScanPlan plan_of(const gleam_gatedscan_desc& d) {
+    ScanPlan p;
+    p.waves = 1;
+    while (p.waves < kScanWaves && p.waves * kScanTokens < d.T) p.waves *= 2;
+    p.chunks = (d.T + p.waves * kScanTokens - 1) / (p.waves * kScanTokens);
+    const long long per = (d.T + p.chunks - 1) / p.chunks;
+    p.tokens = (int)((per + p.waves - 1) / p.waves);
+    p.vec = d.dtype && d.C > 1 ? 2 : 1;
+    p.groups = ((d.C + p.vec - 1) / p.vec * d.P + 63) / 64;
+    p.slots = d.B * p.chunks * d.P * d.C;
+    p.rows = d.B * p.chunks * d.P;
+    const long long col_groups = (d.C + 63) / 64;
+    p.slabs = p.rows / 64 < 1 ? 1 : p.rows / 64;
+    const long long most = col_groups < 1024 ? 1024 / col_groups : 1;
+    if (p.slabs > most) p.slabs = most;
+    p.slab = (p.rows + p.slabs - 1) / p.slabs;
+    return p;
+}
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+ScanArgs args_of(const gleam_gatedscan_desc& d, const ScanPlan& p, const void* x, const void* r, const void* i, const float* lambda,
+                 const int* lengths, const float* state_in) {
+    ScanArgs a{};
+    a.x = x;
+    a.r = r;
+    a.i = i;
+    a.sx = d.x;
+    a.sr = d.r;
+    a.si = d.i;
+    a.sh = d.h;
+    a.lambda = lambda;
+    a.lengths = lengths;
+    a.state_in = state_in;
+    a.B = d.B;
+    a.T = d.T;
+    a.P = d.P;
+    a.C = d.C;
+    a.chunks = p.chunks;
+    a.groups = p.groups;
+    a.kappa = d.kappa;
+    a.tokens = p.tokens;
+    return a;
+}
+
+// Carries of a split sequence.
+template <bool BWD>
+hipError_t find_carries(const ScanArgs& a, const ScanPlan& p, int dtype, hipStream_t st) {
+    if (p.chunks == 1) return hipSuccess;
+    {
+        const double size = (double)a.B * a.T * a.P * a.C;
+        KernelScope ks(BWD ? "scan_chunk_bwd" : "scan_chunk", (BWD ? 30.0 : 25.0) * size, (BWD ? 4.0 : 3.0) * (dtype ? 2 : 4) * size, st);
+        const dim3 grid = grid_of(a.B * p.chunks * p.groups), block(64 * p.waves);
+        if (!dtype) hipLaunchKernelGGL((scan_chunk_kernel<float, 1, BWD>), grid, block, 0, st, a);
+        else if (p.vec == 2) hipLaunchKernelGGL((scan_chunk_kernel<unsigned short, 2, BWD>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((scan_chunk_kernel<unsigned short, 1, BWD>), grid, block, 0, st, a);
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    KernelScope ks("scan_carry", 0.0, (BWD ? 20.0 : 12.0) * p.slots, st);
+    hipLaunchKernelGGL(scan_carry_kernel<BWD>, grid_of((a.B * a.P * a.C + 255) / 256), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t gatedscan_fwd_ws_bytes(const gleam_gatedscan_desc& d) {
+    const ScanPlan p = plan_of(d);
+    return p.chunks > 1 ? 2 * up256(p.slots * sizeof(float)) : 0;
+}
+
+hipError_t gatedscan_forward(const gleam_gatedscan_desc& d, const void* x, const void* r, const void* i, const float* lambda,
+                             const int* lengths, const float* state_in, void* h, float* state_out, void* ws, hipStream_t st) {
+    const ScanPlan p = plan_of(d);
+    ScanArgs a = args_of(d, p, x, r, i, lambda, lengths, state_in);
+    a.out = h;
+    a.state_out = state_out;
+    const size_t each = up256(p.slots * sizeof(float));
+    if (p.chunks > 1) {
+        a.log_a = (float*)ws;
+        a.add_h = (float*)((char*)ws + each);
+    }
+    const hipError_t e = find_carries<false>(a, p, d.dtype, st);
+    if (e != hipSuccess) return e;
+    const double size = (double)d.B * d.T * d.P * d.C;
+    KernelScope ks("scan_fwd", 25.0 * size, 4.0 * (d.dtype ? 2 : 4) * size, st);
+    const dim3 grid = grid_of(d.B * p.chunks * p.groups), block(64 * p.waves);
+    if (!d.dtype) hipLaunchKernelGGL((scan_fwd_kernel<float, 1>), grid, block, 0, st, a);
+    else if (p.vec == 2) hipLaunchKernelGGL((scan_fwd_kernel<unsigned short, 2>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((scan_fwd_kernel<unsigned short, 1>), grid, block, 0, st, a);
+    return hipGetLastError();
+}
+
+size_t gatedscan_bwd_ws_bytes(const gleam_gatedscan_desc& d) {
+    const ScanPlan p = plan_of(d);
+    return (p.chunks > 1 ? 4 : 1) * up256(p.slots * sizeof(float)) + up256(p.slabs * d.C * sizeof(float));
+}
+
+hipError_t gatedscan_backward(const gleam_gatedscan_desc& d, const void* x, const void* r, const void* i, const float* lambda,
+                              const int* lengths, const float* state_in, const void* g_h, const float* g_state_out, void* g_x, void* g_r,
+                              void* g_i, float* g_lambda, float* g_state_in, void* ws, hipStream_t st) {
+    const ScanPlan p = plan_of(d);
+    ScanArgs a = args_of(d, p, x, r, i, lambda, lengths, state_in);
+    a.g = g_h;
+    a.state_end = g_state_out;
+    a.out = g_x;
+    a.out_r = g_r;
+    a.out_i = g_i;
+    a.g_state_in = g_state_in;
+    const size_t each = up256(p.slots * sizeof(float));
+    char* at = (char*)ws;
+    a.part = (float*)at;
+    float* sums = (float*)(at + each);
+    at += each + up256(p.slabs * d.C * sizeof(float));
+    if (p.chunks > 1) {
+        a.log_a = (float*)at;
+        a.add_h = (float*)(at + each);
+        a.add_e = (float*)(at + 2 * each);
+    }
+    hipError_t e = find_carries<true>(a, p, d.dtype, st);
+    if (e != hipSuccess) return e;
+    {
+        const double size = (double)d.B * d.T * d.P * d.C;
+        KernelScope ks("scan_bwd", 50.0 * size, 7.0 * (d.dtype ? 2 : 4) * size, st);
+        const dim3 grid = grid_of(d.B * p.chunks * p.groups), block(64 * p.waves);
+        if (!d.dtype) hipLaunchKernelGGL((scan_bwd_kernel<float, 1>), grid, block, 0, st, a);
+        else if (p.vec == 2) hipLaunchKernelGGL((scan_bwd_kernel<unsigned short, 2>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((scan_bwd_kernel<unsigned short, 1>), grid, block, 0, st, a);
+    }
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const long long col_groups = (d.C + 63) / 64;
+    KernelScope ks("scan_sums", 0.0, 4.0 * p.slots, st);
+    if (p.slabs > 1) {
+        hipLaunchKernelGGL(scan_sums_kernel, grid_of(p.slabs * col_groups), dim3(256), 0, st, a.part, p.rows, (long long)d.C, p.slab, (const float*)nullptr, sums);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(scan_sums_kernel, grid_of(col_groups), dim3(256), 0, st, p.slabs > 1 ? sums : a.part, p.slabs > 1 ? p.slabs : p.rows, (long long)d.C,
+                       p.slabs > 1 ? p.slabs : p.rows, lambda, g_lambda);
+    return hipGetLastError();
+}
+
+}  // namespace gleam

@@ -1,5 +1,5 @@
-// C ABI of the sequence-layer operators: host-side validation, then the kernels of norm.hip, dropout.hip and linattn.hip on the
-// caller's stream.
+// C ABI of the sequence-layer operators: host-side validation, then the kernels of norm.hip, dropout.hip, linattn.hip, qknorm.hip,
+// gatedscan.hip and muon.hip on the caller's stream.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -59,11 +59,11 @@ DropoutArgs dropout_args(const gleam_dropout_desc& d, const uint64_t* step) {
     return a;
 }
 
-// An array of a linear attention call: strides that reach no further than they may, and that keep elements apart where it is written.
-int check_strides(const gleam_linattn_desc& d, const gleam_seq_strides& s, int heads, int width, bool written) {
+// An array [B][T][P][heads][width]: strides that reach no further than they may, and that keep elements apart where it is written.
+int check_strides(long long B, long long T, long long P, const gleam_seq_strides& s, long long heads, long long width, bool written) {
     struct Axis {
         long long n, stride;
-    } axis[4] = {{d.B, s.b}, {d.T, s.t}, {d.P, s.p}, {heads, s.h}};
+    } axis[4] = {{B, s.b}, {T, s.t}, {P, s.p}, {heads, s.h}};
     long long reach = width;
     for (const Axis& x : axis) {
         if (x.stride < 0 || x.stride > kMostElements) return GLEAM_E_DIMS;
@@ -93,11 +93,61 @@ int check_linattn(const gleam_linattn_desc* d, bool gradients) {
     const long long problems = product(product(d->B, d->P), d->heads);
     if (problems < 0 || problems > kMostProblems || product(problems, d->T) < 0) return GLEAM_E_DIMS;
     if (product(problems * d->T, std::max(d->dk, d->dv)) < 0 || product(problems, d->dk * d->dv) < 0) return GLEAM_E_DIMS;
-    int rc = check_strides(*d, d->q, d->q_heads, d->dk, gradients);
-    if (!rc) rc = check_strides(*d, d->k, d->k_heads, d->dk, gradients);
-    if (!rc) rc = check_strides(*d, d->v, d->v_heads, d->dv, gradients);
-    if (!rc) rc = check_strides(*d, d->o, d->heads, d->dv, !gradients);
+    int rc = check_strides(d->B, d->T, d->P, d->q, d->q_heads, d->dk, gradients);
+    if (!rc) rc = check_strides(d->B, d->T, d->P, d->k, d->k_heads, d->dk, gradients);
+    if (!rc) rc = check_strides(d->B, d->T, d->P, d->v, d->v_heads, d->dv, gradients);
+    if (!rc) rc = check_strides(d->B, d->T, d->P, d->o, d->heads, d->dv, !gradients);
     return rc;
+}
+
+bool same(const gleam_seq_strides& a, const gleam_seq_strides& b) { return a.b == b.b && a.t == b.t && a.p == b.p && a.h == b.h; }
+
+int check_qknorm(const gleam_qknorm_desc* d, bool gradients) {
+    if (!d) return GLEAM_E_NULL;
+    if (d->dtype != 0 && d->dtype != 1) return GLEAM_E_DESC;
+    if ((d->pairs != 0 && d->pairs != 1) || (d->each != 0 && d->each != 1)) return GLEAM_E_DESC;
+    if (!(d->eps > 0.f) || !std::isfinite(d->eps)) return GLEAM_E_DESC;
+    if (d->d < 1 || d->d > 256 || d->rot < 0 || d->rot > d->d || d->rot % 2) return GLEAM_E_DIMS;
+    if (d->q_heads < 1 || d->k_heads < 0 || d->B < 1 || d->T < 1 || d->P < 1 || d->T > (1 << 30)) return GLEAM_E_DIMS;
+    const long long heads = (long long)d->q_heads + d->k_heads, tokens = product(d->B, d->T);
+    if (product(d->P, heads) < 0 || d->P * heads > 0x7fffffffLL) return GLEAM_E_DIMS;
+    if (tokens < 0 || product(tokens, d->P * heads) < 0 || product(tokens * d->P * heads, d->d) < 0) return GLEAM_E_DIMS;
+    int rc = check_strides(d->B, d->T, d->P, d->q, d->q_heads, d->d, gradients);
+    if (!rc) rc = check_strides(d->B, d->T, d->P, d->q_out, d->q_heads, d->d, !gradients);
+    if (!rc && d->k_heads) rc = check_strides(d->B, d->T, d->P, d->k, d->k_heads, d->d, gradients);
+    if (!rc && d->k_heads) rc = check_strides(d->B, d->T, d->P, d->k_out, d->k_heads, d->d, !gradients);
+    return rc;
+}
+
+int check_gatedscan(const gleam_gatedscan_desc* d, bool gradients) {
+    if (!d) return GLEAM_E_NULL;
+    if (d->dtype != 0 && d->dtype != 1) return GLEAM_E_DESC;
+    if (!(d->kappa >= 0.f) || !std::isfinite(d->kappa)) return GLEAM_E_DESC;
+    if (d->B < 1 || d->T < 1 || d->P < 1 || d->C < 1 || d->T > (1 << 30) || d->C > 0x7fffffffLL) return GLEAM_E_DIMS;
+    const long long states = product(product(d->B, d->P), d->C);
+    if (states < 0 || product(states, d->T) < 0) return GLEAM_E_DIMS;
+    auto check = [&](const gleam_scan_strides& s, bool written) {
+        return check_strides(d->B, d->T, d->P, gleam_seq_strides{s.b, s.t, s.p, d->C}, 1, d->C, written);
+    };
+    int rc = check(d->x, gradients);
+    if (!rc) rc = check(d->r, gradients);
+    if (!rc) rc = check(d->i, gradients);
+    if (!rc) rc = check(d->h, !gradients);
+    return rc;
+}
+
+int check_muon_sizes(long long count, long long rows, long long cols) {
+    if (count < 1 || rows < 1 || cols < 1 || rows > 65536 || cols > 65536) return GLEAM_E_DIMS;
+    return product(product(rows, cols), count) < 0 ? GLEAM_E_DIMS : GLEAM_OK;
+}
+
+int check_muon(const gleam_muon* p) {
+    if (!p) return GLEAM_E_NULL;
+    for (float v : {p->lr, p->momentum, p->weight_decay, p->eps, p->a, p->b, p->c})
+        if (!std::isfinite(v)) return GLEAM_E_DESC;
+    if (!(p->eps > 0.f) || p->momentum < 0.f || p->momentum >= 1.f) return GLEAM_E_DESC;
+    if (p->steps < 1 || p->steps > 100 || (p->nesterov != 0 && p->nesterov != 1)) return GLEAM_E_DESC;
+    return GLEAM_OK;
 }
 
 int check_ws(const void* ws, size_t ws_bytes, size_t need) {
@@ -200,6 +250,101 @@ int gleam_linattn_bwd(const gleam_linattn_desc* desc, const void* q, const void*
     if (rc) return rc;
     return status_of(linattn_backward(*desc, q, k, v, log_decay, lengths, state_in, g_o, g_state_out, g_q, g_k, g_v, g_state_in, ws,
                                       (hipStream_t)stream));
+}
+
+int gleam_qknorm_fwd(const gleam_qknorm_desc* desc, const void* q, const void* k, const float* gamma_q, const float* gamma_k,
+                     const float* freq, const int32_t* positions, const int32_t* lengths, void* q_out, void* k_out, void* stream) {
+    const int rc = check_qknorm(desc, false);
+    if (rc) return rc;
+    const bool with_k = desc->k_heads > 0;
+    if (!q || !q_out || (with_k && (!k || !k_out)) || (desc->rot && !freq)) return GLEAM_E_NULL;
+    if (q_out == q && !same(desc->q, desc->q_out)) return GLEAM_E_DIMS;
+    if (with_k && ((k_out == k && !same(desc->k, desc->k_out)) || q_out == k || k_out == q || q_out == k_out)) return GLEAM_E_DIMS;
+    return status_of(qknorm_forward(*desc, q, k, gamma_q, gamma_k, freq, positions, lengths, q_out, k_out, (hipStream_t)stream));
+}
+
+int gleam_qknorm_workspace_bytes(const gleam_qknorm_desc* desc, size_t* ws_bytes) {
+    if (!ws_bytes) return GLEAM_E_NULL;
+    const int rc = check_qknorm(desc, true);
+    if (rc) return rc;
+    *ws_bytes = qknorm_ws_bytes(*desc);
+    return GLEAM_OK;
+}
+
+int gleam_qknorm_bwd(const gleam_qknorm_desc* desc, const void* q, const void* k, const float* gamma_q, const float* gamma_k,
+                     const float* freq, const int32_t* positions, const int32_t* lengths, const void* g_q_out, const void* g_k_out,
+                     void* g_q, void* g_k, float* g_gamma_q, float* g_gamma_k, void* ws, size_t ws_bytes, void* stream) {
+    int rc = check_qknorm(desc, true);
+    if (rc) return rc;
+    const bool with_k = desc->k_heads > 0;
+    if (!q || !g_q_out || !g_q || (with_k && (!k || !g_k_out || !g_k)) || (desc->rot && !freq)) return GLEAM_E_NULL;
+    if (g_q == q || (g_q == g_q_out && !same(desc->q, desc->q_out))) return GLEAM_E_DIMS;
+    if (with_k && (g_k == k || g_k == q || g_q == k || g_q == g_k || g_q == g_k_out || g_k == g_q_out || (g_k == g_k_out && !same(desc->k, desc->k_out))))
+        return GLEAM_E_DIMS;
+    if (!with_k) g_gamma_k = nullptr;
+    if (g_gamma_q && g_gamma_q == g_gamma_k) return GLEAM_E_DIMS;
+    rc = check_ws(ws, ws_bytes, g_gamma_q || g_gamma_k ? qknorm_ws_bytes(*desc) : 0);
+    if (rc) return rc;
+    return status_of(qknorm_backward(*desc, q, k, gamma_q, gamma_k, freq, positions, lengths, g_q_out, g_k_out, g_q, g_k, g_gamma_q,
+                                     g_gamma_k, ws, (hipStream_t)stream));
+}
+
+int gleam_gatedscan_workspace_bytes(const gleam_gatedscan_desc* desc, size_t* fwd_bytes, size_t* bwd_bytes) {
+    if (!fwd_bytes || !bwd_bytes) return GLEAM_E_NULL;
+    const int rc = check_gatedscan(desc, false);
+    if (rc) return rc;
+    *fwd_bytes = gatedscan_fwd_ws_bytes(*desc);
+    *bwd_bytes = gatedscan_bwd_ws_bytes(*desc);
+    return GLEAM_OK;
+}
+
+int gleam_gatedscan_fwd(const gleam_gatedscan_desc* desc, const void* x, const void* r, const void* i, const float* lambda,
+                        const int32_t* lengths, const float* state_in, void* h, float* state_out, void* ws, size_t ws_bytes, void* stream) {
+    int rc = check_gatedscan(desc, false);
+    if (rc) return rc;
+    if (!x || !r || !i || !lambda || !h) return GLEAM_E_NULL;
+    if (h == x || h == r || h == i) return GLEAM_E_DIMS;
+    rc = check_ws(ws, ws_bytes, gatedscan_fwd_ws_bytes(*desc));
+    if (rc) return rc;
+    return status_of(gatedscan_forward(*desc, x, r, i, lambda, lengths, state_in, h, state_out, ws, (hipStream_t)stream));
+}
+
+int gleam_gatedscan_bwd(const gleam_gatedscan_desc* desc, const void* x, const void* r, const void* i, const float* lambda,
+                        const int32_t* lengths, const float* state_in, const void* g_h, const float* g_state_out, void* g_x, void* g_r,
+                        void* g_i, float* g_lambda, float* g_state_in, void* ws, size_t ws_bytes, void* stream) {
+    int rc = check_gatedscan(desc, true);
+    if (rc) return rc;
+    if (!x || !r || !i || !lambda || !g_h || !g_x || !g_r || !g_i || !g_lambda) return GLEAM_E_NULL;
+    for (const void* g : {g_x, g_r, g_i})
+        for (const void* a : {x, r, i, g_h})
+            if (g == a) return GLEAM_E_DIMS;
+    if (g_x == g_r || g_x == g_i || g_r == g_i || g_lambda == lambda) return GLEAM_E_DIMS;
+    if (g_state_in && (g_state_in == g_state_out || g_state_in == state_in)) return GLEAM_E_DIMS;
+    rc = check_ws(ws, ws_bytes, gatedscan_bwd_ws_bytes(*desc));
+    if (rc) return rc;
+    return status_of(gatedscan_backward(*desc, x, r, i, lambda, lengths, state_in, g_h, g_state_out, g_x, g_r, g_i, g_lambda, g_state_in,
+                                        ws, (hipStream_t)stream));
+}
+
+int gleam_muon_workspace_bytes(int64_t count, int64_t rows, int64_t cols, size_t* ws_bytes) {
+    if (!ws_bytes) return GLEAM_E_NULL;
+    const int rc = check_muon_sizes(count, rows, cols);
+    if (rc) return rc;
+    *ws_bytes = muon_ws_bytes(count, rows, cols);
+    return GLEAM_OK;
+}
+
+int gleam_muon_step(const gleam_muon* hyper, int64_t count, int64_t rows, int64_t cols, int64_t stride, float* theta, const float* grad,
+                    float* m, void* ws, size_t ws_bytes, void* stream) {
+    int rc = check_muon(hyper);
+    if (!rc) rc = check_muon_sizes(count, rows, cols);
+    if (rc) return rc;
+    if (stride < 0 || (count > 1 && (stride < rows * cols || product(count, stride) < 0))) return GLEAM_E_DIMS;
+    if (!theta || !grad || !m) return GLEAM_E_NULL;
+    if (theta == grad || theta == m || grad == m) return GLEAM_E_DIMS;
+    rc = check_ws(ws, ws_bytes, muon_ws_bytes(count, rows, cols));
+    if (rc) return rc;
+    return status_of(muon_update(*hyper, count, rows, cols, stride, theta, grad, m, ws, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -18,6 +18,14 @@ inline dim3 grid_of(long long groups) {
 }
 __device__ __forceinline__ long long group_of_grid() { return (long long)blockIdx.y * kGridX + blockIdx.x; }
 
+// Another lane's value, by a DPP pattern.
+template <int PATTERN>
+__device__ __forceinline__ float dpp(float v) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), PATTERN, 0xf, 0xf, false));
+}
+template <class V>
+__device__ __forceinline__ float sum_of_pair(V r) { return __uint_as_float(r[0]) + __uint_as_float(r[1]); }
+
 // N elements of type T; 16 bytes, or two times 16 for eight float32.  Global addresses need the alignment of an element only: the
 // memory unit takes 16 bytes from any address (an access that crosses a cache line costs two).
 template <class T, int N>
@@ -44,5 +52,27 @@ struct Pack {
     }
 };
 
+// N elements as float32: a word or more at once, a single bfloat16 by itself.
+template <class T, int N>
+__device__ __forceinline__ void load_vec(const T* p, float* v) {
+    if constexpr (N * sizeof(T) < 4) {
+        v[0] = to_f32(*p);
+    } else {
+        Pack<T, N> k;
+        k.load(p);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = k.get(i);
+    }
+}
+template <class T, int N>
+__device__ __forceinline__ void store_vec(T* p, const float* v) {
+    if constexpr (N * sizeof(T) < 4) {
+        put_f32(p, v[0]);
+    } else {
+        Pack<T, N> k;
+        k.set(v);
+        k.store(p);
+    }
+}
 }  // namespace
 }  // namespace gleam

@@ -1,4 +1,5 @@
-// Internal declarations of the sequence-layer operators: layer norm, dropout, linear attention with a decay for each head.
+// Internal declarations of the sequence-layer operators: layer norm, dropout, linear attention with a decay for each head, norm and
+// rotation of queries and keys, the gated scan, and the orthogonalised update of weight matrices.
 #pragma once
 #include "internal.h"
 
@@ -62,5 +63,27 @@ hipError_t linattn_forward(const gleam_linattn_desc& d, const void* q, const voi
 hipError_t linattn_backward(const gleam_linattn_desc& d, const void* q, const void* k, const void* v, const float* log_decay,
                             const int* lengths, const float* state_in, const void* g_o, const float* g_state_out, void* g_q, void* g_k,
                             void* g_v, float* g_state_in, void* ws, hipStream_t st);
+
+// ------------------------------------------------------------------ norm and rotation of queries and keys (qknorm.hip)
+hipError_t qknorm_forward(const gleam_qknorm_desc& d, const void* q, const void* k, const float* gamma_q, const float* gamma_k,
+                          const float* freq, const int* positions, const int* lengths, void* q_out, void* k_out, hipStream_t st);
+size_t qknorm_ws_bytes(const gleam_qknorm_desc& d);
+hipError_t qknorm_backward(const gleam_qknorm_desc& d, const void* q, const void* k, const float* gamma_q, const float* gamma_k,
+                           const float* freq, const int* positions, const int* lengths, const void* g_q_out, const void* g_k_out, void* g_q,
+                           void* g_k, float* g_gamma_q, float* g_gamma_k, void* ws, hipStream_t st);
+
+// ------------------------------------------------------------------ gated scan (gatedscan.hip)
+size_t gatedscan_fwd_ws_bytes(const gleam_gatedscan_desc& d);
+size_t gatedscan_bwd_ws_bytes(const gleam_gatedscan_desc& d);
+hipError_t gatedscan_forward(const gleam_gatedscan_desc& d, const void* x, const void* r, const void* i, const float* lambda,
+                             const int* lengths, const float* state_in, void* h, float* state_out, void* ws, hipStream_t st);
+hipError_t gatedscan_backward(const gleam_gatedscan_desc& d, const void* x, const void* r, const void* i, const float* lambda,
+                              const int* lengths, const float* state_in, const void* g_h, const float* g_state_out, void* g_x, void* g_r,
+                              void* g_i, float* g_lambda, float* g_state_in, void* ws, hipStream_t st);
+
+// ------------------------------------------------------------------ orthogonalised update (muon.hip)
+size_t muon_ws_bytes(long long count, long long rows, long long cols);
+hipError_t muon_update(const gleam_muon& p, long long count, long long rows, long long cols, long long stride, float* theta,
+                       const float* grad, float* m, void* ws, hipStream_t st);
 
 }  // namespace gleam

@@ -29,14 +29,6 @@ constexpr int vec_of() { return 16 / (int)sizeof(T); }
 template <int LANES>
 constexpr int threads_of() { return LANES > 64 ? LANES : kNormThreads; }
 
-// Another lane's value, by a DPP pattern.
-template <int PATTERN>
-__device__ __forceinline__ float dpp(float v) {
-    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), PATTERN, 0xf, 0xf, false));
-}
-template <class V>
-__device__ __forceinline__ float sum_of_pair(V r) { return __uint_as_float(r[0]) + __uint_as_float(r[1]); }
-
 // Sums over a team of LANES lanes, the same values in all of them.  A team wider than a wave is the workgroup; `red` is then LDS for
 // N floats a wave, and the barrier in front makes its last use over.
 template <int LANES, int N>
