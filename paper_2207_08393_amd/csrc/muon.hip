@@ -30,6 +30,8 @@ struct MuonArgs {
     int rows, cols, tall;                  // tall: X is the transpose of u
     int mb, nb;                            // blocks of 32 of the short and of the long side
     int parts;                             // partial sums of |u|^2
+    float* part;                           // of products split along their sum
+    int splits;
     int nesterov, last;
     float lr_scale, decay, momentum, eps, ca, cb, cc;
 };
@@ -105,27 +107,113 @@ __global__ __launch_bounds__(128) void muon_split_kernel(MuonArgs a) {
 
 enum MuonProduct { kGram, kSquare, kApply };
 
+// What becomes of a 32 x 32 block (bi, bj) of a product, R x Cb blocks in all; `tile`: 32 x 33 floats of LDS of this wave alone.  Lane:
+// column lane % 32, rows 8 q + 4 (lane / 32) + 0..3 in registers 4 q + 0..3.
+template <int MODE>
+__device__ __forceinline__ void put_block(const MuonArgs& a, long long matrix, int bi, int bj, const floatx16& acc, float* tile) {
+    const int lane = threadIdx.x & 63, col = lane & 31, up = lane >> 5, R = a.mb, Cb = MODE == kApply ? a.nb : a.mb;
+    char* across = MODE == kGram ? a.a : MODE == kSquare ? a.b : a.xt_out;   // [column][row] parts
+    char* along = MODE == kGram ? a.a : MODE == kSquare ? a.b : a.x;         // [row][column] parts
+    const bool both = MODE == kApply || bi != bj;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = acc[4 * q + e];
+        const int row0 = 8 * q + 4 * up;
+        const long long to = (q & 1) * 512 + col * 16 + up * 8;
+        if (MODE == kSquare) {
+            const char* from = block_at(a.a, matrix, R, R, bj, 2 * bi + (q >> 1), 0) + to;   // A is symmetric
+            uint2 w[3];
+#pragma unroll
+            for (int p = 0; p < 3; ++p) w[p] = *(const uint2*)(from + p * kBlockBytes);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float av = 0.f;
+#pragma unroll
+                for (int p = 2; p >= 0; --p) {
+                    const unsigned u = e < 2 ? w[p].x : w[p].y;
+                    av += __uint_as_float(e & 1 ? u & 0xffff0000u : u << 16);
+                }
+                v[e] = a.cb * av + a.cc * v[e] + (bi == bj && row0 + e == col ? a.ca : 0.f);
+            }
+        }
+        if (MODE == kApply && a.last) {
+            const int r = 32 * bi + row0, c = 32 * bj + col;
+            float* th = a.theta + matrix * a.stride;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int ur = a.tall ? c : r + e, uc = a.tall ? r + e : c;
+                if (ur < a.rows && uc < a.cols) {
+                    float* p = th + (long long)ur * a.cols + uc;
+                    *p = a.decay * *p - a.lr_scale * v[e];
+                }
+            }
+            continue;
+        }
+        SplitWords s;
+        split_pair(v[0], v[1], 0, s);
+        split_pair(v[2], v[3], 1, s);
+        char* t = block_at(across, matrix, Cb, R, bj, 2 * bi + (q >> 1), 0) + to;
+#pragma unroll
+        for (int p = 0; p < 3; ++p) *(uint2*)(t + p * kBlockBytes) = make_uint2(s.w[p][0], s.w[p][1]);
+        if (both)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) tile[(row0 + e) * 33 + col] = v[e];
+    }
+    if (!both || (MODE == kApply && a.last)) return;
+    // the other way round: a row and eight of its columns a lane
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = tile[col * 33 + 8 * (up + 2 * g) + e];
+        store_parts8(block_at(along, matrix, R, Cb, bi, 2 * bj + g, 0) + up * 512 + col * 16, v);
+    }
+    __builtin_amdgcn_wave_barrier();
+}
+
 // One of the three products of a step, rows of the left operand against rows of the right one:
 //   kGram  A = X X^T;   kSquare  B = a I + b A + c A A;   kApply  X <- B X, or at the last step the weights' update.
-// A workgroup computes 2 WT x 2 WT blocks of 32 x 32, its four waves WT x WT each.
+// A workgroup computes 2 WT x 2 WT blocks of 32 x 32, its four waves WT x WT each, over one of `splits` parts of the sum.  16 columns of both
+// operands are in LDS (24 KB for WT = 2) while the next 16 are written and the ones after those are on their way in registers.
+constexpr int kTileFloats = 32 * 33;
+
 template <int MODE, int WT>
-__global__ __launch_bounds__(256) void muon_product_kernel(MuonArgs a) {
+__global__ __launch_bounds__(256, 2) void muon_product_kernel(MuonArgs a) {
+    constexpr int kRows = 2 * WT, kStage = 2 * kRows * 3 * kBlockBytes, kLoads = kStage / (256 * 16);   // row blocks of an operand in a tile
+    constexpr int kLds = 2 * kStage > 4 * kTileFloats * 4 ? 2 * kStage : 4 * kTileFloats * 4;
+    __shared__ __attribute__((aligned(16))) char lds[kLds];
     const int R = a.mb, Cb = MODE == kApply ? a.nb : a.mb, K = MODE == kGram ? a.nb : a.mb;   // blocks of the result's sides and of the sum
-    const int tr = (R + 2 * WT - 1) / (2 * WT), tc = (Cb + 2 * WT - 1) / (2 * WT);
-    const long long id = group_of_grid(), matrix = id / ((long long)tr * tc);
+    const int tr = (R + kRows - 1) / kRows, tc = (Cb + kRows - 1) / kRows;
+    const long long id = group_of_grid(), all = (long long)tr * tc * a.splits, matrix = id / all;
     if (matrix >= a.count) return;
-    const int tile = (int)(id - matrix * tr * tc), ti = tile / tc, tj = tile - ti * tc;
+    const int rest = (int)(id - matrix * all), split = rest % a.splits, tile = rest / a.splits, ti = tile / tc, tj = tile - ti * tc;
     if (MODE != kApply && ti > tj) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int bi0 = ti * 2 * WT + (wave >> 1) * WT, bj0 = tj * 2 * WT + (wave & 1) * WT;
-    char* left = MODE == kGram ? a.x : MODE == kSquare ? a.a : a.b;
-    char* right = MODE == kGram ? a.x : MODE == kSquare ? a.a : a.xt;
-    const char *pl[WT], *pr[WT];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wi = wave >> 1, wj = wave & 1;
+    const char* left = MODE == kGram ? a.x : MODE == kSquare ? a.a : a.b;
+    const char* right = MODE == kGram ? a.x : MODE == kSquare ? a.a : a.xt;
+    // loads: wave w takes the 1 KB pieces w, w + 4, ... of a stage: operand, row block, part
+    const char* src[kLoads];
 #pragma unroll
-    for (int w = 0; w < WT; ++w) {   // blocks past the end: the last one's, computed and not written
-        pl[w] = block_at(left, matrix, R, K, min(bi0 + w, R - 1), 0, 0) + lane * 16;
-        pr[w] = block_at(right, matrix, Cb, K, min(bj0 + w, Cb - 1), 0, 0) + lane * 16;
+    for (int i = 0; i < kLoads; ++i) {
+        const int piece = wave + 4 * i, op = piece / (kRows * 3), rb = piece / 3 % kRows, p = piece % 3;
+        const int r = op ? min(tj * kRows + rb, Cb - 1) : min(ti * kRows + rb, R - 1);   // blocks past the end: the last one's, not written
+        src[i] = block_at((char*)(op ? right : left), matrix, op ? Cb : R, K, r, 0, p) + lane * 16;
     }
+    const int steps = 2 * K, k0 = (int)((long long)steps * split / a.splits), k1 = (int)((long long)steps * (split + 1) / a.splits);
+    uint4v in[2][kLoads];
+    auto load = [&](int k, uint4v (&to)[kLoads]) {
+        const long long off = (long long)min(k, k1 - 1) * 3 * kBlockBytes;   // past the end: the last again, not used
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) to[i] = *(const uint4v*)(src[i] + off);
+    };
+    auto store = [&](int buf, const uint4v (&from)[kLoads]) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) *(uint4v*)(lds + buf * kStage + (wave + 4 * i) * kBlockBytes + lane * 16) = from[i];
+    };
     floatx16 acc[WT][WT];
 #pragma unroll
     for (int i = 0; i < WT; ++i)
@@ -133,14 +221,15 @@ __global__ __launch_bounds__(256) void muon_product_kernel(MuonArgs a) {
         for (int j = 0; j < WT; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-    for (int k = 0; k < 2 * K; ++k) {
+    auto compute = [&](int buf) {
         bf16x8 l[WT][3], r[WT][3];
+        const char* base = lds + buf * kStage + lane * 16;
 #pragma unroll
         for (int w = 0; w < WT; ++w)
 #pragma unroll
             for (int p = 0; p < 3; ++p) {
-                l[w][p] = *(const bf16x8*)(pl[w] + (k * 3 + p) * kBlockBytes);
-                r[w][p] = *(const bf16x8*)(pr[w] + (k * 3 + p) * kBlockBytes);
+                l[w][p] = *(const bf16x8*)(base + ((wi * WT + w) * 3 + p) * kBlockBytes);
+                r[w][p] = *(const bf16x8*)(base + ((kRows + wj * WT + w) * 3 + p) * kBlockBytes);
             }
 #pragma unroll
         for (int q = 0; q < kProducts; ++q)
@@ -149,73 +238,90 @@ __global__ __launch_bounds__(256) void muon_product_kernel(MuonArgs a) {
 #pragma unroll
                 for (int j = 0; j < WT; ++j)
                     acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(l[i][kPartA[q]], r[j][kPartB[q]], acc[i][j], 0, 0, 0);
+    };
+    load(k0, in[0]);
+    load(k0 + 1, in[1]);
+    store(0, in[0]);
+    load(k0 + 2, in[0]);
+    __syncthreads();
+    for (int k = k0; k < k1; k += 2) {   // stage k is in buffer 0, k + 1 in registers 1, k + 2 in registers 0
+        store(1, in[1]);
+        load(k + 3, in[1]);
+        compute(0);
+        __syncthreads();
+        if (k + 1 == k1) break;
+        store(0, in[0]);
+        load(k + 4, in[0]);
+        compute(1);
+        __syncthreads();
     }
-    // lane: column lane % 32 of the result's block, rows 8 q + 4 (lane / 32) + 0..3 in registers 4 q + 0..3
-    const int col = lane & 31, up = lane >> 5;
+    if (a.splits > 1) {   // as the registers have it: [matrix][tile][split][wave][block][register][lane]
+        float* part = a.part + (((matrix * tr * tc + tile) * a.splits + split) * 4 + wave) * (WT * WT * 1024) + lane;
+#pragma unroll
+        for (int i = 0; i < WT; ++i)
+#pragma unroll
+            for (int j = 0; j < WT; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) part[((i * WT + j) * 16 + r) * 64] = acc[i][j][r];
+        return;
+    }
+    // every wave is past its last reads of the operands (the loop ends with a barrier)
 #pragma unroll
     for (int i = 0; i < WT; ++i)
 #pragma unroll
         for (int j = 0; j < WT; ++j) {
-            const int bi = bi0 + i, bj = bj0 + j;
-            if (bi >= R || bj >= Cb || (MODE != kApply && bi > bj)) continue;
-            char* across = MODE == kGram ? a.a : MODE == kSquare ? a.b : a.xt_out;   // [column][row] parts
-            char* along = MODE == kGram ? a.a : MODE == kSquare ? a.b : a.x;         // [row][column] parts
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                float v[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e];
-                const int row0 = 8 * q + 4 * up;
-                const long long to = (q & 1) * 512 + col * 16 + up * 8;
-                if (MODE == kSquare) {
-                    const char* from = block_at(a.a, matrix, R, R, bj, 2 * bi + (q >> 1), 0) + to;   // A is symmetric
-                    uint2 w[3];
-#pragma unroll
-                    for (int p = 0; p < 3; ++p) w[p] = *(const uint2*)(from + p * kBlockBytes);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float av = 0.f;
-#pragma unroll
-                        for (int p = 2; p >= 0; --p) {
-                            const unsigned u = e < 2 ? w[p].x : w[p].y;
-                            av += __uint_as_float(e & 1 ? u & 0xffff0000u : u << 16);
-                        }
-                        v[e] = a.cb * av + a.cc * v[e] + (bi == bj && row0 + e == col ? a.ca : 0.f);
-                    }
-                }
-                if (MODE == kApply && a.last) {
-                    const int r = 32 * bi + row0, c = 32 * bj + col;
-                    float* th = a.theta + matrix * a.stride;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int ur = a.tall ? c : r + e, uc = a.tall ? r + e : c;
-                        if (ur < a.rows && uc < a.cols) {
-                            float* p = th + (long long)ur * a.cols + uc;
-                            *p = a.decay * *p - a.lr_scale * v[e];
-                        }
-                    }
-                    continue;
-                }
-                SplitWords s;
-                split_pair(v[0], v[1], 0, s);
-                split_pair(v[2], v[3], 1, s);
-                char* t = block_at(across, matrix, Cb, R, bj, 2 * bi + (q >> 1), 0) + to;
-#pragma unroll
-                for (int p = 0; p < 3; ++p) *(uint2*)(t + p * kBlockBytes) = make_uint2(s.w[p][0], s.w[p][1]);
-                if (MODE != kApply && bi == bj) continue;
-                char* d = block_at(along, matrix, R, Cb, bi, 2 * bj + (col >> 4), 0) + ((col >> 3) & 1) * 512 + row0 * 16 + (col & 7) * 2;
-#pragma unroll
-                for (int p = 0; p < 3; ++p)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        *(unsigned short*)(d + p * kBlockBytes + e * 16) = (unsigned short)(s.w[p][e >> 1] >> (e & 1 ? 16 : 0));
-            }
+            const int bi = (ti * 2 + wi) * WT + i, bj = (tj * 2 + wj) * WT + j;
+            if (bi < R && bj < Cb && (MODE == kApply || bi <= bj)) put_block<MODE>(a, matrix, bi, bj, acc[i][j], (float*)lds + wave * kTileFloats);
         }
 }
 
+// Sums the parts of a split product, a wave a block, in order.
+template <int MODE, int WT>
+__global__ __launch_bounds__(64) void muon_join_kernel(MuonArgs a) {
+    __shared__ float lds[kTileFloats];
+    constexpr int kBlocks = 4 * WT * WT;
+    const int R = a.mb, Cb = MODE == kApply ? a.nb : a.mb, tr = (R + 2 * WT - 1) / (2 * WT), tc = (Cb + 2 * WT - 1) / (2 * WT);
+    const long long id = group_of_grid(), tile_id = id / kBlocks, matrix = tile_id / ((long long)tr * tc);
+    if (matrix >= a.count) return;
+    const int block = (int)(id - tile_id * kBlocks), tile = (int)(tile_id - matrix * tr * tc), ti = tile / tc, tj = tile - ti * tc;
+    const int wave = block / (WT * WT), i = block / WT % WT, j = block % WT;
+    const int bi = (ti * 2 + (wave >> 1)) * WT + i, bj = (tj * 2 + (wave & 1)) * WT + j;
+    if (bi >= R || bj >= Cb || (MODE != kApply && bi > bj)) return;
+    const float* part = a.part + tile_id * a.splits * (kBlocks * 1024) + block * 1024 + (threadIdx.x & 63);
+    floatx16 acc;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[r] = part[r * 64];
+    for (int s = 1; s < a.splits; ++s) {
+        part += kBlocks * 1024;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[r] += part[r * 64];
+    }
+    put_block<MODE>(a, matrix, bi, bj, acc, lds);
+}
+
+// Blocks of a wave's side, and parts of the sum: a product of few tiles is split so that the chip has two workgroups for each CU, no part
+// under four steps.
+struct ProductPlan {
+    int wt, splits;
+    long long tiles;          // of a matrix
+};
+ProductPlan product_plan(long long count, int mb, int nb, MuonProduct mode) {
+    const long long R = mb, C = mode == kApply ? nb : mb, steps = 2LL * (mode == kGram ? nb : mb);
+    ProductPlan p;
+    p.wt = mb <= 2 ? 1 : 2;
+    const long long tr = (R + 2 * p.wt - 1) / (2 * p.wt), tc = (C + 2 * p.wt - 1) / (2 * p.wt);
+    p.tiles = tr * tc;
+    const long long work = count * (mode == kApply ? tr * tc : tr * (tr + 1) / 2);
+    long long s = 512 / work;
+    if (s > steps / 4) s = steps / 4;
+    p.splits = (int)(s < 1 ? 1 : s > 32 ? 32 : s);
+    return p;
+}
+size_t part_bytes(long long count, const ProductPlan& p) { return p.splits > 1 ? (size_t)count * p.tiles * p.splits * p.wt * p.wt * 4 * 4096 : 0; }
+
 struct MuonPlan {
     int mb, nb, parts;
-    size_t x_bytes, a_bytes, norm_bytes;
+    size_t x_bytes, a_bytes, norm_bytes, part_bytes;
 };
 MuonPlan plan_of(long long count, long long rows, long long cols) {
     MuonPlan p;
@@ -227,22 +333,38 @@ MuonPlan plan_of(long long count, long long rows, long long cols) {
     p.x_bytes = (size_t)count * p.mb * p.nb * 6 * kBlockBytes;
     p.a_bytes = (size_t)count * p.mb * p.mb * 6 * kBlockBytes;
     p.norm_bytes = (size_t)count * kMuonNorms * sizeof(double);
+    p.part_bytes = 0;
+    for (MuonProduct mode : {kGram, kSquare, kApply}) {
+        const size_t n = part_bytes(count, product_plan(count, p.mb, p.nb, mode));
+        if (n > p.part_bytes) p.part_bytes = n;
+    }
     return p;
 }
 
+template <int MODE, int WT>
+void launch_tiles(const MuonArgs& a, const ProductPlan& p, double work, hipStream_t st) {
+    {
+        KernelScope ks(MODE == kGram ? "muon_gram" : MODE == kSquare ? "muon_square" : "muon_apply", work, 0.0, st, 6.0 * work);
+        hipLaunchKernelGGL((muon_product_kernel<MODE, WT>), grid_of(a.count * p.tiles * p.splits), dim3(256), 0, st, a);
+    }
+    if (p.splits == 1) return;
+    KernelScope ks("muon_join", 0.0, (double)part_bytes(a.count, p), st);
+    hipLaunchKernelGGL((muon_join_kernel<MODE, WT>), grid_of(a.count * p.tiles * 4 * WT * WT), dim3(64), 0, st, a);
+}
 template <int MODE>
-void launch_product(const MuonArgs& a, hipStream_t st) {
-    const long long R = a.mb, C = MODE == kApply ? a.nb : a.mb, K = MODE == kGram ? a.nb : a.mb;
-    const double work = 2.0 * 32768.0 * R * C * K * a.count;
-    KernelScope ks(MODE == kGram ? "muon_gram" : MODE == kSquare ? "muon_square" : "muon_apply", work, 0.0, st, 6.0 * work);
-    hipLaunchKernelGGL((muon_product_kernel<MODE, 1>), grid_of(a.count * ((R + 1) / 2) * ((C + 1) / 2)), dim3(256), 0, st, a);
+void launch_product(MuonArgs& a, hipStream_t st) {
+    const ProductPlan p = product_plan(a.count, a.mb, a.nb, (MuonProduct)MODE);
+    const double R = a.mb, C = MODE == kApply ? a.nb : (a.mb + 1) * 0.5, K = MODE == kGram ? a.nb : a.mb, work = 65536.0 * R * C * K * a.count;
+    a.splits = p.splits;
+    if (p.wt == 1) launch_tiles<MODE, 1>(a, p, work, st);
+    else launch_tiles<MODE, 2>(a, p, work, st);
 }
 
 }  // namespace
 
 size_t muon_ws_bytes(long long count, long long rows, long long cols) {
     const MuonPlan p = plan_of(count, rows, cols);
-    return 3 * p.x_bytes + 2 * p.a_bytes + p.norm_bytes;
+    return 3 * p.x_bytes + 2 * p.a_bytes + p.norm_bytes + p.part_bytes;
 }
 
 hipError_t muon_update(const gleam_muon& h, long long count, long long rows, long long cols, long long stride, float* theta,
@@ -259,6 +381,7 @@ hipError_t muon_update(const gleam_muon& h, long long count, long long rows, lon
     a.a = at + 3 * p.x_bytes;
     a.b = a.a + p.a_bytes;
     a.norms = (double*)(a.b + p.a_bytes);
+    a.part = (float*)(a.b + p.a_bytes + p.norm_bytes);
     a.stride = stride;
     a.count = count;
     a.rows = (int)rows;
