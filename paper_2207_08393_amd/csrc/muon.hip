@@ -1,25 +1,34 @@
 // Orthogonalised update of weight matrices (gfx950): momentum, X = u / |u|, Newton-Schulz steps X <- (a I + b A + c A^2) X with A = X X^T of
 // the smaller side, and the update of the weights.
 //
-// A step amplifies small singular values by a = 3.4 and with them what X was rounded by, so products are as good as float32 ones: every
-// matrix is kept as three bfloat16 parts (split.h), and a product is six of the bfloat16 matrix cores' (2.7 times as fast as the
-// float32 ones at equal work).  Matrices are split once, by the kernel that writes them, and kept as the matrix instruction reads its operands:
+// A step amplifies small singular values by a = 3.4 and with them what X was rounded by, so products are about as good as float32 ones: every
+// matrix is kept as the sum of two float16 numbers, 11 bits each, and a product is three of the float16 matrix cores' (the product of the two
+// second parts, 2^-22 of the whole at most, is left out).  That is 5 times as fast as the float32 matrix cores, and twice as fast as three
+// bfloat16 parts and six products.  Float16 has a range to mind: every matrix is scaled by a power of two that keeps it under 2^15, from the
+// largest singular value that the polynomial can make of [0, 1], which the host works out; small second parts may be subnormal.
+// Matrices are split once, by the kernel that writes them, and kept as the matrix instruction reads its operands:
 // blocks of 32 rows x 16 columns, each 1 KB of a part (half of the columns, row, 8 columns), so that a wave's operand is one access of 16
 // bytes a lane, without conflicts in LDS.  X is kept in that form both ways round, since X X^T sums over its columns and (..) X over its rows.
 // A and the polynomial B = a I + b A + c A^2 are symmetric: only blocks on and above the diagonal are computed, and written twice.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "layer_common.h"
 #include "layer_ops.h"
-#include "split.h"
 
 namespace gleam {
 namespace {
 
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef unsigned uint4v __attribute__((ext_vector_type(4)));
+typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+typedef _Float16 halfx4 __attribute__((ext_vector_type(4)));
+
 constexpr int kBlockBytes = 1024;          // a part of 32 x 16
-constexpr int kMuonNorms = 128;            // partial sums of |u|^2 of a matrix, at most
+constexpr int kParts = 2;
+constexpr int kMuonNorms = 512;            // partial sums of |u|^2 of a matrix, at most
 
 struct MuonArgs {
     float *theta, *m;
@@ -32,13 +41,14 @@ struct MuonArgs {
     int parts;                             // partial sums of |u|^2
     float* part;                           // of products split along their sum
     int splits;
-    int nesterov, last;
-    float lr_scale, decay, momentum, eps, ca, cb, cc;
+    int nesterov, last, no_square;
+    float lr_scale, decay, momentum, eps;
+    float x_scale, gram_scale, apply_scale, ca, cb, cc;   // of the sums, so that results have their scale; B = ca I + cc (cb A + A A)
 };
 
 // A matrix of R x K blocks of 32 x 32: part p of the 16 columns k16 of rows 32 r ..
 __device__ __forceinline__ char* block_at(char* base, long long matrix, int R, int K, int r, int k16, int p) {
-    return base + (((matrix * R + r) * (2 * K) + k16) * 3 + p) * kBlockBytes;
+    return base + (((matrix * R + r) * (2 * K) + k16) * kParts + p) * kBlockBytes;
 }
 
 // m <- momentum m + g and the partial sums of |u|^2, in 64 bits: squares of float32 numbers stay in range
@@ -51,11 +61,35 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(MuonArgs a) {
     const float* g = a.grad + matrix * a.stride;
     float* m = a.m + matrix * a.stride;
     double sum = 0.0;
-    for (long long e = part * 256 + threadIdx.x; e < size; e += a.parts * 256) {
-        const float gv = g[e], mv = __builtin_fmaf(a.momentum, m[e], gv);
-        m[e] = mv;
+    // four elements a lane at a time, all requested before the first is used; the end one by one
+    const long long quads = size / 4, step = a.parts * 256LL;
+    auto one = [&](float gv, float& mv) {
+        mv = __builtin_fmaf(a.momentum, mv, gv);
         const double u = a.nesterov ? __builtin_fmaf(a.momentum, mv, gv) : mv;
         sum += u * u;
+    };
+    for (long long q = part * 256 + threadIdx.x; q < quads; q += 2 * step) {
+        const bool more = q + step < quads;
+        const long long q2 = more ? q + step : q;
+        Pack<float, 4> g0, g1, m0, m1;
+        g0.load(g + 4 * q), m0.load(m + 4 * q), g1.load(g + 4 * q2), m1.load(m + 4 * q2);
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) one(g0.get(i), v[i] = m0.get(i));
+        m0.set(v);
+        m0.store(m + 4 * q);
+        if (more) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) one(g1.get(i), v[i] = m1.get(i));
+            m1.set(v);
+            m1.store(m + 4 * q2);
+        }
+    }
+    if (part == 0 && threadIdx.x < size - 4 * quads) {
+        const long long e = 4 * quads + threadIdx.x;
+        float v = m[e];
+        one(g[e], v);
+        m[e] = v;
     }
     for (int o = 1; o < 64; o *= 2) sum += __shfl_xor(sum, o);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = sum;
@@ -65,11 +99,14 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(MuonArgs a) {
 
 // The parts of 8 values in a row, to block + offset of each part.
 __device__ __forceinline__ void store_parts8(char* block, const float* v) {
-    SplitWords s;
+    halfx8 hi, lo;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) split_pair(v[2 * i], v[2 * i + 1], i, s);
-#pragma unroll
-    for (int p = 0; p < 3; ++p) *(uint4*)(block + p * kBlockBytes) = make_uint4(s.w[p][0], s.w[p][1], s.w[p][2], s.w[p][3]);
+    for (int i = 0; i < 8; ++i) {
+        hi[i] = (_Float16)v[i];
+        lo[i] = (_Float16)(v[i] - (float)hi[i]);
+    }
+    *(halfx8*)block = hi;
+    *(halfx8*)(block + kBlockBytes) = lo;
 }
 
 // X = u / (|u| + eps), both ways round; a workgroup takes blocks of 32 x 32.
@@ -78,21 +115,27 @@ __global__ __launch_bounds__(128) void muon_split_kernel(MuonArgs a) {
     const long long id = group_of_grid(), per = (long long)a.mb * a.nb, matrix = id / per;
     if (matrix >= a.count) return;
     const int at = (int)(id - matrix * per), bi = at / a.nb, bj = at - bi * a.nb;   // of X
+    const int lane = threadIdx.x & 63;
     double norm = 0.0;
-    for (int i = 0; i < a.parts; ++i) norm += a.norms[matrix * kMuonNorms + i];
-    const float scale = (float)(1.0 / (sqrt(norm) + (double)a.eps));
+#pragma unroll
+    for (int i = 0; i < kMuonNorms; i += 64) norm += lane + i < a.parts ? a.norms[matrix * kMuonNorms + lane + i] : 0.0;
+    for (int o = 1; o < 64; o *= 2) norm += __shfl_xor(norm, o);
+    const float scale = (float)((double)a.x_scale / (sqrt(norm) + (double)a.eps));
     const float *g = a.grad + matrix * a.stride, *m = a.m + matrix * a.stride;
     const int r0 = 32 * (a.tall ? bj : bi), c0 = 32 * (a.tall ? bi : bj);           // of u
-    for (int e = threadIdx.x; e < 1024; e += 128) {
-        const int r = e >> 5, c = e & 31;
-        float u = 0.f;
-        if (r0 + r < a.rows && c0 + c < a.cols) {
-            const long long o = (long long)(r0 + r) * a.cols + c0 + c;
-            u = m[o];
-            if (a.nesterov) u = __builtin_fmaf(a.momentum, u, g[o]);
-            u *= scale;
-        }
-        tile[a.tall ? c : r][a.tall ? r : c] = u;
+    float mv[8], gv[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int e = threadIdx.x + 128 * i, r = e >> 5, c = e & 31;
+        const bool in = r0 + r < a.rows && c0 + c < a.cols;
+        const long long o = in ? (long long)(r0 + r) * a.cols + c0 + c : 0;
+        mv[i] = in ? m[o] : 0.f;
+        gv[i] = in && a.nesterov ? g[o] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int e = threadIdx.x + 128 * i, r = e >> 5, c = e & 31;
+        tile[a.tall ? c : r][a.tall ? r : c] = (a.nesterov ? __builtin_fmaf(a.momentum, mv[i], gv[i]) : mv[i]) * scale;
     }
     __syncthreads();
     const int line = threadIdx.x & 31, k8 = threadIdx.x >> 5;   // a row, or column, and which 8 of its values
@@ -107,172 +150,252 @@ __global__ __launch_bounds__(128) void muon_split_kernel(MuonArgs a) {
 
 enum MuonProduct { kGram, kSquare, kApply };
 
-// What becomes of a 32 x 32 block (bi, bj) of a product, R x Cb blocks in all; `tile`: 32 x 33 floats of LDS of this wave alone.  Lane:
-// column lane % 32, rows 8 q + 4 (lane / 32) + 0..3 in registers 4 q + 0..3.
+// Blocks of 32 x 32 on their way out, in LDS: 32 rows of 33 floats.
+constexpr int kTileFloats = 32 * 33;
+
+// Lane: column lane % 32, rows 8 q + 4 (lane / 32) + 0..3 in registers 4 q + 0..3.
+__device__ __forceinline__ void stage_block(const floatx16& acc, float* tile) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) tile[(8 * (i >> 2) + 4 * (lane >> 5) + (i & 3)) * 33 + (lane & 31)] = acc[i];
+}
+
+// A block (bi, bj) of a product, R x Cb blocks in all, out of LDS by one wave: the parts of its rows and of its columns, eight values a lane, or
+// the weights' update.
 template <int MODE>
-__device__ __forceinline__ void put_block(const MuonArgs& a, long long matrix, int bi, int bj, const floatx16& acc, float* tile) {
-    const int lane = threadIdx.x & 63, col = lane & 31, up = lane >> 5, R = a.mb, Cb = MODE == kApply ? a.nb : a.mb;
-    char* across = MODE == kGram ? a.a : MODE == kSquare ? a.b : a.xt_out;   // [column][row] parts
-    char* along = MODE == kGram ? a.a : MODE == kSquare ? a.b : a.x;         // [row][column] parts
-    const bool both = MODE == kApply || bi != bj;
+__device__ __forceinline__ void put_block(const MuonArgs& a, long long matrix, int bi, int bj, const float* tile) {
+    const int lane = threadIdx.x & 63, line = lane & 31, up = lane >> 5, R = a.mb, Cb = MODE == kApply ? a.nb : a.mb;
+    if (MODE == kApply && a.last) {   // rows of the weights: of X, or its columns; two of them at a time
+        const int row0 = 32 * (a.tall ? bj : bi) + up, col = 32 * (a.tall ? bi : bj) + line;
+        float* th = a.theta + matrix * a.stride + (long long)row0 * a.cols + col;
+        if (col >= a.cols) return;
+        float v[16];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        float v[4];
+        for (int i = 0; i < 16; ++i) v[i] = row0 + 2 * i < a.rows ? th[(long long)2 * i * a.cols] : 0.f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[4 * q + e];
-        const int row0 = 8 * q + 4 * up;
-        const long long to = (q & 1) * 512 + col * 16 + up * 8;
-        if (MODE == kSquare) {
-            const char* from = block_at(a.a, matrix, R, R, bj, 2 * bi + (q >> 1), 0) + to;   // A is symmetric
-            uint2 w[3];
-#pragma unroll
-            for (int p = 0; p < 3; ++p) w[p] = *(const uint2*)(from + p * kBlockBytes);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float av = 0.f;
-#pragma unroll
-                for (int p = 2; p >= 0; --p) {
-                    const unsigned u = e < 2 ? w[p].x : w[p].y;
-                    av += __uint_as_float(e & 1 ? u & 0xffff0000u : u << 16);
-                }
-                v[e] = a.cb * av + a.cc * v[e] + (bi == bj && row0 + e == col ? a.ca : 0.f);
-            }
+        for (int i = 0; i < 16; ++i) {
+            const int k = 2 * i + up;
+            if (row0 + 2 * i < a.rows) th[(long long)2 * i * a.cols] = a.decay * v[i] - a.lr_scale * tile[a.tall ? line * 33 + k : k * 33 + line];
         }
-        if (MODE == kApply && a.last) {
-            const int r = 32 * bi + row0, c = 32 * bj + col;
-            float* th = a.theta + matrix * a.stride;
+        return;
+    }
+    const int sides = MODE == kApply || bi != bj ? 2 : 1;   // a block on the diagonal is its own transpose
+#pragma unroll 1
+    for (int side = 0; side < sides; ++side) {
+        const int sl = side ? 1 : 33, sk = side ? 33 : 1;
+        char* out = MODE == kGram ? block_at(a.a, matrix, R, R, side ? bj : bi, 2 * (side ? bi : bj), 0)
+                    : MODE == kSquare ? block_at(a.b, matrix, R, R, side ? bj : bi, 2 * (side ? bi : bj), 0)
+                    : side ? block_at(a.xt_out, matrix, Cb, R, bj, 2 * bi, 0) : block_at(a.x, matrix, R, Cb, bi, 2 * bj, 0);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int ur = a.tall ? c : r + e, uc = a.tall ? r + e : c;
-                if (ur < a.rows && uc < a.cols) {
-                    float* p = th + (long long)ur * a.cols + uc;
-                    *p = a.decay * *p - a.lr_scale * v[e];
-                }
+        for (int g = 0; g < 2; ++g) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int k = 8 * (up + 2 * g) + e;
+                v[e] = (MODE == kGram ? a.gram_scale : MODE == kSquare ? a.cc : a.apply_scale) * tile[line * sl + k * sk];
+                if (MODE == kSquare) v[e] += bi == bj && k == line ? a.ca : 0.f;
             }
-            continue;
+            store_parts8(out + g * kParts * kBlockBytes + up * 512 + line * 16, v);
         }
-        SplitWords s;
-        split_pair(v[0], v[1], 0, s);
-        split_pair(v[2], v[3], 1, s);
-        char* t = block_at(across, matrix, Cb, R, bj, 2 * bi + (q >> 1), 0) + to;
-#pragma unroll
-        for (int p = 0; p < 3; ++p) *(uint2*)(t + p * kBlockBytes) = make_uint2(s.w[p][0], s.w[p][1]);
-        if (both)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) tile[(row0 + e) * 33 + col] = v[e];
     }
-    if (!both || (MODE == kApply && a.last)) return;
-    // the other way round: a row and eight of its columns a lane
-    __builtin_amdgcn_wave_barrier();
+}
+
+// (b / c) A, which A A is added to: c times the sum and a on the diagonal are B.  Registers as the matrix instruction has them; A is symmetric.
+__device__ __forceinline__ floatx16 start_of_square(const MuonArgs& a, long long matrix, int bi, int bj) {
+    const int lane = threadIdx.x & 63;
+    floatx16 acc;
+    halfx4 w[4][kParts];
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-        float v[8];
+    for (int q = 0; q < 4; ++q)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = tile[col * 33 + 8 * (up + 2 * g) + e];
-        store_parts8(block_at(along, matrix, R, Cb, bi, 2 * bj + g, 0) + up * 512 + col * 16, v);
+        for (int p = 0; p < kParts; ++p)
+            w[q][p] = *(const halfx4*)(block_at(a.a, matrix, a.mb, a.mb, bj, 2 * bi + (q >> 1), p) + (q & 1) * 512 + (lane & 31) * 16 + (lane >> 5) * 8);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[i] = a.cb * ((float)w[i >> 2][1][i & 3] + (float)w[i >> 2][0][i & 3]);
+    return acc;
+}
+
+// The tile of a result that a workgroup computes, and its part of the sum.  Workgroups go round the eight XCDs, each with an L2 of its own:
+// an XCD gets neighbours in [matrix][part of the sum][column of tiles][row of tiles], so that its workgroups read the same rows of both
+// operands at about the same time.
+struct Tile {
+    long long matrix, tile;   // tile: of all matrices' stored ones
+    int split, ti, tj;
+};
+template <int MODE>
+__device__ __forceinline__ void place_tile(int at, int tr, Tile& t) {
+    if (MODE == kApply) {
+        t.tj = at / tr;
+        t.ti = at - t.tj * tr;
+    } else {   // on and above the diagonal, column by column
+        t.tj = (int)((sqrtf(8.f * at + 1.f) - 1.f) * 0.5f);
+        if (t.tj * (t.tj + 1) / 2 > at) --t.tj;
+        if ((t.tj + 1) * (t.tj + 2) / 2 <= at) ++t.tj;
+        t.ti = at - t.tj * (t.tj + 1) / 2;
     }
-    __builtin_amdgcn_wave_barrier();
+}
+template <int MODE>
+__device__ __forceinline__ bool find_tile(const MuonArgs& a, int tr, int tc, Tile& t) {
+    const long long per_split = MODE == kApply ? (long long)tr * tc : (long long)tr * (tr + 1) / 2, per = per_split * a.splits, all = per * a.count;
+    const long long id = group_of_grid(), each = (all + 7) / 8, item = (id & 7) * each + (id >> 3);
+    if ((id >> 3) >= each || item >= all) return false;
+    t.matrix = item / per;
+    const long long rest = item - t.matrix * per;
+    t.split = (int)(rest / per_split);
+    const int at = (int)(rest - t.split * per_split);
+    place_tile<MODE>(at, tr, t);
+    t.tile = t.matrix * per_split + at;
+    return true;
 }
 
 // One of the three products of a step, rows of the left operand against rows of the right one:
 //   kGram  A = X X^T;   kSquare  B = a I + b A + c A A;   kApply  X <- B X, or at the last step the weights' update.
-// A workgroup computes 2 WT x 2 WT blocks of 32 x 32, its four waves WT x WT each, over one of `splits` parts of the sum.  16 columns of both
-// operands are in LDS (24 KB for WT = 2) while the next 16 are written and the ones after those are on their way in registers.
-constexpr int kTileFloats = 32 * 33;
+// A workgroup computes 2 WT x 2 WT blocks of 32 x 32, its four waves WT x WT each, over one of `splits` parts of the sum, in steps of 32 columns
+// of both operands (32 KB for WT = 2).  While the matrix instructions of step k run, the operands of step k + 1 go from LDS into registers, those of
+// k + 3 from registers into LDS, and those of k + 7 are requested: one barrier a step, and four steps for memory to answer.
+constexpr int kProducts = 3;
+__device__ constexpr int kPartA[kProducts] = {1, 0, 0}, kPartB[kProducts] = {0, 1, 0};   // small ones first
+
+// Order of a step's instructions: LDS reads, LDS writes and requests one by one among the matrix instructions.
+template <int WT>
+__device__ __forceinline__ void order() {
+    constexpr int kMfma = 2 * kProducts * WT * WT, kReads = 8 * WT, kWrites = 4 * WT;   // 24, 16, 8 or 6, 8, 4
+#pragma unroll
+    for (int i = 0; i < kMfma; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        constexpr int per = (kReads + 2 * kWrites + kMfma - 1) / kMfma;
+#pragma unroll
+        for (int j = 0; j < per; ++j) {
+            const int at = i * per + j;
+            if (at < kReads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            else if (at < kReads + kWrites) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+            else if (at < kReads + 2 * kWrites) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        }
+    }
+}
 
 template <int MODE, int WT>
-__global__ __launch_bounds__(256, 2) void muon_product_kernel(MuonArgs a) {
-    constexpr int kRows = 2 * WT, kStage = 2 * kRows * 3 * kBlockBytes, kLoads = kStage / (256 * 16);   // row blocks of an operand in a tile
-    constexpr int kLds = 2 * kStage > 4 * kTileFloats * 4 ? 2 * kStage : 4 * kTileFloats * 4;
-    __shared__ __attribute__((aligned(16))) char lds[kLds];
+__global__ __launch_bounds__(256, 1) void muon_product_kernel(MuonArgs a) {
+    constexpr int kRows = 2 * WT, kStage = 2 * kRows * 2 * kParts * kBlockBytes, kLoads = kStage / (256 * 16);   // row blocks of an operand in a tile
+    constexpr int kRing = 4;
+    static_assert(kRing * kStage >= 4 * WT * WT * kTileFloats * 4, "blocks are turned round in the same memory");
+    __shared__ __attribute__((aligned(16))) char lds[kRing * kStage];
     const int R = a.mb, Cb = MODE == kApply ? a.nb : a.mb, K = MODE == kGram ? a.nb : a.mb;   // blocks of the result's sides and of the sum
-    const int tr = (R + kRows - 1) / kRows, tc = (Cb + kRows - 1) / kRows;
-    const long long id = group_of_grid(), all = (long long)tr * tc * a.splits, matrix = id / all;
-    if (matrix >= a.count) return;
-    const int rest = (int)(id - matrix * all), split = rest % a.splits, tile = rest / a.splits, ti = tile / tc, tj = tile - ti * tc;
-    if (MODE != kApply && ti > tj) return;
+    Tile t;
+    if (!find_tile<MODE>(a, (R + kRows - 1) / kRows, (Cb + kRows - 1) / kRows, t)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave >> 1, wj = wave & 1;
     const char* left = MODE == kGram ? a.x : MODE == kSquare ? a.a : a.b;
     const char* right = MODE == kGram ? a.x : MODE == kSquare ? a.a : a.xt;
-    // loads: wave w takes the 1 KB pieces w, w + 4, ... of a stage: operand, row block, part
+    // loads: wave w takes the 1 KB pieces w, w + 4, ... of a stage: operand, row block, half of the columns, part
+    constexpr int kPiece = 2 * kParts;   // pieces of a row block
     const char* src[kLoads];
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-        const int piece = wave + 4 * i, op = piece / (kRows * 3), rb = piece / 3 % kRows, p = piece % 3;
-        const int r = op ? min(tj * kRows + rb, Cb - 1) : min(ti * kRows + rb, R - 1);   // blocks past the end: the last one's, not written
-        src[i] = block_at((char*)(op ? right : left), matrix, op ? Cb : R, K, r, 0, p) + lane * 16;
+        const int piece = wave + 4 * i, op = piece / (kRows * kPiece), rb = piece / kPiece % kRows, p = piece % kPiece;
+        const int r = op ? min(t.tj * kRows + rb, Cb - 1) : min(t.ti * kRows + rb, R - 1);   // blocks past the end: the last one's, not written
+        src[i] = block_at((char*)(op ? right : left), t.matrix, op ? Cb : R, K, r, 0, 0) + p * kBlockBytes + lane * 16;
     }
-    const int steps = 2 * K, k0 = (int)((long long)steps * split / a.splits), k1 = (int)((long long)steps * (split + 1) / a.splits);
-    uint4v in[2][kLoads];
+    const int k0 = (int)((long long)K * t.split / a.splits), k1 = (int)((long long)K * (t.split + 1) / a.splits);   // steps
+    uint4v in[kRing][kLoads];
+    halfx8 op[2][2][2][WT][kParts];   // of two steps: half of the columns; left, right
     auto load = [&](int k, uint4v (&to)[kLoads]) {
-        const long long off = (long long)min(k, k1 - 1) * 3 * kBlockBytes;   // past the end: the last again, not used
+        const long long off = (long long)min(k, k1 - 1) * (kPiece * kBlockBytes);   // past the end: the last again, not used
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) to[i] = *(const uint4v*)(src[i] + off);
     };
-    auto store = [&](int buf, const uint4v (&from)[kLoads]) {
+    auto store = [&](int slot, const uint4v (&from)[kLoads]) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) *(uint4v*)(lds + buf * kStage + (wave + 4 * i) * kBlockBytes + lane * 16) = from[i];
+        for (int i = 0; i < kLoads; ++i) *(uint4v*)(lds + slot * kStage + (wave + 4 * i) * kBlockBytes + lane * 16) = from[i];
+    };
+    auto fetch = [&](int slot, halfx8 (&to)[2][2][WT][kParts]) {
+        const char* base = lds + slot * kStage + lane * 16;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int p = 0; p < kParts; ++p)
+#pragma unroll
+                for (int w = 0; w < WT; ++w) {
+                    to[h][0][w][1 - p] = *(const halfx8*)(base + ((wi * WT + w) * kPiece + h * kParts + 1 - p) * kBlockBytes);
+                    to[h][1][w][p] = *(const halfx8*)(base + ((kRows + wj * WT + w) * kPiece + h * kParts + p) * kBlockBytes);
+                }
     };
     floatx16 acc[WT][WT];
+    auto multiply = [&](const halfx8 (&o)[2][2][WT][kParts]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int q = 0; q < kProducts; ++q)
+#pragma unroll
+                for (int i = 0; i < WT; ++i)
+#pragma unroll
+                    for (int j = 0; j < WT; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o[h][0][i][kPartA[q]], o[h][1][j][kPartB[q]], acc[i][j], 0, 0, 0);
+    };
+#pragma unroll
+    for (int i = 0; i < kRing; ++i) load(k0 + i, in[i]);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        store(i, in[i]);
+        load(k0 + 4 + i, in[i]);
+    }
+    const int bi0 = (t.ti * 2 + wi) * WT, bj0 = (t.tj * 2 + wj) * WT;
 #pragma unroll
     for (int i = 0; i < WT; ++i)
 #pragma unroll
-        for (int j = 0; j < WT; ++j)
+        for (int j = 0; j < WT; ++j) {
+            if (MODE == kSquare && t.split == 0) acc[i][j] = start_of_square(a, t.matrix, min(bi0 + i, R - 1), min(bj0 + j, R - 1));
+            else
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-    auto compute = [&](int buf) {
-        bf16x8 l[WT][3], r[WT][3];
-        const char* base = lds + buf * kStage + lane * 16;
-#pragma unroll
-        for (int w = 0; w < WT; ++w)
-#pragma unroll
-            for (int p = 0; p < 3; ++p) {
-                l[w][p] = *(const bf16x8*)(base + ((wi * WT + w) * 3 + p) * kBlockBytes);
-                r[w][p] = *(const bf16x8*)(base + ((kRows + wj * WT + w) * 3 + p) * kBlockBytes);
-            }
-#pragma unroll
-        for (int q = 0; q < kProducts; ++q)
-#pragma unroll
-            for (int i = 0; i < WT; ++i)
-#pragma unroll
-                for (int j = 0; j < WT; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(l[i][kPartA[q]], r[j][kPartB[q]], acc[i][j], 0, 0, 0);
-    };
-    load(k0, in[0]);
-    load(k0 + 1, in[1]);
-    store(0, in[0]);
-    load(k0 + 2, in[0]);
+                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+        }
     __syncthreads();
-    for (int k = k0; k < k1; k += 2) {   // stage k is in buffer 0, k + 1 in registers 1, k + 2 in registers 0
-        store(1, in[1]);
-        load(k + 3, in[1]);
-        compute(0);
+    fetch(0, op[0]);
+    // s = (k - k0) % 4, the slot of step k
+    auto step = [&](int k, auto at) {
+        constexpr int s = decltype(at)::value;
+        fetch((s + 1) & 3, op[(s & 1) ^ 1]);
+        store((s + 3) & 3, in[(s + 3) & 3]);
+        load(k + 7, in[(s + 3) & 3]);
+        multiply(op[s & 1]);
+        order<WT>();
         __syncthreads();
-        if (k + 1 == k1) break;
-        store(0, in[0]);
-        load(k + 4, in[0]);
-        compute(1);
-        __syncthreads();
+    };
+    int k = MODE == kSquare && a.no_square ? k1 : k0;
+    for (; k + 4 <= k1; k += 4) {
+        step(k, std::integral_constant<int, 0>{});
+        step(k + 1, std::integral_constant<int, 1>{});
+        step(k + 2, std::integral_constant<int, 2>{});
+        step(k + 3, std::integral_constant<int, 3>{});
     }
-    if (a.splits > 1) {   // as the registers have it: [matrix][tile][split][wave][block][register][lane]
-        float* part = a.part + (((matrix * tr * tc + tile) * a.splits + split) * 4 + wave) * (WT * WT * 1024) + lane;
+    if (k < k1) step(k, std::integral_constant<int, 0>{});
+    if (k + 1 < k1) step(k + 1, std::integral_constant<int, 1>{});
+    if (k + 2 < k1) step(k + 2, std::integral_constant<int, 2>{});
+    if (a.splits > 1) {   // as the registers have it: [tile][split][wave][block][four registers][lane]
+        float* part = a.part + ((t.tile * a.splits + t.split) * 4 + wave) * (WT * WT * 1024) + lane * 4;
 #pragma unroll
         for (int i = 0; i < WT; ++i)
 #pragma unroll
             for (int j = 0; j < WT; ++j)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) part[((i * WT + j) * 16 + r) * 64] = acc[i][j][r];
+                for (int q = 0; q < 4; ++q) {
+                    const floatx4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                    *(floatx4*)(part + ((i * WT + j) * 4 + q) * 256) = v;
+                }
         return;
     }
-    // every wave is past its last reads of the operands (the loop ends with a barrier)
+    // every wave is past its last reads of the operands (a step ends with a barrier)
+    float* tiles = (float*)lds + wave * (WT * WT * kTileFloats);
 #pragma unroll
     for (int i = 0; i < WT; ++i)
 #pragma unroll
-        for (int j = 0; j < WT; ++j) {
-            const int bi = (ti * 2 + wi) * WT + i, bj = (tj * 2 + wj) * WT + j;
-            if (bi < R && bj < Cb && (MODE == kApply || bi <= bj)) put_block<MODE>(a, matrix, bi, bj, acc[i][j], (float*)lds + wave * kTileFloats);
-        }
+        for (int j = 0; j < WT; ++j) stage_block(acc[i][j], tiles + (i * WT + j) * kTileFloats);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+    for (int e = 0; e < WT * WT; ++e) {
+        const int bi = bi0 + e / WT, bj = bj0 + e % WT;
+        if (bi < R && bj < Cb && (MODE == kApply || bi <= bj)) put_block<MODE>(a, t.matrix, bi, bj, tiles + e * kTileFloats);
+    }
 }
 
 // Sums the parts of a split product, a wave a block, in order.
@@ -281,39 +404,46 @@ __global__ __launch_bounds__(64) void muon_join_kernel(MuonArgs a) {
     __shared__ float lds[kTileFloats];
     constexpr int kBlocks = 4 * WT * WT;
     const int R = a.mb, Cb = MODE == kApply ? a.nb : a.mb, tr = (R + 2 * WT - 1) / (2 * WT), tc = (Cb + 2 * WT - 1) / (2 * WT);
-    const long long id = group_of_grid(), tile_id = id / kBlocks, matrix = tile_id / ((long long)tr * tc);
+    const long long id = group_of_grid(), tile_id = id / kBlocks, per = MODE == kApply ? (long long)tr * tc : (long long)tr * (tr + 1) / 2;
+    const long long matrix = tile_id / per;
     if (matrix >= a.count) return;
-    const int block = (int)(id - tile_id * kBlocks), tile = (int)(tile_id - matrix * tr * tc), ti = tile / tc, tj = tile - ti * tc;
+    const int block = (int)(id - tile_id * kBlocks), at = (int)(tile_id - matrix * per);
+    Tile t;
+    place_tile<MODE>(at, tr, t);
     const int wave = block / (WT * WT), i = block / WT % WT, j = block % WT;
-    const int bi = (ti * 2 + (wave >> 1)) * WT + i, bj = (tj * 2 + (wave & 1)) * WT + j;
+    const int bi = (t.ti * 2 + (wave >> 1)) * WT + i, bj = (t.tj * 2 + (wave & 1)) * WT + j;
     if (bi >= R || bj >= Cb || (MODE != kApply && bi > bj)) return;
-    const float* part = a.part + tile_id * a.splits * (kBlocks * 1024) + block * 1024 + (threadIdx.x & 63);
+    const float* part = a.part + tile_id * a.splits * (kBlocks * 1024) + block * 1024 + (threadIdx.x & 63) * 4;
     floatx16 acc;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) acc[r] = part[r * 64];
-    for (int s = 1; s < a.splits; ++s) {
-        part += kBlocks * 1024;
+    for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[r] += part[r * 64];
+        for (int q = 0; q < 4; ++q) {
+            const floatx4 v = *(const floatx4*)(part + s * (kBlocks * 1024) + q * 256);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[4 * q + e] += v[e];
+        }
     }
-    put_block<MODE>(a, matrix, bi, bj, acc, lds);
+    stage_block(acc, lds);
+    __builtin_amdgcn_wave_barrier();
+    put_block<MODE>(a, matrix, bi, bj, lds);
 }
 
-// Blocks of a wave's side, and parts of the sum: a product of few tiles is split so that the chip has two workgroups for each CU, no part
-// under four steps.
+// Blocks of a wave's side, and parts of the sum: a product of few tiles is split so that every CU has a workgroup, no part under three steps.
 struct ProductPlan {
     int wt, splits;
     long long tiles;          // of a matrix
 };
 ProductPlan product_plan(long long count, int mb, int nb, MuonProduct mode) {
-    const long long R = mb, C = mode == kApply ? nb : mb, steps = 2LL * (mode == kGram ? nb : mb);
+    const long long R = mb, C = mode == kApply ? nb : mb, steps = mode == kGram ? nb : mb;
     ProductPlan p;
     p.wt = mb <= 2 ? 1 : 2;
     const long long tr = (R + 2 * p.wt - 1) / (2 * p.wt), tc = (C + 2 * p.wt - 1) / (2 * p.wt);
-    p.tiles = tr * tc;
-    const long long work = count * (mode == kApply ? tr * tc : tr * (tr + 1) / 2);
-    long long s = 512 / work;
-    if (s > steps / 4) s = steps / 4;
+    p.tiles = mode == kApply ? tr * tc : tr * (tr + 1) / 2;
+    long long s = 256 / (count * p.tiles);
+    if (s > steps / 3) s = steps / 3;
     p.splits = (int)(s < 1 ? 1 : s > 32 ? 32 : s);
     return p;
 }
@@ -330,8 +460,8 @@ MuonPlan plan_of(long long count, long long rows, long long cols) {
     p.nb = (int)((n + 31) / 32);
     const long long parts = (rows * cols + 2047) / 2048;
     p.parts = (int)(parts < kMuonNorms ? parts : kMuonNorms);
-    p.x_bytes = (size_t)count * p.mb * p.nb * 6 * kBlockBytes;
-    p.a_bytes = (size_t)count * p.mb * p.mb * 6 * kBlockBytes;
+    p.x_bytes = (size_t)count * p.mb * p.nb * 2 * kParts * kBlockBytes;
+    p.a_bytes = (size_t)count * p.mb * p.mb * 2 * kParts * kBlockBytes;
     p.norm_bytes = (size_t)count * kMuonNorms * sizeof(double);
     p.part_bytes = 0;
     for (MuonProduct mode : {kGram, kSquare, kApply}) {
@@ -344,8 +474,8 @@ MuonPlan plan_of(long long count, long long rows, long long cols) {
 template <int MODE, int WT>
 void launch_tiles(const MuonArgs& a, const ProductPlan& p, double work, hipStream_t st) {
     {
-        KernelScope ks(MODE == kGram ? "muon_gram" : MODE == kSquare ? "muon_square" : "muon_apply", work, 0.0, st, 6.0 * work);
-        hipLaunchKernelGGL((muon_product_kernel<MODE, WT>), grid_of(a.count * p.tiles * p.splits), dim3(256), 0, st, a);
+        KernelScope ks(MODE == kGram ? "muon_gram" : MODE == kSquare ? "muon_square" : "muon_apply", work, 0.0, st, kProducts * work);
+        hipLaunchKernelGGL((muon_product_kernel<MODE, WT>), grid_of((a.count * p.tiles * p.splits + 7) / 8 * 8), dim3(256), 0, st, a);
     }
     if (p.splits == 1) return;
     KernelScope ks("muon_join", 0.0, (double)part_bytes(a.count, p), st);
@@ -361,6 +491,34 @@ void launch_product(MuonArgs& a, hipStream_t st) {
 }
 
 }  // namespace
+
+bool muon_scales(const gleam_muon& p, double& sx, double& sa, double& sb) {
+    const double a = p.a, b = p.b, c = p.c;
+    double most = 1.0, top = 1.0;   // singular values of any X, and of this one: |u|_F bounds the largest
+    for (int k = 0; k + 1 < p.steps; ++k) {   // the last X goes to the weights in float32
+        // largest |s (a + b s^2 + c s^4)| of 0 <= s <= top: there, or where the slope a + 3 b z + 5 c z^2 is 0, z = s^2
+        auto value = [&](double z) { return z > 0.0 && z < top * top ? std::sqrt(z) * std::fabs(a + z * (b + z * c)) : 0.0; };
+        double next = top * std::fabs(a + top * top * (b + top * top * c));
+        const double disc = 9.0 * b * b - 20.0 * a * c;
+        if (c != 0.0 && disc >= 0.0)
+            for (double sign : {-1.0, 1.0}) next = std::max(next, value((-3.0 * b + sign * std::sqrt(disc)) / (10.0 * c)));
+        if (c == 0.0 && b != 0.0) next = std::max(next, value(-a / (3.0 * b)));
+        top = 1.001 * next;         // and what products are rounded by
+        if (!(top < 128.0)) return false;
+        most = std::max(most, top);
+    }
+    const double z1 = most * most, vertex = c != 0.0 ? -b / (2.0 * c) : 0.0;
+    auto poly = [&](double z) { return std::fabs(a + z * (b + z * c)); };
+    double most_b = std::max(poly(0.0), poly(z1));
+    if (vertex > 0.0 && vertex < z1) most_b = std::max(most_b, poly(vertex));
+    most_b = std::max(most_b, 1e-3);
+    if (!(most_b < 16384.0)) return false;
+    auto scale = [](double v) { return std::ldexp(1.0, 14 - (int)std::ceil(std::log2(v))); };   // v scale in (2^13, 2^14]
+    sx = scale(most);
+    sa = scale(z1);
+    sb = scale(most_b);
+    return true;
+}
 
 size_t muon_ws_bytes(long long count, long long rows, long long cols) {
     const MuonPlan p = plan_of(count, rows, cols);
@@ -391,13 +549,20 @@ hipError_t muon_update(const gleam_muon& h, long long count, long long rows, lon
     a.nb = p.nb;
     a.parts = p.parts;
     a.nesterov = h.nesterov;
-    a.lr_scale = (float)((double)h.lr * std::sqrt(a.tall ? (double)rows / (double)cols : 1.0));
     a.decay = (float)(1.0 - (double)h.lr * h.weight_decay);
     a.momentum = h.momentum;
     a.eps = h.eps;
-    a.ca = h.a;
-    a.cb = h.b;
-    a.cc = h.c;
+    // b A + c A A = c ((b / c) A + A A); where c A A is below 2^-60 of b A, or c is 0, it is b A alone
+    a.no_square = std::fabs((double)h.c) <= std::fabs((double)h.b) * 0x1p-60;
+    double sx = 1.0, sa = 1.0, sb = 1.0;
+    muon_scales(h, sx, sa, sb);
+    a.x_scale = (float)sx;
+    a.gram_scale = (float)(sa / (sx * sx));
+    a.apply_scale = (float)(1.0 / sb);
+    a.lr_scale = (float)((double)h.lr * std::sqrt(a.tall ? (double)rows / (double)cols : 1.0) / (sb * sx));
+    a.ca = (float)(h.a * sb);
+    a.cb = (float)(a.no_square ? sa : sa * (double)h.b / (double)h.c);
+    a.cc = (float)((a.no_square ? h.b : h.c) * (sb / (sa * sa)));
     {
         KernelScope ks("muon_momentum", 4.0 * count * rows * cols, 12.0 * count * rows * cols, st);
         hipLaunchKernelGGL(muon_momentum_kernel, grid_of(count * p.parts), dim3(256), 0, st, a);

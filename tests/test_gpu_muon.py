@@ -1,9 +1,10 @@
 """The orthogonalised update through the C ABI against the float64 oracle.
 
-Tolerances, relative to the norm of X.  A step's three products round by at most about 8 of 2^-24 of what they add up (sums of at most a few
-thousand terms of random signs, three parts of 8 bits each an operand), and the steps behind it amplify small singular values by 3.4445 each:
+Tolerances, relative to the norm of X.  Operands are two float16 parts, 22 bits and half a step of the last: 2^-23 of each, and the product of the
+second parts that is left out is 2^-22 at most: 8 of 2^-24 in all for what a step's products add up (their float32 sums, of at most a few thousand terms
+of random signs, are far below that).  The steps behind it amplify small singular values by 3.4445 each:
 8 2^-24 (1 + 3.4 + 11.9 + 40.9 + 140.8 + 485) = 3.3e-4 at the very worst after five steps, where all of X is small singular values that
-were lost at the first; 8 2^-24 (1 + 3.4) = 2.1e-6 after one.  Two parts instead of three would be off by 2^-16 (3.4445)^k, 7e-3 and 5e-5.  m is
+were lost at the first; 8 2^-24 (1 + 3.4) = 2.1e-6 after one.  One part alone would be off by 2^-12 (3.4445)^k, 0.1 and 8e-4.  m is
 formed in one fused multiply-add: 2^-24."""
 import numpy as np
 import pytest
