@@ -137,7 +137,7 @@ int check_gatedscan(const gleam_gatedscan_desc* d, bool gradients) {
 }
 
 int check_muon_sizes(long long count, long long rows, long long cols) {
-    if (count < 1 || rows < 1 || cols < 1 || rows > 65536 || cols > 65536) return GLEAM_E_DIMS;
+    if (count < 1 || rows < 1 || cols < 1 || count > (1 << 20) || rows > 65536 || cols > 65536) return GLEAM_E_DIMS;
     return product(product(rows, cols), count) < 0 ? GLEAM_E_DIMS : GLEAM_OK;
 }
 

@@ -236,184 +236,137 @@ __device__ __forceinline__ void place_tile(int at, int tr, Tile& t) {
 }
 template <int MODE>
 __device__ __forceinline__ bool find_tile(const MuonArgs& a, int tr, int tc, Tile& t) {
-    const long long per_split = MODE == kApply ? (long long)tr * tc : (long long)tr * (tr + 1) / 2, per = per_split * a.splits, all = per * a.count;
-    const long long id = group_of_grid(), each = (all + 7) / 8, item = (id & 7) * each + (id >> 3);
+    const unsigned per_split = MODE == kApply ? tr * tc : tr * (tr + 1) / 2, per = per_split * a.splits, all = per * (unsigned)a.count;   // below 2^31
+    const unsigned id = (unsigned)group_of_grid(), each = (all + 7) / 8, item = (id & 7) * each + (id >> 3);
     if ((id >> 3) >= each || item >= all) return false;
-    t.matrix = item / per;
-    const long long rest = item - t.matrix * per;
-    t.split = (int)(rest / per_split);
-    const int at = (int)(rest - t.split * per_split);
-    place_tile<MODE>(at, tr, t);
-    t.tile = t.matrix * per_split + at;
+    const unsigned matrix = item / per, rest = item - matrix * per, split = rest / per_split, at = rest - split * per_split;
+    t.matrix = matrix;
+    t.split = (int)split;
+    place_tile<MODE>((int)at, tr, t);
+    t.tile = (long long)matrix * per_split + at;
     return true;
 }
 
 // One of the three products of a step, rows of the left operand against rows of the right one:
 //   kGram  A = X X^T;   kSquare  B = a I + b A + c A A;   kApply  X <- B X, or at the last step the weights' update.
-// A workgroup computes 2 WT x 2 WT blocks of 32 x 32, its four waves WT x WT each, over one of `splits` parts of the sum, in steps of 32 columns
-// of both operands (32 KB for WT = 2).  While the matrix instructions of step k run, the operands of step k + 1 go from LDS into registers, those of
-// k + 3 from registers into LDS, and those of k + 7 are requested: one barrier a step, and four steps for memory to answer.
+// A workgroup computes WR x WC blocks of 32 x 32 over one of `splits` parts of the sum, and each of its four waves all of them over a quarter of that: no
+// operand is needed by two waves, so they go from memory into registers as they lie there, kAhead steps of 16 columns before their use, with
+// no barrier until the four sums meet in LDS.
 constexpr int kProducts = 3;
 __device__ constexpr int kPartA[kProducts] = {1, 0, 0}, kPartB[kProducts] = {0, 1, 0};   // small ones first
 
-// Order of a step's instructions: LDS reads, LDS writes and requests one by one among the matrix instructions.
-template <int WT>
-__device__ __forceinline__ void order() {
-    constexpr int kMfma = 2 * kProducts * WT * WT, kReads = 8 * WT, kWrites = 4 * WT;   // 24, 16, 8 or 6, 8, 4
-#pragma unroll
-    for (int i = 0; i < kMfma; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        constexpr int per = (kReads + 2 * kWrites + kMfma - 1) / kMfma;
-#pragma unroll
-        for (int j = 0; j < per; ++j) {
-            const int at = i * per + j;
-            if (at < kReads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            else if (at < kReads + kWrites) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
-            else if (at < kReads + 2 * kWrites) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
-        }
-    }
-}
-
-template <int MODE, int WT>
-__global__ __launch_bounds__(256, 1) void muon_product_kernel(MuonArgs a) {
-    constexpr int kRows = 2 * WT, kStage = 2 * kRows * 2 * kParts * kBlockBytes, kLoads = kStage / (256 * 16);   // row blocks of an operand in a tile
-    constexpr int kRing = 4;
-    static_assert(kRing * kStage >= 4 * WT * WT * kTileFloats * 4, "blocks are turned round in the same memory");
-    __shared__ __attribute__((aligned(16))) char lds[kRing * kStage];
+template <int MODE, int WR, int WC>
+__global__ __launch_bounds__(256, 2) void muon_product_kernel(MuonArgs a) {
+    constexpr int kAhead = 4, kBlocks = WR * WC;
+    static_assert(kBlocks == 4, "a wave sums one block");
+    __shared__ __attribute__((aligned(16))) float lds[4][kBlocks][kTileFloats];
     const int R = a.mb, Cb = MODE == kApply ? a.nb : a.mb, K = MODE == kGram ? a.nb : a.mb;   // blocks of the result's sides and of the sum
     Tile t;
-    if (!find_tile<MODE>(a, (R + kRows - 1) / kRows, (Cb + kRows - 1) / kRows, t)) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wi = wave >> 1, wj = wave & 1;
+    if (!find_tile<MODE>(a, (R + WR - 1) / WR, (Cb + WC - 1) / WC, t)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const char* left = MODE == kGram ? a.x : MODE == kSquare ? a.a : a.b;
     const char* right = MODE == kGram ? a.x : MODE == kSquare ? a.a : a.xt;
-    // loads: wave w takes the 1 KB pieces w, w + 4, ... of a stage: operand, row block, half of the columns, part
-    constexpr int kPiece = 2 * kParts;   // pieces of a row block
-    const char* src[kLoads];
+    const int part = t.split * 4 + wave, parts = a.splits * 4;
+    const int k0 = (int)((long long)2 * K * part / parts), k1 = (int)((long long)2 * K * (part + 1) / parts);   // steps
+    const char *pl[WR], *pr[WC];   // blocks past the end: the last one's, computed and not written
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-        const int piece = wave + 4 * i, op = piece / (kRows * kPiece), rb = piece / kPiece % kRows, p = piece % kPiece;
-        const int r = op ? min(t.tj * kRows + rb, Cb - 1) : min(t.ti * kRows + rb, R - 1);   // blocks past the end: the last one's, not written
-        src[i] = block_at((char*)(op ? right : left), t.matrix, op ? Cb : R, K, r, 0, 0) + p * kBlockBytes + lane * 16;
-    }
-    const int k0 = (int)((long long)K * t.split / a.splits), k1 = (int)((long long)K * (t.split + 1) / a.splits);   // steps
-    uint4v in[kRing][kLoads];
-    halfx8 op[2][2][2][WT][kParts];   // of two steps: half of the columns; left, right
-    auto load = [&](int k, uint4v (&to)[kLoads]) {
-        const long long off = (long long)min(k, k1 - 1) * (kPiece * kBlockBytes);   // past the end: the last again, not used
+    for (int w = 0; w < WR; ++w) pl[w] = block_at((char*)left, t.matrix, R, K, min(t.ti * WR + w, R - 1), k0, 0) + lane * 16;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) to[i] = *(const uint4v*)(src[i] + off);
-    };
-    auto store = [&](int slot, const uint4v (&from)[kLoads]) {
+    for (int w = 0; w < WC; ++w) pr[w] = block_at((char*)right, t.matrix, Cb, K, min(t.tj * WC + w, Cb - 1), k0, 0) + lane * 16;
+    floatx16 acc[WR][WC];
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) *(uint4v*)(lds + slot * kStage + (wave + 4 * i) * kBlockBytes + lane * 16) = from[i];
-    };
-    auto fetch = [&](int slot, halfx8 (&to)[2][2][WT][kParts]) {
-        const char* base = lds + slot * kStage + lane * 16;
+    for (int i = 0; i < WR; ++i)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int j = 0; j < WC; ++j)
 #pragma unroll
-            for (int p = 0; p < kParts; ++p)
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    const int steps = MODE == kSquare && a.no_square ? 0 : k1 - k0;
+    halfx8 l[kAhead][WR][kParts], r[kAhead][WC][kParts];
+    auto load = [&](int k, int at) {
+        const int off = min(k, steps - 1) * (kParts * kBlockBytes);   // past the end: the last again, not used
 #pragma unroll
-                for (int w = 0; w < WT; ++w) {
-                    to[h][0][w][1 - p] = *(const halfx8*)(base + ((wi * WT + w) * kPiece + h * kParts + 1 - p) * kBlockBytes);
-                    to[h][1][w][p] = *(const halfx8*)(base + ((kRows + wj * WT + w) * kPiece + h * kParts + p) * kBlockBytes);
-                }
-    };
-    floatx16 acc[WT][WT];
-    auto multiply = [&](const halfx8 (&o)[2][2][WT][kParts]) {
+        for (int p = 0; p < kParts; ++p) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+            for (int w = 0; w < WR; ++w) l[at][w][p] = *(const halfx8*)(pl[w] + off + p * kBlockBytes);
 #pragma unroll
-            for (int q = 0; q < kProducts; ++q)
-#pragma unroll
-                for (int i = 0; i < WT; ++i)
-#pragma unroll
-                    for (int j = 0; j < WT; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o[h][0][i][kPartA[q]], o[h][1][j][kPartB[q]], acc[i][j], 0, 0, 0);
-    };
-#pragma unroll
-    for (int i = 0; i < kRing; ++i) load(k0 + i, in[i]);
-#pragma unroll
-    for (int i = 0; i < 3; ++i) {
-        store(i, in[i]);
-        load(k0 + 4 + i, in[i]);
-    }
-    const int bi0 = (t.ti * 2 + wi) * WT, bj0 = (t.tj * 2 + wj) * WT;
-#pragma unroll
-    for (int i = 0; i < WT; ++i)
-#pragma unroll
-        for (int j = 0; j < WT; ++j) {
-            if (MODE == kSquare && t.split == 0) acc[i][j] = start_of_square(a, t.matrix, min(bi0 + i, R - 1), min(bj0 + j, R - 1));
-            else
-#pragma unroll
-                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+            for (int w = 0; w < WC; ++w) r[at][w][p] = *(const halfx8*)(pr[w] + off + p * kBlockBytes);
         }
-    __syncthreads();
-    fetch(0, op[0]);
-    // s = (k - k0) % 4, the slot of step k
-    auto step = [&](int k, auto at) {
-        constexpr int s = decltype(at)::value;
-        fetch((s + 1) & 3, op[(s & 1) ^ 1]);
-        store((s + 3) & 3, in[(s + 3) & 3]);
-        load(k + 7, in[(s + 3) & 3]);
-        multiply(op[s & 1]);
-        order<WT>();
-        __syncthreads();
     };
-    int k = MODE == kSquare && a.no_square ? k1 : k0;
-    for (; k + 4 <= k1; k += 4) {
-        step(k, std::integral_constant<int, 0>{});
-        step(k + 1, std::integral_constant<int, 1>{});
-        step(k + 2, std::integral_constant<int, 2>{});
-        step(k + 3, std::integral_constant<int, 3>{});
+    auto multiply = [&](int at) {
+#pragma unroll
+        for (int q = 0; q < kProducts; ++q)
+#pragma unroll
+            for (int i = 0; i < WR; ++i)
+#pragma unroll
+                for (int j = 0; j < WC; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[at][i][kPartA[q]], r[at][j][kPartB[q]], acc[i][j], 0, 0, 0);
+    };
+    if (steps > 0) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) load(i, i);
+        int k = 0;
+        for (; k + kAhead <= steps; k += kAhead)
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                multiply(i);
+                load(k + i + kAhead, i);
+            }
+#pragma unroll
+        for (int i = 0; i < kAhead - 1; ++i)
+            if (k + i < steps) multiply(i);
     }
-    if (k < k1) step(k, std::integral_constant<int, 0>{});
-    if (k + 1 < k1) step(k + 1, std::integral_constant<int, 1>{});
-    if (k + 2 < k1) step(k + 2, std::integral_constant<int, 2>{});
-    if (a.splits > 1) {   // as the registers have it: [tile][split][wave][block][four registers][lane]
-        float* part = a.part + ((t.tile * a.splits + t.split) * 4 + wave) * (WT * WT * 1024) + lane * 4;
 #pragma unroll
-        for (int i = 0; i < WT; ++i)
+    for (int i = 0; i < WR; ++i)
 #pragma unroll
-            for (int j = 0; j < WT; ++j)
+        for (int j = 0; j < WC; ++j)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const floatx4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-                    *(floatx4*)(part + ((i * WT + j) * 4 + q) * 256) = v;
-                }
+            for (int q = 0; q < 4; ++q)
+                *(floatx4*)(lds[wave][i * WC + j] + (q * 64 + lane) * 4) = floatx4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    const int bi = t.ti * WR + wave / WC, bj = t.tj * WC + wave % WC;   // this wave's block from here on
+    const bool mine = bi < R && bj < Cb && (MODE == kApply || bi <= bj);
+    floatx16 sum;
+    if (MODE == kSquare && t.split == 0 && mine) sum = start_of_square(a, t.matrix, bi, bj);
+    else
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+    __syncthreads();
+    if (!mine) return;
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const floatx4 v = *(const floatx4*)(lds[w][wave] + (q * 64 + lane) * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[4 * q + e] += v[e];
+        }
+    if (a.splits > 1) {   // as the registers have it: [tile][split][block][four registers][lane]
+        float* to = a.part + ((t.tile * a.splits + t.split) * kBlocks + wave) * 1024 + lane * 4;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) *(floatx4*)(to + q * 256) = floatx4{sum[4 * q], sum[4 * q + 1], sum[4 * q + 2], sum[4 * q + 3]};
         return;
     }
-    // every wave is past its last reads of the operands (a step ends with a barrier)
-    float* tiles = (float*)lds + wave * (WT * WT * kTileFloats);
-#pragma unroll
-    for (int i = 0; i < WT; ++i)
-#pragma unroll
-        for (int j = 0; j < WT; ++j) stage_block(acc[i][j], tiles + (i * WT + j) * kTileFloats);
+    float* tile = lds[wave][wave];   // read by this wave alone
     __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-    for (int e = 0; e < WT * WT; ++e) {
-        const int bi = bi0 + e / WT, bj = bj0 + e % WT;
-        if (bi < R && bj < Cb && (MODE == kApply || bi <= bj)) put_block<MODE>(a, t.matrix, bi, bj, tiles + e * kTileFloats);
-    }
+    stage_block(sum, tile);
+    __builtin_amdgcn_wave_barrier();
+    put_block<MODE>(a, t.matrix, bi, bj, tile);
 }
 
 // Sums the parts of a split product, a wave a block, in order.
-template <int MODE, int WT>
+template <int MODE, int WR, int WC>
 __global__ __launch_bounds__(64) void muon_join_kernel(MuonArgs a) {
     __shared__ float lds[kTileFloats];
-    constexpr int kBlocks = 4 * WT * WT;
-    const int R = a.mb, Cb = MODE == kApply ? a.nb : a.mb, tr = (R + 2 * WT - 1) / (2 * WT), tc = (Cb + 2 * WT - 1) / (2 * WT);
-    const long long id = group_of_grid(), tile_id = id / kBlocks, per = MODE == kApply ? (long long)tr * tc : (long long)tr * (tr + 1) / 2;
-    const long long matrix = tile_id / per;
-    if (matrix >= a.count) return;
+    constexpr int kBlocks = WR * WC;
+    const int R = a.mb, Cb = MODE == kApply ? a.nb : a.mb, tr = (R + WR - 1) / WR, tc = (Cb + WC - 1) / WC;
+    const unsigned id = (unsigned)group_of_grid(), tile_id = id / kBlocks, per = MODE == kApply ? tr * tc : tr * (tr + 1) / 2;
+    const unsigned matrix = tile_id / per;
+    if (matrix >= (unsigned)a.count) return;
     const int block = (int)(id - tile_id * kBlocks), at = (int)(tile_id - matrix * per);
     Tile t;
     place_tile<MODE>(at, tr, t);
-    const int wave = block / (WT * WT), i = block / WT % WT, j = block % WT;
-    const int bi = (t.ti * 2 + (wave >> 1)) * WT + i, bj = (t.tj * 2 + (wave & 1)) * WT + j;
+    const int bi = t.ti * WR + block / WC, bj = t.tj * WC + block % WC;
     if (bi >= R || bj >= Cb || (MODE != kApply && bi > bj)) return;
-    const float* part = a.part + tile_id * a.splits * (kBlocks * 1024) + block * 1024 + (threadIdx.x & 63) * 4;
+    const float* part = a.part + (long long)tile_id * a.splits * (kBlocks * 1024) + block * 1024 + (threadIdx.x & 63) * 4;
     floatx16 acc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[r] = 0.f;
@@ -431,23 +384,21 @@ __global__ __launch_bounds__(64) void muon_join_kernel(MuonArgs a) {
     put_block<MODE>(a, matrix, bi, bj, lds);
 }
 
-// Blocks of a wave's side, and parts of the sum: a product of few tiles is split so that every CU has a workgroup, no part under three steps.
+// Tiles of 64 x 64, and parts of the sum: a product of few tiles is split so that every CU has a workgroup, no part under eight steps of 32 columns.
 struct ProductPlan {
-    int wt, splits;
+    int splits;
     long long tiles;          // of a matrix
 };
 ProductPlan product_plan(long long count, int mb, int nb, MuonProduct mode) {
-    const long long R = mb, C = mode == kApply ? nb : mb, steps = mode == kGram ? nb : mb;
+    const long long R = mb, C = mode == kApply ? nb : mb, steps = mode == kGram ? nb : mb, tr = (R + 1) / 2, tc = (C + 1) / 2;
     ProductPlan p;
-    p.wt = mb <= 2 ? 1 : 2;
-    const long long tr = (R + 2 * p.wt - 1) / (2 * p.wt), tc = (C + 2 * p.wt - 1) / (2 * p.wt);
     p.tiles = mode == kApply ? tr * tc : tr * (tr + 1) / 2;
     long long s = 256 / (count * p.tiles);
-    if (s > steps / 3) s = steps / 3;
+    if (s > steps / 8) s = steps / 8;
     p.splits = (int)(s < 1 ? 1 : s > 32 ? 32 : s);
     return p;
 }
-size_t part_bytes(long long count, const ProductPlan& p) { return p.splits > 1 ? (size_t)count * p.tiles * p.splits * p.wt * p.wt * 4 * 4096 : 0; }
+size_t part_bytes(long long count, const ProductPlan& p) { return p.splits > 1 ? (size_t)count * p.tiles * p.splits * 4 * 4096 : 0; }
 
 struct MuonPlan {
     int mb, nb, parts;
@@ -471,23 +422,18 @@ MuonPlan plan_of(long long count, long long rows, long long cols) {
     return p;
 }
 
-template <int MODE, int WT>
-void launch_tiles(const MuonArgs& a, const ProductPlan& p, double work, hipStream_t st) {
-    {
-        KernelScope ks(MODE == kGram ? "muon_gram" : MODE == kSquare ? "muon_square" : "muon_apply", work, 0.0, st, kProducts * work);
-        hipLaunchKernelGGL((muon_product_kernel<MODE, WT>), grid_of((a.count * p.tiles * p.splits + 7) / 8 * 8), dim3(256), 0, st, a);
-    }
-    if (p.splits == 1) return;
-    KernelScope ks("muon_join", 0.0, (double)part_bytes(a.count, p), st);
-    hipLaunchKernelGGL((muon_join_kernel<MODE, WT>), grid_of(a.count * p.tiles * 4 * WT * WT), dim3(64), 0, st, a);
-}
 template <int MODE>
 void launch_product(MuonArgs& a, hipStream_t st) {
     const ProductPlan p = product_plan(a.count, a.mb, a.nb, (MuonProduct)MODE);
     const double R = a.mb, C = MODE == kApply ? a.nb : (a.mb + 1) * 0.5, K = MODE == kGram ? a.nb : a.mb, work = 65536.0 * R * C * K * a.count;
     a.splits = p.splits;
-    if (p.wt == 1) launch_tiles<MODE, 1>(a, p, work, st);
-    else launch_tiles<MODE, 2>(a, p, work, st);
+    {
+        KernelScope ks(MODE == kGram ? "muon_gram" : MODE == kSquare ? "muon_square" : "muon_apply", work, 0.0, st, kProducts * work);
+        hipLaunchKernelGGL((muon_product_kernel<MODE, 2, 2>), grid_of((a.count * p.tiles * p.splits + 7) / 8 * 8), dim3(256), 0, st, a);
+    }
+    if (p.splits == 1) return;
+    KernelScope ks("muon_join", 0.0, (double)part_bytes(a.count, p), st);
+    hipLaunchKernelGGL((muon_join_kernel<MODE, 2, 2>), grid_of(a.count * p.tiles * 4), dim3(64), 0, st, a);
 }
 
 }  // namespace
