@@ -257,7 +257,7 @@ __device__ constexpr int kPartA[kProducts] = {1, 0, 0}, kPartB[kProducts] = {0, 
 
 template <int MODE, int WR, int WC>
 __global__ __launch_bounds__(256, 2) void muon_product_kernel(MuonArgs a) {
-    constexpr int kAhead = 4, kBlocks = WR * WC;
+    constexpr int kAhead = 3, kBlocks = WR * WC;
     static_assert(kBlocks == 4, "a wave sums one block");
     __shared__ __attribute__((aligned(16))) float lds[4][kBlocks][kTileFloats];
     const int R = a.mb, Cb = MODE == kApply ? a.nb : a.mb, K = MODE == kGram ? a.nb : a.mb;   // blocks of the result's sides and of the sum
@@ -303,13 +303,19 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(MuonArgs a) {
     };
     if (steps > 0) {
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) load(i, i);
+        for (int i = 0; i < kAhead - 1; ++i) load(i, i);
         int k = 0;
         for (; k + kAhead <= steps; k += kAhead)
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
+            for (int i = 0; i < kAhead; ++i) {   // requests, into the operands of the step before, among the matrix instructions
+                load(k + i + kAhead - 1, (i + kAhead - 1) % kAhead);
                 multiply(i);
-                load(k + i + kAhead, i);
+#pragma unroll
+                for (int j = 0; j < kProducts * WR * WC; ++j) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    if (j < kParts * (WR + WC)) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
         for (int i = 0; i < kAhead - 1; ++i)
