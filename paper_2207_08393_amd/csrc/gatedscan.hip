@@ -16,14 +16,16 @@
 // (a chunk) takes two more launches: what every chunk does to a state, and the carries at the chunks' starts from that, in order.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "layer_common.h"
 #include "layer_ops.h"
 
 namespace gleam {
 namespace {
 
-constexpr int kScanTokens = 8;     // of a wave
-constexpr int kScanWaves = 16;     // of a workgroup, at most
+constexpr int kTokensFwd = 16, kTokensBwd = 8;   // of a wave, at most
+constexpr int kScanWaves = 16;                  // of a workgroup, at most
 
 struct ScanArgs {
     const void *x, *r, *i, *g;
@@ -37,59 +39,59 @@ struct ScanArgs {
     long long B, T, P, C, chunks, groups; // groups of 64 columns
     float kappa;
     int tokens;                           // of a wave
+    int few;                              // groups of workgroups and columns of a sequence are numbers of 32 bits
 };
 
-// e^x for x <= 0: the product with log2 e in two parts.  From -200 on it is 0 in float32.
+constexpr float kLog2e = 1.44269504f;
+
+// e^x for x <= 0, of sums over many tokens: the product with log2 e in two parts.  From -200 on it is 0 in float32.
 __device__ __forceinline__ float exp_neg(float x) {
     x = x < -200.f ? -200.f : x;
-    const float hi = x * 1.44269502f, lo = __builtin_fmaf(x, 1.44269502f, -hi) + x * 1.92596299e-8f;
+    const float hi = x * kLog2e, lo = __builtin_fmaf(x, kLog2e, -hi) + x * 1.92596299e-8f;
     const float e = __builtin_amdgcn_exp2f(hi);
     return __builtin_fmaf(e, lo * 0.693147181f, e);
 }
-// e^-y of y >= 0 as it is kept, w: e^-y - 1 (negative, or -0) below 1/2, by the series to y^8 / 8! (what is left out is 1e-8 of it), e^-y above.
-__device__ __forceinline__ float kept_of(float y) {
-    float p = 1.f / 40320.f;
-    p = __builtin_fmaf(p, y, -1.f / 5040.f);
-    p = __builtin_fmaf(p, y, 1.f / 720.f);
-    p = __builtin_fmaf(p, y, -1.f / 120.f);
-    p = __builtin_fmaf(p, y, 1.f / 24.f);
-    p = __builtin_fmaf(p, y, -1.f / 6.f);
-    p = __builtin_fmaf(p, y, 0.5f);
-    p = __builtin_fmaf(p, y, -1.f);
-    return y < 0.5f ? p * y : exp_neg(-y);
-}
-__device__ __forceinline__ bool near_one(float w) { return __float_as_int(w) < 0; }
-__device__ __forceinline__ float a_of(float w) { return near_one(w) ? 1.f + w : w; }
-__device__ __forceinline__ float lost_of(float w) { return near_one(w) ? -w : 1.f - w; }      // 1 - a
-__device__ __forceinline__ float level_of(float w) {                                        // sqrt(1 - a^2)
-    const float d = lost_of(w);
-    return __builtin_amdgcn_sqrtf(d * (2.f - d));
-}
-__device__ __forceinline__ float step_h(float h, float w, float b) { return __builtin_fmaf(w, h, b) + (near_one(w) ? h : 0.f); }   // a h + b
-// sigmoid(v) and 1 - sigmoid(v), both to their last bits
-__device__ __forceinline__ void sigmoids(float v, float& s, float& rest) {
-    const float t = exp_neg(-fabsf(v)), p = __builtin_amdgcn_rcpf(1.f + t), q = t * p;
-    s = v < 0.f ? q : p;
-    rest = v < 0.f ? p : q;
+// The gates are worked out for every token and channel, and the kernels are bound by vector instructions: a product with log2 e
+// rounded once does there, which puts 2^-24 |v| of its value on e^-v.
+__device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * v)); }
+__device__ __forceinline__ void sigmoids(float v, float& s, float& rest) {   // and 1 - sigmoid(v), to its last bits too
+    float x = -kLog2e * v;
+    x = x > 126.f ? 126.f : x;   // (a NaN stays)
+    const float e = __builtin_amdgcn_exp2f(x);
+    s = __builtin_amdgcn_rcpf(1.f + e);
+    rest = e * s;
 }
 __device__ __forceinline__ float softplus(float v) { return fmaxf(v, 0.f) + log1pf(expf(-fabsf(v))); }
 
-// The token's gates of one channel: c s, a as it is kept, and b = sqrt(1 - a^2) u.
+__device__ __forceinline__ bool near_one(float w) { return __float_as_int(w) < 0; }
+__device__ __forceinline__ float a_of(float w) { return near_one(w) ? 1.f + w : w; }
+// a h + b: the sign of w says whether h itself is added
+__device__ __forceinline__ float step_h(float h, float w, float b) {
+    return __builtin_fmaf(w, h, b) + __int_as_float(__float_as_int(h) & (__float_as_int(w) >> 31));
+}
+
+// The token's gates of one channel: y = c s, a = e^-y as it is kept (w: a - 1 below y = 1/4, by the series to y^6 / 6!, whose rest is 5e-8 of it; a
+// above), m = sqrt(1 - a^2) = sqrt(d (2 - d)).
 struct Gate {
-    float cs, w, b;
+    float y, w, m;
 };
-__device__ __forceinline__ Gate gate_of(float x, float r, float i, float c) {
-    float s, si, rest;
-    sigmoids(r, s, rest);
-    sigmoids(i, si, rest);
+__device__ __forceinline__ Gate gate_of(float y) {
+    float p = __builtin_fmaf(-1.f / 720.f, y, 1.f / 120.f);
+    p = __builtin_fmaf(p, y, -1.f / 24.f);
+    p = __builtin_fmaf(p, y, 1.f / 6.f);
+    p = __builtin_fmaf(p, y, -0.5f);
+    p = __builtin_fmaf(p, y, 1.f);
+    const float lost = p * y, a = __builtin_amdgcn_exp2f(-kLog2e * y);
+    const bool near = y < 0.25f;
     Gate g;
-    g.cs = c * s;
-    g.w = kept_of(g.cs);
-    g.b = level_of(g.w) * (si * x);
+    g.y = y;
+    g.w = near ? -lost : a;
+    const float d = near ? lost : 1.f - a;
+    g.m = __builtin_amdgcn_sqrtf(d * (2.f - d));
     return g;
 }
 
-// Where a workgroup and a lane are.
+// Where a wave and a lane are.
 template <int V>
 struct Spot {
     long long b, k, col;       // sequence, chunk, p * C + first channel
@@ -97,38 +99,51 @@ struct Spot {
     int c, back;               // first channel; 1: the vector's second channel does not exist, and it is read from the one before on
     bool live;                 // lanes past the last column do the last one's work too, and write nothing
     int t0, t1, t2;            // tokens of the wave: from t0, those before t1 are there, those before t2 in the array
-    __device__ __forceinline__ bool set(const ScanArgs& a) {
-        const long long id = group_of_grid(), rest = id / a.groups;
-        b = rest / a.chunks;
-        k = rest - b * a.chunks;
+    // group: of 64 columns of a chunk of a sequence; first, count: the wave's tokens
+    __device__ __forceinline__ bool set(const ScanArgs& a, long long group) {
+        if (a.few) {   // numbers of 32 bits
+            const unsigned rest = (unsigned)group / (unsigned)a.groups, sb = rest / (unsigned)a.chunks;
+            b = sb;
+            k = rest - sb * (unsigned)a.chunks;
+            group = (unsigned)group - rest * (unsigned)a.groups;
+        } else {
+            const long long rest = group / a.groups;
+            b = rest / a.chunks;
+            k = rest - b * a.chunks;
+            group -= rest * a.groups;
+        }
         if (b >= a.B) return false;
-        const long long vecs = (a.C + V - 1) / V, all = vecs * a.P, mine = (id - rest * a.groups) * 64 + (threadIdx.x & 63);
+        const long long vecs = (a.C + V - 1) / V, all = vecs * a.P, mine = group * 64 + (threadIdx.x & 63);
         live = mine < all;
         const long long n = live ? mine : all - 1;
-        p = all < 0x7fffffff ? (long long)((unsigned)n / (unsigned)vecs) : n / vecs;
-        const long long v = n - p * vecs;
-        c = (int)(v * V);
+        p = a.P == 1 ? 0 : a.few ? (long long)((unsigned)n / (unsigned)vecs) : n / vecs;
+        c = (int)((n - p * vecs) * V);
         back = V > 1 && c + V > a.C;
         col = p * a.C + c;
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-        const long long first = (k * waves + wave) * a.tokens;
+        return true;
+    }
+    __device__ __forceinline__ void tokens(const ScanArgs& a, long long first, int count) {
         int len = (int)a.T;
         if (a.lengths) {
             len = a.lengths[b];
             len = len < 0 ? 0 : len > a.T ? (int)a.T : len;
         }
-        const long long end = first + a.tokens;
+        const long long end = first + count;
         t0 = (int)(first < a.T ? first : a.T);
         t2 = (int)(end < a.T ? end : a.T);
         t1 = t2 < len ? t2 : len > t0 ? len : t0;
+    }
+    // of a workgroup whose waves stand one behind the other along a chunk
+    __device__ __forceinline__ bool set_chunk(const ScanArgs& a) {
+        if (!set(a, group_of_grid())) return false;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+        tokens(a, (k * waves + wave) * a.tokens, a.tokens);
         return true;
     }
     __device__ __forceinline__ long long at(const gleam_scan_strides& s) const { return b * s.b + p * s.p + c; }
-    template <class T>
-    __device__ __forceinline__ void load(const T* p, float* v) const {   // p: of the first channel
-        load_vec<T, V>(p - back, v);
-        if (V > 1) v[0] = back ? v[V - 1] : v[0];
-    }
+    // values as they were read from `back` before the first channel
+    template <class R>
+    __device__ __forceinline__ float value(const R& raw, int e) const { return V > 1 && e == 0 ? (back ? raw.get(V - 1) : raw.get(0)) : raw.get(e); }
     template <class T>
     __device__ __forceinline__ void store(T* p, const float* v) const {
         if (!live) return;
@@ -148,64 +163,79 @@ struct Spot {
     __device__ __forceinline__ long long state(const ScanArgs& a) const { return b * a.P * a.C + col; }
 };
 
+// V values of a token as they lie in memory.
+template <class T, int V>
+struct Raw {
+    static constexpr bool kHalf = V * sizeof(T) < 4;   // one bfloat16
+    typename std::conditional<kHalf, T, Pack<T, kHalf ? 2 : V>>::type v;
+    __device__ __forceinline__ void load(const T* p) {
+        if constexpr (kHalf) v = *p;
+        else v.load(p);
+    }
+    __device__ __forceinline__ float get(int e) const {
+        if constexpr (kHalf) return to_f32(v);
+        else return v.get(e);
+    }
+};
 // A wave's tokens as it reads them.
-template <class T, int V, bool WITH_G>
+template <class T, int V, int L, bool WITH_G>
 struct Tokens {
-    static constexpr int L = kScanTokens;
-    float x[L][V], r[L][V], i[L][V], g[WITH_G ? L : 1][V];
+    Raw<T, V> x[L], r[L], i[L], g[WITH_G ? L : 1];
     __device__ __forceinline__ void load(const ScanArgs& a, const Spot<V>& s) {
-        const T *px = (const T*)a.x + s.at(a.sx) + s.t0 * a.sx.t, *pr = (const T*)a.r + s.at(a.sr) + s.t0 * a.sr.t;
-        const T *pi = (const T*)a.i + s.at(a.si) + s.t0 * a.si.t, *pg = WITH_G ? (const T*)a.g + s.at(a.sh) + s.t0 * a.sh.t : nullptr;
+        const T *px = (const T*)a.x + s.at(a.sx) + s.t0 * a.sx.t - s.back, *pr = (const T*)a.r + s.at(a.sr) + s.t0 * a.sr.t - s.back;
+        const T *pi = (const T*)a.i + s.at(a.si) + s.t0 * a.si.t - s.back, *pg = WITH_G ? (const T*)a.g + s.at(a.sh) + s.t0 * a.sh.t - s.back : nullptr;
 #pragma unroll
         for (int j = 0; j < L; ++j)
             if (s.t0 + j < s.t1) {
-                s.load(px + j * a.sx.t, x[j]);
-                s.load(pr + j * a.sr.t, r[j]);
-                s.load(pi + j * a.si.t, i[j]);
-                if (WITH_G) s.load(pg + j * a.sh.t, g[j]);
+                x[j].load(px + j * a.sx.t);
+                r[j].load(pr + j * a.sr.t);
+                i[j].load(pi + j * a.si.t);
+                if (WITH_G) g[j].load(pg + j * a.sh.t);
             }
     }
 };
 
+// c of a workgroup's columns, worked out by its first wave; a barrier stands between this and `rates`.
 template <int V>
-__device__ __forceinline__ void rates(const ScanArgs& a, const Spot<V>& s, float* c) {
+__device__ __forceinline__ void put_rates(const ScanArgs& a, const Spot<V>& s, float (&shared)[V][64]) {
+    if (threadIdx.x < 64)
 #pragma unroll
-    for (int e = 0; e < V; ++e) c[e] = a.kappa * softplus(a.lambda[s.c + (e && s.back ? 0 : e)]);
+        for (int e = 0; e < V; ++e) shared[e][threadIdx.x] = a.kappa * softplus(a.lambda[s.c + (e && s.back ? 0 : e)]);
 }
 
 // What the chunk does to a state: h' = exp(log_a) h + add_h, and backwards E' = exp(log_a) E + add_e.
-template <class T, int V, bool BWD>
+template <class T, int V, int L, bool BWD>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_chunk_kernel(ScanArgs a) {
-    constexpr int L = kScanTokens;
-    __shared__ float ends[kScanWaves][BWD ? 3 : 2][V][64];
+    __shared__ float ends[kScanWaves][BWD ? 3 : 2][V][64], shared[V][64];
     Spot<V> s;
-    if (!s.set(a)) return;
+    if (!s.set_chunk(a)) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    float c[V], sum[V], h[V], e_add[V];
-    rates(a, s, c);
-#pragma unroll
-    for (int e = 0; e < V; ++e) sum[e] = h[e] = e_add[e] = 0.f;
-    Tokens<T, V, BWD> tok;
+    Tokens<T, V, L, BWD> tok;
     tok.load(a, s);
-    float w[L][V];
+    put_rates(a, s, shared);
+    __syncthreads();
+    float c[V], sum[V], h[V], e_add[V], w[BWD ? L : 1][V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        c[e] = shared[e][lane];
+        sum[e] = h[e] = e_add[e] = 0.f;
+    }
 #pragma unroll
     for (int j = 0; j < L; ++j)
         if (s.t0 + j < s.t1)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const Gate g = gate_of(tok.x[j][e], tok.r[j][e], tok.i[j][e], c[e]);
-                w[j][e] = g.w;
-                sum[e] -= g.cs;
-                h[e] = step_h(h[e], g.w, g.b);
+                const Gate g = gate_of(c[e] * sigmoid(s.value(tok.r[j], e)));
+                if (BWD) w[j][e] = g.w;
+                sum[e] -= g.y;
+                h[e] = step_h(h[e], g.w, g.m * (sigmoid(s.value(tok.i[j], e)) * s.value(tok.x[j], e)));
             }
     if (BWD)
 #pragma unroll
         for (int j = L - 1; j >= 0; --j)
             if (s.t0 + j < s.t1)
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    e_add[e] = step_h(tok.g[j][e] + e_add[e], w[j][e], 0.f);
-                }
+                for (int e = 0; e < V; ++e) e_add[e] = step_h(s.value(tok.g[j], e) + e_add[e], w[j][e], 0.f);
 #pragma unroll
     for (int e = 0; e < V; ++e) {
         ends[wave][0][e][lane] = sum[e];
@@ -228,45 +258,123 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_chunk_kernel(ScanArgs a)
     if (BWD) s.store_state(a.add_e + at, e_add);
 }
 
-// Carries at the chunks' starts (and ends, backwards), in the place of what the chunks add.
+// Carries at the chunks' starts (and ends, backwards), in the place of what the chunks add: 64 states a workgroup, sixteen waves one behind the
+// other along the chunks.
 template <bool BWD>
-__global__ __launch_bounds__(256) void scan_carry_kernel(ScanArgs a) {
-    const long long n = group_of_grid() * 256 + threadIdx.x, pc = a.P * a.C;
-    if (n >= a.B * pc) return;
-    const long long b = n / pc, col = n - b * pc, base = b * a.chunks * pc + col;
-    float h = a.state_in ? a.state_in[n] : 0.f;
-    for (long long k = 0; k < a.chunks; ++k) {
-        const long long at = base + k * pc;
-        const float add = a.add_h[at];
-        a.add_h[at] = h;
-        h = __builtin_fmaf(exp_neg(a.log_a[at]), h, add);
+__global__ __launch_bounds__(1024) void scan_carry_kernel(ScanArgs a) {
+    __shared__ float ends[16][BWD ? 3 : 2][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long pc = a.P * a.C, all = a.B * pc, mine = group_of_grid() * 64 + lane, n = mine < all ? mine : all - 1;
+    const long long b = a.B == 1 ? 0 : n / pc, base = b * a.chunks * pc + (n - b * pc);
+    const int k0 = (int)(a.chunks * wave / 16), k1 = (int)(a.chunks * (wave + 1) / 16);
+    float sum = 0.f, h = 0.f, e = 0.f;
+#pragma unroll 8
+    for (int k = k0; k < k1; ++k) {
+        const float la = a.log_a[base + k * pc];
+        h = __builtin_fmaf(exp_neg(la), h, a.add_h[base + k * pc]);
+        if (BWD) e += exp_neg(sum) * a.add_e[base + k * pc];
+        sum += la;
+    }
+    ends[wave][0][lane] = sum;
+    ends[wave][1][lane] = h;
+    if (BWD) ends[wave][2][lane] = e;
+    __syncthreads();
+    h = a.state_in ? a.state_in[n] : 0.f;
+    for (int v = 0; v < wave; ++v) h = __builtin_fmaf(exp_neg(ends[v][0][lane]), h, ends[v][1][lane]);
+    if (BWD) {
+        e = a.state_end ? a.state_end[n] : 0.f;
+        for (int v = 15; v > wave; --v) e = __builtin_fmaf(exp_neg(ends[v][0][lane]), e, ends[v][2][lane]);
+    }
+    if (mine >= all) return;
+    // four chunks' numbers are read before the first of them is written over
+    for (int k = k0; k < k1; k += 4) {
+        float la[4], add[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const long long at = base + (k + i < k1 ? k + i : k) * pc;
+            la[i] = a.log_a[at], add[i] = a.add_h[at];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (k + i < k1) {
+                a.add_h[base + (k + i) * pc] = h;
+                h = __builtin_fmaf(exp_neg(la[i]), h, add[i]);
+            }
     }
     if (!BWD) return;
-    float e = a.state_end ? a.state_end[n] : 0.f;
-    for (long long k = a.chunks - 1; k >= 0; --k) {
-        const long long at = base + k * pc;
-        const float add = a.add_e[at];
-        a.add_e[at] = e;
-        e = __builtin_fmaf(exp_neg(a.log_a[at]), e, add);
+    for (int k = k1 - 1; k >= k0; k -= 4) {
+        float la[4], add[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const long long at = base + (k - i >= k0 ? k - i : k) * pc;
+            la[i] = a.log_a[at], add[i] = a.add_e[at];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (k - i >= k0) {
+                a.add_e[base + (k - i) * pc] = e;
+                e = __builtin_fmaf(exp_neg(la[i]), e, add[i]);
+            }
     }
 }
 
+// One wave, all tokens of 64 columns: where there are columns enough, and for few tokens.  Four tokens are on their way while four are
+// worked on.
 template <class T, int V>
-__global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs a) {
-    constexpr int L = kScanTokens;
-    __shared__ float ends[kScanWaves][2][V][64];
+__global__ __launch_bounds__(256) void scan_walk_kernel(ScanArgs a) {
+    constexpr int L = 4;
     Spot<V> s;
-    if (!s.set(a)) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    float c[V], sum[V], h[V], w[L][V], b[L][V];
-    rates(a, s, c);
-    Tokens<T, V, false> tok;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (!s.set(a, group_of_grid() * 4 + wave)) return;
+    s.tokens(a, 0, (int)a.T);
+    const int len = s.t1, T_all = s.t2;
+    Tokens<T, V, L, false> tok;
+    auto place = [&](int t) {
+        s.t0 = t < len ? t : len;
+        s.t1 = len;
+    };
+    place(0);
     tok.load(a, s);
-    const float* from = a.chunks > 1 ? a.add_h + s.slot(a) : a.state_in ? a.state_in + s.state(a) : nullptr;
-    float carry[V];
-    s.load_state(from, carry);
+    float c[V], h[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) c[e] = a.kappa * softplus(a.lambda[s.c + (e && s.back ? 0 : e)]);
+    s.load_state(a.state_in ? a.state_in + s.state(a) : nullptr, h);
+    T* out = (T*)a.out + s.at(a.sh);
+    for (int t = 0; t < len; t += L) {
+        const Tokens<T, V, L, false> now = tok;
+        place(t + L);
+        tok.load(a, s);
+#pragma unroll
+        for (int j = 0; j < L; ++j)
+            if (t + j < len) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const Gate g = gate_of(c[e] * sigmoid(s.value(now.r[j], e)));
+                    h[e] = step_h(h[e], g.w, g.m * (sigmoid(s.value(now.i[j], e)) * s.value(now.x[j], e)));
+                }
+                s.store(out + (t + j) * a.sh.t, h);
+            }
+    }
+    const float none[V] = {};
+    for (int t = len; t < T_all; ++t) s.store(out + t * a.sh.t, none);
+    if (a.state_out) s.store_state(a.state_out + s.state(a), h);
+}
+
+template <class T, int V, int L>
+__global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs a) {
+    __shared__ float ends[kScanWaves][2][V][64], shared[V][64];
+    Spot<V> s;
+    if (!s.set_chunk(a)) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    Tokens<T, V, L, false> tok;
+    tok.load(a, s);
+    float c[V], sum[V], h[V], carry[V], w[L][V], b[L][V];
+    s.load_state(a.chunks > 1 ? a.add_h + s.slot(a) : a.state_in ? a.state_in + s.state(a) : nullptr, carry);
+    put_rates(a, s, shared);
+    __syncthreads();
 #pragma unroll
     for (int e = 0; e < V; ++e) {
+        c[e] = shared[e][lane];
         sum[e] = h[e] = 0.f;
     }
 #pragma unroll
@@ -274,23 +382,21 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs a) {
         if (s.t0 + j < s.t1)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const Gate g = gate_of(tok.x[j][e], tok.r[j][e], tok.i[j][e], c[e]);
+                const Gate g = gate_of(c[e] * sigmoid(s.value(tok.r[j], e)));
                 w[j][e] = g.w;
-                b[j][e] = g.b;
-                sum[e] -= g.cs;
-                h[e] = step_h(h[e], g.w, g.b);
+                b[j][e] = g.m * (sigmoid(s.value(tok.i[j], e)) * s.value(tok.x[j], e));
+                sum[e] -= g.y;
+                h[e] = step_h(h[e], g.w, b[j][e]);
             }
-    if (waves > 1) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            ends[wave][0][e][lane] = sum[e];
-            ends[wave][1][e][lane] = h[e];
-        }
-        __syncthreads();
-        for (int v = 0; v < wave; ++v)
-#pragma unroll
-            for (int e = 0; e < V; ++e) carry[e] = __builtin_fmaf(exp_neg(ends[v][0][e][lane]), carry[e], ends[v][1][e][lane]);
+    for (int e = 0; e < V; ++e) {
+        ends[wave][0][e][lane] = sum[e];
+        ends[wave][1][e][lane] = h[e];
     }
+    __syncthreads();
+    for (int v = 0; v < wave; ++v)
+#pragma unroll
+        for (int e = 0; e < V; ++e) carry[e] = __builtin_fmaf(exp_neg(ends[v][0][e][lane]), carry[e], ends[v][1][e][lane]);
     T* out = (T*)a.out + s.at(a.sh) + s.t0 * a.sh.t;
 #pragma unroll
     for (int j = 0; j < L; ++j) {
@@ -306,25 +412,23 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs a) {
     if (a.state_out && s.k == a.chunks - 1 && wave == waves - 1) s.store_state(a.state_out + s.state(a), carry);
 }
 
-template <class T, int V>
+template <class T, int V, int L>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs a) {
-    constexpr int L = kScanTokens;
-    __shared__ float ends[kScanWaves][3][V][64];
+    __shared__ float ends[kScanWaves][3][V][64], shared[V][64];
     Spot<V> s;
-    if (!s.set(a)) return;
+    if (!s.set_chunk(a)) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    float c[V], sum[V], h[V], e_add[V], w[L][V], b[L][V], w_sum[V];
-    rates(a, s, c);
-    Tokens<T, V, true> tok;
+    Tokens<T, V, L, true> tok;
     tok.load(a, s);
     const bool split = a.chunks > 1;
-    const float* from = split ? a.add_h + s.slot(a) : a.state_in ? a.state_in + s.state(a) : nullptr;
-    const float* back = split ? a.add_e + s.slot(a) : a.state_end ? a.state_end + s.state(a) : nullptr;
-    float carry[V], ahead[V];
-    s.load_state(from, carry);
-    s.load_state(back, ahead);
+    float c[V], sum[V], h[V], e_add[V], carry[V], ahead[V], w_sum[V], w[L][V], b[L][V];
+    s.load_state(split ? a.add_h + s.slot(a) : a.state_in ? a.state_in + s.state(a) : nullptr, carry);
+    s.load_state(split ? a.add_e + s.slot(a) : a.state_end ? a.state_end + s.state(a) : nullptr, ahead);
+    put_rates(a, s, shared);
+    __syncthreads();
 #pragma unroll
     for (int e = 0; e < V; ++e) {
+        c[e] = shared[e][lane];
         sum[e] = h[e] = e_add[e] = w_sum[e] = 0.f;
     }
 #pragma unroll
@@ -332,20 +436,18 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs a) {
         if (s.t0 + j < s.t1)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const Gate g = gate_of(tok.x[j][e], tok.r[j][e], tok.i[j][e], c[e]);
+                const Gate g = gate_of(c[e] * sigmoid(s.value(tok.r[j], e)));
                 w[j][e] = g.w;
-                b[j][e] = g.b;
-                sum[e] -= g.cs;
-                h[e] = step_h(h[e], g.w, g.b);
+                b[j][e] = g.m * (sigmoid(s.value(tok.i[j], e)) * s.value(tok.x[j], e));
+                sum[e] -= g.y;
+                h[e] = step_h(h[e], g.w, b[j][e]);
             }
     if (waves > 1) {
 #pragma unroll
         for (int j = L - 1; j >= 0; --j)
             if (s.t0 + j < s.t1)
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    e_add[e] = step_h(tok.g[j][e] + e_add[e], w[j][e], 0.f);
-                }
+                for (int e = 0; e < V; ++e) e_add[e] = step_h(s.value(tok.g[j], e) + e_add[e], w[j][e], 0.f);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             ends[wave][0][e][lane] = sum[e];
@@ -378,14 +480,14 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs a) {
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 float sr, rest, si, rest_i;
-                sigmoids(tok.r[j][e], sr, rest);
-                sigmoids(tok.i[j][e], si, rest_i);
-                const float G = tok.g[j][e] + ahead[e], wj = w[j][e], x = tok.x[j][e], cs = c[e] * sr;
-                const float m = level_of(wj), gu = G * m, al = a_of(wj);
-                const float q = m > 0.f ? cs * __builtin_amdgcn_rcpf(m) : 0.f;
-                const float W = G * al * (al * (si * x) * q - b[j][e] * cs);
+                sigmoids(s.value(tok.r[j], e), sr, rest);
+                sigmoids(s.value(tok.i[j], e), si, rest_i);
+                const float G = s.value(tok.g[j], e) + ahead[e], wj = w[j][e], y = c[e] * sr, al = a_of(wj), d = near_one(wj) ? -wj : 1.f - wj;
+                const float m2 = d * (2.f - d), one_m = m2 < 0x1p-126f ? 0.f : __builtin_amdgcn_rsqf(m2), q = y * one_m, m = m2 * one_m;   // (a NaN stays)
+                const float u = si * s.value(tok.x[j], e), gu = G * m;
+                const float W = G * al * (al * u * q - b[j][e] * y);
                 ox[e] = gu * si;
-                oi[e] = gu * x * (si * rest_i);
+                oi[e] = gu * (u * rest_i);
                 orr[e] = W * rest;
                 w_sum[e] += W;
                 ahead[e] = step_h(G, wj, 0.f);
@@ -433,25 +535,29 @@ __global__ __launch_bounds__(256) void scan_sums_kernel(const float* part, long 
 }
 
 struct ScanPlan {
+    bool walk;
     int waves, tokens, vec;
     long long chunks, groups, slots;     // slots: states of all chunks
     long long rows, slabs, slab;         // of the sums of W
 };
-ScanPlan plan_of(const gleam_gatedscan_desc& d) {
+ScanPlan plan_of(const gleam_gatedscan_desc& d, bool backward) {
     ScanPlan p;
-    p.waves = 1;
-    while (p.waves < kScanWaves && p.waves * kScanTokens < d.T) p.waves *= 2;
-    p.chunks = (d.T + p.waves * kScanTokens - 1) / (p.waves * kScanTokens);
-    const long long per = (d.T + p.chunks - 1) / p.chunks;
-    p.tokens = (int)((per + p.waves - 1) / p.waves);
     p.vec = d.dtype && d.C > 1 ? 2 : 1;
     p.groups = ((d.C + p.vec - 1) / p.vec * d.P + 63) / 64;
+    // forward, a wave may walk all tokens of its columns: two for each SIMD do, or few tokens
+    p.walk = !backward && (d.T <= 4 || d.B * p.groups >= 2048);
+    const int most = backward ? kTokensBwd : kTokensFwd, most_waves = backward ? kScanWaves : kScanWaves / 2;
+    p.waves = 1;
+    while (p.waves < most_waves && p.waves * most < d.T) p.waves *= 2;
+    p.chunks = p.walk ? 1 : (d.T + p.waves * most - 1) / (p.waves * most);
+    const long long per = (d.T + p.chunks - 1) / p.chunks;
+    p.tokens = (int)((per + p.waves - 1) / p.waves);
     p.slots = d.B * p.chunks * d.P * d.C;
     p.rows = d.B * p.chunks * d.P;
     const long long col_groups = (d.C + 63) / 64;
     p.slabs = p.rows / 64 < 1 ? 1 : p.rows / 64;
-    const long long most = col_groups < 1024 ? 1024 / col_groups : 1;
-    if (p.slabs > most) p.slabs = most;
+    const long long most_slabs = col_groups < 1024 ? 1024 / col_groups : 1;
+    if (p.slabs > most_slabs) p.slabs = most_slabs;
     p.slab = (p.rows + p.slabs - 1) / p.slabs;
     return p;
 }
@@ -478,6 +584,7 @@ ScanArgs args_of(const gleam_gatedscan_desc& d, const ScanPlan& p, const void* x
     a.groups = p.groups;
     a.kappa = d.kappa;
     a.tokens = p.tokens;
+    a.few = d.B * p.chunks * p.groups < 0x7fffffff && p.groups < 0x1ffffff;
     return a;
 }
 
@@ -489,27 +596,27 @@ hipError_t find_carries(const ScanArgs& a, const ScanPlan& p, int dtype, hipStre
         const double size = (double)a.B * a.T * a.P * a.C;
         KernelScope ks(BWD ? "scan_chunk_bwd" : "scan_chunk", (BWD ? 30.0 : 25.0) * size, (BWD ? 4.0 : 3.0) * (dtype ? 2 : 4) * size, st);
         const dim3 grid = grid_of(a.B * p.chunks * p.groups), block(64 * p.waves);
-        if (!dtype) hipLaunchKernelGGL((scan_chunk_kernel<float, 1, BWD>), grid, block, 0, st, a);
-        else if (p.vec == 2) hipLaunchKernelGGL((scan_chunk_kernel<unsigned short, 2, BWD>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((scan_chunk_kernel<unsigned short, 1, BWD>), grid, block, 0, st, a);
+        if (!dtype) hipLaunchKernelGGL((scan_chunk_kernel<float, 1, BWD ? kTokensBwd : kTokensFwd, BWD>), grid, block, 0, st, a);
+        else if (p.vec == 2) hipLaunchKernelGGL((scan_chunk_kernel<unsigned short, 2, BWD ? kTokensBwd : kTokensFwd, BWD>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((scan_chunk_kernel<unsigned short, 1, BWD ? kTokensBwd : kTokensFwd, BWD>), grid, block, 0, st, a);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     KernelScope ks("scan_carry", 0.0, (BWD ? 20.0 : 12.0) * p.slots, st);
-    hipLaunchKernelGGL(scan_carry_kernel<BWD>, grid_of((a.B * a.P * a.C + 255) / 256), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(scan_carry_kernel<BWD>, grid_of((a.B * a.P * a.C + 63) / 64), dim3(1024), 0, st, a);
     return hipGetLastError();
 }
 
 }  // namespace
 
 size_t gatedscan_fwd_ws_bytes(const gleam_gatedscan_desc& d) {
-    const ScanPlan p = plan_of(d);
+    const ScanPlan p = plan_of(d, false);
     return p.chunks > 1 ? 2 * up256(p.slots * sizeof(float)) : 0;
 }
 
 hipError_t gatedscan_forward(const gleam_gatedscan_desc& d, const void* x, const void* r, const void* i, const float* lambda,
                              const int* lengths, const float* state_in, void* h, float* state_out, void* ws, hipStream_t st) {
-    const ScanPlan p = plan_of(d);
+    const ScanPlan p = plan_of(d, false);
     ScanArgs a = args_of(d, p, x, r, i, lambda, lengths, state_in);
     a.out = h;
     a.state_out = state_out;
@@ -522,22 +629,29 @@ hipError_t gatedscan_forward(const gleam_gatedscan_desc& d, const void* x, const
     if (e != hipSuccess) return e;
     const double size = (double)d.B * d.T * d.P * d.C;
     KernelScope ks("scan_fwd", 25.0 * size, 4.0 * (d.dtype ? 2 : 4) * size, st);
+    if (p.walk) {
+        const dim3 walk = grid_of((d.B * p.groups + 3) / 4);
+        if (!d.dtype) hipLaunchKernelGGL((scan_walk_kernel<float, 1>), walk, dim3(256), 0, st, a);
+        else if (p.vec == 2) hipLaunchKernelGGL((scan_walk_kernel<unsigned short, 2>), walk, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((scan_walk_kernel<unsigned short, 1>), walk, dim3(256), 0, st, a);
+        return hipGetLastError();
+    }
     const dim3 grid = grid_of(d.B * p.chunks * p.groups), block(64 * p.waves);
-    if (!d.dtype) hipLaunchKernelGGL((scan_fwd_kernel<float, 1>), grid, block, 0, st, a);
-    else if (p.vec == 2) hipLaunchKernelGGL((scan_fwd_kernel<unsigned short, 2>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((scan_fwd_kernel<unsigned short, 1>), grid, block, 0, st, a);
+    if (!d.dtype) hipLaunchKernelGGL((scan_fwd_kernel<float, 1, kTokensFwd>), grid, block, 0, st, a);
+    else if (p.vec == 2) hipLaunchKernelGGL((scan_fwd_kernel<unsigned short, 2, kTokensFwd>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((scan_fwd_kernel<unsigned short, 1, kTokensFwd>), grid, block, 0, st, a);
     return hipGetLastError();
 }
 
 size_t gatedscan_bwd_ws_bytes(const gleam_gatedscan_desc& d) {
-    const ScanPlan p = plan_of(d);
+    const ScanPlan p = plan_of(d, true);
     return (p.chunks > 1 ? 4 : 1) * up256(p.slots * sizeof(float)) + up256(p.slabs * d.C * sizeof(float));
 }
 
 hipError_t gatedscan_backward(const gleam_gatedscan_desc& d, const void* x, const void* r, const void* i, const float* lambda,
                               const int* lengths, const float* state_in, const void* g_h, const float* g_state_out, void* g_x, void* g_r,
                               void* g_i, float* g_lambda, float* g_state_in, void* ws, hipStream_t st) {
-    const ScanPlan p = plan_of(d);
+    const ScanPlan p = plan_of(d, true);
     ScanArgs a = args_of(d, p, x, r, i, lambda, lengths, state_in);
     a.g = g_h;
     a.state_end = g_state_out;
@@ -561,9 +675,9 @@ hipError_t gatedscan_backward(const gleam_gatedscan_desc& d, const void* x, cons
         const double size = (double)d.B * d.T * d.P * d.C;
         KernelScope ks("scan_bwd", 50.0 * size, 7.0 * (d.dtype ? 2 : 4) * size, st);
         const dim3 grid = grid_of(d.B * p.chunks * p.groups), block(64 * p.waves);
-        if (!d.dtype) hipLaunchKernelGGL((scan_bwd_kernel<float, 1>), grid, block, 0, st, a);
-        else if (p.vec == 2) hipLaunchKernelGGL((scan_bwd_kernel<unsigned short, 2>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((scan_bwd_kernel<unsigned short, 1>), grid, block, 0, st, a);
+        if (!d.dtype) hipLaunchKernelGGL((scan_bwd_kernel<float, 1, kTokensBwd>), grid, block, 0, st, a);
+        else if (p.vec == 2) hipLaunchKernelGGL((scan_bwd_kernel<unsigned short, 2, kTokensBwd>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((scan_bwd_kernel<unsigned short, 1, kTokensBwd>), grid, block, 0, st, a);
     }
     e = hipGetLastError();
     if (e != hipSuccess) return e;
