@@ -177,21 +177,23 @@ struct Raw {
         else return v.get(e);
     }
 };
-// A wave's tokens as it reads them.
+// A wave's tokens as it reads them.  Where there are fewer than L, the last one is read again: requests without branches between them can be
+// waited for one by one.
 template <class T, int V, int L, bool WITH_G>
 struct Tokens {
     Raw<T, V> x[L], r[L], i[L], g[WITH_G ? L : 1];
     __device__ __forceinline__ void load(const ScanArgs& a, const Spot<V>& s) {
         const T *px = (const T*)a.x + s.at(a.sx) + s.t0 * a.sx.t - s.back, *pr = (const T*)a.r + s.at(a.sr) + s.t0 * a.sr.t - s.back;
         const T *pi = (const T*)a.i + s.at(a.si) + s.t0 * a.si.t - s.back, *pg = WITH_G ? (const T*)a.g + s.at(a.sh) + s.t0 * a.sh.t - s.back : nullptr;
+        if (s.t0 >= s.t1) return;
 #pragma unroll
-        for (int j = 0; j < L; ++j)
-            if (s.t0 + j < s.t1) {
-                x[j].load(px + j * a.sx.t);
-                r[j].load(pr + j * a.sr.t);
-                i[j].load(pi + j * a.si.t);
-                if (WITH_G) g[j].load(pg + j * a.sh.t);
-            }
+        for (int j = 0; j < L; ++j) {
+            const long long t = s.t0 + j < s.t1 ? j : s.t1 - 1 - s.t0;
+            r[j].load(pr + t * a.sr.t);
+            i[j].load(pi + t * a.si.t);
+            x[j].load(px + t * a.sx.t);
+            if (WITH_G) g[j].load(pg + t * a.sh.t);
+        }
     }
 };
 
