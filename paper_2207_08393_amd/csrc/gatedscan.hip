@@ -24,8 +24,8 @@
 namespace gleam {
 namespace {
 
-constexpr int kTokensFwd = 16, kTokensBwd = 8;   // of a wave, at most
-constexpr int kScanWaves = 16;                  // of a workgroup, at most
+constexpr int kTokens = 8;         // of a wave that keeps them in registers, at most
+constexpr int kScanWaves = 8;      // of a workgroup, at most
 
 struct ScanArgs {
     const void *x, *r, *i, *g;
@@ -205,18 +205,18 @@ __device__ __forceinline__ void put_rates(const ScanArgs& a, const Spot<V>& s, f
         for (int e = 0; e < V; ++e) shared[e][threadIdx.x] = a.kappa * softplus(a.lambda[s.c + (e && s.back ? 0 : e)]);
 }
 
-// What the chunk does to a state: h' = exp(log_a) h + add_h, and backwards E' = exp(log_a) E + add_e.
-template <class T, int V, int L, bool BWD>
+// What a chunk does to a state, h' = exp(log_a) h + add_h, and backwards, E' = exp(log_a) E + add_e.
+template <class T, int V, int L>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_chunk_kernel(ScanArgs a) {
-    __shared__ float ends[kScanWaves][BWD ? 3 : 2][V][64], shared[V][64];
+    __shared__ float ends[kScanWaves][3][V][64], shared[V][64];
     Spot<V> s;
     if (!s.set_chunk(a)) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    Tokens<T, V, L, BWD> tok;
+    Tokens<T, V, L, true> tok;
     tok.load(a, s);
     put_rates(a, s, shared);
     __syncthreads();
-    float c[V], sum[V], h[V], e_add[V], w[BWD ? L : 1][V];
+    float c[V], sum[V], h[V], e_add[V], w[L][V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
         c[e] = shared[e][lane];
@@ -228,21 +228,20 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_chunk_kernel(ScanArgs a)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const Gate g = gate_of(c[e] * sigmoid(s.value(tok.r[j], e)));
-                if (BWD) w[j][e] = g.w;
+                w[j][e] = g.w;
                 sum[e] -= g.y;
                 h[e] = step_h(h[e], g.w, g.m * (sigmoid(s.value(tok.i[j], e)) * s.value(tok.x[j], e)));
             }
-    if (BWD)
 #pragma unroll
-        for (int j = L - 1; j >= 0; --j)
-            if (s.t0 + j < s.t1)
+    for (int j = L - 1; j >= 0; --j)
+        if (s.t0 + j < s.t1)
 #pragma unroll
-                for (int e = 0; e < V; ++e) e_add[e] = step_h(s.value(tok.g[j], e) + e_add[e], w[j][e], 0.f);
+            for (int e = 0; e < V; ++e) e_add[e] = step_h(s.value(tok.g[j], e) + e_add[e], w[j][e], 0.f);
 #pragma unroll
     for (int e = 0; e < V; ++e) {
         ends[wave][0][e][lane] = sum[e];
         ends[wave][1][e][lane] = h[e];
-        if (BWD) ends[wave][2][e][lane] = e_add[e];
+        ends[wave][2][e][lane] = e_add[e];
     }
     __syncthreads();
     if (wave) return;
@@ -250,14 +249,14 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_chunk_kernel(ScanArgs a)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const float more = ends[v][0][e][lane];
-            if (BWD) e_add[e] += exp_neg(sum[e]) * ends[v][2][e][lane];
+            e_add[e] += exp_neg(sum[e]) * ends[v][2][e][lane];
             h[e] = __builtin_fmaf(exp_neg(more), h[e], ends[v][1][e][lane]);
             sum[e] += more;
         }
     const long long at = s.slot(a);
     s.store_state(a.log_a + at, sum);
     s.store_state(a.add_h + at, h);
-    if (BWD) s.store_state(a.add_e + at, e_add);
+    s.store_state(a.add_e + at, e_add);
 }
 
 // Carries at the chunks' starts (and ends, backwards), in the place of what the chunks add: 64 states a workgroup, sixteen waves one behind the
@@ -320,31 +319,29 @@ __global__ __launch_bounds__(1024) void scan_carry_kernel(ScanArgs a) {
     }
 }
 
-// One wave, all tokens of 64 columns: where there are columns enough, and for few tokens.  Four tokens are on their way while four are
-// worked on.
-template <class T, int V>
+// Forward, one wave, one chunk of 64 columns from its first token to its last: all of a sequence where there are columns enough, or few tokens.
+// Four tokens are on their way while four are worked on.  SUM: what the chunk does to a state, instead of h.
+template <class T, int V, bool SUM>
 __global__ __launch_bounds__(256) void scan_walk_kernel(ScanArgs a) {
     constexpr int L = 4;
     Spot<V> s;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (!s.set(a, group_of_grid() * 4 + wave)) return;
-    s.tokens(a, 0, (int)a.T);
-    const int len = s.t1, T_all = s.t2;
+    s.tokens(a, s.k * a.tokens, a.tokens);
+    const int first = s.t0, len = s.t1, end = s.t2;
     Tokens<T, V, L, false> tok;
-    auto place = [&](int t) {
-        s.t0 = t < len ? t : len;
-        s.t1 = len;
-    };
-    place(0);
     tok.load(a, s);
-    float c[V], h[V];
+    float c[V], h[V], sum[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) c[e] = a.kappa * softplus(a.lambda[s.c + (e && s.back ? 0 : e)]);
-    s.load_state(a.state_in ? a.state_in + s.state(a) : nullptr, h);
+    for (int e = 0; e < V; ++e) {
+        c[e] = a.kappa * softplus(a.lambda[s.c + (e && s.back ? 0 : e)]);
+        sum[e] = 0.f;
+    }
+    s.load_state(SUM ? nullptr : a.chunks > 1 ? a.add_h + s.slot(a) : a.state_in ? a.state_in + s.state(a) : nullptr, h);
     T* out = (T*)a.out + s.at(a.sh);
-    for (int t = 0; t < len; t += L) {
+    for (int t = first; t < len; t += L) {
         const Tokens<T, V, L, false> now = tok;
-        place(t + L);
+        s.t0 = t + L < len ? t + L : len;
         tok.load(a, s);
 #pragma unroll
         for (int j = 0; j < L; ++j)
@@ -353,15 +350,22 @@ __global__ __launch_bounds__(256) void scan_walk_kernel(ScanArgs a) {
                 for (int e = 0; e < V; ++e) {
                     const Gate g = gate_of(c[e] * sigmoid(s.value(now.r[j], e)));
                     h[e] = step_h(h[e], g.w, g.m * (sigmoid(s.value(now.i[j], e)) * s.value(now.x[j], e)));
+                    if (SUM) sum[e] -= g.y;
                 }
-                s.store(out + (t + j) * a.sh.t, h);
+                if (!SUM) s.store(out + (t + j) * a.sh.t, h);
             }
     }
+    if (SUM) {
+        s.store_state(a.log_a + s.slot(a), sum);
+        s.store_state(a.add_h + s.slot(a), h);
+        return;
+    }
     const float none[V] = {};
-    for (int t = len; t < T_all; ++t) s.store(out + t * a.sh.t, none);
-    if (a.state_out) s.store_state(a.state_out + s.state(a), h);
+    for (int t = len; t < end; ++t) s.store(out + t * a.sh.t, none);
+    if (a.state_out && s.k == a.chunks - 1) s.store_state(a.state_out + s.state(a), h);
 }
 
+// Forward, few tokens and few columns: one workgroup's waves one behind the other.
 template <class T, int V, int L>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs a) {
     __shared__ float ends[kScanWaves][2][V][64], shared[V][64];
@@ -371,7 +375,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs a) {
     Tokens<T, V, L, false> tok;
     tok.load(a, s);
     float c[V], sum[V], h[V], carry[V], w[L][V], b[L][V];
-    s.load_state(a.chunks > 1 ? a.add_h + s.slot(a) : a.state_in ? a.state_in + s.state(a) : nullptr, carry);
+    s.load_state(a.state_in ? a.state_in + s.state(a) : nullptr, carry);
     put_rates(a, s, shared);
     __syncthreads();
 #pragma unroll
@@ -411,7 +415,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs a) {
             s.store(out + j * a.sh.t, none);
         }
     }
-    if (a.state_out && s.k == a.chunks - 1 && wave == waves - 1) s.store_state(a.state_out + s.state(a), carry);
+    if (a.state_out && wave == waves - 1) s.store_state(a.state_out + s.state(a), carry);
 }
 
 template <class T, int V, int L>
@@ -516,18 +520,18 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs a) {
 }
 
 // Sums over rows of C columns: 64 columns and a slab of rows a workgroup.  lambda not null: the last sum, out = g_lambda.
-__global__ __launch_bounds__(256) void scan_sums_kernel(const float* part, long long rows, long long C, long long slab, const float* lambda, float* out) {
-    __shared__ float red[4][64];
+__global__ __launch_bounds__(1024) void scan_sums_kernel(const float* part, long long rows, long long C, long long slab, const float* lambda, float* out) {
+    __shared__ float red[16][64];
     const long long col_groups = (C + 63) / 64, id = group_of_grid(), s = id / col_groups;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const long long c = (id - s * col_groups) * 64 + lane, end = (s + 1) * slab < rows ? (s + 1) * slab : rows;
     float v = 0.f;
     if (c < C)
-        for (long long r = s * slab + wave; r < end; r += 4) v += part[r * C + c];
+        for (long long r = s * slab + wave; r < end; r += 16) v += part[r * C + c];
     red[wave][lane] = v;
     __syncthreads();
     if (wave || c >= C || s * slab >= rows) return;
-    v = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
+    for (int i = 1; i < 16; ++i) v += red[i][lane];
     if (lambda) {
         // d softplus / softplus: goes to 1 where both vanish
         const float l = lambda[c];
@@ -546,18 +550,27 @@ ScanPlan plan_of(const gleam_gatedscan_desc& d, bool backward) {
     ScanPlan p;
     p.vec = d.dtype && d.C > 1 ? 2 : 1;
     p.groups = ((d.C + p.vec - 1) / p.vec * d.P + 63) / 64;
-    // forward, a wave may walk all tokens of its columns: two for each SIMD do, or few tokens
-    p.walk = !backward && (d.T <= 4 || d.B * p.groups >= 2048);
-    const int most = backward ? kTokensBwd : kTokensFwd, most_waves = backward ? kScanWaves : kScanWaves / 2;
-    p.waves = 1;
-    while (p.waves < most_waves && p.waves * most < d.T) p.waves *= 2;
-    p.chunks = p.walk ? 1 : (d.T + p.waves * most - 1) / (p.waves * most);
-    const long long per = (d.T + p.chunks - 1) / p.chunks;
-    p.tokens = (int)((per + p.waves - 1) / p.waves);
+    const long long columns = d.B * p.groups;   // waves
+    // Forward, waves that walk: all tokens where there are waves for every SIMD twice, or few tokens; sequences of more than a workgroup of
+    // the other kind takes in pieces of 16 tokens, or more as long as 4096 waves remain (a wave works out c first, 110 instructions a channel).
+    p.walk = !backward && (d.T <= 4 || d.T > kTokens * kScanWaves || columns >= 2048);
+    if (p.walk) {
+        long long per = columns >= 2048 || d.T <= 4 ? d.T : d.T * columns / 4096;
+        per = (per < 16 ? 16 : per + 3) / 4 * 4;
+        p.waves = 1;
+        p.chunks = (d.T + per - 1) / per;
+        p.tokens = (int)(p.chunks == 1 ? d.T : per);
+    } else {
+        p.waves = 1;
+        while (p.waves < kScanWaves && p.waves * kTokens < d.T) p.waves *= 2;
+        p.chunks = (d.T + p.waves * kTokens - 1) / (p.waves * kTokens);
+        const long long per = (d.T + p.chunks - 1) / p.chunks;
+        p.tokens = (int)((per + p.waves - 1) / p.waves);
+    }
     p.slots = d.B * p.chunks * d.P * d.C;
     p.rows = d.B * p.chunks * d.P;
     const long long col_groups = (d.C + 63) / 64;
-    p.slabs = p.rows / 64 < 1 ? 1 : p.rows / 64;
+    p.slabs = p.rows <= 512 ? 1 : p.rows / 128;
     const long long most_slabs = col_groups < 1024 ? 1024 / col_groups : 1;
     if (p.slabs > most_slabs) p.slabs = most_slabs;
     p.slab = (p.rows + p.slabs - 1) / p.slabs;
@@ -590,17 +603,30 @@ ScanArgs args_of(const gleam_gatedscan_desc& d, const ScanPlan& p, const void* x
     return a;
 }
 
-// Carries of a split sequence.
+template <bool SUM>
+void launch_walk(const ScanArgs& a, const ScanPlan& p, int dtype, hipStream_t st) {
+    const dim3 grid = grid_of((a.B * p.chunks * p.groups + 3) / 4), block(256);
+    if (!dtype) hipLaunchKernelGGL((scan_walk_kernel<float, 1, SUM>), grid, block, 0, st, a);
+    else if (p.vec == 2) hipLaunchKernelGGL((scan_walk_kernel<unsigned short, 2, SUM>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((scan_walk_kernel<unsigned short, 1, SUM>), grid, block, 0, st, a);
+}
+
+// What chunks do to a state, one way or both, and the carries of a split sequence from that.
 template <bool BWD>
 hipError_t find_carries(const ScanArgs& a, const ScanPlan& p, int dtype, hipStream_t st) {
     if (p.chunks == 1) return hipSuccess;
     {
         const double size = (double)a.B * a.T * a.P * a.C;
         KernelScope ks(BWD ? "scan_chunk_bwd" : "scan_chunk", (BWD ? 30.0 : 25.0) * size, (BWD ? 4.0 : 3.0) * (dtype ? 2 : 4) * size, st);
-        const dim3 grid = grid_of(a.B * p.chunks * p.groups), block(64 * p.waves);
-        if (!dtype) hipLaunchKernelGGL((scan_chunk_kernel<float, 1, BWD ? kTokensBwd : kTokensFwd, BWD>), grid, block, 0, st, a);
-        else if (p.vec == 2) hipLaunchKernelGGL((scan_chunk_kernel<unsigned short, 2, BWD ? kTokensBwd : kTokensFwd, BWD>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((scan_chunk_kernel<unsigned short, 1, BWD ? kTokensBwd : kTokensFwd, BWD>), grid, block, 0, st, a);
+        const long long groups = a.B * p.chunks * p.groups;
+        if constexpr (BWD) {
+            const dim3 grid = grid_of(groups), block(64 * p.waves);
+            if (!dtype) hipLaunchKernelGGL((scan_chunk_kernel<float, 1, kTokens>), grid, block, 0, st, a);
+            else if (p.vec == 2) hipLaunchKernelGGL((scan_chunk_kernel<unsigned short, 2, kTokens>), grid, block, 0, st, a);
+            else hipLaunchKernelGGL((scan_chunk_kernel<unsigned short, 1, kTokens>), grid, block, 0, st, a);
+        } else {
+            launch_walk<true>(a, p, dtype, st);
+        }
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -632,16 +658,13 @@ hipError_t gatedscan_forward(const gleam_gatedscan_desc& d, const void* x, const
     const double size = (double)d.B * d.T * d.P * d.C;
     KernelScope ks("scan_fwd", 25.0 * size, 4.0 * (d.dtype ? 2 : 4) * size, st);
     if (p.walk) {
-        const dim3 walk = grid_of((d.B * p.groups + 3) / 4);
-        if (!d.dtype) hipLaunchKernelGGL((scan_walk_kernel<float, 1>), walk, dim3(256), 0, st, a);
-        else if (p.vec == 2) hipLaunchKernelGGL((scan_walk_kernel<unsigned short, 2>), walk, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((scan_walk_kernel<unsigned short, 1>), walk, dim3(256), 0, st, a);
+        launch_walk<false>(a, p, d.dtype, st);
         return hipGetLastError();
     }
     const dim3 grid = grid_of(d.B * p.chunks * p.groups), block(64 * p.waves);
-    if (!d.dtype) hipLaunchKernelGGL((scan_fwd_kernel<float, 1, kTokensFwd>), grid, block, 0, st, a);
-    else if (p.vec == 2) hipLaunchKernelGGL((scan_fwd_kernel<unsigned short, 2, kTokensFwd>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((scan_fwd_kernel<unsigned short, 1, kTokensFwd>), grid, block, 0, st, a);
+    if (!d.dtype) hipLaunchKernelGGL((scan_fwd_kernel<float, 1, kTokens>), grid, block, 0, st, a);
+    else if (p.vec == 2) hipLaunchKernelGGL((scan_fwd_kernel<unsigned short, 2, kTokens>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((scan_fwd_kernel<unsigned short, 1, kTokens>), grid, block, 0, st, a);
     return hipGetLastError();
 }
 
@@ -677,20 +700,20 @@ hipError_t gatedscan_backward(const gleam_gatedscan_desc& d, const void* x, cons
         const double size = (double)d.B * d.T * d.P * d.C;
         KernelScope ks("scan_bwd", 50.0 * size, 7.0 * (d.dtype ? 2 : 4) * size, st);
         const dim3 grid = grid_of(d.B * p.chunks * p.groups), block(64 * p.waves);
-        if (!d.dtype) hipLaunchKernelGGL((scan_bwd_kernel<float, 1, kTokensBwd>), grid, block, 0, st, a);
-        else if (p.vec == 2) hipLaunchKernelGGL((scan_bwd_kernel<unsigned short, 2, kTokensBwd>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((scan_bwd_kernel<unsigned short, 1, kTokensBwd>), grid, block, 0, st, a);
+        if (!d.dtype) hipLaunchKernelGGL((scan_bwd_kernel<float, 1, kTokens>), grid, block, 0, st, a);
+        else if (p.vec == 2) hipLaunchKernelGGL((scan_bwd_kernel<unsigned short, 2, kTokens>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((scan_bwd_kernel<unsigned short, 1, kTokens>), grid, block, 0, st, a);
     }
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     const long long col_groups = (d.C + 63) / 64;
     KernelScope ks("scan_sums", 0.0, 4.0 * p.slots, st);
     if (p.slabs > 1) {
-        hipLaunchKernelGGL(scan_sums_kernel, grid_of(p.slabs * col_groups), dim3(256), 0, st, a.part, p.rows, (long long)d.C, p.slab, (const float*)nullptr, sums);
+        hipLaunchKernelGGL(scan_sums_kernel, grid_of(p.slabs * col_groups), dim3(1024), 0, st, a.part, p.rows, (long long)d.C, p.slab, (const float*)nullptr, sums);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(scan_sums_kernel, grid_of(col_groups), dim3(256), 0, st, p.slabs > 1 ? sums : a.part, p.slabs > 1 ? p.slabs : p.rows, (long long)d.C,
+    hipLaunchKernelGGL(scan_sums_kernel, grid_of(col_groups), dim3(1024), 0, st, p.slabs > 1 ? sums : a.part, p.slabs > 1 ? p.slabs : p.rows, (long long)d.C,
                        p.slabs > 1 ? p.slabs : p.rows, lambda, g_lambda);
     return hipGetLastError();
 }

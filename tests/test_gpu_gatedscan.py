@@ -236,7 +236,8 @@ def test_gatedscan_offsets_past_32_bits():
         at(n).copy_(torch.from_numpy(rng.normal(size=(1, T, 1, C)).astype(np.float32)))
     lam, hlam = dev(np.full(C, -3.0), torch.float32)
     d = gb.make_gatedscan(at(0), at(1), at(2), at(3), 8.0)
-    gb.gleam_gatedscan_fwd(d, at(0), at(1), at(2), lam, None, None, at(3), None, None)
+    ws = torch.empty(gb.gleam_gatedscan_workspace_bytes(d)[0], dtype=torch.uint8, device="cuda")
+    gb.gleam_gatedscan_fwd(d, at(0), at(1), at(2), lam, None, None, at(3), None, ws)
     assert_close(host(at(3)), mo.gatedscan(host(at(0)), host(at(1)), host(at(2)), hlam, 8.0)[0], F32 + ONCE, "h")
 
 
