@@ -403,11 +403,11 @@ int gleam_linattn_bwd(const gleam_linattn_desc* desc, const void* q, const void*
  * position.  Where the mean square passes the range of a float32, r = 0; infinities and NaN stay in their head.
  * gamma_q, gamma_k: [d] float32, shared by the heads of a tensor, or NULL (1).  freq: [rot/2] float32, radians a position (NULL where rot is 0).
  * positions: device int32, [B] (each = 0: token t of sequence b is at positions[b] + t) or [B][T] (each = 1), or NULL: token t is at t.
- * lengths: device int32 [B] or NULL, tokens of each sequence that are there, as for linear attention: others are not read, their results
- * are written as zeros, and they take no part in the gradients of gamma.
+ * lengths: device int32 [B] or NULL, tokens of each sequence that are there, as for linear attention: what others hold does not matter, their
+ * results are written as zeros, and they take no part in the gradients of gamma.
  * Arrays [B][T][P][heads][d] with strides as for linear attention (q_out, k_out: of results, and of their gradients); those of arrays that
- * are written must keep elements apart.  k_heads = 0: no k, all its pointers are ignored.  1 <= d <= 256, rot even, 0 <= rot <= d, eps > 0, T <= 2^30,
- * P (q_heads + k_heads) < 2^31, B T P heads <= 2^40. */
+ * are written must keep elements apart.  k_heads = 0: no k, all its pointers are ignored.  1 <= d <= 256, rot even, 0 <= rot <= d, eps > 0 and no subnormal,
+ * T <= 2^30, P (q_heads + k_heads) < 2^31, B T P heads d <= 2^40. */
 typedef struct {
     int32_t dtype, q_heads, k_heads, d, rot, pairs, each;
     float eps;

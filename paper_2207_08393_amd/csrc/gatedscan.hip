@@ -163,20 +163,6 @@ struct Spot {
     __device__ __forceinline__ long long state(const ScanArgs& a) const { return b * a.P * a.C + col; }
 };
 
-// V values of a token as they lie in memory.
-template <class T, int V>
-struct Raw {
-    static constexpr bool kHalf = V * sizeof(T) < 4;   // one bfloat16
-    typename std::conditional<kHalf, T, Pack<T, kHalf ? 2 : V>>::type v;
-    __device__ __forceinline__ void load(const T* p) {
-        if constexpr (kHalf) v = *p;
-        else v.load(p);
-    }
-    __device__ __forceinline__ float get(int e) const {
-        if constexpr (kHalf) return to_f32(v);
-        else return v.get(e);
-    }
-};
 // A wave's tokens as it reads them.  Where there are fewer than L, the last one is read again: requests without branches between them can be
 // waited for one by one.
 template <class T, int V, int L, bool WITH_G>
@@ -259,15 +245,15 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_chunk_kernel(ScanArgs a)
     s.store_state(a.add_e + at, e_add);
 }
 
-// Carries at the chunks' starts (and ends, backwards), in the place of what the chunks add: 64 states a workgroup, sixteen waves one behind the
-// other along the chunks.
+// Carries at the chunks' starts (and ends, backwards), in the place of what the chunks add: 32 states a workgroup, 32 lanes of each one behind
+// the other along the chunks.
 template <bool BWD>
 __global__ __launch_bounds__(1024) void scan_carry_kernel(ScanArgs a) {
-    __shared__ float ends[16][BWD ? 3 : 2][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long pc = a.P * a.C, all = a.B * pc, mine = group_of_grid() * 64 + lane, n = mine < all ? mine : all - 1;
+    __shared__ float ends[32][BWD ? 3 : 2][32];
+    const int lane = threadIdx.x & 31, wave = threadIdx.x >> 5;   // a state, and the stretch of chunks
+    const long long pc = a.P * a.C, all = a.B * pc, mine = group_of_grid() * 32 + lane, n = mine < all ? mine : all - 1;
     const long long b = a.B == 1 ? 0 : n / pc, base = b * a.chunks * pc + (n - b * pc);
-    const int k0 = (int)(a.chunks * wave / 16), k1 = (int)(a.chunks * (wave + 1) / 16);
+    const int k0 = (int)(a.chunks * wave / 32), k1 = (int)(a.chunks * (wave + 1) / 32);
     float sum = 0.f, h = 0.f, e = 0.f;
 #pragma unroll 8
     for (int k = k0; k < k1; ++k) {
@@ -284,7 +270,7 @@ __global__ __launch_bounds__(1024) void scan_carry_kernel(ScanArgs a) {
     for (int v = 0; v < wave; ++v) h = __builtin_fmaf(exp_neg(ends[v][0][lane]), h, ends[v][1][lane]);
     if (BWD) {
         e = a.state_end ? a.state_end[n] : 0.f;
-        for (int v = 15; v > wave; --v) e = __builtin_fmaf(exp_neg(ends[v][0][lane]), e, ends[v][2][lane]);
+        for (int v = 31; v > wave; --v) e = __builtin_fmaf(exp_neg(ends[v][0][lane]), e, ends[v][2][lane]);
     }
     if (mine >= all) return;
     // four chunks' numbers are read before the first of them is written over
@@ -631,7 +617,7 @@ hipError_t find_carries(const ScanArgs& a, const ScanPlan& p, int dtype, hipStre
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     KernelScope ks("scan_carry", 0.0, (BWD ? 20.0 : 12.0) * p.slots, st);
-    hipLaunchKernelGGL(scan_carry_kernel<BWD>, grid_of((a.B * a.P * a.C + 63) / 64), dim3(1024), 0, st, a);
+    hipLaunchKernelGGL(scan_carry_kernel<BWD>, grid_of((a.B * a.P * a.C + 31) / 32), dim3(1024), 0, st, a);
     return hipGetLastError();
 }
 

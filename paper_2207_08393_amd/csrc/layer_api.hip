@@ -106,7 +106,7 @@ int check_qknorm(const gleam_qknorm_desc* d, bool gradients) {
     if (!d) return GLEAM_E_NULL;
     if (d->dtype != 0 && d->dtype != 1) return GLEAM_E_DESC;
     if ((d->pairs != 0 && d->pairs != 1) || (d->each != 0 && d->each != 1)) return GLEAM_E_DESC;
-    if (!(d->eps > 0.f) || !std::isfinite(d->eps)) return GLEAM_E_DESC;
+    if (!(d->eps > 0.f) || !std::isnormal(d->eps)) return GLEAM_E_DESC;
     if (d->d < 1 || d->d > 256 || d->rot < 0 || d->rot > d->d || d->rot % 2) return GLEAM_E_DIMS;
     if (d->q_heads < 1 || d->k_heads < 0 || d->B < 1 || d->T < 1 || d->P < 1 || d->T > (1 << 30)) return GLEAM_E_DIMS;
     const long long heads = (long long)d->q_heads + d->k_heads, tokens = product(d->B, d->T);

@@ -1,5 +1,7 @@
 // What the kernels of the sequence-layer operators share (gfx950 device code): 16 bytes of float32 or bfloat16 elements in registers.
 #pragma once
+#include <type_traits>
+
 #include "prox_common.h"
 
 namespace gleam {
@@ -74,5 +76,20 @@ __device__ __forceinline__ void store_vec(T* p, const float* v) {
         k.store(p);
     }
 }
+// V values as they lie in memory.
+template <class T, int V>
+struct Raw {
+    static constexpr bool kHalf = V * sizeof(T) < 4;   // one bfloat16
+    typename std::conditional<kHalf, T, Pack<T, kHalf ? 2 : V>>::type v;
+    __device__ __forceinline__ void load(const T* p) {
+        if constexpr (kHalf) v = *p;
+        else v.load(p);
+    }
+    __device__ __forceinline__ float get(int e) const {
+        if constexpr (kHalf) return to_f32(v);
+        else return v.get(e);
+    }
+};
+
 }  // namespace
 }  // namespace gleam

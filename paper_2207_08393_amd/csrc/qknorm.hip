@@ -2,12 +2,14 @@
 // and its gradients (gfx950).
 //
 // A row is one head of one token: a team of 2^k lanes holds it in registers, in pairs that turn together, so that the rotation needs no
-// exchange between lanes and the norm one sum over the team.  A wave works on one token's rows at a time (all heads of q and k, all
-// pixels, or a part of them): the angles are formed once and serve every row.  An angle is pos * freq in 64 bits, taken to turns and
-// to its fraction there, which float32 would lose from a few thousand positions on; the float32 rest goes to sincospi.
+// exchange between lanes and the norm one sum over the team.  A wave works on the rows of one token, or of several where one has few: the
+// angles are formed once, a lane an angle, and handed round in LDS.  An angle is pos * freq in 64 bits, taken to turns and to its
+// fraction there, which float32 would lose from a few thousand positions on; the float32 rest goes to sincospi.
 // Backward: the row's x and g in registers, nothing stored by the forward pass; gradients of gamma are summed by lane over all rows of a
 // wave, a workgroup writes one partial sum per column and a second launch adds them up in a fixed order.
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "layer_common.h"
 #include "layer_ops.h"
@@ -23,15 +25,19 @@ struct QkTensor {
     void* out;
     gleam_seq_strides sx, so; // of x, and of the results; out has those of so forward, of sx backward
     const float* gamma;
+    unsigned heads, rows;     // rows of a token: P heads
+    unsigned magic, shift;    // r / heads = r * magic >> (32 + shift) of r < 2^31; magic 0: one head
+    int steps;                // of a wave through a token's rows
 };
 struct QkArgs {
     QkTensor t[2];            // queries, keys
     const float* freq;
     const int *positions, *lengths;
     float* part;              // backward: [workgroup][2][d] partial sums, or null
-    long long T, units;       // units of work: rows_unit rows of a token
-    unsigned rows, rows_unit, parts;   // rows of a token, of a unit, units of a token
-    int d, rot, H, Hq, each, lanes_log;
+    long long T, tokens, units;   // units of work: `per` steps through the rows of 2^tokens_log tokens
+    int per, parts;           // units of these tokens
+    int few;                  // units and tokens are numbers of 32 bits
+    int d, rot, each, lanes_log, tokens_log;
     float eps;
 };
 
@@ -61,15 +67,6 @@ struct Place {
         if (!on) e0 = 0;
         if (!two) e1 = e0;
     }
-    __device__ __forceinline__ void load(const T* row, float* v) const {
-        load_vec<T, W>(row + e0, v);
-        load_vec<T, W>(row + e1, v + W);
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            v[i] = on ? v[i] : 0.f;
-            v[W + i] = two ? v[W + i] : 0.f;
-        }
-    }
     __device__ __forceinline__ void store(T* row, const float* v) const {
         if (on) store_vec<T, W>(row + e0, v);
         if (two) store_vec<T, W>(row + e1, v + W);
@@ -94,116 +91,182 @@ __device__ __forceinline__ void turn(float* v, const float* c, const float* s, f
     }
 }
 
+// A lane's part of a row on its way.
+template <class T, int W, int NV>
+struct Row {
+    Raw<T, W> v[NV][2];
+    __device__ __forceinline__ void load(const T* row, const Place<T, W> (&at)[NV]) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            v[j][0].load(row + at[j].e0);
+            v[j][1].load(row + at[j].e1);
+        }
+    }
+    __device__ __forceinline__ void get(const Place<T, W> (&at)[NV], float (&to)[NV][2 * W]) const {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                to[j][i] = at[j].on ? v[j][0].get(i) : 0.f;
+                to[j][W + i] = at[j].two ? v[j][1].get(i) : 0.f;
+            }
+    }
+};
+
 template <class T, int W, bool HALVES, bool BWD>
 __global__ __launch_bounds__(kQkThreads) void qknorm_kernel(QkArgs a) {
     constexpr int NV = W == 1 ? 2 : 1, E = 2 * W;   // vectors of pairs of a lane, values of one
-    __shared__ float red[BWD ? kQkWaves : 1][2][256];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, L = 1 << a.lanes_log;
-    const int sub = lane & (L - 1), first_row = lane >> a.lanes_log, rows_step = 64 >> a.lanes_log;
+    constexpr int kAngles = 64 * W * NV;            // of a wave, at most
+    __shared__ __attribute__((aligned(16))) float turns[kQkWaves][2][kAngles];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), L = 1 << a.lanes_log, half = a.rot / 2;
+    const int sub = lane & (L - 1), team = lane >> a.lanes_log;
+    const int rows_log = 6 - a.lanes_log - a.tokens_log;        // of the teams of a token
+    const int my_token = team >> rows_log, my_row = team & ((1 << rows_log) - 1);
     Place<T, W> at[NV];
-    float gamma[2][NV][E], sums[2][NV][E];
+    float sums[2][NV][E];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         at[j].set((sub + j * L) * W, HALVES, a.d, a.rot);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            at[j].load_gamma(a.t[k].gamma, gamma[k][j]);
-#pragma unroll
-            for (int i = 0; i < E; ++i) sums[k][j][i] = 0.f;
-        }
+        for (int i = 0; i < E; ++i) sums[0][j][i] = sums[1][j][i] = 0.f;
     }
     const float inv_d = 1.f / (float)a.d;
     for (long long unit = (long long)blockIdx.x * kQkWaves + wave; unit < a.units; unit += (long long)gridDim.x * kQkWaves) {
-        const long long token = unit / a.parts, b = token / a.T, t = token - b * a.T;
-        const unsigned row0 = (unsigned)(unit - token * a.parts) * a.rows_unit;
-        const unsigned row1 = row0 + a.rows_unit < a.rows ? row0 + a.rows_unit : a.rows;
-        const bool there = !a.lengths || t < a.lengths[b];
-        float c[NV][W], s[NV][W];
-        if (there && a.rot) {
-            const double pos = !a.positions ? (double)t : a.each ? (double)a.positions[token] : (double)a.positions[b] + (double)t;
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int i = 0; i < W; ++i) {
-                    const int pair = (sub + j * L) * W + i;
-                    c[j][i] = 1.f, s[j][i] = 0.f;
-                    if (2 * pair < a.rot) {
-                        double turns = pos * (double)a.freq[pair] * 0.15915494309189533577;   // 1 / (2 pi)
-                        turns -= rint(turns);
-                        sincospif((float)(2.0 * turns), &s[j][i], &c[j][i]);
-                    }
-                }
-        } else {
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int i = 0; i < W; ++i) c[j][i] = 1.f, s[j][i] = 0.f;
+        long long group = a.few ? (long long)((unsigned)unit / (unsigned)a.parts) : unit / a.parts;
+        const int step0 = (int)(unit - group * a.parts) * a.per;
+        const long long first = group << a.tokens_log, b0 = a.few ? (long long)((unsigned)first / (unsigned)a.T) : first / a.T;
+        const unsigned t_first = (unsigned)(first - b0 * a.T);
+        // sequence and place of the token that is `ahead` of the first
+        auto find = [&](unsigned ahead, long long& b, unsigned& t) {
+            const unsigned over = a.tokens_log ? (t_first + ahead) / (unsigned)a.T : 0;
+            b = b0 + over;
+            t = t_first + ahead - over * (unsigned)a.T;
+        };
+        const int n_angles = half << a.tokens_log;
+        for (int i = lane; i < n_angles; i += 64) {
+            const unsigned ahead = a.tokens_log ? (unsigned)i / (unsigned)half : 0, pair = i - ahead * half;
+            float sn = 0.f, cs = 1.f;
+            if (first + ahead < a.tokens) {
+                long long b;
+                unsigned t;
+                find(ahead, b, t);
+                const double pos = !a.positions ? (double)t : a.each ? (double)a.positions[first + ahead] : (double)a.positions[b] + (double)t;
+                double part = pos * (double)a.freq[pair] * 0.15915494309189533577;   // 1 / (2 pi)
+                part -= rint(part);
+                sincospif((float)(2.0 * part), &sn, &cs);
+            }
+            turns[wave][0][i] = cs;
+            turns[wave][1][i] = sn;
         }
-        for (unsigned first = row0; first < row1; first += rows_step) {
-            const bool mine = first + first_row < row1;
-            const unsigned row = mine ? first + first_row : row1 - 1;   // lanes without a row work on the last one and write nothing
-            const unsigned p = row / (unsigned)a.H, hh = row - p * (unsigned)a.H;
-            const int k = hh < (unsigned)a.Hq ? 0 : 1;
-            const QkTensor& q = a.t[0];
-            const QkTensor& w = a.t[1];
-            const long long h = k ? hh - (unsigned)a.Hq : hh;
-            const gleam_seq_strides sx = k ? w.sx : q.sx, so = k ? w.so : q.so;
-            const long long off_x = b * sx.b + t * sx.t + p * sx.p + h * sx.h, off_o = b * so.b + t * so.t + p * so.p + h * so.h;
-            T* out = (T*)(k ? w.out : q.out) + (BWD ? off_x : off_o);
-            float v[NV][E], g[NV][E];
-            if (!there) {
+        __builtin_amdgcn_wave_barrier();
+        float c[NV][W], s[NV][W];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int pair = (sub + j * L) * W, from = my_token * half + pair;
+            const bool turned = 2 * pair < a.rot;
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                c[j][i] = turned ? turns[wave][0][from + i] : 1.f;
+                s[j][i] = turned ? turns[wave][1][from + i] : 0.f;
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+        long long b;
+        unsigned t;
+        find((unsigned)my_token, b, t);
+        const bool exists = first + my_token < a.tokens, there = exists && (!a.lengths || (int)t < a.lengths[b]);
+        const bool any = __ballot(there) != 0;
+        if (!exists) b = b0, t = t_first;   // work on the first token, and nothing is written
+        auto tensor = [&](auto which) {
+            constexpr int k = decltype(which)::value;
+            const QkTensor& q = a.t[k];
+            const int from = step0 - (k ? a.t[0].steps : 0), lo = from < 0 ? 0 : from, hi = from + a.per < q.steps ? from + a.per : q.steps;
+            if (lo >= hi) return;
+            float gamma[NV][E];
+#pragma unroll
+            for (int j = 0; j < NV; ++j) at[j].load_gamma(q.gamma, gamma[j]);
+            const long long base_x = b * q.sx.b + t * q.sx.t, base_o = b * q.so.b + t * q.so.t;
+            // offsets of the row of a step; a lane without one works on the token's last row and writes nothing
+            auto place = [&](int step, long long& off_x, long long& off_o) {
+                const unsigned row = ((unsigned)step << rows_log) + my_row, r = row < q.rows ? row : q.rows - 1;
+                const unsigned p = q.magic ? __umulhi(r, q.magic) >> q.shift : r;
+                const long long h = r - p * q.heads;
+                off_x = base_x + p * q.sx.p + h * q.sx.h;
+                off_o = base_o + p * q.so.p + h * q.so.h;
+                return row < q.rows && exists;
+            };
+            if (!any) {   // tokens behind their sequences' ends
+                for (int step = lo; step < hi; ++step) {
+                    long long off_x, off_o;
+                    const bool mine = place(step, off_x, off_o);
+                    const float none[E] = {};
+#pragma unroll
+                    for (int j = 0; j < NV; ++j)
+                        if (mine) at[j].store((T*)q.out + (BWD ? off_x : off_o), none);
+                }
+                return;
+            }
+            Row<T, W, NV> next_x, next_g;
+            long long next_at_x, next_at_o;
+            bool next_mine = place(lo, next_at_x, next_at_o);
+            next_x.load((const T*)q.x + next_at_x, at);
+            if (BWD) next_g.load((const T*)q.g + next_at_o, at);
+            for (int step = lo; step < hi; ++step) {
+                float v[NV][E], g[NV][E];
+                next_x.get(at, v);
+                if (BWD) next_g.get(at, g);
+                const bool mine = next_mine;
+                T* out = (T*)q.out + (BWD ? next_at_x : next_at_o);
+                if (step + 1 < hi) {
+                    next_mine = place(step + 1, next_at_x, next_at_o);
+                    next_x.load((const T*)q.x + next_at_x, at);
+                    if (BWD) next_g.load((const T*)q.g + next_at_o, at);
+                }
+                float ss = 0.f, dot = 0.f;
 #pragma unroll
                 for (int j = 0; j < NV; ++j) {
-#pragma unroll
-                    for (int i = 0; i < E; ++i) v[j][i] = 0.f;
-                    if (mine) at[j].store(out, v[j]);
-                }
-                continue;
-            }
-            const T* x = (const T*)(k ? w.x : q.x) + off_x;
-            const T* gr = BWD ? (const T*)(k ? w.g : q.g) + off_o : nullptr;
-#pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                at[j].load(x, v[j]);
-                if (BWD) at[j].load(gr, g[j]);
-            }
-            float ss = 0.f, dot = 0.f;
-#pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                if (BWD) turn<W, HALVES>(g[j], c[j], s[j], -1.f);
-#pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    ss += v[j][i] * v[j][i];
-                    if (BWD) dot += g[j][i] * (k ? gamma[1][j][i] : gamma[0][j][i]) * v[j][i];
-                }
-            }
-            const float r = 1.f / sqrtf(team_sum(ss, a.lanes_log) * inv_d + a.eps);
-            if (!BWD) {
-#pragma unroll
-                for (int j = 0; j < NV; ++j) {
-#pragma unroll
-                    for (int i = 0; i < E; ++i) v[j][i] *= r * (k ? gamma[1][j][i] : gamma[0][j][i]);
-                    turn<W, HALVES>(v[j], c[j], s[j], 1.f);
-                    if (mine) at[j].store(out, v[j]);
-                }
-            } else {
-                const float along = r * r * (team_sum(dot, a.lanes_log) * inv_d);
-#pragma unroll
-                for (int j = 0; j < NV; ++j) {
+                    if (BWD) turn<W, HALVES>(g[j], c[j], s[j], -1.f);
 #pragma unroll
                     for (int i = 0; i < E; ++i) {
-                        const float own = mine ? g[j][i] * (v[j][i] * r) : 0.f;
-                        sums[0][j][i] += k ? 0.f : own;
-                        sums[1][j][i] += k ? own : 0.f;
-                        g[j][i] = r * (g[j][i] * (k ? gamma[1][j][i] : gamma[0][j][i]) - v[j][i] * along);
+                        ss += v[j][i] * v[j][i];
+                        if (BWD) dot += g[j][i] * gamma[j][i] * v[j][i];
                     }
-                    if (mine) at[j].store(out, g[j]);
+                }
+                const float r = __builtin_amdgcn_rsqf(team_sum(ss, a.lanes_log) * inv_d + a.eps);
+                if (!BWD) {
+#pragma unroll
+                    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+                        for (int i = 0; i < E; ++i) v[j][i] *= r * gamma[j][i];
+                        turn<W, HALVES>(v[j], c[j], s[j], 1.f);
+#pragma unroll
+                        for (int i = 0; i < E; ++i) v[j][i] = there ? v[j][i] : 0.f;
+                        if (mine) at[j].store(out, v[j]);
+                    }
+                } else {
+                    const float along = r * r * (team_sum(dot, a.lanes_log) * inv_d);
+#pragma unroll
+                    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+                        for (int i = 0; i < E; ++i) {
+                            sums[k][j][i] += mine && there ? g[j][i] * (v[j][i] * r) : 0.f;
+                            g[j][i] = there ? r * (g[j][i] * gamma[j][i] - v[j][i] * along) : 0.f;
+                        }
+                        if (mine) at[j].store(out, g[j]);
+                    }
                 }
             }
-        }
+        };
+        tensor(std::integral_constant<int, 0>{});
+        tensor(std::integral_constant<int, 1>{});
     }
     if constexpr (BWD) {
         if (!a.part) return;
+        float (*red)[2][256] = (float (*)[2][256])turns;   // [wave][tensor][column]
+        static_assert(sizeof(turns) >= kQkWaves * 2 * 256 * sizeof(float) || W < 4, "the sums meet in the same memory");
+        __shared__ float more[W < 4 ? kQkWaves : 1][2][256];
+        if (W < 4) red = more;
+        __syncthreads();
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -212,7 +275,7 @@ __global__ __launch_bounds__(kQkThreads) void qknorm_kernel(QkArgs a) {
                 for (int i = 0; i < E; ++i) {
                     float v = sums[k][j][i];
                     for (int o = L; o < 64; o *= 2) v += __shfl_xor(v, o);
-                    if (first_row == 0 && at[j].on && (i < W || at[j].two)) red[wave][k][i < W ? at[j].e0 + i : at[j].e1 + i - W] = v;
+                    if (team == 0 && at[j].on && (i < W || at[j].two)) red[wave][k][i < W ? at[j].e0 + i : at[j].e1 + i - W] = v;
                 }
         __syncthreads();
         for (int e = threadIdx.x; e < 2 * a.d; e += kQkThreads) {
@@ -225,17 +288,22 @@ __global__ __launch_bounds__(kQkThreads) void qknorm_kernel(QkArgs a) {
     }
 }
 
-// Sums of the partial sums: 16 columns a workgroup, 16 lanes of each.
-__global__ __launch_bounds__(256) void qknorm_sums_kernel(const float* part, int groups, int d, float* g_q, float* g_k) {
-    __shared__ float red[16][17];
+// Sums of the partial sums: 16 columns a workgroup, 64 lanes of each.
+__global__ __launch_bounds__(1024) void qknorm_sums_kernel(const float* part, int groups, int d, float* g_q, float* g_k) {
+    __shared__ float red[64][17];
     const int col = threadIdx.x & 15, slice = threadIdx.x >> 4, e = blockIdx.x * 16 + col;
     float v = 0.f;
     if (e < 2 * d)
-        for (int g = slice; g < groups; g += 16) v += part[(long long)g * 2 * d + e];
+#pragma unroll 4
+        for (int g = slice; g < groups; g += 64) v += part[(long long)g * 2 * d + e];
     red[slice][col] = v;
     __syncthreads();
+    if (slice >= 4) return;
+    for (int i = slice + 4; i < 64; i += 4) v += red[i][col];
+    red[slice][col] = v;
+    __builtin_amdgcn_wave_barrier();
     if (slice || e >= 2 * d) return;
-    for (int i = 1; i < 16; ++i) v += red[i][col];
+    v = (red[0][col] + red[1][col]) + (red[2][col] + red[3][col]);
     float* out = e < d ? g_q : g_k;
     if (out) out[e < d ? e : e - d] = v;
 }
@@ -248,8 +316,7 @@ int vector_of(const gleam_qknorm_desc& d) {
 }
 
 struct QkPlan {
-    int w, lanes_log;
-    unsigned rows, rows_unit, parts;
+    int w, lanes_log, tokens_log, steps[2], per, parts;
     long long units, groups;
 };
 QkPlan plan_of(const gleam_qknorm_desc& d, bool backward) {
@@ -257,15 +324,30 @@ QkPlan plan_of(const gleam_qknorm_desc& d, bool backward) {
     p.w = vector_of(d);
     const int nv = p.w == 1 ? 2 : 1, lanes = ((d.d + 1) / 2 + nv * p.w - 1) / (nv * p.w);
     for (p.lanes_log = 0; 1 << p.lanes_log < lanes;) ++p.lanes_log;
-    p.rows = (unsigned)(d.P * (d.q_heads + d.k_heads));
-    const long long step = 64 >> p.lanes_log, steps = (p.rows + step - 1) / step, tokens = d.B * d.T;
+    const long long tokens = d.B * d.T, rows[2] = {d.P * d.q_heads, d.P * d.k_heads};
+    // Teams of a token: as many as leave the fewest without a row, the most of these; with fewer, a wave takes several tokens.
+    long long best = -1;
+    for (int log = 0; log <= 6 - p.lanes_log; ++log) {
+        const long long teams = 1LL << log, taken = ((rows[0] + teams - 1) / teams + (rows[1] + teams - 1) / teams) * teams;
+        if (best < 0 || taken <= best) {
+            best = taken;
+            p.tokens_log = 6 - p.lanes_log - log;
+            p.steps[0] = (int)((rows[0] + teams - 1) / teams);
+            p.steps[1] = (int)((rows[1] + teams - 1) / teams);
+        }
+    }
+    while (p.tokens_log > 0 && tokens < 1LL << p.tokens_log) {   // no more tokens than there are
+        --p.tokens_log;
+        const long long teams = 1LL << (6 - p.lanes_log - p.tokens_log);
+        for (int k = 0; k < 2; ++k) p.steps[k] = (int)((rows[k] + teams - 1) / teams);
+    }
+    const long long steps = (long long)p.steps[0] + p.steps[1], groups = (tokens + (1LL << p.tokens_log) - 1) >> p.tokens_log;
     // up to 16 steps of a wave share the angles, fewer where waves would be missing
-    long long per = steps * tokens / 16384;
+    long long per = steps * groups / 8192;
     per = per < 1 ? 1 : per > 16 ? 16 : per;
-    per = per < steps ? per : steps;
-    p.rows_unit = (unsigned)(per * step);
-    p.parts = (unsigned)((steps + per - 1) / per);
-    p.units = tokens * p.parts;
+    p.per = (int)(per < steps ? per : steps);
+    p.parts = (int)((steps + p.per - 1) / p.per);
+    p.units = groups * p.parts;
     const long long most = backward ? kQkGroupsBwd : kQkGroupsFwd, all = (p.units + kQkWaves - 1) / kQkWaves;
     p.groups = all < most ? all : most;
     return p;
@@ -299,17 +381,29 @@ QkArgs args_of(const gleam_qknorm_desc& d, const QkPlan& p, const void* q, const
     a.freq = freq;
     a.positions = positions;
     a.lengths = lengths;
+    for (int k = 0; k < 2; ++k) {
+        QkTensor& t = a.t[k];
+        t.heads = (unsigned)(k ? d.k_heads : d.q_heads);
+        t.rows = (unsigned)(d.P * t.heads);
+        t.steps = p.steps[k];
+        if (t.heads > 1) {   // n / h = n ceil(2^(31 + l) / h) >> (31 + l) of n < 2^31, 2^(l - 1) < h <= 2^l
+            unsigned l = 1;
+            while (1ull << l < t.heads) ++l;
+            t.magic = (unsigned)(((1ull << (31 + l)) + t.heads - 1) / t.heads);
+            t.shift = l - 1;
+        }
+    }
     a.T = d.T;
+    a.tokens = d.B * d.T;
     a.units = p.units;
-    a.rows = p.rows;
-    a.rows_unit = p.rows_unit;
+    a.per = p.per;
     a.parts = p.parts;
+    a.few = p.units < 0x7fffffff && a.tokens < 0x7fffffff;
     a.d = d.d;
     a.rot = d.rot;
-    a.H = d.q_heads + d.k_heads;
-    a.Hq = d.q_heads;
     a.each = d.each;
     a.lanes_log = p.lanes_log;
+    a.tokens_log = p.tokens_log;
     a.eps = d.eps;
     return a;
 }
@@ -322,7 +416,7 @@ hipError_t qknorm_forward(const gleam_qknorm_desc& d, const void* q, const void*
     QkArgs a = args_of(d, p, q, k, gamma_q, gamma_k, freq, positions, lengths);
     a.t[0].out = q_out;
     a.t[1].out = k_out;
-    const double size = (double)d.B * d.T * p.rows * d.d;
+    const double size = (double)d.B * d.T * d.P * (d.q_heads + d.k_heads) * d.d;
     KernelScope ks("qknorm_fwd", 8.0 * size, 2.0 * (d.dtype ? 2 : 4) * size, st);
     if (d.dtype) launch<unsigned short, false>(a, p, !d.pairs, st);
     else launch<float, false>(a, p, !d.pairs, st);
@@ -342,7 +436,7 @@ hipError_t qknorm_backward(const gleam_qknorm_desc& d, const void* q, const void
     a.t[1].out = g_k;
     a.part = g_gamma_q || g_gamma_k ? (float*)ws : nullptr;
     {
-        const double size = (double)d.B * d.T * p.rows * d.d;
+        const double size = (double)d.B * d.T * d.P * (d.q_heads + d.k_heads) * d.d;
         KernelScope ks("qknorm_bwd", 16.0 * size, 3.0 * (d.dtype ? 2 : 4) * size, st);
         if (d.dtype) launch<unsigned short, true>(a, p, !d.pairs, st);
         else launch<float, true>(a, p, !d.pairs, st);
@@ -350,7 +444,7 @@ hipError_t qknorm_backward(const gleam_qknorm_desc& d, const void* q, const void
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.part) return e;
     KernelScope ks("qknorm_sums", 0.0, 8.0 * p.groups * d.d, st);
-    hipLaunchKernelGGL(qknorm_sums_kernel, dim3((unsigned)((2 * d.d + 15) / 16)), dim3(256), 0, st, a.part, (int)p.groups, d.d, g_gamma_q, g_gamma_k);
+    hipLaunchKernelGGL(qknorm_sums_kernel, dim3((unsigned)((2 * d.d + 15) / 16)), dim3(1024), 0, st, a.part, (int)p.groups, d.d, g_gamma_q, g_gamma_k);
     return hipGetLastError();
 }
 
