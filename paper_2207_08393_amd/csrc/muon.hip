@@ -249,56 +249,58 @@ __device__ __forceinline__ bool find_tile(const MuonArgs& a, int tr, int tc, Til
 
 // One of the three products of a step, rows of the left operand against rows of the right one:
 //   kGram  A = X X^T;   kSquare  B = a I + b A + c A A;   kApply  X <- B X, or at the last step the weights' update.
-// A workgroup computes WR x WC blocks of 32 x 32 over one of `splits` parts of the sum, and each of its four waves all of them over a quarter of that: no
+// A workgroup computes 2 x 2 blocks of 32 x 32 over one of `splits` parts of the sum, and each of its four waves all of them over a quarter of that: no
 // operand is needed by two waves, so they go from memory into registers as they lie there, kAhead steps of 16 columns before their use, with
-// no barrier until the four sums meet in LDS.
+// no barrier until the four sums meet in LDS.  Short sums (SHORT) are not shared out: a wave computes one block, and the waves do not meet.
 constexpr int kProducts = 3;
 __device__ constexpr int kPartA[kProducts] = {1, 0, 0}, kPartB[kProducts] = {0, 1, 0};   // small ones first
 
-template <int MODE, int WR, int WC>
+template <int MODE, bool SHORT>
 __global__ __launch_bounds__(256, 2) void muon_product_kernel(MuonArgs a) {
-    constexpr int kAhead = 3, kBlocks = WR * WC;
-    static_assert(kBlocks == 4, "a wave sums one block");
-    __shared__ __attribute__((aligned(16))) float lds[4][kBlocks][kTileFloats];
+    constexpr int kAhead = 3, W = SHORT ? 1 : 2;   // blocks of a wave's sides
+    __shared__ __attribute__((aligned(16))) float lds[4][SHORT ? 1 : 4][kTileFloats];
     const int R = a.mb, Cb = MODE == kApply ? a.nb : a.mb, K = MODE == kGram ? a.nb : a.mb;   // blocks of the result's sides and of the sum
     Tile t;
-    if (!find_tile<MODE>(a, (R + WR - 1) / WR, (Cb + WC - 1) / WC, t)) return;
+    if (!find_tile<MODE>(a, (R + 1) / 2, (Cb + 1) / 2, t)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const char* left = MODE == kGram ? a.x : MODE == kSquare ? a.a : a.b;
     const char* right = MODE == kGram ? a.x : MODE == kSquare ? a.a : a.xt;
-    const int part = t.split * 4 + wave, parts = a.splits * 4;
+    const int part = SHORT ? 0 : t.split * 4 + wave, parts = SHORT ? 1 : a.splits * 4;
+    const int bi = 2 * t.ti + (wave >> 1), bj = 2 * t.tj + (wave & 1);   // the block that this wave writes
+    const bool mine = bi < R && bj < Cb && (MODE == kApply || bi <= bj);
+    if (SHORT && !mine) return;
     const int k0 = (int)((long long)2 * K * part / parts), k1 = (int)((long long)2 * K * (part + 1) / parts);   // steps
-    const char *pl[WR], *pr[WC];   // blocks past the end: the last one's, computed and not written
+    const char *pl[W], *pr[W];   // blocks past the end: the last one's, computed and not written
 #pragma unroll
-    for (int w = 0; w < WR; ++w) pl[w] = block_at((char*)left, t.matrix, R, K, min(t.ti * WR + w, R - 1), k0, 0) + lane * 16;
+    for (int w = 0; w < W; ++w) pl[w] = block_at((char*)left, t.matrix, R, K, SHORT ? bi : min(2 * t.ti + w, R - 1), k0, 0) + lane * 16;
 #pragma unroll
-    for (int w = 0; w < WC; ++w) pr[w] = block_at((char*)right, t.matrix, Cb, K, min(t.tj * WC + w, Cb - 1), k0, 0) + lane * 16;
-    floatx16 acc[WR][WC];
+    for (int w = 0; w < W; ++w) pr[w] = block_at((char*)right, t.matrix, Cb, K, SHORT ? bj : min(2 * t.tj + w, Cb - 1), k0, 0) + lane * 16;
+    floatx16 acc[W][W];
 #pragma unroll
-    for (int i = 0; i < WR; ++i)
+    for (int i = 0; i < W; ++i)
 #pragma unroll
-        for (int j = 0; j < WC; ++j)
+        for (int j = 0; j < W; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
     const int steps = MODE == kSquare && a.no_square ? 0 : k1 - k0;
-    halfx8 l[kAhead][WR][kParts], r[kAhead][WC][kParts];
+    halfx8 l[kAhead][W][kParts], r[kAhead][W][kParts];
     auto load = [&](int k, int at) {
         const int off = min(k, steps - 1) * (kParts * kBlockBytes);   // past the end: the last again, not used
 #pragma unroll
         for (int p = 0; p < kParts; ++p) {
 #pragma unroll
-            for (int w = 0; w < WR; ++w) l[at][w][p] = *(const halfx8*)(pl[w] + off + p * kBlockBytes);
+            for (int w = 0; w < W; ++w) l[at][w][p] = *(const halfx8*)(pl[w] + off + p * kBlockBytes);
 #pragma unroll
-            for (int w = 0; w < WC; ++w) r[at][w][p] = *(const halfx8*)(pr[w] + off + p * kBlockBytes);
+            for (int w = 0; w < W; ++w) r[at][w][p] = *(const halfx8*)(pr[w] + off + p * kBlockBytes);
         }
     };
     auto multiply = [&](int at) {
 #pragma unroll
         for (int q = 0; q < kProducts; ++q)
 #pragma unroll
-            for (int i = 0; i < WR; ++i)
+            for (int i = 0; i < W; ++i)
 #pragma unroll
-                for (int j = 0; j < WC; ++j)
+                for (int j = 0; j < W; ++j)
                     acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[at][i][kPartA[q]], r[at][j][kPartB[q]], acc[i][j], 0, 0, 0);
     };
     if (steps > 0) {
@@ -311,9 +313,9 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(MuonArgs a) {
                 load(k + i + kAhead - 1, (i + kAhead - 1) % kAhead);
                 multiply(i);
 #pragma unroll
-                for (int j = 0; j < kProducts * WR * WC; ++j) {
+                for (int j = 0; j < kProducts * W * W; ++j) {
                     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                    if (j < kParts * (WR + WC)) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+                    if (j < kParts * 2 * W) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -321,37 +323,41 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(MuonArgs a) {
         for (int i = 0; i < kAhead - 1; ++i)
             if (k + i < steps) multiply(i);
     }
+    if constexpr (!SHORT)
 #pragma unroll
-    for (int i = 0; i < WR; ++i)
+        for (int i = 0; i < W; ++i)
 #pragma unroll
-        for (int j = 0; j < WC; ++j)
+            for (int j = 0; j < W; ++j)
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *(floatx4*)(lds[wave][i * WC + j] + (q * 64 + lane) * 4) = floatx4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-    const int bi = t.ti * WR + wave / WC, bj = t.tj * WC + wave % WC;   // this wave's block from here on
-    const bool mine = bi < R && bj < Cb && (MODE == kApply || bi <= bj);
+                for (int q = 0; q < 4; ++q)
+                    *(floatx4*)(lds[wave][i * W + j] + (q * 64 + lane) * 4) = floatx4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
     floatx16 sum;
     if (MODE == kSquare && t.split == 0 && mine) sum = start_of_square(a, t.matrix, bi, bj);
     else
 #pragma unroll
         for (int i = 0; i < 16; ++i) sum[i] = 0.f;
-    __syncthreads();
-    if (!mine) return;
+    if constexpr (SHORT) {
 #pragma unroll
-    for (int w = 0; w < 4; ++w)
+        for (int i = 0; i < 16; ++i) sum[i] += acc[0][0][i];
+    } else {
+        __syncthreads();
+        if (!mine) return;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const floatx4 v = *(const floatx4*)(lds[w][wave] + (q * 64 + lane) * 4);
+        for (int w = 0; w < 4; ++w)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum[4 * q + e] += v[e];
-        }
-    if (a.splits > 1) {   // as the registers have it: [tile][split][block][four registers][lane]
-        float* to = a.part + ((t.tile * a.splits + t.split) * kBlocks + wave) * 1024 + lane * 4;
+            for (int q = 0; q < 4; ++q) {
+                const floatx4 v = *(const floatx4*)(lds[w][wave] + (q * 64 + lane) * 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[4 * q + e] += v[e];
+            }
+    }
+    if (!SHORT && a.splits > 1) {   // as the registers have it: [tile][split][block][four registers][lane]
+        float* to = a.part + ((t.tile * a.splits + t.split) * 4 + wave) * 1024 + lane * 4;
 #pragma unroll
         for (int q = 0; q < 4; ++q) *(floatx4*)(to + q * 256) = floatx4{sum[4 * q], sum[4 * q + 1], sum[4 * q + 2], sum[4 * q + 3]};
         return;
     }
-    float* tile = lds[wave][wave];   // read by this wave alone
+    float* tile = lds[wave][SHORT ? 0 : wave];   // read by this wave alone
     __builtin_amdgcn_wave_barrier();
     stage_block(sum, tile);
     __builtin_amdgcn_wave_barrier();
@@ -359,18 +365,18 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(MuonArgs a) {
 }
 
 // Sums the parts of a split product, a wave a block, in order.
-template <int MODE, int WR, int WC>
+template <int MODE>
 __global__ __launch_bounds__(64) void muon_join_kernel(MuonArgs a) {
     __shared__ float lds[kTileFloats];
-    constexpr int kBlocks = WR * WC;
-    const int R = a.mb, Cb = MODE == kApply ? a.nb : a.mb, tr = (R + WR - 1) / WR, tc = (Cb + WC - 1) / WC;
+    constexpr int kBlocks = 4;
+    const int R = a.mb, Cb = MODE == kApply ? a.nb : a.mb, tr = (R + 1) / 2, tc = (Cb + 1) / 2;
     const unsigned id = (unsigned)group_of_grid(), tile_id = id / kBlocks, per = MODE == kApply ? tr * tc : tr * (tr + 1) / 2;
     const unsigned matrix = tile_id / per;
     if (matrix >= (unsigned)a.count) return;
     const int block = (int)(id - tile_id * kBlocks), at = (int)(tile_id - matrix * per);
     Tile t;
     place_tile<MODE>(at, tr, t);
-    const int bi = t.ti * WR + block / WC, bj = t.tj * WC + block % WC;
+    const int bi = 2 * t.ti + (block >> 1), bj = 2 * t.tj + (block & 1);
     if (bi >= R || bj >= Cb || (MODE != kApply && bi > bj)) return;
     const float* part = a.part + (long long)tile_id * a.splits * (kBlocks * 1024) + block * 1024 + (threadIdx.x & 63) * 4;
     floatx16 acc;
@@ -390,8 +396,181 @@ __global__ __launch_bounds__(64) void muon_join_kernel(MuonArgs a) {
     put_block<MODE>(a, matrix, bi, bj, lds);
 }
 
+// Small matrices, of up to 16 blocks: all of a step in one workgroup.  A wave keeps one block of X in registers, as the matrix instruction returns
+// it; parts of X by rows, then of its transpose, and of A, then of B, stand in LDS.
+constexpr int kSmallBlocks = 16, kSmallLds = 32 * 2 * kParts * kBlockBytes;
+bool is_small(int mb, int nb) { return mb * nb <= kSmallBlocks && mb * nb + mb * mb <= 32; }
+
+// The lane, as a number that is not known to stay the same: addresses made of it are worked out where they are used, and not kept through the loop
+// over the steps (they were more than there are registers).
+__device__ __forceinline__ int lane_now() {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+// Rows r of `left` against rows c of `right`, both of K blocks.
+__device__ __forceinline__ floatx16 small_product(const char* left, int r, const char* right, int c, int K, floatx16 acc) {
+    const int lane = lane_now();
+    const char *pl = left + r * 2 * K * kParts * kBlockBytes + lane * 16, *pr = right + c * 2 * K * kParts * kBlockBytes + lane * 16;
+#pragma unroll 4
+    for (int k = 0; k < 2 * K; ++k) {
+        halfx8 l[kParts], rt[kParts];
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) {
+            l[p] = *(const halfx8*)(pl + (k * kParts + p) * kBlockBytes);
+            rt[p] = *(const halfx8*)(pr + (k * kParts + p) * kBlockBytes);
+        }
+#pragma unroll
+        for (int q = 0; q < kProducts; ++q) acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[kPartA[q]], rt[kPartB[q]], acc, 0, 0, 0);
+    }
+    return acc;
+}
+// The parts of a block (bi, bj) of registers: by columns (rows of the transpose, K blocks each), and by rows.
+__device__ __forceinline__ void small_across(char* base, int K, int bi, int bj, const floatx16& v) {
+    const int lane = lane_now(), col = lane & 31, up = lane >> 5;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        halfx4 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            hi[e] = (_Float16)v[4 * q + e];
+            lo[e] = (_Float16)(v[4 * q + e] - (float)hi[e]);
+        }
+        char* to = base + ((bj * 2 * K + 2 * bi + (q >> 1)) * kParts) * kBlockBytes + (q & 1) * 512 + col * 16 + up * 8;
+        *(halfx4*)to = hi;
+        *(halfx4*)(to + kBlockBytes) = lo;
+    }
+}
+// The transpose of a block, in the same registers, through 4 KB where column c of row r stands at c ^ r, so that neither a row nor a column is on
+// one bank.
+__device__ __forceinline__ floatx16 turned_block(float* tile, const floatx16& v) {
+    const int lane = lane_now(), line = lane & 31, up = lane >> 5;
+    floatx16 to;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int row = 8 * (i >> 2) + 4 * up + (i & 3);
+        tile[row * 32 + (line ^ row)] = v[i];
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int row = 8 * (i >> 2) + 4 * up + (i & 3);
+        to[i] = tile[line * 32 + (row ^ line)];
+    }
+    __builtin_amdgcn_wave_barrier();
+    return to;
+}
+// By rows: through the block's own 4 KB (its two times 16 columns and parts lie in a row), as above.
+__device__ __forceinline__ void small_along(char* base, int K, int bi, int bj, const floatx16& v) {
+    const int lane = lane_now(), line = lane & 31, up = lane >> 5;
+    char* block = base + ((bi * 2 * K + 2 * bj) * kParts) * kBlockBytes;
+    float* tile = (float*)block;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int row = 8 * (i >> 2) + 4 * up + (i & 3);
+        tile[row * 32 + (line ^ row)] = v[i];
+    }
+    __builtin_amdgcn_wave_barrier();
+    float w[2][8];
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[g][e] = tile[line * 32 + ((8 * (up + 2 * g) + e) ^ line)];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int g = 0; g < 2; ++g) store_parts8(block + g * kParts * kBlockBytes + up * 512 + line * 16, w[g]);
+}
+
+__global__ __launch_bounds__(64 * kSmallBlocks) void muon_small_kernel(MuonArgs a, int steps) {
+    __shared__ __attribute__((aligned(16))) char lds[kSmallLds];
+    __shared__ double norms[kSmallBlocks];
+    const long long matrix = group_of_grid();
+    if (matrix >= a.count) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+    const int mb = a.mb, nb = a.nb, bi = wave / nb, bj = wave - bi * nb;
+    const bool mine = wave < mb * nb;                       // of X; the others may have a block of A
+    Tile t;
+    place_tile<kGram>(wave, mb, t);
+    const bool of_a = wave < mb * (mb + 1) / 2;
+    char *xs = lds, *as = lds + mb * nb * 2 * kParts * kBlockBytes;
+    // this lane's elements of u as they lie in memory: column lane % 32, rows 8 q + 4 (lane / 32) + e of a block that is X's or its transpose
+    const int r0 = 32 * (a.tall ? bj : bi) + 4 * (lane >> 5), c = 32 * (a.tall ? bi : bj) + (lane & 31);
+    auto row_of = [&](int i) { return r0 + 8 * (i >> 2) + (i & 3); };
+    auto in = [&](int i) { return mine && c < a.cols && row_of(i) < a.rows; };
+    auto at = [&](int i) { return in(i) ? row_of(i) * a.cols + c : 0; };
+    const float* g = a.grad + matrix * a.stride;
+    float *m = a.m + matrix * a.stride, *theta = a.theta + matrix * a.stride;
+    char* own = xs + (mine ? wave : 0) * 2 * kParts * kBlockBytes;   // 4 KB
+    floatx16 x;
+    {
+        float gv[16], mv[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) gv[i] = g[at(i)], mv[i] = m[at(i)];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float now = __builtin_fmaf(a.momentum, mv[i], gv[i]);
+            if (in(i)) m[at(i)] = now;
+            x[i] = in(i) ? (a.nesterov ? __builtin_fmaf(a.momentum, now, gv[i]) : now) : 0.f;
+        }
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum += (double)x[i] * (double)x[i];
+    for (int o = 1; o < 64; o *= 2) sum += __shfl_xor(sum, o);
+    if (lane == 0) norms[wave] = sum;
+    __syncthreads();
+    sum = 0.0;
+    for (int w = 0; w < waves; ++w) sum += norms[w];
+    const float scale = (float)((double)a.x_scale / (sqrt(sum) + (double)a.eps));
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] *= scale;
+    if (a.tall && mine) x = turned_block((float*)own, x);
+    const floatx16 zero = {};
+    for (int s = 0;; ++s) {
+        if (mine) small_along(xs, nb, bi, bj, x);
+        __syncthreads();
+        floatx16 av = zero;
+        if (of_a) {
+            av = small_product(xs, t.ti, xs, t.tj, nb, zero);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) av[i] *= a.gram_scale;
+            if (t.ti != t.tj) small_along(as, mb, t.ti, t.tj, av);
+            small_across(as, mb, t.ti, t.tj, av);
+        }
+        __syncthreads();   // A is there, and X has been read
+        if (mine) small_across(xs, mb, bi, bj, x);
+        if (of_a) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) av[i] *= a.cb;
+            if (!a.no_square) av = small_product(as, t.ti, as, t.tj, mb, av);
+        }
+        __syncthreads();   // A has been read
+        if (of_a) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) av[i] = a.cc * av[i] + (t.ti == t.tj && 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) == (lane & 31) ? a.ca : 0.f);
+            if (t.ti != t.tj) small_along(as, mb, t.ti, t.tj, av);
+            small_across(as, mb, t.ti, t.tj, av);
+        }
+        __syncthreads();
+        if (mine) x = small_product(as, bi, xs, bj, mb, zero);
+        if (s + 1 == steps) break;
+        __syncthreads();   // B and the transpose of X have been read
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] *= a.apply_scale;
+    }
+    __syncthreads();
+    if (a.tall && mine) x = turned_block((float*)own, x);
+    float old[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) old[i] = theta[at(i)];
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (in(i)) theta[at(i)] = a.decay * old[i] - a.lr_scale * x[i];
+}
+
 // Tiles of 64 x 64, and parts of the sum: a product of few tiles is split so that every CU has a workgroup, no part under eight steps of 32 columns.
 struct ProductPlan {
+    bool is_short;            // sums of up to eight steps of 32 columns
     int splits;
     long long tiles;          // of a matrix
 };
@@ -402,6 +581,7 @@ ProductPlan product_plan(long long count, int mb, int nb, MuonProduct mode) {
     long long s = 256 / (count * p.tiles);
     if (s > steps / 8) s = steps / 8;
     p.splits = (int)(s < 1 ? 1 : s > 32 ? 32 : s);
+    p.is_short = p.splits == 1 && steps <= 8;
     return p;
 }
 size_t part_bytes(long long count, const ProductPlan& p) { return p.splits > 1 ? (size_t)count * p.tiles * p.splits * 4 * 4096 : 0; }
@@ -435,11 +615,13 @@ void launch_product(MuonArgs& a, hipStream_t st) {
     a.splits = p.splits;
     {
         KernelScope ks(MODE == kGram ? "muon_gram" : MODE == kSquare ? "muon_square" : "muon_apply", work, 0.0, st, kProducts * work);
-        hipLaunchKernelGGL((muon_product_kernel<MODE, 2, 2>), grid_of((a.count * p.tiles * p.splits + 7) / 8 * 8), dim3(256), 0, st, a);
+        const dim3 grid = grid_of((a.count * p.tiles * p.splits + 7) / 8 * 8), block(256);
+        if (p.is_short) hipLaunchKernelGGL((muon_product_kernel<MODE, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((muon_product_kernel<MODE, false>), grid, block, 0, st, a);
     }
     if (p.splits == 1) return;
     KernelScope ks("muon_join", 0.0, (double)part_bytes(a.count, p), st);
-    hipLaunchKernelGGL((muon_join_kernel<MODE, 2, 2>), grid_of(a.count * p.tiles * 4), dim3(64), 0, st, a);
+    hipLaunchKernelGGL((muon_join_kernel<MODE>), grid_of(a.count * p.tiles * 4), dim3(64), 0, st, a);
 }
 
 }  // namespace
@@ -474,6 +656,7 @@ bool muon_scales(const gleam_muon& p, double& sx, double& sa, double& sb) {
 
 size_t muon_ws_bytes(long long count, long long rows, long long cols) {
     const MuonPlan p = plan_of(count, rows, cols);
+    if (is_small(p.mb, p.nb)) return 0;
     return 3 * p.x_bytes + 2 * p.a_bytes + p.norm_bytes + p.part_bytes;
 }
 
@@ -515,6 +698,11 @@ hipError_t muon_update(const gleam_muon& h, long long count, long long rows, lon
     a.ca = (float)(h.a * sb);
     a.cb = (float)(a.no_square ? sa : sa * (double)h.b / (double)h.c);
     a.cc = (float)((a.no_square ? h.b : h.c) * (sb / (sa * sa)));
+    if (is_small(p.mb, p.nb)) {
+        KernelScope ks("muon_small", (double)count * h.steps * 65536.0 * p.mb * (p.mb * p.nb + (p.mb + 1) * 0.5 * (p.nb + p.mb)), 20.0 * count * rows * cols, st);
+        hipLaunchKernelGGL(muon_small_kernel, grid_of(count), dim3(64 * std::max(p.mb * p.nb, p.mb * (p.mb + 1) / 2)), 0, st, a, (int)h.steps);
+        return hipGetLastError();
+    }
     {
         KernelScope ks("muon_momentum", 4.0 * count * rows * cols, 12.0 * count * rows * cols, st);
         hipLaunchKernelGGL(muon_momentum_kernel, grid_of(count * p.parts), dim3(256), 0, st, a);

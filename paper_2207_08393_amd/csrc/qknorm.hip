@@ -342,11 +342,12 @@ QkPlan plan_of(const gleam_qknorm_desc& d, bool backward) {
         for (int k = 0; k < 2; ++k) p.steps[k] = (int)((rows[k] + teams - 1) / teams);
     }
     const long long steps = (long long)p.steps[0] + p.steps[1], groups = (tokens + (1LL << p.tokens_log) - 1) >> p.tokens_log;
-    // up to 16 steps of a wave share the angles, fewer where waves would be missing
-    long long per = steps * groups / 8192;
-    per = per < 1 ? 1 : per > 16 ? 16 : per;
-    p.per = (int)(per < steps ? per : steps);
-    p.parts = (int)((steps + p.per - 1) / p.per);
+    // up to 16 steps of a wave share the angles, fewer where waves would be missing (backward, those of the largest launch are there at once)
+    const long long waves = backward ? kQkGroupsBwd * kQkWaves : 8192;
+    long long per = (steps * groups + waves - 1) / waves;
+    per = per > 16 ? 16 : per < steps ? per : steps;
+    p.parts = (int)((steps + per - 1) / per);
+    p.per = (int)((steps + p.parts - 1) / p.parts);
     p.units = groups * p.parts;
     const long long most = backward ? kQkGroupsBwd : kQkGroupsFwd, all = (p.units + kQkWaves - 1) / kQkWaves;
     p.groups = all < most ? all : most;

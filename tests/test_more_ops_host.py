@@ -65,7 +65,7 @@ def scan(B=2, T=300, P=1, C_=6, dtype=torch.float32, **more):
 def test_gatedscan_refusals():
     L, d = gb.lib(), scan()
     fwd, bwd = gb.gleam_gatedscan_workspace_bytes(d)
-    assert fwd > 0 and bwd > fwd and fwd % 256 == 0 and bwd % 256 == 0
+    assert fwd > 0 and bwd > 0 and fwd % 256 == 0 and bwd % 256 == 0
     bad = [(0, None, gb.GLEAM_E_NULL)]
     bad += [(0, changed(d, **{f: v}), gb.GLEAM_E_DESC) for f, v in (("dtype", 2), ("kappa", -1.0), ("kappa", float("nan")), ("kappa", float("inf")))]
     bad += [(0, changed(d, **{f: v}), gb.GLEAM_E_DIMS) for f, v in (("B", 0), ("T", 0), ("P", -1), ("C", 0), ("T", (1 << 30) + 1), ("B", 1 << 35), ("C", 1 << 31), ("P", 1 << 62),
@@ -98,19 +98,21 @@ def test_gatedscan_binding_compares_arrays():
 
 def test_muon_refusals():
     L, h = gb.lib(), gb.make_muon(0.02)
-    need = gb.gleam_muon_workspace_bytes(3, 40, 70)
+    need = gb.gleam_muon_workspace_bytes(3, 140, 170)
     assert need > 0 and need % 256 == 0
-    assert gb.gleam_muon_workspace_bytes(3, 70, 40) == need
+    assert gb.gleam_muon_workspace_bytes(3, 170, 140) == need
+    assert gb.gleam_muon_workspace_bytes(3, 40, 70) == 0                              # in one workgroup each
     n = C.c_size_t(0)
     assert L.gleam_muon_workspace_bytes(3, 40, 70, None) == gb.GLEAM_E_NULL
     for sizes in ((0, 4, 4), (1, 0, 4), (1, 4, -1), (1, 65537, 4), (1, 4, 65537), (1 << 40, 40, 70), (1 << 62, 65536, 65536)):
         assert L.gleam_muon_workspace_bytes(*sizes, C.byref(n)) == gb.GLEAM_E_DIMS
-    args = [C.byref(h), 3, 40, 70, 2800, *FAKE[:3], FAKE[3], need, None]
+    args = [C.byref(h), 3, 140, 170, 23800, *FAKE[:3], FAKE[3], need, None]
     nan, inf = float("nan"), float("inf")
     bad = [(0, changed(h, **{f: v}), gb.GLEAM_E_DESC) for f, v in (("lr", nan), ("momentum", -0.1), ("momentum", 1.0), ("momentum", nan), ("weight_decay", inf), ("eps", 0.0),
-                                                                 ("eps", nan), ("a", inf), ("b", nan), ("c", inf), ("steps", 0), ("steps", 101), ("nesterov", 2))]
+                                                                 ("eps", nan), ("a", inf), ("b", nan), ("c", inf), ("steps", 0), ("steps", 101), ("nesterov", 2), ("a", 200.0), ("c", 20000.0))]
+    assert L.gleam_muon_step(changed(h, a=200.0, steps=1), *args[1:4], 5, *args[5:]) == gb.GLEAM_E_DIMS   # one step never passes 128 before the last
     refused(L.gleam_muon_step, args, bad + [(i, None, gb.GLEAM_E_NULL) for i in (0, 5, 6, 7, 8)] +
-            [(1, 0, gb.GLEAM_E_DIMS), (2, 0, gb.GLEAM_E_DIMS), (3, 65537, gb.GLEAM_E_DIMS), (4, 2799, gb.GLEAM_E_DIMS), (4, -1, gb.GLEAM_E_DIMS), (4, 1 << 62, gb.GLEAM_E_DIMS),
+            [(1, 0, gb.GLEAM_E_DIMS), (2, 0, gb.GLEAM_E_DIMS), (3, 65537, gb.GLEAM_E_DIMS), (4, 23799, gb.GLEAM_E_DIMS), (4, -1, gb.GLEAM_E_DIMS), (4, 1 << 62, gb.GLEAM_E_DIMS),
              (6, FAKE[0], gb.GLEAM_E_DIMS), (7, FAKE[0], gb.GLEAM_E_DIMS), (7, FAKE[1], gb.GLEAM_E_DIMS), (9, need - 256, gb.GLEAM_E_WORKSPACE),
              (8, FAKE[3] + 4, gb.GLEAM_E_WORKSPACE)])
 
