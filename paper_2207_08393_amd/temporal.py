@@ -1,16 +1,19 @@
-"""A causal temporal layer for feature maps of a dynamic series: every pixel's frames are mixed by linear attention whose heads forget at
-rates of their own.
+"""Causal temporal layers for feature maps of a dynamic series: every pixel's frames are mixed by linear attention whose heads forget at
+rates of their own (TemporalLayer), or by a scan whose memory the frames themselves open and close (GatedLayer).
 
     y = layer_norm(x);  q, k, v = y W_qkv^T;  h = x + dropout(linear_attention(q, k, v) W_o^T)
+    with `rotate`, q and k are normed head by head and turned by their frame's number first
+    y = layer_norm(x);  u, r, i = y W_qkv^T;  h = x + dropout(gated_scan(u, r, i) W_o^T)
 
 x, h: [B][T][P][C], P pixels of T frames, channels last, as the prox networks hold them.  A recorded series goes through `forward` (and
 `backward` in training), a running one through `frame`, which takes the next frame of every pixel and keeps a state of fixed size instead
 of the frames before.  Both give the same result.  The projections are plain library products; everything else is
-the framework's own kernels through `binding`.  `python -m paper_2207_08393_amd.temporal` trains such a layer on a synthetic series and then
-streams it."""
+the framework's own kernels through `binding`.  `python -m paper_2207_08393_amd.temporal [rotate | gated] [muon]` trains such a layer on a synthetic
+series, its matrices by orthogonalised updates if so asked, and then streams it."""
 from __future__ import annotations
 
 import math
+import sys
 
 import torch
 
@@ -19,24 +22,25 @@ from .runner import byte_buffer
 
 
 class TemporalLayer:
-    """Parameters, gradients and Adam moments are flat float32 arrays: gamma [C], beta [C], W_qkv [3C][C], W_o [C][C].  Layers of one network
-    take a seed each: with the same one they start alike and drop the same elements."""
+    """Parameters, gradients and moments are flat float32 arrays: gamma [C], beta [C], W_qkv [3C][C], W_o [C][C], and where `rotate` is given
+    gamma_q [d], gamma_k [d].  Layers of one network take a seed each: with the same one they start alike and drop the same elements.
+    rotate: how many of a head's d = C / heads values turn with the frame's number (even, 0: queries and keys are normed only); None: queries and
+    keys go into the attention as the projection leaves them."""
 
-    def __init__(self, B, T, P, C, heads, dtype=torch.bfloat16, dropout=0.1, seed=0, eps=1e-5, longest=64.0):
+    def __init__(self, B, T, P, C, heads, dtype=torch.bfloat16, dropout=0.1, seed=0, eps=1e-5, longest=64.0, rotate=None):
         if C % heads:
             raise ValueError("channels are split evenly over the heads")
         self.shape, self.C, self.H, self.d, self.dtype = (B, T, P, C), C, heads, C // heads, dtype
-        sizes = (C, C, 3 * C * C, C * C)
+        self.rotate, self.longest, self.muon_ws = rotate, longest, None
+        extra = self._extra()
+        sizes = (C, C, 3 * C * C, C * C, sum(e.numel() for e in extra))
         gen = torch.Generator().manual_seed(seed)
-        parts = [torch.ones(C), torch.zeros(C), torch.randn(3 * C * C, generator=gen) / math.sqrt(C), torch.randn(C * C, generator=gen) / math.sqrt(C)]
+        parts = [torch.ones(C), torch.zeros(C), torch.randn(3 * C * C, generator=gen) / math.sqrt(C), torch.randn(C * C, generator=gen) / math.sqrt(C), *extra]
         self.theta = torch.cat(parts).cuda()
         self.grad, self.m, self.v = (torch.zeros_like(self.theta) for _ in range(3))
-        self.gamma, self.beta, self.w_qkv, self.w_o = self._views(self.theta, sizes)
-        self.g_gamma, self.g_beta, self.g_qkv_w, self.g_o_w = self._views(self.grad, sizes)
-        # from a memory of one frame to one of `longest` frames, in equal ratios
-        frames = longest ** torch.linspace(0.0, 1.0, heads)
-        self.log_decay = (-1.0 / frames).cuda()
-        rows, scale = B * T * P, self.d ** -0.5
+        self.gamma, self.beta, self.w_qkv, self.w_o, self.extra = self._views(self.theta, sizes)
+        self.g_gamma, self.g_beta, self.g_qkv_w, self.g_o_w, self.g_extra = self._views(self.grad, sizes)
+        rows = B * T * P
         new = lambda *s: torch.empty(*s, dtype=dtype, device="cuda")  # noqa: E731
         self.y, self.qkv, self.o, self.z, self.h = new(B, T, P, C), new(B, T, P, 3 * C), new(B, T, P, heads, self.d), new(rows, C), new(B, T, P, C)
         self.mean, self.rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
@@ -44,21 +48,69 @@ class TemporalLayer:
         self.norm = gb.make_layer_norm(dtype, rows, C, eps)
         self.drop = gb.make_dropout(dtype, rows, C, dropout, seed)
         self.keep = gb.make_dropout(dtype, rows, C, 0.0, seed)
-        self.mix = gb.make_linattn(*self._heads(self.qkv), self.o, scale)
-        self.ws = byte_buffer(max(*gb.gleam_linattn_workspace_bytes(self.mix), gb.gleam_layer_norm_workspace_bytes(self.norm)))
         # one frame of every pixel
-        self.state = torch.zeros(B, P, heads, self.d, self.d, device="cuda")
         self.frame_qkv, self.frame_o, self.frame_y, self.frame_h = new(B, 1, P, 3 * C), new(B, 1, P, heads, self.d), new(B, P, C), new(B, P, C)
         self.frame_norm = gb.make_layer_norm(dtype, B * P, C, eps)
         self.frame_keep = gb.make_dropout(dtype, B * P, C, 0.0, seed)
-        self.frame_mix = gb.make_linattn(*self._heads(self.frame_qkv), self.frame_o, scale)
+        self.ws = byte_buffer(max(self._plan(), gb.gleam_layer_norm_workspace_bytes(self.norm)))
 
     def _views(self, flat, sizes):
-        a, b, c, d = flat.split(sizes)
-        return a, b, c.view(3 * self.C, self.C), d.view(self.C, self.C)
+        a, b, c, d, e = flat.split(sizes)
+        return a, b, c.view(3 * self.C, self.C), d.view(self.C, self.C), e
 
     def _heads(self, qkv):
         return [x.unflatten(3, (self.H, self.d)) for x in qkv.split(self.C, 3)]
+
+    def _extra(self):
+        """What the mixing has parameters of its own of, as they start."""
+        return [] if self.rotate is None else [torch.ones(2 * self.d)]
+
+    def _plan(self):
+        """Plans and arrays of the mixing, for a series and for a frame; bytes of workspace that it needs."""
+        B, T, P, C = self.shape
+        new = lambda t: torch.empty(B, t, P, self.H, self.d, dtype=self.dtype, device="cuda")  # noqa: E731
+        # from a memory of one frame to one of `longest` frames, in equal ratios
+        frames = self.longest ** torch.linspace(0.0, 1.0, self.H)
+        self.log_decay = (-1.0 / frames).cuda()
+        scale, need = self.d ** -0.5, 0
+        self.state = torch.zeros(B, P, self.H, self.d, self.d, device="cuda")
+        (q, k, v), (fq, fk, fv) = self._heads(self.qkv), self._heads(self.frame_qkv)
+        if self.rotate is not None:
+            self.freq = 1000.0 ** (-torch.arange(self.rotate // 2, device="cuda") / max(self.rotate // 2, 1)) if self.rotate else None
+            self.place = torch.zeros(B, dtype=torch.int32, device="cuda")                       # of the next frame
+            self.q, self.k, self.frame_q, self.frame_k = new(T), new(T), new(1), new(1)
+            self.turn = gb.make_qknorm(q, k, self.q, self.k, self.rotate)
+            self.frame_turn = gb.make_qknorm(fq, fk, self.frame_q, self.frame_k, self.rotate)
+            need = gb.gleam_qknorm_workspace_bytes(self.turn)
+            q, k, fq, fk = self.q, self.k, self.frame_q, self.frame_k
+        self.mix = gb.make_linattn(q, k, v, self.o, scale)
+        self.frame_mix = gb.make_linattn(fq, fk, fv, self.frame_o, scale)
+        return max(need, *gb.gleam_linattn_workspace_bytes(self.mix))
+
+    def _mix(self, lengths):
+        q, k, v = self._heads(self.qkv)
+        if self.rotate is not None:
+            gb.gleam_qknorm_fwd(self.turn, q, k, *self.extra.split(self.d), self.freq, None, lengths, self.q, self.k)
+            q, k = self.q, self.k
+        gb.gleam_linattn_fwd(self.mix, q, k, v, self.log_decay, lengths, None, self.o, None, self.ws)
+
+    def _mix_back(self, g_o, g_qkv):
+        (q, k, v), (g_q, g_k, g_v) = self._heads(self.qkv), self._heads(g_qkv)
+        g_o = g_o.view_as(self.o)
+        if self.rotate is None:
+            gb.gleam_linattn_bwd(self.mix, q, k, v, self.log_decay, self.lengths, None, g_o, None, g_q, g_k, g_v, None, self.ws)
+            return
+        t_q, t_k = torch.empty_like(self.q), torch.empty_like(self.k)
+        gb.gleam_linattn_bwd(self.mix, self.q, self.k, v, self.log_decay, self.lengths, None, g_o, None, t_q, t_k, g_v, None, self.ws)
+        gb.gleam_qknorm_bwd(self.turn, q, k, *self.extra.split(self.d), self.freq, None, self.lengths, t_q, t_k, g_q, g_k, *self.g_extra.split(self.d), self.ws)
+
+    def _mix_frame(self):
+        q, k, v = self._heads(self.frame_qkv)
+        if self.rotate is not None:
+            gb.gleam_qknorm_fwd(self.frame_turn, q, k, *self.extra.split(self.d), self.freq, self.place, None, self.frame_q, self.frame_k)
+            self.place += 1
+            q, k = self.frame_q, self.frame_k
+        gb.gleam_linattn_fwd(self.frame_mix, q, k, v, self.log_decay, None, self.state, self.frame_o, self.state, None)
 
     def forward(self, x, lengths=None, training=True):
         """h from x: [B][T][P][C]; lengths: int32 [B], frames that are there, or None.  h is the layer's own buffer, which the next call
@@ -68,7 +120,7 @@ class TemporalLayer:
         self.x, self.lengths = x, lengths
         gb.gleam_layer_norm_fwd(self.norm, x, self.gamma, self.beta, self.y, self.mean, self.rstd)
         torch.mm(self.y.view(-1, self.C), self.w_qkv.to(self.dtype).t(), out=self.qkv.view(-1, 3 * self.C))
-        gb.gleam_linattn_fwd(self.mix, *self._heads(self.qkv), self.log_decay, lengths, None, self.o, None, self.ws)
+        self._mix(lengths)
         torch.mm(self.o.view(-1, self.C), self.w_o.to(self.dtype).t(), out=self.z)
         self.drop_now = self.drop if training else self.keep
         gb.gleam_dropout_fwd(self.drop_now, self.z, x, self.h, self.step)
@@ -79,46 +131,87 @@ class TemporalLayer:
         g_z, g_qkv, g_x = torch.empty_like(self.z), torch.empty_like(self.qkv), torch.empty_like(self.y)
         gb.gleam_dropout_bwd(self.drop_now, g_h, g_z, self.step)
         torch.mm(g_z.float().t(), self.o.view(-1, self.C).float(), out=self.g_o_w)
-        g_o = (g_z @ self.w_o.to(self.dtype)).view_as(self.o)
-        gb.gleam_linattn_bwd(self.mix, *self._heads(self.qkv), self.log_decay, self.lengths, None, g_o, None, *self._heads(g_qkv), None, self.ws)
+        self._mix_back(g_z @ self.w_o.to(self.dtype), g_qkv)
         rows = g_qkv.view(-1, 3 * self.C)
         torch.mm(rows.float().t(), self.y.view(-1, self.C).float(), out=self.g_qkv_w)
         g_y = rows @ self.w_qkv.to(self.dtype)
         gb.gleam_layer_norm_bwd(self.norm, self.x, self.gamma, self.mean, self.rstd, g_y, g_x, self.g_gamma, self.g_beta, self.ws)
         return g_x.add_(g_h)
 
-    def update(self, hyper, t):
-        """One Adam step with the gradients of the last backward pass, and the next step's mask."""
-        gb.gleam_adam_step(hyper, t, self.theta, self.grad, self.m, self.v)
+    def update(self, hyper, t, muon=None):
+        """One step with the gradients of the last backward pass, and the next step's mask: Adam (`hyper`), or for the four C x C matrices in W_qkv and
+        W_o the orthogonalised update `muon`, which keeps its momentum where Adam keeps its first moment, and Adam for the rest."""
+        if muon is None:
+            gb.gleam_adam_step(hyper, t, self.theta, self.grad, self.m, self.v)
+        else:
+            C, ends = self.C, (2 * self.C, 2 * self.C + 4 * self.C ** 2)
+            if self.muon_ws is None:
+                self.muon_ws = byte_buffer(max(1, gb.gleam_muon_workspace_bytes(4, C, C)))
+            gb.gleam_muon_step(muon, *(a[ends[0]:ends[1]].view(4, C, C) for a in (self.theta, self.grad, self.m)), self.muon_ws)
+            for part in (slice(0, ends[0]), slice(ends[1], None))[:2 if self.extra.numel() else 1]:
+                gb.gleam_adam_step(hyper, t, *(a[part] for a in (self.theta, self.grad, self.m, self.v)))
         self.step += 1
 
     def restart(self):
         """Before the first frame of a new series."""
         self.state.zero_()
+        if self.rotate is not None:
+            self.place.zero_()
 
     def frame(self, x):
         """The next frame [B][P][C] of every pixel; no dropout.  The result is the layer's own buffer, which the next frame overwrites."""
         gb.gleam_layer_norm_fwd(self.frame_norm, x, self.gamma, self.beta, self.frame_y)
         torch.mm(self.frame_y.view(-1, self.C), self.w_qkv.to(self.dtype).t(), out=self.frame_qkv.view(-1, 3 * self.C))
-        gb.gleam_linattn_fwd(self.frame_mix, *self._heads(self.frame_qkv), self.log_decay, None, self.state, self.frame_o, self.state, None)
+        self._mix_frame()
         z = self.frame_o.view(-1, self.C) @ self.w_o.to(self.dtype).t()
         gb.gleam_dropout_fwd(self.frame_keep, z, x, self.frame_h)
         return self.frame_h
 
 
-def main(steps=200, B=1, T=20, P=96 * 80, C=64, heads=4):
+class GatedLayer(TemporalLayer):
+    """The same around a gated scan: the projection's three parts are what enters, the gate of the memory and the gate of what enters, and
+    the parameters behind W_o are lambda [C].  A channel's memory reaches from two frames to `longest` where its gate is half open."""
+
+    def __init__(self, B, T, P, C, dtype=torch.bfloat16, dropout=0.1, seed=0, eps=1e-5, longest=64.0, kappa=8.0):
+        self.kappa = kappa
+        super().__init__(B, T, P, C, 1, dtype, dropout, seed, eps, longest)
+
+    def _extra(self):
+        frames = 2.0 * (self.longest / 2.0) ** torch.linspace(0.0, 1.0, self.C)
+        return [torch.log(torch.expm1(2.0 / (self.kappa * frames)))]
+
+    def _plan(self):
+        B, T, P, C = self.shape
+        self.state = torch.zeros(B, P, C, device="cuda")
+        self.scan = gb.make_gatedscan(*self.qkv.split(C, 3), self.o.view(B, T, P, C), self.kappa)
+        self.frame_scan = gb.make_gatedscan(*self.frame_qkv.split(C, 3), self.frame_o.view(B, 1, P, C), self.kappa)
+        return max(gb.gleam_gatedscan_workspace_bytes(self.scan))
+
+    def _mix(self, lengths):
+        gb.gleam_gatedscan_fwd(self.scan, *self.qkv.split(self.C, 3), self.extra, lengths, None, self.o.view(*self.shape), None, self.ws)
+
+    def _mix_back(self, g_o, g_qkv):
+        gb.gleam_gatedscan_bwd(self.scan, *self.qkv.split(self.C, 3), self.extra, self.lengths, None, g_o.view(*self.shape), None, *g_qkv.split(self.C, 3),
+                               self.g_extra, None, self.ws)
+
+    def _mix_frame(self):
+        B, _, P, C = self.shape
+        gb.gleam_gatedscan_fwd(self.frame_scan, *self.frame_qkv.split(C, 3), self.extra, None, self.state, self.frame_o.view(B, 1, P, C), self.state, None)
+
+
+def main(kind="", muon=False, steps=200, B=1, T=20, P=96 * 80, C=64, heads=4):
     """Learns to take noise off a slowly changing series from its past frames, then runs it frame by frame."""
     gen = torch.Generator(device="cuda").manual_seed(1)
     t = torch.arange(T, device="cuda")[None, :, None, None] / T
     phase, amount = torch.rand(B, 1, P, C, device="cuda", generator=gen), torch.randn(B, 1, P, C, device="cuda", generator=gen)
     clean = amount * torch.cos(2 * math.pi * (0.5 * t + phase))
-    layer = TemporalLayer(B, T, P, C, heads)
-    hyper = gb.make_adam(2e-3)
+    layer = GatedLayer(B, T, P, C) if kind == "gated" else TemporalLayer(B, T, P, C, heads, rotate=C // heads if kind == "rotate" else None)
+    hyper, matrices = gb.make_adam(2e-3), gb.make_muon(5e-3) if muon else None
     for k in range(1, steps + 1):
         x = (clean + 0.5 * torch.randn(clean.shape, device="cuda", generator=gen)).to(layer.dtype)
         d = layer.forward(x).float() - clean
         layer.backward((2.0 / d.numel() * d).to(layer.dtype))
-        layer.update(hyper, k)
+        layer.update(hyper, k, matrices)
         if k == 1 or k % 40 == 0:
             print(f"step {k}: mean squared error {float((d * d).mean()):.4f} (noise alone: 0.25)", flush=True)
     whole = layer.forward(x, training=False).clone()
@@ -128,4 +221,7 @@ def main(steps=200, B=1, T=20, P=96 * 80, C=64, heads=4):
 
 
 if __name__ == "__main__":
-    main()
+    words = set(sys.argv[1:])
+    if words - {"rotate", "gated", "muon"} or {"rotate", "gated"} <= words:
+        sys.exit("usage: python -m paper_2207_08393_amd.temporal [rotate | gated] [muon]")
+    main(next((w for w in ("rotate", "gated") if w in words), ""), "muon" in words)
