@@ -380,7 +380,7 @@ def _flat(t, code: int, count: int, what: str) -> Optional[int]:
     """Address of a contiguous device array of `count` elements of type code 0 / 1 (2: int32, 3: int64 words)."""
     if t is None or type(t) is int:
         return t
-    if t.dtype is not _types()[code] or t.numel() != count or not t.is_cuda or not t.is_contiguous():
+    if t.dtype is not (_DTYPES or _types())[code] or t.numel() != count or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{what}: {t.numel()} elements of {t.dtype} on {t.device} with strides {t.stride()}, {count} contiguous ones of "
                          f"{_types()[code]} on the GPU expected")
     return t.data_ptr()

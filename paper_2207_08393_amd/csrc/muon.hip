@@ -568,7 +568,8 @@ __global__ __launch_bounds__(64 * kSmallBlocks) void muon_small_kernel(MuonArgs 
         if (in(i)) theta[at(i)] = a.decay * old[i] - a.lr_scale * x[i];
 }
 
-// Tiles of 64 x 64, and parts of the sum: a product of few tiles is split so that every CU has a workgroup, no part under eight steps of 32 columns.
+// Tiles of 64 x 64, and parts of the sum: a product of few tiles is split so that every CU has a workgroup, sums of 32 steps of 32 columns and more, no
+// part under eight (24 x 100 x 900, 29 steps: 122 us whole, 131 in three parts; 300 x 1000, 32 steps: 133 whole, 123 in four).
 struct ProductPlan {
     bool is_short;            // sums of up to eight steps of 32 columns
     int splits;
@@ -580,6 +581,7 @@ ProductPlan product_plan(long long count, int mb, int nb, MuonProduct mode) {
     p.tiles = mode == kApply ? tr * tc : tr * (tr + 1) / 2;
     long long s = 256 / (count * p.tiles);
     if (s > steps / 8) s = steps / 8;
+    if (steps < 32) s = 1;
     p.splits = (int)(s < 1 ? 1 : s > 32 ? 32 : s);
     p.is_short = p.splits == 1 && steps <= 8;
     return p;
