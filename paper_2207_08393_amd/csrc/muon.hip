@@ -249,7 +249,7 @@ __device__ __forceinline__ bool find_tile(const MuonArgs& a, int tr, int tc, Til
 
 // One of the three products of a step, rows of the left operand against rows of the right one:
 //   kGram  A = X X^T;   kSquare  B = a I + b A + c A A;   kApply  X <- B X, or at the last step the weights' update.
-// A workgroup computes 2 x 2 blocks of 32 x 32 over one of `splits` parts of the sum, and each of its four waves all of them over a quarter of that: no
+// A workgroup computes 2 x 2 blocks of 32 x 32 over one of `splits` parts of the sum, and each of its four waves all of them over every fourth step of that: no
 // operand is needed by two waves, so they go from memory into registers as they lie there, kAhead steps of 16 columns before their use, with
 // no barrier until the four sums meet in LDS.  Short sums (SHORT) are not shared out: a wave computes one block, and the waves do not meet.
 constexpr int kProducts = 3;
@@ -265,11 +265,13 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(MuonArgs a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const char* left = MODE == kGram ? a.x : MODE == kSquare ? a.a : a.b;
     const char* right = MODE == kGram ? a.x : MODE == kSquare ? a.a : a.xt;
-    const int part = SHORT ? 0 : t.split * 4 + wave, parts = SHORT ? 1 : a.splits * 4;
+    // steps k0, k0 + kEvery ..: the waves go through the sum side by side, so that workgroups that share rows read them at about the same time
+    constexpr int kEvery = SHORT ? 1 : 4;
+    const int s0 = (int)((long long)2 * K * t.split / a.splits), s1 = (int)((long long)2 * K * (t.split + 1) / a.splits);
+    const int k0 = SHORT ? s0 : s0 + wave;
     const int bi = 2 * t.ti + (wave >> 1), bj = 2 * t.tj + (wave & 1);   // the block that this wave writes
     const bool mine = bi < R && bj < Cb && (MODE == kApply || bi <= bj);
     if (SHORT && !mine) return;
-    const int k0 = (int)((long long)2 * K * part / parts), k1 = (int)((long long)2 * K * (part + 1) / parts);   // steps
     const char *pl[W], *pr[W];   // blocks past the end: the last one's, computed and not written
 #pragma unroll
     for (int w = 0; w < W; ++w) pl[w] = block_at((char*)left, t.matrix, R, K, SHORT ? bi : min(2 * t.ti + w, R - 1), k0, 0) + lane * 16;
@@ -282,10 +284,10 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(MuonArgs a) {
         for (int j = 0; j < W; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-    const int steps = MODE == kSquare && a.no_square ? 0 : k1 - k0;
+    const int steps = MODE == kSquare && a.no_square ? 0 : (s1 - k0 + kEvery - 1) / kEvery;
     halfx8 l[kAhead][W][kParts], r[kAhead][W][kParts];
     auto load = [&](int k, int at) {
-        const int off = min(k, steps - 1) * (kParts * kBlockBytes);   // past the end: the last again, not used
+        const int off = min(k, steps - 1) * (kEvery * kParts * kBlockBytes);   // past the end: the last again, not used
 #pragma unroll
         for (int p = 0; p < kParts; ++p) {
 #pragma unroll
