@@ -28,6 +28,14 @@ __device__ __forceinline__ float dpp(float v) {
 template <class V>
 __device__ __forceinline__ float sum_of_pair(V r) { return __uint_as_float(r[0]) + __uint_as_float(r[1]); }
 
+// Between what lanes of a wave write into LDS and what others of the same wave read there, or the other way round: the accesses stay on their
+// sides, and the wave's own order does the rest.
+__device__ __forceinline__ void wave_sync() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // N elements of type T; 16 bytes, or two times 16 for eight float32.  Global addresses need the alignment of an element only: the
 // memory unit takes 16 bytes from any address (an access that crosses a cache line costs two).
 template <class T, int N>

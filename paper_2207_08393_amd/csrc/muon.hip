@@ -360,9 +360,9 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(MuonArgs a) {
         return;
     }
     float* tile = lds[wave][SHORT ? 0 : wave];   // read by this wave alone
-    __builtin_amdgcn_wave_barrier();
+    wave_sync();
     stage_block(sum, tile);
-    __builtin_amdgcn_wave_barrier();
+    wave_sync();
     put_block<MODE>(a, t.matrix, bi, bj, tile);
 }
 
@@ -394,7 +394,7 @@ __global__ __launch_bounds__(64) void muon_join_kernel(MuonArgs a) {
         }
     }
     stage_block(acc, lds);
-    __builtin_amdgcn_wave_barrier();
+    wave_sync();
     put_block<MODE>(a, matrix, bi, bj, lds);
 }
 
@@ -453,13 +453,13 @@ __device__ __forceinline__ floatx16 turned_block(float* tile, const floatx16& v)
         const int row = 8 * (i >> 2) + 4 * up + (i & 3);
         tile[row * 32 + (line ^ row)] = v[i];
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_sync();
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const int row = 8 * (i >> 2) + 4 * up + (i & 3);
         to[i] = tile[line * 32 + (row ^ line)];
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_sync();
     return to;
 }
 // By rows: through the block's own 4 KB (its two times 16 columns and parts lie in a row), as above.
@@ -472,13 +472,13 @@ __device__ __forceinline__ void small_along(char* base, int K, int bi, int bj, c
         const int row = 8 * (i >> 2) + 4 * up + (i & 3);
         tile[row * 32 + (line ^ row)] = v[i];
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_sync();
     float w[2][8];
 #pragma unroll
     for (int g = 0; g < 2; ++g)
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[g][e] = tile[line * 32 + ((8 * (up + 2 * g) + e) ^ line)];
-    __builtin_amdgcn_wave_barrier();
+    wave_sync();
 #pragma unroll
     for (int g = 0; g < 2; ++g) store_parts8(block + g * kParts * kBlockBytes + up * 512 + line * 16, w[g]);
 }

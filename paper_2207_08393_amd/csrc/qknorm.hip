@@ -158,7 +158,7 @@ __global__ __launch_bounds__(kQkThreads) void qknorm_kernel(QkArgs a) {
             turns[wave][0][i] = cs;
             turns[wave][1][i] = sn;
         }
-        __builtin_amdgcn_wave_barrier();
+        wave_sync();
         float c[NV][W], s[NV][W];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -170,7 +170,7 @@ __global__ __launch_bounds__(kQkThreads) void qknorm_kernel(QkArgs a) {
                 s[j][i] = turned ? turns[wave][1][from + i] : 0.f;
             }
         }
-        __builtin_amdgcn_wave_barrier();
+        wave_sync();
         long long b;
         unsigned t;
         find((unsigned)my_token, b, t);
@@ -301,16 +301,17 @@ __global__ __launch_bounds__(1024) void qknorm_sums_kernel(const float* part, in
     if (slice >= 4) return;
     for (int i = slice + 4; i < 64; i += 4) v += red[i][col];
     red[slice][col] = v;
-    __builtin_amdgcn_wave_barrier();
+    wave_sync();
     if (slice || e >= 2 * d) return;
     v = (red[0][col] + red[1][col]) + (red[2][col] + red[3][col]);
     float* out = e < d ? g_q : g_k;
     if (out) out[e < d ? e : e - d] = v;
 }
 
-// Pairs of a lane's vector: as many as 16 bytes take and divide both the rotated part and the rest.
+// Pairs of a lane's vector: up to four, as many as divide both the rotated part and the rest.  (Eight, 16 bytes of bfloat16, took 74 us backward at
+// 16384 tokens where four take 66, with twice the registers, and as long forward.)
 int vector_of(const gleam_qknorm_desc& d) {
-    int w = d.dtype ? 8 : 4;
+    int w = 4;
     while (w > 1 && (d.rot / 2 % w || (d.d - d.rot) % (2 * w))) w /= 2;
     return w;
 }
@@ -364,8 +365,7 @@ template <class T, bool BWD>
 void launch(const QkArgs& a, const QkPlan& p, bool halves, hipStream_t st) {
     if (p.w == 1) launch_pairs<T, 1, BWD>(a, p, halves, st);
     else if (p.w == 2) launch_pairs<T, 2, BWD>(a, p, halves, st);
-    else if (p.w == 4) launch_pairs<T, 4, BWD>(a, p, halves, st);
-    else if constexpr (sizeof(T) == 2) launch_pairs<T, 8, BWD>(a, p, halves, st);
+    else launch_pairs<T, 4, BWD>(a, p, halves, st);
 }
 
 QkArgs args_of(const gleam_qknorm_desc& d, const QkPlan& p, const void* q, const void* k, const float* gamma_q, const float* gamma_k,
