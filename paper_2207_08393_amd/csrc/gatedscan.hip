@@ -34,30 +34,25 @@ struct ScanArgs {
     const float *lambda, *state_in, *state_end;   // state_end: gradient of the last state
     const int* lengths;
     float *state_out, *g_state_in;
-    float *log_a, *add_h, *add_e;         // [b][chunk][p][c]: sum of log a, what a chunk adds to h and to E; then h and E that enter it
+    float *log_a, *add_h, *add_e;         // [b][chunk][p][c]: sum of log2 a, what a chunk adds to h and to E; then h and E that enter it
     float* part;                          // [b][chunk][p][c]: sums of W
     long long B, T, P, C, chunks, groups; // groups of 64 columns
     float kappa;
     int tokens;                           // of a wave
+    int odd;                              // C is odd
     int few;                              // groups of workgroups and columns of a sequence are numbers of 32 bits
 };
 
 constexpr float kLog2e = 1.44269504f;
 
-// e^x for x <= 0, of sums over many tokens: the product with log2 e in two parts.  From -200 on it is 0 in float32.
-__device__ __forceinline__ float exp_neg(float x) {
-    x = x < -200.f ? -200.f : x;
-    const float hi = x * kLog2e, lo = __builtin_fmaf(x, kLog2e, -hi) + x * 1.92596299e-8f;
-    const float e = __builtin_amdgcn_exp2f(hi);
-    return __builtin_fmaf(e, lo * 0.693147181f, e);
-}
-// The gates are worked out for every token and channel, and the kernels are bound by vector instructions: a product with log2 e
-// rounded once does there, which puts 2^-24 |v| of its value on e^-v.
-__device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * v)); }
+// The gates are worked out for every token and channel, and the kernels are bound by vector instructions: decays are kept as their logarithms to
+// base 2, which the exponential instruction takes, and a product with log2 e is rounded once, which puts 2^-24 |v| of its value on e^-v.
+__device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }
+__device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + exp2_of(-kLog2e * v)); }
 __device__ __forceinline__ void sigmoids(float v, float& s, float& rest) {   // and 1 - sigmoid(v), to its last bits too
     float x = -kLog2e * v;
     x = x > 126.f ? 126.f : x;   // (a NaN stays)
-    const float e = __builtin_amdgcn_exp2f(x);
+    const float e = exp2_of(x);
     s = __builtin_amdgcn_rcpf(1.f + e);
     rest = e * s;
 }
@@ -65,28 +60,35 @@ __device__ __forceinline__ float softplus(float v) { return fmaxf(v, 0.f) + log1
 
 __device__ __forceinline__ bool near_one(float w) { return __float_as_int(w) < 0; }
 __device__ __forceinline__ float a_of(float w) { return near_one(w) ? 1.f + w : w; }
-// a h + b: the sign of w says whether h itself is added
-__device__ __forceinline__ float step_h(float h, float w, float b) {
-    return __builtin_fmaf(w, h, b) + __int_as_float(__float_as_int(h) & (__float_as_int(w) >> 31));
-}
+// a h + b: where a is near 1, w is a - 1 and h itself is added
+__device__ __forceinline__ float step_h(float h, float w, float b, bool near) { return __builtin_fmaf(w, h, b) + (near ? h : 0.f); }
+__device__ __forceinline__ float step_h(float h, float w, float b) { return step_h(h, w, b, near_one(w)); }
 
-// The token's gates of one channel: y = c s, a = e^-y as it is kept (w: a - 1 below y = 1/4, by the series to y^6 / 6!, whose rest is 5e-8 of it; a
-// above), m = sqrt(1 - a^2) = sqrt(d (2 - d)).
+// The token's gates of one channel from z = log2 a <= 0: a as it is kept, w (2^z - 1 above z = -0.36, by the series to z^6, whose rest is 5e-8 of it;
+// 2^z below), m = sqrt(1 - a^2) = sqrt(d (2 - d)).  The coefficients, (ln 2)^k / k!, stand in scalar registers: as literals each would be moved
+// into a vector register first.
 struct Gate {
-    float y, w, m;
+    float w, m;
+    bool near;
 };
-__device__ __forceinline__ Gate gate_of(float y) {
-    float p = __builtin_fmaf(-1.f / 720.f, y, 1.f / 120.f);
-    p = __builtin_fmaf(p, y, -1.f / 24.f);
-    p = __builtin_fmaf(p, y, 1.f / 6.f);
-    p = __builtin_fmaf(p, y, -0.5f);
-    p = __builtin_fmaf(p, y, 1.f);
-    const float lost = p * y, a = __builtin_amdgcn_exp2f(-kLog2e * y);
-    const bool near = y < 0.25f;
+struct Series {
+    float c[6];
+    __device__ __forceinline__ Series() : c{0.693147181f, 0.240226507f, 0.0555041087f, 0.00961812911f, 0.00133335581f, 0.000154035304f} {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) asm("" : "+s"(c[i]));
+    }
+};
+__device__ __forceinline__ Gate gate_of(float z, const Series& k) {
+    float p = __builtin_fmaf(k.c[5], z, k.c[4]);
+    p = __builtin_fmaf(p, z, k.c[3]);
+    p = __builtin_fmaf(p, z, k.c[2]);
+    p = __builtin_fmaf(p, z, k.c[1]);
+    p = __builtin_fmaf(p, z, k.c[0]);
+    const float less = p * z, a = exp2_of(z);   // a - 1, and a
     Gate g;
-    g.y = y;
-    g.w = near ? -lost : a;
-    const float d = near ? lost : 1.f - a;
+    g.near = z > -0.36f;
+    g.w = g.near ? less : a;
+    const float d = g.near ? -less : 1.f - a;
     g.m = __builtin_amdgcn_sqrtf(d * (2.f - d));
     return g;
 }
@@ -141,9 +143,6 @@ struct Spot {
         return true;
     }
     __device__ __forceinline__ long long at(const gleam_scan_strides& s) const { return b * s.b + p * s.p + c; }
-    // values as they were read from `back` before the first channel
-    template <class R>
-    __device__ __forceinline__ float value(const R& raw, int e) const { return V > 1 && e == 0 ? (back ? raw.get(V - 1) : raw.get(0)) : raw.get(e); }
     template <class T>
     __device__ __forceinline__ void store(T* p, const float* v) const {
         if (!live) return;
@@ -181,17 +180,30 @@ struct Tokens {
             if (WITH_G) g[j].load(pg + t * a.sh.t);
         }
     }
+    // Where C is odd, a vector that was read from `back` before its first channel has that channel behind.
+    __device__ __forceinline__ void settle(const ScanArgs& a, const Spot<V>& s) {
+        if constexpr (V == 2 && sizeof(T) == 2) {
+            if (!a.odd) return;
+#pragma unroll
+            for (int j = 0; j < L; ++j) {
+                x[j].v.w[0] >>= 16 * s.back;
+                r[j].v.w[0] >>= 16 * s.back;
+                i[j].v.w[0] >>= 16 * s.back;
+                if (WITH_G) g[j].v.w[0] >>= 16 * s.back;
+            }
+        }
+    }
 };
 
-// c of a workgroup's columns, worked out by its first wave; a barrier stands between this and `rates`.
+// -log2 e times c of a workgroup's columns, worked out by its first wave; a barrier stands behind it.
 template <int V>
 __device__ __forceinline__ void put_rates(const ScanArgs& a, const Spot<V>& s, float (&shared)[V][64]) {
     if (threadIdx.x < 64)
 #pragma unroll
-        for (int e = 0; e < V; ++e) shared[e][threadIdx.x] = a.kappa * softplus(a.lambda[s.c + (e && s.back ? 0 : e)]);
+        for (int e = 0; e < V; ++e) shared[e][threadIdx.x] = -kLog2e * a.kappa * softplus(a.lambda[s.c + (e && s.back ? 0 : e)]);
 }
 
-// What a chunk does to a state, h' = exp(log_a) h + add_h, and backwards, E' = exp(log_a) E + add_e.
+// What a chunk does to a state, h' = 2^log_a h + add_h, and backwards, E' = 2^log_a E + add_e.
 template <class T, int V, int L>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_chunk_kernel(ScanArgs a) {
     __shared__ float ends[kScanWaves][3][V][64], shared[V][64];
@@ -202,6 +214,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_chunk_kernel(ScanArgs a)
     tok.load(a, s);
     put_rates(a, s, shared);
     __syncthreads();
+    tok.settle(a, s);
+    const Series series;
     float c[V], sum[V], h[V], e_add[V], w[L][V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
@@ -213,16 +227,17 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_chunk_kernel(ScanArgs a)
         if (s.t0 + j < s.t1)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const Gate g = gate_of(c[e] * sigmoid(s.value(tok.r[j], e)));
+                const float z = c[e] * sigmoid(tok.r[j].get(e));
+                const Gate g = gate_of(z, series);
                 w[j][e] = g.w;
-                sum[e] -= g.y;
-                h[e] = step_h(h[e], g.w, g.m * (sigmoid(s.value(tok.i[j], e)) * s.value(tok.x[j], e)));
+                sum[e] += z;
+                h[e] = step_h(h[e], g.w, g.m * (sigmoid(tok.i[j].get(e)) * tok.x[j].get(e)), g.near);
             }
 #pragma unroll
     for (int j = L - 1; j >= 0; --j)
         if (s.t0 + j < s.t1)
 #pragma unroll
-            for (int e = 0; e < V; ++e) e_add[e] = step_h(s.value(tok.g[j], e) + e_add[e], w[j][e], 0.f);
+            for (int e = 0; e < V; ++e) e_add[e] = step_h(tok.g[j].get(e) + e_add[e], w[j][e], 0.f);
 #pragma unroll
     for (int e = 0; e < V; ++e) {
         ends[wave][0][e][lane] = sum[e];
@@ -235,8 +250,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_chunk_kernel(ScanArgs a)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const float more = ends[v][0][e][lane];
-            e_add[e] += exp_neg(sum[e]) * ends[v][2][e][lane];
-            h[e] = __builtin_fmaf(exp_neg(more), h[e], ends[v][1][e][lane]);
+            e_add[e] += exp2_of(sum[e]) * ends[v][2][e][lane];
+            h[e] = __builtin_fmaf(exp2_of(more), h[e], ends[v][1][e][lane]);
             sum[e] += more;
         }
     const long long at = s.slot(a);
@@ -258,8 +273,8 @@ __global__ __launch_bounds__(1024) void scan_carry_kernel(ScanArgs a) {
 #pragma unroll 8
     for (int k = k0; k < k1; ++k) {
         const float la = a.log_a[base + k * pc];
-        h = __builtin_fmaf(exp_neg(la), h, a.add_h[base + k * pc]);
-        if (BWD) e += exp_neg(sum) * a.add_e[base + k * pc];
+        h = __builtin_fmaf(exp2_of(la), h, a.add_h[base + k * pc]);
+        if (BWD) e += exp2_of(sum) * a.add_e[base + k * pc];
         sum += la;
     }
     ends[wave][0][lane] = sum;
@@ -267,10 +282,10 @@ __global__ __launch_bounds__(1024) void scan_carry_kernel(ScanArgs a) {
     if (BWD) ends[wave][2][lane] = e;
     __syncthreads();
     h = a.state_in ? a.state_in[n] : 0.f;
-    for (int v = 0; v < wave; ++v) h = __builtin_fmaf(exp_neg(ends[v][0][lane]), h, ends[v][1][lane]);
+    for (int v = 0; v < wave; ++v) h = __builtin_fmaf(exp2_of(ends[v][0][lane]), h, ends[v][1][lane]);
     if (BWD) {
         e = a.state_end ? a.state_end[n] : 0.f;
-        for (int v = 31; v > wave; --v) e = __builtin_fmaf(exp_neg(ends[v][0][lane]), e, ends[v][2][lane]);
+        for (int v = 31; v > wave; --v) e = __builtin_fmaf(exp2_of(ends[v][0][lane]), e, ends[v][2][lane]);
     }
     if (mine >= all) return;
     // four chunks' numbers are read before the first of them is written over
@@ -285,7 +300,7 @@ __global__ __launch_bounds__(1024) void scan_carry_kernel(ScanArgs a) {
         for (int i = 0; i < 4; ++i)
             if (k + i < k1) {
                 a.add_h[base + (k + i) * pc] = h;
-                h = __builtin_fmaf(exp_neg(la[i]), h, add[i]);
+                h = __builtin_fmaf(exp2_of(la[i]), h, add[i]);
             }
     }
     if (!BWD) return;
@@ -300,7 +315,7 @@ __global__ __launch_bounds__(1024) void scan_carry_kernel(ScanArgs a) {
         for (int i = 0; i < 4; ++i)
             if (k - i >= k0) {
                 a.add_e[base + (k - i) * pc] = e;
-                e = __builtin_fmaf(exp_neg(la[i]), e, add[i]);
+                e = __builtin_fmaf(exp2_of(la[i]), e, add[i]);
             }
     }
 }
@@ -320,13 +335,15 @@ __global__ __launch_bounds__(256) void scan_walk_kernel(ScanArgs a) {
     float c[V], h[V], sum[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-        c[e] = a.kappa * softplus(a.lambda[s.c + (e && s.back ? 0 : e)]);
+        c[e] = -kLog2e * a.kappa * softplus(a.lambda[s.c + (e && s.back ? 0 : e)]);
         sum[e] = 0.f;
     }
     s.load_state(SUM ? nullptr : a.chunks > 1 ? a.add_h + s.slot(a) : a.state_in ? a.state_in + s.state(a) : nullptr, h);
     T* out = (T*)a.out + s.at(a.sh);
+    const Series series;
     for (int t = first; t < len; t += L) {
-        const Tokens<T, V, L, false> now = tok;
+        Tokens<T, V, L, false> now = tok;
+        now.settle(a, s);
         s.t0 = t + L < len ? t + L : len;
         tok.load(a, s);
 #pragma unroll
@@ -334,9 +351,10 @@ __global__ __launch_bounds__(256) void scan_walk_kernel(ScanArgs a) {
             if (t + j < len) {
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const Gate g = gate_of(c[e] * sigmoid(s.value(now.r[j], e)));
-                    h[e] = step_h(h[e], g.w, g.m * (sigmoid(s.value(now.i[j], e)) * s.value(now.x[j], e)));
-                    if (SUM) sum[e] -= g.y;
+                    const float z = c[e] * sigmoid(now.r[j].get(e));
+                    const Gate g = gate_of(z, series);
+                    h[e] = step_h(h[e], g.w, g.m * (sigmoid(now.i[j].get(e)) * now.x[j].get(e)), g.near);
+                    if (SUM) sum[e] += z;
                 }
                 if (!SUM) s.store(out + (t + j) * a.sh.t, h);
             }
@@ -364,6 +382,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs a) {
     s.load_state(a.state_in ? a.state_in + s.state(a) : nullptr, carry);
     put_rates(a, s, shared);
     __syncthreads();
+    tok.settle(a, s);
+    const Series series;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
         c[e] = shared[e][lane];
@@ -374,11 +394,12 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs a) {
         if (s.t0 + j < s.t1)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const Gate g = gate_of(c[e] * sigmoid(s.value(tok.r[j], e)));
+                const float z = c[e] * sigmoid(tok.r[j].get(e));
+                const Gate g = gate_of(z, series);
                 w[j][e] = g.w;
-                b[j][e] = g.m * (sigmoid(s.value(tok.i[j], e)) * s.value(tok.x[j], e));
-                sum[e] -= g.y;
-                h[e] = step_h(h[e], g.w, b[j][e]);
+                b[j][e] = g.m * (sigmoid(tok.i[j].get(e)) * tok.x[j].get(e));
+                sum[e] += z;
+                h[e] = step_h(h[e], g.w, b[j][e], g.near);
             }
 #pragma unroll
     for (int e = 0; e < V; ++e) {
@@ -388,7 +409,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs a) {
     __syncthreads();
     for (int v = 0; v < wave; ++v)
 #pragma unroll
-        for (int e = 0; e < V; ++e) carry[e] = __builtin_fmaf(exp_neg(ends[v][0][e][lane]), carry[e], ends[v][1][e][lane]);
+        for (int e = 0; e < V; ++e) carry[e] = __builtin_fmaf(exp2_of(ends[v][0][e][lane]), carry[e], ends[v][1][e][lane]);
     T* out = (T*)a.out + s.at(a.sh) + s.t0 * a.sh.t;
 #pragma unroll
     for (int j = 0; j < L; ++j) {
@@ -418,6 +439,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs a) {
     s.load_state(split ? a.add_e + s.slot(a) : a.state_end ? a.state_end + s.state(a) : nullptr, ahead);
     put_rates(a, s, shared);
     __syncthreads();
+    tok.settle(a, s);
+    const Series series;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
         c[e] = shared[e][lane];
@@ -428,18 +451,19 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs a) {
         if (s.t0 + j < s.t1)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const Gate g = gate_of(c[e] * sigmoid(s.value(tok.r[j], e)));
+                const float z = c[e] * sigmoid(tok.r[j].get(e));
+                const Gate g = gate_of(z, series);
                 w[j][e] = g.w;
-                b[j][e] = g.m * (sigmoid(s.value(tok.i[j], e)) * s.value(tok.x[j], e));
-                sum[e] -= g.y;
-                h[e] = step_h(h[e], g.w, b[j][e]);
+                b[j][e] = g.m * (sigmoid(tok.i[j].get(e)) * tok.x[j].get(e));
+                sum[e] += z;
+                h[e] = step_h(h[e], g.w, b[j][e], g.near);
             }
     if (waves > 1) {
 #pragma unroll
         for (int j = L - 1; j >= 0; --j)
             if (s.t0 + j < s.t1)
 #pragma unroll
-                for (int e = 0; e < V; ++e) e_add[e] = step_h(s.value(tok.g[j], e) + e_add[e], w[j][e], 0.f);
+                for (int e = 0; e < V; ++e) e_add[e] = step_h(tok.g[j].get(e) + e_add[e], w[j][e], 0.f);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             ends[wave][0][e][lane] = sum[e];
@@ -449,10 +473,10 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs a) {
         __syncthreads();
         for (int v = 0; v < wave; ++v)
 #pragma unroll
-            for (int e = 0; e < V; ++e) carry[e] = __builtin_fmaf(exp_neg(ends[v][0][e][lane]), carry[e], ends[v][1][e][lane]);
+            for (int e = 0; e < V; ++e) carry[e] = __builtin_fmaf(exp2_of(ends[v][0][e][lane]), carry[e], ends[v][1][e][lane]);
         for (int v = waves - 1; v > wave; --v)
 #pragma unroll
-            for (int e = 0; e < V; ++e) ahead[e] = __builtin_fmaf(exp_neg(ends[v][0][e][lane]), ahead[e], ends[v][2][e][lane]);
+            for (int e = 0; e < V; ++e) ahead[e] = __builtin_fmaf(exp2_of(ends[v][0][e][lane]), ahead[e], ends[v][2][e][lane]);
     }
     // h before each token, in the place of b
 #pragma unroll
@@ -472,11 +496,11 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs a) {
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 float sr, rest, si, rest_i;
-                sigmoids(s.value(tok.r[j], e), sr, rest);
-                sigmoids(s.value(tok.i[j], e), si, rest_i);
-                const float G = s.value(tok.g[j], e) + ahead[e], wj = w[j][e], y = c[e] * sr, al = a_of(wj), d = near_one(wj) ? -wj : 1.f - wj;
+                sigmoids(tok.r[j].get(e), sr, rest);
+                sigmoids(tok.i[j].get(e), si, rest_i);
+                const float G = tok.g[j].get(e) + ahead[e], wj = w[j][e], y = (-0.693147181f * c[e]) * sr, al = a_of(wj), d = near_one(wj) ? -wj : 1.f - wj;
                 const float m2 = d * (2.f - d), one_m = m2 < 0x1p-126f ? 0.f : __builtin_amdgcn_rsqf(m2), q = y * one_m, m = m2 * one_m;   // (a NaN stays)
-                const float u = si * s.value(tok.x[j], e), gu = G * m;
+                const float u = si * tok.x[j].get(e), gu = G * m;
                 const float W = G * al * (al * u * q - b[j][e] * y);
                 ox[e] = gu * si;
                 oi[e] = gu * (u * rest_i);
@@ -585,6 +609,7 @@ ScanArgs args_of(const gleam_gatedscan_desc& d, const ScanPlan& p, const void* x
     a.groups = p.groups;
     a.kappa = d.kappa;
     a.tokens = p.tokens;
+    a.odd = d.C & 1;
     a.few = d.B * p.chunks * p.groups < 0x7fffffff && p.groups < 0x1ffffff;
     return a;
 }
