@@ -120,7 +120,7 @@ struct Spot {
         const long long n = live ? mine : all - 1;
         p = a.P == 1 ? 0 : a.few ? (long long)((unsigned)n / (unsigned)vecs) : n / vecs;
         c = (int)((n - p * vecs) * V);
-        back = V > 1 && c + V > a.C;
+        back = V > 1 && (long long)c + V > a.C;
         col = p * a.C + c;
         return true;
     }

@@ -120,7 +120,7 @@ __global__ __launch_bounds__(128) void muon_split_kernel(MuonArgs a) {
 #pragma unroll
     for (int i = 0; i < kMuonNorms; i += 64) norm += lane + i < a.parts ? a.norms[matrix * kMuonNorms + lane + i] : 0.0;
     for (int o = 1; o < 64; o *= 2) norm += __shfl_xor(norm, o);
-    const float scale = (float)((double)a.x_scale / (sqrt(norm) + (double)a.eps));
+    const double scale = (double)a.x_scale / (sqrt(norm) + (double)a.eps);   // may lie outside the range of a float32 where u is small
     const float *g = a.grad + matrix * a.stride, *m = a.m + matrix * a.stride;
     const int r0 = 32 * (a.tall ? bj : bi), c0 = 32 * (a.tall ? bi : bj);           // of u
     float mv[8], gv[8];
@@ -135,7 +135,7 @@ __global__ __launch_bounds__(128) void muon_split_kernel(MuonArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int e = threadIdx.x + 128 * i, r = e >> 5, c = e & 31;
-        tile[a.tall ? c : r][a.tall ? r : c] = (a.nesterov ? __builtin_fmaf(a.momentum, mv[i], gv[i]) : mv[i]) * scale;
+        tile[a.tall ? c : r][a.tall ? r : c] = (float)((double)(a.nesterov ? __builtin_fmaf(a.momentum, mv[i], gv[i]) : mv[i]) * scale);
     }
     __syncthreads();
     const int line = threadIdx.x & 31, k8 = threadIdx.x >> 5;   // a row, or column, and which 8 of its values
@@ -523,9 +523,9 @@ __global__ __launch_bounds__(64 * kSmallBlocks) void muon_small_kernel(MuonArgs 
     __syncthreads();
     sum = 0.0;
     for (int w = 0; w < waves; ++w) sum += norms[w];
-    const float scale = (float)((double)a.x_scale / (sqrt(sum) + (double)a.eps));
+    const double scale = (double)a.x_scale / (sqrt(sum) + (double)a.eps);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] *= scale;
+    for (int i = 0; i < 16; ++i) x[i] = (float)((double)x[i] * scale);
     if (a.tall && mine) x = turned_block((float*)own, x);
     const floatx16 zero = {};
     for (int s = 0;; ++s) {

@@ -124,6 +124,20 @@ def test_muon_zero_infinite_and_extreme_gradients():
         assert np.linalg.norm(1.0 - t[k] - x) <= bound(5) * max(np.linalg.norm(x), 1e-3)
 
 
+@pytest.mark.parametrize("rows,cols", [(40, 50), (100, 300)])
+def test_muon_with_an_eps_that_is_no_guard(rows, cols):
+    """1 / (|u| + eps) passes the range of a float32 where u is zero or tiny; X = u / (|u| + eps) does not."""
+    g = torch.randn(2, rows, cols, device="cuda", generator=torch.Generator(device="cuda").manual_seed(rows))
+    g[0] = 0.0
+    g[1] *= 1e-37
+    theta, m = torch.ones_like(g), torch.zeros_like(g)
+    step(theta, g, m, lr=1.0, momentum=0.0, eps=2e-38)
+    t = host(theta)
+    assert np.array_equal(t[0], np.ones((rows, cols)))
+    x = mo.orthogonalise(host(g)[1], 5, float(np.float32(2e-38)), [float(np.float32(v)) for v in mo.COEFFICIENTS])
+    assert np.linalg.norm(1.0 - t[1] - x) <= bound(5) * np.linalg.norm(x) + 2.0 ** -24 * np.sqrt(rows * cols)   # theta = 1 - X is rounded to 2^-24
+
+
 def test_muon_repeats_streams_and_graphs():
     """Two steps in a row go on from the state; the same bits on another stream and from a graph."""
     rng = np.random.default_rng(4)
