@@ -200,6 +200,26 @@ def test_gatedscan_infinities_stay_in_their_channel():
     assert torch.equal(torch.where(touched, clean, h), clean) and not bool(torch.isfinite(h[touched]).any())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [3, 50, 200])
+@pytest.mark.parametrize("C", [6, 7])
+def test_gatedscan_of_inputs_that_stand_for_many(C, T, dtype):
+    """Forward inputs with strides of 0 give what their copies give, bit by bit."""
+    B, P, type_ = 3, 4, TYPES[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    new = lambda *s: torch.randn(*s, device="cuda", generator=gen).to(type_)  # noqa: E731
+    x, r, i = new(1, T, P, C).expand(B, T, P, C), new(B, T, 1, C).expand(B, T, P, C), new(B, 1, P, C).expand(B, T, P, C)
+    lam = torch.randn(C, device="cuda", generator=gen)
+    out = []
+    for args in ((x, r, i), tuple(t.contiguous() for t in (x, r, i))):
+        h = torch.full((B, T, P, C), POISON, dtype=type_, device="cuda")
+        d = gb.make_gatedscan(*args, h)
+        ws = torch.full((gb.gleam_gatedscan_workspace_bytes(d)[0],), 255, dtype=torch.uint8, device="cuda")
+        gb.gleam_gatedscan_fwd(d, *args, lam, None, None, h, None, ws)
+        out.append(h)
+    assert torch.equal(out[0], out[1]) and bool(torch.isfinite(out[0]).all())
+
+
 def test_gatedscan_state_out_of_nothing_and_not_wanted():
     m = Scan(2, 140, 1, 6, "bf16", lengths=[140, 0], state=False)
     S = m.fwd()[1]

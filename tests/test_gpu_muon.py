@@ -124,6 +124,32 @@ def test_muon_zero_infinite_and_extreme_gradients():
         assert np.linalg.norm(1.0 - t[k] - x) <= bound(5) * max(np.linalg.norm(x), 1e-3)
 
 
+@pytest.mark.parametrize("rows,cols", [(40, 50), (100, 300), (40, 1100)])
+def test_muon_of_a_cubic(rows, cols):
+    """c = 0: no A A.  A step amplifies by 1.5 and not by 3.4, so that the tolerance holds."""
+    g = torch.randn(rows, cols, device="cuda", generator=torch.Generator(device="cuda").manual_seed(cols))
+    theta, m = torch.zeros_like(g), torch.zeros_like(g)
+    step(theta, g, m, lr=1.0, momentum=0.0, a=1.5, b=-0.5, c=0.0, steps=8)
+    want = mo.orthogonalise(host(g), 8, float(np.float32(1e-7)), (1.5, -0.5, 0.0))
+    assert rel_l2(-host(theta), want) <= bound(8)
+
+
+@pytest.mark.parametrize("count,rows,cols", [(700, 9, 40), (300, 70, 40), (520, 33, 530)])
+def test_muon_of_many_matrices(count, rows, cols):
+    """More matrices than the chip has workgroups at once: each gets what it gets alone."""
+    gen = torch.Generator(device="cuda").manual_seed(count)
+    start = [torch.randn(count, rows, cols, device="cuda", generator=gen) for _ in range(3)]
+    all_at_once = [t.clone() for t in start]
+    step(*all_at_once, lr=0.1)
+    for k in (0, 1, 255, 256, count - 1):
+        alone = [t[k].clone() for t in start]
+        t, m = mo.muon(*(host(x) for x in alone), lr=0.1, momentum=float(np.float32(0.95)), weight_decay=0.0, nesterov=True, steps=5, eps=float(np.float32(1e-7)),
+                       coefficients=[float(np.float32(c)) for c in mo.COEFFICIENTS])
+        x = t - host(alone[0])
+        assert np.linalg.norm(host(all_at_once[0][k]) - t) <= bound(5) * np.linalg.norm(x) + 2.0 ** -24 * np.linalg.norm(t), k   # theta is rounded
+        assert np.abs(host(all_at_once[2][k]) - m).max() <= 2.0 ** -23 * np.abs(m).max()
+
+
 @pytest.mark.parametrize("rows,cols", [(40, 50), (100, 300)])
 def test_muon_with_an_eps_that_is_no_guard(rows, cols):
     """1 / (|u| + eps) passes the range of a float32 where u is zero or tiny; X = u / (|u| + eps) does not."""

@@ -143,6 +143,22 @@ def test_qknorm_in_place_and_without_sums(dtype):
     assert all(torch.equal(a, b) for a, b in zip(out, x))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d,rot", [(16, 8), (5, 4)])
+def test_qknorm_of_inputs_that_stand_for_many(d, rot, dtype):
+    """Inputs with strides of 0 (a head for all heads, a token for all tokens) give what their copies give, bit by bit."""
+    B, T, P, H, type_ = 2, 7, 3, 4, TYPES[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    new = lambda *s: torch.randn(*s, device="cuda", generator=gen).to(type_)  # noqa: E731
+    q, k = new(B, T, P, 1, d).expand(B, T, P, H, d), new(1, 1, P, 2, d).expand(B, T, P, 2, d)
+    freq, gamma, out = torch.rand(rot // 2, device="cuda", generator=gen), torch.rand(d, device="cuda", generator=gen), []
+    for a, b in ((q, k), (q.contiguous(), k.contiguous())):
+        to = [torch.full(t.shape, POISON, dtype=type_, device="cuda") for t in (a, b)]
+        gb.gleam_qknorm_fwd(gb.make_qknorm(a, b, *to, rot), a, b, gamma, None, freq, None, None, *to)
+        out.append(to)
+    assert all(torch.equal(x, y) and bool(torch.isfinite(x).all()) for x, y in zip(*out))
+
+
 def test_qknorm_writes_nothing_else():
     """Values between the heads, and rows of an array that the call does not name."""
     m = Qk(2, 3, 2, 3, 2, 20, 8, "bf16", layout="gaps")
