@@ -147,8 +147,7 @@ int check_muon(const gleam_muon* p) {
         if (!std::isfinite(v)) return GLEAM_E_DESC;
     if (!(p->eps > 0.f) || p->momentum < 0.f || p->momentum >= 1.f) return GLEAM_E_DESC;
     if (p->steps < 1 || p->steps > 100 || (p->nesterov != 0 && p->nesterov != 1)) return GLEAM_E_DESC;
-    double sx, sa, sb;
-    return muon_scales(*p, sx, sa, sb) ? GLEAM_OK : GLEAM_E_DESC;
+    return muon_scales(*p) ? GLEAM_OK : GLEAM_E_DESC;
 }
 
 int check_ws(const void* ws, size_t ws_bytes, size_t need) {

@@ -82,8 +82,8 @@ hipError_t gatedscan_backward(const gleam_gatedscan_desc& d, const void* x, cons
                               void* g_i, float* g_lambda, float* g_state_in, void* ws, hipStream_t st);
 
 // ------------------------------------------------------------------ orthogonalised update (muon.hip)
-// Powers of two that X, A = X X^T and the polynomial B of it are scaled by; false: the polynomial's values leave what they may reach.
-bool muon_scales(const gleam_muon& p, double& sx, double& sa, double& sb);
+// Whether X, A = X X^T and the polynomial B of it stay in the range that they may reach.
+bool muon_scales(const gleam_muon& p);
 size_t muon_ws_bytes(long long count, long long rows, long long cols);
 hipError_t muon_update(const gleam_muon& p, long long count, long long rows, long long cols, long long stride, float* theta,
                        const float* grad, float* m, void* ws, hipStream_t st);

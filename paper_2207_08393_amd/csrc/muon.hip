@@ -10,6 +10,13 @@
 // blocks of 32 rows x 16 columns, each 1 KB of a part (half of the columns, row, 8 columns), so that a wave's operand is one access of 16
 // bytes a lane, without conflicts in LDS.  X is kept in that form both ways round, since X X^T sums over its columns and (..) X over its rows.
 // A and the polynomial B = a I + b A + c A^2 are symmetric: only blocks on and above the diagonal are computed, and written twice.
+//
+// What bounds it.  Matrices of up to 16 blocks: the latency of six phases a step, one workgroup (192 x 64: 35 us, of which a launch is 6).
+// Larger ones: launches and the latency of one wave's share while the chip is not full (24 x 100 x 900: 110 us, 16 of it bytes and matrix
+// instructions), then operands on their way through the L1 caches, 50 bytes a clock and CU (1024 x 4096: X X^T 28 us, 460 TFLOP/s of
+// float16 products, B X 35 us, 740 TFLOP/s; a library product of that type reaches 1211), and in a product of the short side, 10 us, the 120 CUs that 136 tiles leave
+// without one.  Momentum and split move 5 and 7 bytes an element
+// at 4 to 6 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -35,6 +42,9 @@ struct MuonArgs {
     const float* grad;
     double* norms;                         // [matrix][kMuonNorms]
     char *x, *xt, *xt_out, *a, *b;         // parts of X [short][long], of its transpose, of A and B
+    const char *left, *right;              // of a symmetric product, and of kApply the left one
+    char* sym;                             // where a symmetric product goes
+    int sum;                               // blocks of its sum
     long long stride, count;
     int rows, cols, tall;                  // tall: X is the transpose of u
     int mb, nb;                            // blocks of 32 of the short and of the long side
@@ -43,7 +53,7 @@ struct MuonArgs {
     int splits;
     int nesterov, last, no_square;
     float lr_scale, decay, momentum, eps;
-    float x_scale, gram_scale, apply_scale, ca, cb, cc;   // of the sums, so that results have their scale; B = ca I + cc (cb A + A A)
+    float x_scale, sym_scale, apply_scale, ca, cb, cc;   // of the sums, so that results have their scale; B = ca I + cc (cb A + A A)
 };
 
 // A matrix of R x K blocks of 32 x 32: part p of the 16 columns k16 of rows 32 r ..
@@ -148,7 +158,7 @@ __global__ __launch_bounds__(128) void muon_split_kernel(MuonArgs a) {
     store_parts8(block_at(a.xt, matrix, a.nb, a.mb, bj, 2 * bi + (k8 >> 1), 0) + (k8 & 1) * 512 + line * 16, v);
 }
 
-enum MuonProduct { kGram, kSquare, kApply };
+enum MuonProduct { kSym, kSquare, kApply };
 
 // Blocks of 32 x 32 on their way out, in LDS: 32 rows of 33 floats.
 constexpr int kTileFloats = 32 * 33;
@@ -183,7 +193,7 @@ __device__ __forceinline__ void put_block(const MuonArgs& a, long long matrix, i
 #pragma unroll 1
     for (int side = 0; side < sides; ++side) {
         const int sl = side ? 1 : 33, sk = side ? 33 : 1;
-        char* out = MODE == kGram ? block_at(a.a, matrix, R, R, side ? bj : bi, 2 * (side ? bi : bj), 0)
+        char* out = MODE == kSym ? block_at(a.sym, matrix, R, R, side ? bj : bi, 2 * (side ? bi : bj), 0)
                     : MODE == kSquare ? block_at(a.b, matrix, R, R, side ? bj : bi, 2 * (side ? bi : bj), 0)
                     : side ? block_at(a.xt_out, matrix, Cb, R, bj, 2 * bi, 0) : block_at(a.x, matrix, R, Cb, bi, 2 * bj, 0);
 #pragma unroll
@@ -192,7 +202,7 @@ __device__ __forceinline__ void put_block(const MuonArgs& a, long long matrix, i
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int k = 8 * (up + 2 * g) + e;
-                v[e] = (MODE == kGram ? a.gram_scale : MODE == kSquare ? a.cc : a.apply_scale) * tile[line * sl + k * sk];
+                v[e] = (MODE == kSym ? a.sym_scale : MODE == kSquare ? a.cc : a.apply_scale) * tile[line * sl + k * sk];
                 if (MODE == kSquare) v[e] += bi == bj && k == line ? a.ca : 0.f;
             }
             store_parts8(out + g * kParts * kBlockBytes + up * 512 + line * 16, v);
@@ -247,8 +257,9 @@ __device__ __forceinline__ bool find_tile(const MuonArgs& a, int tr, int tc, Til
     return true;
 }
 
-// One of the three products of a step, rows of the left operand against rows of the right one:
-//   kGram  A = X X^T;   kSquare  B = a I + b A + c A A;   kApply  X <- B X, or at the last step the weights' update.
+// One of the products of a step, rows of the left operand against rows of the right one:
+//   kSym  A = X X^T, or a product of two symmetric matrices that commute;   kSquare  B = a I + b A + c A A;   kApply  X <- B X, or at the end
+//   the weights' update.
 // A workgroup computes 2 x 2 blocks of 32 x 32 over one of `splits` parts of the sum, and each of its four waves all of them over every fourth step of that: no
 // operand is needed by two waves, so they go from memory into registers as they lie there, kAhead steps of 16 columns before their use, with
 // no barrier until the four sums meet in LDS.  Short sums (SHORT) are not shared out: a wave computes one block, and the waves do not meet.
@@ -259,12 +270,12 @@ template <int MODE, bool SHORT>
 __global__ __launch_bounds__(256, 2) void muon_product_kernel(MuonArgs a) {
     constexpr int kAhead = 3, W = SHORT ? 1 : 2;   // blocks of a wave's sides
     __shared__ __attribute__((aligned(16))) float lds[4][SHORT ? 1 : 4][kTileFloats];
-    const int R = a.mb, Cb = MODE == kApply ? a.nb : a.mb, K = MODE == kGram ? a.nb : a.mb;   // blocks of the result's sides and of the sum
+    const int R = a.mb, Cb = MODE == kApply ? a.nb : a.mb, K = MODE == kSym ? a.sum : a.mb;   // blocks of the result's sides and of the sum
     Tile t;
     if (!find_tile<MODE>(a, (R + 1) / 2, (Cb + 1) / 2, t)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const char* left = MODE == kGram ? a.x : MODE == kSquare ? a.a : a.b;
-    const char* right = MODE == kGram ? a.x : MODE == kSquare ? a.a : a.xt;
+    const char* left = MODE == kSquare ? a.a : a.left;
+    const char* right = MODE == kSym ? a.right : MODE == kSquare ? a.a : a.xt;
     // steps k0, k0 + kEvery ..: the waves go through the sum side by side, so that workgroups that share rows read them at about the same time
     constexpr int kEvery = SHORT ? 1 : 4;
     const int s0 = (int)((long long)2 * K * t.split / a.splits), s1 = (int)((long long)2 * K * (t.split + 1) / a.splits);
@@ -492,7 +503,7 @@ __global__ __launch_bounds__(64 * kSmallBlocks) void muon_small_kernel(MuonArgs 
     const int mb = a.mb, nb = a.nb, bi = wave / nb, bj = wave - bi * nb;
     const bool mine = wave < mb * nb;                       // of X; the others may have a block of A
     Tile t;
-    place_tile<kGram>(wave, mb, t);
+    place_tile<kSym>(wave, mb, t);
     const bool of_a = wave < mb * (mb + 1) / 2;
     char *xs = lds, *as = lds + mb * nb * 2 * kParts * kBlockBytes;
     // this lane's elements of u as they lie in memory: column lane % 32, rows 8 q + 4 (lane / 32) + e of a block that is X's or its transpose
@@ -535,7 +546,7 @@ __global__ __launch_bounds__(64 * kSmallBlocks) void muon_small_kernel(MuonArgs 
         if (of_a) {
             av = small_product(xs, t.ti, xs, t.tj, nb, zero);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) av[i] *= a.gram_scale;
+            for (int i = 0; i < 16; ++i) av[i] *= a.sym_scale;
             if (t.ti != t.tj) small_along(as, mb, t.ti, t.tj, av);
             small_across(as, mb, t.ti, t.tj, av);
         }
@@ -571,14 +582,15 @@ __global__ __launch_bounds__(64 * kSmallBlocks) void muon_small_kernel(MuonArgs 
 }
 
 // Tiles of 64 x 64, and parts of the sum: a product of few tiles is split so that every CU has a workgroup, sums of 32 steps of 32 columns and more, no
-// part under eight (24 x 100 x 900, 29 steps: 122 us whole, 131 in three parts; 300 x 1000, 32 steps: 133 whole, 123 in four).
+// part under eight (24 x 100 x 900, 29 steps: 122 us whole, 131 in three parts; 300 x 1000, 32 steps: 133 whole, 123 in four; one step of the
+// update at a time).
 struct ProductPlan {
     bool is_short;            // sums of up to eight steps of 32 columns
     int splits;
     long long tiles;          // of a matrix
 };
-ProductPlan product_plan(long long count, int mb, int nb, MuonProduct mode) {
-    const long long R = mb, C = mode == kApply ? nb : mb, steps = mode == kGram ? nb : mb, tr = (R + 1) / 2, tc = (C + 1) / 2;
+ProductPlan product_plan(long long count, int mb, int nb, MuonProduct mode, int sum) {
+    const long long R = mb, C = mode == kApply ? nb : mb, steps = sum, tr = (R + 1) / 2, tc = (C + 1) / 2;
     ProductPlan p;
     p.tiles = mode == kApply ? tr * tc : tr * (tr + 1) / 2;
     long long s = 256 / (count * p.tiles);
@@ -590,8 +602,15 @@ ProductPlan product_plan(long long count, int mb, int nb, MuonProduct mode) {
 }
 size_t part_bytes(long long count, const ProductPlan& p) { return p.splits > 1 ? (size_t)count * p.tiles * p.splits * 4 * 4096 : 0; }
 
+// Several steps at a time (below) leave out two products over the long side, 1.5 mb^2 nb blocks, and take three over the short one, 1.5 mb^3, and a launch more:
+// worth it from 8192 blocks on.  us, one at a time against three and two: 300x1000 (2200 blocks) 114, 122; 512x1024 (4096) 137, 148; 24x128x512 (4608)
+// 105, 103; 24x100x900 (9600) 127, 115; 512x2048 (12288) 154, 152; 512x4096 (28672) 179, 167; 1024x1536 (16384, but one and a half as wide as high) 216, 219;
+// 1024x4096 (98304) 382, 291; 4 of it 1251, 866.
+bool is_wide(long long count, int mb, int nb) { return nb >= 2 * mb && count * (nb - mb) * mb * mb > 8192; }
+
 struct MuonPlan {
     int mb, nb, parts;
+    int squares;              // matrices of mb x mb: A and B, and where several steps are taken at a time another B and what they are multiplied to
     size_t x_bytes, a_bytes, norm_bytes, part_bytes;
 };
 MuonPlan plan_of(long long count, long long rows, long long cols) {
@@ -603,22 +622,22 @@ MuonPlan plan_of(long long count, long long rows, long long cols) {
     p.parts = (int)(parts < kMuonNorms ? parts : kMuonNorms);
     p.x_bytes = (size_t)count * p.mb * p.nb * 2 * kParts * kBlockBytes;
     p.a_bytes = (size_t)count * p.mb * p.mb * 2 * kParts * kBlockBytes;
+    p.squares = is_wide(count, p.mb, p.nb) ? 4 : 2;
     p.norm_bytes = (size_t)count * kMuonNorms * sizeof(double);
     p.part_bytes = 0;
-    for (MuonProduct mode : {kGram, kSquare, kApply}) {
-        const size_t n = part_bytes(count, product_plan(count, p.mb, p.nb, mode));
-        if (n > p.part_bytes) p.part_bytes = n;
-    }
+    for (const ProductPlan& q : {product_plan(count, p.mb, p.nb, kSym, p.nb), product_plan(count, p.mb, p.nb, kSquare, p.mb), product_plan(count, p.mb, p.nb, kApply, p.mb)})
+        p.part_bytes = std::max(p.part_bytes, part_bytes(count, q));
     return p;
 }
 
 template <int MODE>
 void launch_product(MuonArgs& a, hipStream_t st) {
-    const ProductPlan p = product_plan(a.count, a.mb, a.nb, (MuonProduct)MODE);
-    const double R = a.mb, C = MODE == kApply ? a.nb : (a.mb + 1) * 0.5, K = MODE == kGram ? a.nb : a.mb, work = 65536.0 * R * C * K * a.count;
+    const int sum = MODE == kSym ? a.sum : a.mb;
+    const ProductPlan p = product_plan(a.count, a.mb, a.nb, (MuonProduct)MODE, sum);
+    const double R = a.mb, C = MODE == kApply ? a.nb : (a.mb + 1) * 0.5, K = sum, work = 65536.0 * R * C * K * a.count;
     a.splits = p.splits;
     {
-        KernelScope ks(MODE == kGram ? "muon_gram" : MODE == kSquare ? "muon_square" : "muon_apply", work, 0.0, st, kProducts * work);
+        KernelScope ks(MODE == kSym ? "muon_sym" : MODE == kSquare ? "muon_square" : "muon_apply", work, 0.0, st, kProducts * work);
         const dim3 grid = grid_of((a.count * p.tiles * p.splits + 7) / 8 * 8), block(256);
         if (p.is_short) hipLaunchKernelGGL((muon_product_kernel<MODE, true>), grid, block, 0, st, a);
         else hipLaunchKernelGGL((muon_product_kernel<MODE, false>), grid, block, 0, st, a);
@@ -628,9 +647,11 @@ void launch_product(MuonArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((muon_join_kernel<MODE>), grid_of(a.count * p.tiles * 4), dim3(64), 0, st, a);
 }
 
-}  // namespace
+// The power of two that takes v to (2^13, 2^14].
+double scale_of(double v) { return std::ldexp(1.0, 14 - (int)std::ceil(std::log2(v))); }
 
-bool muon_scales(const gleam_muon& p, double& sx, double& sa, double& sb) {
+// Scales of X, A and B, and the largest value of the polynomial; false where numbers would leave their range.
+bool bounds_of(const gleam_muon& p, double& sx, double& sa, double& sb, double& most_b) {
     const double a = p.a, b = p.b, c = p.c;
     double most = 1.0, top = 1.0;   // singular values of any X, and of this one: |u|_F bounds the largest
     for (int k = 0; k + 1 < p.steps; ++k) {   // the last X goes to the weights in float32
@@ -647,21 +668,37 @@ bool muon_scales(const gleam_muon& p, double& sx, double& sa, double& sb) {
     }
     const double z1 = most * most, vertex = c != 0.0 ? -b / (2.0 * c) : 0.0;
     auto poly = [&](double z) { return std::fabs(a + z * (b + z * c)); };
-    double most_b = std::max(poly(0.0), poly(z1));
+    most_b = std::max(poly(0.0), poly(z1));
     if (vertex > 0.0 && vertex < z1) most_b = std::max(most_b, poly(vertex));
     most_b = std::max(most_b, 1e-3);
     if (!(most_b < 16384.0)) return false;
-    auto scale = [](double v) { return std::ldexp(1.0, 14 - (int)std::ceil(std::log2(v))); };   // v scale in (2^13, 2^14]
-    sx = scale(most);
-    sa = scale(z1);
-    sb = scale(most_b);
+    sx = scale_of(most);
+    sa = scale_of(z1);
+    sb = scale_of(most_b);
     return true;
+}
+
+// Several steps at a time, of wide matrices: B is a polynomial of A and commutes with it, so the next step's A is (B A) B, and the steps'
+// B multiply to one Q that X is multiplied by: instead of X X^T and B X, sums over the long side, three products of the short one.  What A is
+// rounded by, 2^-24 of its largest eigenvalue, is then not found again in the next X X^T: an eigenvalue near 0 grows by a^2 a step and Q changes by 2 b / a
+// of that, 2^-23 |b / a| (1 + a^2 + a^4) of itself after three steps (2.5e-5 of the smallest singular values with the default polynomial,
+// of which a step at a time leaves 2^-21 a^5 of the largest, 2.3e-4); so no more than three, and fewer where a is larger.
+int steps_at_once(const gleam_muon& h) {
+    const double a2 = (double)h.a * h.a, loss = 0x1p-23 * std::fabs((double)h.b) / std::max(std::fabs((double)h.a), 1e-3);
+    return loss * (1.0 + a2 + a2 * a2) < 3e-5 ? 3 : loss * (1.0 + a2) < 3e-5 ? 2 : 1;
+}
+
+}  // namespace
+
+bool muon_scales(const gleam_muon& p) {
+    double sx, sa, sb, most_b;
+    return bounds_of(p, sx, sa, sb, most_b);
 }
 
 size_t muon_ws_bytes(long long count, long long rows, long long cols) {
     const MuonPlan p = plan_of(count, rows, cols);
     if (is_small(p.mb, p.nb)) return 0;
-    return 3 * p.x_bytes + 2 * p.a_bytes + p.norm_bytes + p.part_bytes;
+    return 3 * p.x_bytes + p.squares * p.a_bytes + p.norm_bytes + p.part_bytes;
 }
 
 hipError_t muon_update(const gleam_muon& h, long long count, long long rows, long long cols, long long stride, float* theta,
@@ -677,8 +714,9 @@ hipError_t muon_update(const gleam_muon& h, long long count, long long rows, lon
     a.xt_out = at + 2 * p.x_bytes;
     a.a = at + 3 * p.x_bytes;
     a.b = a.a + p.a_bytes;
-    a.norms = (double*)(a.b + p.a_bytes);
-    a.part = (float*)(a.b + p.a_bytes + p.norm_bytes);
+    char *b[2] = {a.a + p.a_bytes, p.squares > 2 ? a.a + 2 * p.a_bytes : nullptr}, *t = p.squares > 2 ? a.a + 3 * p.a_bytes : nullptr;
+    a.norms = (double*)(a.a + p.squares * p.a_bytes);
+    a.part = (float*)(a.a + p.squares * p.a_bytes + p.norm_bytes);
     a.stride = stride;
     a.count = count;
     a.rows = (int)rows;
@@ -693,12 +731,13 @@ hipError_t muon_update(const gleam_muon& h, long long count, long long rows, lon
     a.eps = h.eps;
     // b A + c A A = c ((b / c) A + A A); where c A A is below 2^-60 of b A, or c is 0, it is b A alone
     a.no_square = std::fabs((double)h.c) <= std::fabs((double)h.b) * 0x1p-60;
-    double sx = 1.0, sa = 1.0, sb = 1.0;
-    muon_scales(h, sx, sa, sb);
+    double sx = 1.0, sa = 1.0, sb = 1.0, most_b = 1.0;
+    bounds_of(h, sx, sa, sb, most_b);
+    const double lr = (double)h.lr * std::sqrt(a.tall ? (double)rows / (double)cols : 1.0);
     a.x_scale = (float)sx;
-    a.gram_scale = (float)(sa / (sx * sx));
+    a.sym_scale = (float)(sa / (sx * sx));
     a.apply_scale = (float)(1.0 / sb);
-    a.lr_scale = (float)((double)h.lr * std::sqrt(a.tall ? (double)rows / (double)cols : 1.0) / (sb * sx));
+    a.lr_scale = (float)(lr / (sb * sx));
     a.ca = (float)(h.a * sb);
     a.cb = (float)(a.no_square ? sa : sa * (double)h.b / (double)h.c);
     a.cc = (float)((a.no_square ? h.b : h.c) * (sb / (sa * sa)));
@@ -718,14 +757,45 @@ hipError_t muon_update(const gleam_muon& h, long long count, long long rows, lon
         hipLaunchKernelGGL(muon_split_kernel, grid_of(count * p.mb * p.nb), dim3(128), 0, st, a);
     }
     e = hipGetLastError();
-    for (int k = 0; k < h.steps && e == hipSuccess; ++k) {
-        a.last = k == h.steps - 1;
-        launch_product<kGram>(a, st);
-        launch_product<kSquare>(a, st);
+    // symmetric products of `left` and `right`, whose numbers have these scales, to `to`
+    auto sym = [&](const char* left, double sl, const char* right, double sr, int sum, char* to, double s_to) {
+        a.left = left;
+        a.right = right;
+        a.sum = sum;
+        a.sym = to;
+        a.sym_scale = (float)(s_to / (sl * sr));
+        launch_product<kSym>(a, st);
+    };
+    const int most = p.squares > 2 ? steps_at_once(h) : 1, rounds = (h.steps + most - 1) / most;
+    for (int k = 0, round = 0; k < h.steps && e == hipSuccess; ++round) {
+        const int now = (h.steps - k + rounds - round - 1) / (rounds - round);   // steps of this round, as even as they go
+        sym(a.x, sx, a.x, sx, a.nb, a.a, sa);
+        const char* q = nullptr;
+        double sq = sb;
+        for (int j = 0; j < now; ++j) {
+            a.b = b[j & 1];
+            launch_product<kSquare>(a, st);
+            if (j + 1 < now) {
+                sym(a.b, sb, a.a, sa, a.mb, t, sa);      // B A, under the largest singular values of two X
+                sym(t, sa, a.b, sb, a.mb, a.a, sa);      // A of the next step
+            }
+            if (j == 0) {
+                q = a.b;
+                continue;
+            }
+            char* to = j == 1 ? t : b[~j & 1];           // T is not needed any more; the B before neither
+            const double s_to = scale_of(std::pow(most_b, j + 1));
+            sym(a.b, sb, q, sq, a.mb, to, s_to);
+            q = to;
+            sq = s_to;
+        }
+        k += now;
+        a.last = k == h.steps;
+        a.left = q;
+        a.apply_scale = (float)(1.0 / sq);
+        a.lr_scale = (float)(lr / (sq * sx));
         launch_product<kApply>(a, st);
-        char* t = a.xt;
-        a.xt = a.xt_out;
-        a.xt_out = t;
+        std::swap(a.xt, a.xt_out);
         e = hipGetLastError();
     }
     return e;

@@ -73,6 +73,29 @@ def test_muon_steps(steps):
     check(1, 96, 160, steps=steps, momentum=0.0)
 
 
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 7, 10])
+@pytest.mark.parametrize("rows,cols", [(100, 2000), (2000, 100)])
+def test_muon_of_wide_matrices(rows, cols, steps):
+    """Wide enough for several steps at a time."""
+    check(12, rows, cols, steps=steps)
+
+
+@pytest.mark.parametrize("coefficients,steps", [((6.0, -10.0, 5.0), 2), ((1.5, -0.5, 0.0), 8), ((1.0, 0.0, 0.0), 3)])
+def test_muon_of_wide_matrices_and_other_polynomials(coefficients, steps):
+    g = torch.randn(12, 100, 2000, device="cuda", generator=torch.Generator(device="cuda").manual_seed(steps))
+    theta, m = torch.zeros_like(g), torch.zeros_like(g)
+    a, b, c = coefficients
+    step(theta, g, m, lr=1.0, momentum=0.0, a=a, b=b, c=c, steps=steps)
+    for k in (0, 11):
+        err = rel_l2(-host(theta[k]), mo.orthogonalise(host(g[k]), steps, float(np.float32(1e-7)), coefficients))
+        print("muon", coefficients, steps, "error", err, flush=True)
+        assert err <= 8 * 2.0 ** -24 * sum(a ** k for k in range(steps + 1))
+
+
+def test_muon_of_wide_matrices_with_few_strong_directions():
+    check(12, 100, 2000, low=3)
+
+
 def test_muon_of_few_strong_directions():
     check(1, 200, 300, low=5)
     check(1, 300, 200, low=1)
