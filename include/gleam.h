@@ -302,7 +302,8 @@ int gleam_unrolled_infer(const gleam_geom* geom, const gleam_prox_desc* prox, in
 /* ---- Sequence layers: layer norm, dropout, linear attention along the frames -----------------------------------------
  * Operators of their own: a prox network (gleam_prox_desc) has convolutions only and does not call them.  They take feature maps
  * [..][channels], channels last, and mix the frames of a dynamic series, or the tokens of any sequence: y = layer_norm(x); q, k, v =
- * projections of y; h = x + dropout(projection of linear_attention(q, k, v)).  Activations are float32 (dtype 0) or bfloat16 (dtype 1) and
+ * projections of y; h = x + dropout(projection of linear_attention(q, k, v)).  Further below: norm and rotation of q and k, a gated
+ * scan that takes the attention's place, and an update for the projections' matrices.  Activations are float32 (dtype 0) or bfloat16 (dtype 1) and
  * are computed on in float32 (products of bfloat16 arrays on the bfloat16 matrix cores with float32 sums); scales, shifts, statistics,
  * decays and states are float32.  Conventions are those above, except that arrays may have strides (rows: fewer than 2^31, arrays of at
  * most 2^40 elements).  Pointers need the alignment of their element type; accesses are fastest where base addresses and strides are

@@ -14,9 +14,9 @@
 // What bounds it.  Matrices of up to 16 blocks: the latency of six phases a step, one workgroup (192 x 64: 35 us, of which a launch is 6).
 // Larger ones: launches and the latency of one wave's share while the chip is not full (24 x 100 x 900: 110 us, 16 of it bytes and matrix
 // instructions), then operands on their way through the L1 caches, 50 bytes a clock and CU (1024 x 4096: X X^T 28 us, 460 TFLOP/s of
-// float16 products, B X 35 us, 740 TFLOP/s; a library product of that type reaches 1211), and in a product of the short side, 10 us, the 120 CUs that 136 tiles leave
-// without one.  Momentum and split move 5 and 7 bytes an element
-// at 4 to 6 TB/s.
+// float16 products, B X 35 us, 740 TFLOP/s; a library product of that type reaches 1211),
+// and in a product of the short side, 10 us, the 120 CUs that 136 tiles leave without one.  Momentum and split move 12 and 16 bytes an element
+// at 4.4 and 5.2 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -766,9 +766,9 @@ hipError_t muon_update(const gleam_muon& h, long long count, long long rows, lon
         a.sym_scale = (float)(s_to / (sl * sr));
         launch_product<kSym>(a, st);
     };
-    const int most = p.squares > 2 ? steps_at_once(h) : 1, rounds = (h.steps + most - 1) / most;
-    for (int k = 0, round = 0; k < h.steps && e == hipSuccess; ++round) {
-        const int now = (h.steps - k + rounds - round - 1) / (rounds - round);   // steps of this round, as even as they go
+    const int most = p.squares > 2 ? steps_at_once(h) : 1, turns = (h.steps + most - 1) / most;
+    for (int k = 0, turn = 0; k < h.steps && e == hipSuccess; ++turn) {
+        const int now = (h.steps - k + turns - turn - 1) / (turns - round);   // steps taken together, as even as they go
         sym(a.x, sx, a.x, sx, a.nb, a.a, sa);
         const char* q = nullptr;
         double sq = sb;
