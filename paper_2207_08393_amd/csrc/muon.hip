@@ -768,7 +768,7 @@ hipError_t muon_update(const gleam_muon& h, long long count, long long rows, lon
     };
     const int most = p.squares > 2 ? steps_at_once(h) : 1, turns = (h.steps + most - 1) / most;
     for (int k = 0, turn = 0; k < h.steps && e == hipSuccess; ++turn) {
-        const int now = (h.steps - k + turns - turn - 1) / (turns - round);   // steps taken together, as even as they go
+        const int now = (h.steps - k + turns - turn - 1) / (turns - turn);   // steps taken together, as even as they go
         sym(a.x, sx, a.x, sx, a.nb, a.a, sa);
         const char* q = nullptr;
         double sq = sb;
