@@ -53,6 +53,7 @@ struct MuonArgs {
     int splits;
     int nesterov, last, no_square;
     float lr_scale, decay, momentum, eps;
+    float turn_scale, q_scale[2];          // of B A and (B A) B, and of the second and third Q
     float x_scale, sym_scale, apply_scale, ca, cb, cc;   // of the sums, so that results have their scale; B = ca I + cc (cb A + A A)
 };
 
@@ -581,6 +582,67 @@ __global__ __launch_bounds__(64 * kSmallBlocks) void muon_small_kernel(MuonArgs 
         if (in(i)) theta[at(i)] = a.decay * old[i] - a.lr_scale * x[i];
 }
 
+// Several steps (below) of a short side of up to four blocks, in one workgroup a matrix: from A to Q, the product of the steps' B.  A wave computes one block of
+// mb x mb of each product; the two operands stand in LDS as parts.  All these matrices are symmetric, so a block may be written as its transpose.
+constexpr int kCoreSide = 4;
+__global__ __launch_bounds__(64 * kCoreSide * kCoreSide) void muon_core_kernel(MuonArgs a, int steps) {
+    constexpr int kMost = kCoreSide * kCoreSide * 2 * kParts * kBlockBytes;
+    __shared__ __attribute__((aligned(16))) char first[kMost], second[kMost];   // A, then B A, then Q; and B
+    const long long matrix = group_of_grid();
+    if (matrix >= a.count) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, mb = a.mb, bi = wave / mb, bj = wave - bi * mb;
+    const char* from = block_at(a.a, matrix, mb, mb, 0, 0, 0) + threadIdx.x * 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)   // 4 KB a wave
+        *(uint4v*)(first + (i * blockDim.x + threadIdx.x) * 16) = *(const uint4v*)(from + i * blockDim.x * 16);
+    __syncthreads();
+    const floatx16 zero = {};
+    floatx16 v, q;   // A, and Q
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const char* at = first + ((bj * 2 * mb + 2 * bi + (k >> 1)) * kParts) * kBlockBytes + (k & 1) * 512 + (lane & 31) * 16 + (lane >> 5) * 8;
+        const halfx4 hi = *(const halfx4*)at, lo = *(const halfx4*)(at + kBlockBytes);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * k + e] = (float)lo[e] + (float)hi[e];
+    }
+    auto times = [](floatx16& m, float by) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) m[i] *= by;
+    };
+    for (int s = 0;; ++s) {
+        const bool last = s + 1 == steps;
+        times(v, a.cb);
+        if (!a.no_square) v = small_product(first, bi, first, bj, mb, v);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = a.cc * v[i] + (bi == bj && 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) == (lane & 31) ? a.ca : 0.f);
+        if (s == 0) q = v;
+        if (s == 0 && last) break;
+        small_across(second, mb, bi, bj, v);
+        __syncthreads();                     // B is there; where it is the last, A has been read
+        if (!last) {
+            v = small_product(second, bi, first, bj, mb, zero);
+            times(v, a.turn_scale);
+            __syncthreads();                 // A has been read
+            small_across(first, mb, bi, bj, v);
+            __syncthreads();
+            v = small_product(first, bi, second, bj, mb, zero);   // the next A
+            times(v, a.turn_scale);
+            if (s > 0) __syncthreads();      // B A has been read
+        }
+        if (s > 0) {
+            small_across(first, mb, bi, bj, q);
+            __syncthreads();
+            q = small_product(second, bi, first, bj, mb, zero);
+            times(q, a.q_scale[s - 1]);
+        }
+        if (last) break;
+        __syncthreads();                     // B A, or Q, has been read, and B
+        small_across(first, mb, bi, bj, v);
+        __syncthreads();
+    }
+    small_across(block_at(a.b, matrix, mb, mb, 0, 0, 0), mb, bi, bj, q);
+}
+
 // Tiles of 64 x 64, and parts of the sum: a product of few tiles is split so that every CU has a workgroup, sums of 32 steps of 32 columns and more, no
 // part under eight (24 x 100 x 900, 29 steps: 122 us whole, 131 in three parts; 300 x 1000, 32 steps: 133 whole, 123 in four; one step of the
 // update at a time).
@@ -606,7 +668,7 @@ size_t part_bytes(long long count, const ProductPlan& p) { return p.splits > 1 ?
 // worth it from 8192 blocks on.  us, one at a time against three and two: 300x1000 (2200 blocks) 114, 122; 512x1024 (4096) 137, 148; 24x128x512 (4608)
 // 105, 103; 24x100x900 (9600) 127, 115; 512x2048 (12288) 154, 152; 512x4096 (28672) 179, 167; 1024x1536 (16384, but one and a half as wide as high) 216, 219;
 // 1024x4096 (98304) 382, 291; 4 of it 1251, 866.
-bool is_wide(long long count, int mb, int nb) { return nb >= 2 * mb && count * (nb - mb) * mb * mb > 8192; }
+bool is_wide(long long count, int mb, int nb) { return mb > kCoreSide && nb >= 2 * mb && count * (nb - mb) * mb * mb > 8192; }
 
 struct MuonPlan {
     int mb, nb, parts;
@@ -766,13 +828,26 @@ hipError_t muon_update(const gleam_muon& h, long long count, long long rows, lon
         a.sym_scale = (float)(s_to / (sl * sr));
         launch_product<kSym>(a, st);
     };
-    const int most = p.squares > 2 ? steps_at_once(h) : 1, turns = (h.steps + most - 1) / most;
+    const bool core = p.mb <= kCoreSide;
+    const int most = core || p.squares > 2 ? steps_at_once(h) : 1, turns = (h.steps + most - 1) / most;
     for (int k = 0, turn = 0; k < h.steps && e == hipSuccess; ++turn) {
         const int now = (h.steps - k + turns - turn - 1) / (turns - turn);   // steps taken together, as even as they go
         sym(a.x, sx, a.x, sx, a.nb, a.a, sa);
         const char* q = nullptr;
         double sq = sb;
-        for (int j = 0; j < now; ++j) {
+        if (core) {
+            a.turn_scale = (float)(1.0 / sb);
+            for (int j = 1; j < now; ++j) {
+                const double s_to = scale_of(std::pow(most_b, j + 1));
+                a.q_scale[j - 1] = (float)(s_to / (sb * sq));
+                sq = s_to;
+            }
+            q = a.b = b[0];
+            const double work = 65536.0 * p.mb * p.mb * p.mb * count * (now == 1 ? 1 : 4 * now - 3);
+            KernelScope ks("muon_core", work, 0.0, st, kProducts * work);
+            hipLaunchKernelGGL(muon_core_kernel, grid_of(count), dim3(64 * p.mb * p.mb), 0, st, a, now);
+        }
+        for (int j = 0; j < (core ? 0 : now); ++j) {
             a.b = b[j & 1];
             launch_product<kSquare>(a, st);
             if (j + 1 < now) {
