@@ -12,7 +12,7 @@
 // A and the polynomial B = a I + b A + c A^2 are symmetric: only blocks on and above the diagonal are computed, and written twice.
 //
 // What bounds it.  Matrices of up to 16 blocks: the latency of six phases a step, one workgroup (192 x 64: 35 us, of which a launch is 6).
-// Larger ones: launches and the latency of one wave's share while the chip is not full (24 x 100 x 900: 110 us, 16 of it bytes and matrix
+// Larger ones: launches and the latency of one wave's share while the chip is not full (24 x 100 x 900: 90 us, 12 of it bytes and matrix
 // instructions), then operands on their way through the L1 caches, 50 bytes a clock and CU (1024 x 4096: X X^T 28 us, 460 TFLOP/s of
 // float16 products, B X 35 us, 740 TFLOP/s; a library product of that type reaches 1211),
 // and in a product of the short side, 10 us, the 120 CUs that 136 tiles leave without one.  Momentum and split move 12 and 16 bytes an element
@@ -584,6 +584,9 @@ __global__ __launch_bounds__(64 * kSmallBlocks) void muon_small_kernel(MuonArgs 
 
 // Several steps (below) of a short side of up to four blocks, in one workgroup a matrix: from A to Q, the product of the steps' B.  A wave computes one block of
 // mb x mb of each product; the two operands stand in LDS as parts.  All these matrices are symmetric, so a block may be written as its transpose.
+// Latency bounds it: 3.5 us a product of 128 x 128, 25 us for the seven of a round of two or three steps, where a launch for each takes 4.6 to 5 us
+// (64 x 576, five steps: 77 -> 48 us in all, 24 x 100 x 900 115 -> 95).  Ten waves that compute the blocks on and above the diagonal alone, and write each twice, took
+// 29 us where these sixteen take 25.
 constexpr int kCoreSide = 4;
 __global__ __launch_bounds__(64 * kCoreSide * kCoreSide) void muon_core_kernel(MuonArgs a, int steps) {
     constexpr int kMost = kCoreSide * kCoreSide * 2 * kParts * kBlockBytes;
@@ -665,9 +668,8 @@ ProductPlan product_plan(long long count, int mb, int nb, MuonProduct mode, int 
 size_t part_bytes(long long count, const ProductPlan& p) { return p.splits > 1 ? (size_t)count * p.tiles * p.splits * 4 * 4096 : 0; }
 
 // Several steps at a time (below) leave out two products over the long side, 1.5 mb^2 nb blocks, and take three over the short one, 1.5 mb^3, and a launch more:
-// worth it from 8192 blocks on.  us, one at a time against three and two: 300x1000 (2200 blocks) 114, 122; 512x1024 (4096) 137, 148; 24x128x512 (4608)
-// 105, 103; 24x100x900 (9600) 127, 115; 512x2048 (12288) 154, 152; 512x4096 (28672) 179, 167; 1024x1536 (16384, but one and a half as wide as high) 216, 219;
-// 1024x4096 (98304) 382, 291; 4 of it 1251, 866.
+// worth it from 8192 blocks on.  us, one at a time against three and two: 300x1000 (2200 blocks) 114, 122; 512x1024 (4096) 137, 148; 512x2048 (12288) 154, 152; 512x4096 (28672) 179, 167; 1024x1536 (16384, but one and a half as wide as high) 216, 219;
+// 1024x4096 (98304) 382, 291; 4 of it 1251, 866.  A short side of up to kCoreSide blocks goes by the kernel above in any case.
 bool is_wide(long long count, int mb, int nb) { return mb > kCoreSide && nb >= 2 * mb && count * (nb - mb) * mb * mb > 8192; }
 
 struct MuonPlan {
