@@ -584,9 +584,9 @@ __global__ __launch_bounds__(64 * kSmallBlocks) void muon_small_kernel(MuonArgs 
 
 // Several steps (below) of a short side of up to four blocks, in one workgroup a matrix: from A to Q, the product of the steps' B.  A wave computes one block of
 // mb x mb of each product; the two operands stand in LDS as parts.  All these matrices are symmetric, so a block may be written as its transpose.
-// Latency bounds it: 3.5 us a product of 128 x 128, 25 us for the seven of a round of two or three steps, where a launch for each takes 4.6 to 5 us
-// (64 x 576, five steps: 77 -> 48 us in all, 24 x 100 x 900 115 -> 95).  Ten waves that compute the blocks on and above the diagonal alone, and write each twice, took
-// 29 us where these sixteen take 25.
+// Latency bounds it: 2.9 us a product of 128 x 128 (24 of 100 x 900: 41 us for the 14 of five steps), where a launch for each takes 4.6 to 5 us
+// (64 x 576, five steps: 77 -> 48 us in all, 24 x 100 x 900 115 -> 95).  Ten waves that compute the blocks on and above the diagonal alone, and write
+// each twice, took 29 us for three steps where these sixteen take 25.
 constexpr int kCoreSide = 4;
 __global__ __launch_bounds__(64 * kCoreSide * kCoreSide) void muon_core_kernel(MuonArgs a, int steps) {
     constexpr int kMost = kCoreSide * kCoreSide * 2 * kParts * kBlockBytes;
