@@ -592,6 +592,7 @@ ScanPlan plan_of(const gleam_gatedscan_desc& d, bool backward) {
     const long long most_slabs = col_groups < 1024 ? 1024 / col_groups : 1;
     if (p.slabs > most_slabs) p.slabs = most_slabs;
     p.slab = (p.rows + p.slabs - 1) / p.slabs;
+    p.slabs = (p.rows + p.slab - 1) / p.slab;   // rounded up, fewer slabs may hold all rows: none is without one, every sum is written that is read
     return p;
 }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }

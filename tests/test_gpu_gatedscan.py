@@ -132,6 +132,14 @@ def test_gatedscan_many_columns(dtype):
     Scan(1, 6000, 1, 5, dtype).check()
 
 
+@pytest.mark.parametrize("B,P,C,dtype", [(1, 16641, 7, "f32"), (1, 16641, 300, "bf16"), (1, 30000, 64, "bf16"), (2, 150 * 150, 64, "f32"), (1, 200 * 200, 7, "bf16"),
+                                         (1, 131073, 7, "f32"), (1, 368 * 368, 3, "f32")])
+def test_gatedscan_gradients_of_many_pixels(B, P, C, dtype):
+    """Numbers of pixels that the slabs of rows, which the sums over pixels are split into, do not divide; the workspace starts as NaN."""
+    print("case scan pixels", B, P, C, dtype, flush=True)
+    Scan(B, 2, P, C, dtype).check()
+
+
 def test_gatedscan_of_long_memories_and_closed_gates():
     """Memories of 100 000 tokens, where a itself, rounded to float32, would be off by 0.3 % of 1 - a; gates that are shut or wide open, with
     decays from none to all."""
