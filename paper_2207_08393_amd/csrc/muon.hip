@@ -747,9 +747,14 @@ bool bounds_of(const gleam_muon& p, double& sx, double& sa, double& sb, double& 
 // rounded by, 2^-24 of its largest eigenvalue, is then not found again in the next X X^T: an eigenvalue near 0 grows by a^2 a step and Q changes by 2 b / a
 // of that, 2^-23 |b / a| (1 + a^2 + a^4) of itself after three steps (2.5e-5 of the smallest singular values with the default polynomial,
 // of which a step at a time leaves 2^-21 a^5 of the largest, 2.3e-4); so no more than three, and fewer where a is larger.
-int steps_at_once(const gleam_muon& h) {
+// And Q has to be in reach of its scale, which is made for the largest value the steps' B could have, most_b^n of n steps, where what is there is about
+// a^n, and 1 beside it: above 2^12 of that its second parts would begin to go below the smallest float16 (at 2^16 of it; (1, -3, 6) has 2^21 for two
+// steps: 2500 x 700 X off by 1.2e-4 of itself together, 2.4e-7 one by one).
+int steps_at_once(const gleam_muon& h, double most_b) {
     const double a2 = (double)h.a * h.a, loss = 0x1p-23 * std::fabs((double)h.b) / std::max(std::fabs((double)h.a), 1e-3);
-    return loss * (1.0 + a2 + a2 * a2) < 3e-5 ? 3 : loss * (1.0 + a2) < 3e-5 ? 2 : 1;
+    const double over = most_b / std::min(std::max(std::fabs((double)h.a), 1e-6), 1.0);
+    auto may = [&](int n, double grown) { return loss * grown < 3e-5 && std::pow(over, n) <= 0x1p12; };
+    return may(3, 1.0 + a2 + a2 * a2) ? 3 : may(2, 1.0 + a2) ? 2 : 1;
 }
 
 }  // namespace
@@ -831,7 +836,7 @@ hipError_t muon_update(const gleam_muon& h, long long count, long long rows, lon
         launch_product<kSym>(a, st);
     };
     const bool core = p.mb <= kCoreSide;
-    const int most = core || p.squares > 2 ? steps_at_once(h) : 1, turns = (h.steps + most - 1) / most;
+    const int most = core || p.squares > 2 ? steps_at_once(h, most_b) : 1, turns = (h.steps + most - 1) / most;
     for (int k = 0, turn = 0; k < h.steps && e == hipSuccess; ++turn) {
         const int now = (h.steps - k + turns - turn - 1) / (turns - turn);   // steps taken together, as even as they go
         sym(a.x, sx, a.x, sx, a.nb, a.a, sa);
