@@ -1,9 +1,11 @@
 // Orthogonalised update of weight matrices (gfx950): momentum, X = u / |u|, Newton-Schulz steps X <- (a I + b A + c A^2) X with A = X X^T of
 // the smaller side, and the update of the weights.
 //
-// A step amplifies small singular values by a = 3.4 and with them what X was rounded by, so products are about as good as float32 ones: every
+// A step amplifies small singular values by a = 3.4 and with them what X was rounded by, so products are made nearly as good as float32 ones: every
 // matrix is kept as the sum of two float16 numbers, 11 bits each, and a product is three of the float16 matrix cores' (the product of the two
-// second parts, 2^-22 of the whole at most, is left out).  That is 5 times as fast as the float32 matrix cores, and twice as fast as three
+// second parts, 2^-22 of the whole at most, is left out): 2^-21 where float32 operands bring 2^-23, and the same sums.  After five steps X is 0.4 to 1.7
+// times as far from exact as float32 products leave it (30 x 800 to 512 x 2048, noise, strong directions over noise, singular values spread from 1
+// to 1e-4).  That is 5 times as fast as the float32 matrix cores, and twice as fast as three
 // bfloat16 parts and six products.  Float16 has a range to mind: every matrix is scaled by a power of two that keeps it under 2^15, from the
 // largest singular value that the polynomial can make of [0, 1], which the host works out; small second parts may be subnormal.
 // Matrices are split once, by the kernel that writes them, and kept as the matrix instruction reads its operands:
@@ -53,7 +55,7 @@ struct MuonArgs {
     int splits;
     int nesterov, last, no_square;
     float lr_scale, decay, momentum, eps;
-    float turn_scale, q_scale[2];          // of B A and (B A) B, and of the second and third Q
+    float turn_scale, q_scale;             // of B A and (B A) B, and of Q
     float x_scale, sym_scale, apply_scale, ca, cb, cc;   // of the sums, so that results have their scale; B = ca I + cc (cb A + A A)
 };
 
@@ -582,15 +584,12 @@ __global__ __launch_bounds__(64 * kSmallBlocks) void muon_small_kernel(MuonArgs 
         if (in(i)) theta[at(i)] = a.decay * old[i] - a.lr_scale * x[i];
 }
 
-// Several steps (below) of a short side of up to four blocks, in one workgroup a matrix: from A to Q, the product of the steps' B.  A wave computes one block of
-// mb x mb of each product; the two operands stand in LDS as parts.  All these matrices are symmetric, so a block may be written as its transpose.
-// Latency bounds it: 2.9 us a product of 128 x 128 (24 of 100 x 900: 41 us for the 14 of five steps), where a launch for each takes 4.6 to 5 us
-// (64 x 576, five steps: 77 -> 48 us in all, 24 x 100 x 900 115 -> 95).  Ten waves that compute the blocks on and above the diagonal alone, and write
-// each twice, took 29 us for three steps where these sixteen take 25.
+// One step or two (below) of a short side of up to four blocks, in one workgroup a matrix: from A to Q, the product of the steps' B.  A wave computes one
+// block of mb x mb of each product; the two operands stand in LDS as parts.  All these matrices are symmetric, so a block may be written as its transpose.
 constexpr int kCoreSide = 4;
 __global__ __launch_bounds__(64 * kCoreSide * kCoreSide) void muon_core_kernel(MuonArgs a, int steps) {
     constexpr int kMost = kCoreSide * kCoreSide * 2 * kParts * kBlockBytes;
-    __shared__ __attribute__((aligned(16))) char first[kMost], second[kMost];   // A, then B A, then Q; and B
+    __shared__ __attribute__((aligned(16))) char first[kMost], second[kMost];   // A, then B A, the next A and its B; and B
     const long long matrix = group_of_grid();
     if (matrix >= a.count) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, mb = a.mb, bi = wave / mb, bj = wave - bi * mb;
@@ -600,7 +599,7 @@ __global__ __launch_bounds__(64 * kCoreSide * kCoreSide) void muon_core_kernel(M
         *(uint4v*)(first + (i * blockDim.x + threadIdx.x) * 16) = *(const uint4v*)(from + i * blockDim.x * 16);
     __syncthreads();
     const floatx16 zero = {};
-    floatx16 v, q;   // A, and Q
+    floatx16 v;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const char* at = first + ((bj * 2 * mb + 2 * bi + (k >> 1)) * kParts) * kBlockBytes + (k & 1) * 512 + (lane & 31) * 16 + (lane >> 5) * 8;
@@ -608,42 +607,40 @@ __global__ __launch_bounds__(64 * kCoreSide * kCoreSide) void muon_core_kernel(M
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[4 * k + e] = (float)lo[e] + (float)hi[e];
     }
-    auto times = [](floatx16& m, float by) {
+    auto times = [&](float by) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) m[i] *= by;
+        for (int i = 0; i < 16; ++i) v[i] *= by;
     };
-    for (int s = 0;; ++s) {
-        const bool last = s + 1 == steps;
-        times(v, a.cb);
-        if (!a.no_square) v = small_product(first, bi, first, bj, mb, v);
+    // B of A, which is there.  A A is summed from zero: added to one by one, (b / c) A would be rounded with every 16 columns (96 x 200: 2.6 times as far
+    // from exact as float32 products, 1.2 this way).
+    auto polynomial = [&]() {
+        floatx16 square = zero;
+        if (!a.no_square) square = small_product(first, bi, first, bj, mb, zero);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = a.cc * v[i] + (bi == bj && 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) == (lane & 31) ? a.ca : 0.f);
-        if (s == 0) q = v;
-        if (s == 0 && last) break;
-        small_across(second, mb, bi, bj, v);
-        __syncthreads();                     // B is there; where it is the last, A has been read
-        if (!last) {
-            v = small_product(second, bi, first, bj, mb, zero);
-            times(v, a.turn_scale);
-            __syncthreads();                 // A has been read
-            small_across(first, mb, bi, bj, v);
-            __syncthreads();
-            v = small_product(first, bi, second, bj, mb, zero);   // the next A
-            times(v, a.turn_scale);
-            if (s > 0) __syncthreads();      // B A has been read
-        }
-        if (s > 0) {
-            small_across(first, mb, bi, bj, q);
-            __syncthreads();
-            q = small_product(second, bi, first, bj, mb, zero);
-            times(q, a.q_scale[s - 1]);
-        }
-        if (last) break;
-        __syncthreads();                     // B A, or Q, has been read, and B
-        small_across(first, mb, bi, bj, v);
+        for (int i = 0; i < 16; ++i) v[i] = a.cc * (a.cb * v[i] + square[i]) + (bi == bj && 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) == (lane & 31) ? a.ca : 0.f);
+    };
+    auto put = [&](char* to) {
+        small_across(to, mb, bi, bj, v);
         __syncthreads();
+    };
+    polynomial();
+    if (steps > 1) {
+        put(second);
+        v = small_product(second, bi, first, bj, mb, zero);
+        times(a.turn_scale);
+        __syncthreads();   // A has been read
+        put(first);
+        v = small_product(first, bi, second, bj, mb, zero);
+        times(a.turn_scale);
+        __syncthreads();   // B A has been read
+        put(first);        // the next A
+        polynomial();
+        __syncthreads();   // it has been read
+        put(first);
+        v = small_product(second, bi, first, bj, mb, zero);
+        times(a.q_scale);
     }
-    small_across(block_at(a.b, matrix, mb, mb, 0, 0, 0), mb, bi, bj, q);
+    small_across(block_at(a.b, matrix, mb, mb, 0, 0, 0), mb, bi, bj, v);
 }
 
 // Tiles of 64 x 64, and parts of the sum: a product of few tiles is split so that every CU has a workgroup, sums of 32 steps of 32 columns and more, no
@@ -667,14 +664,15 @@ ProductPlan product_plan(long long count, int mb, int nb, MuonProduct mode, int 
 }
 size_t part_bytes(long long count, const ProductPlan& p) { return p.splits > 1 ? (size_t)count * p.tiles * p.splits * 4 * 4096 : 0; }
 
-// Several steps at a time (below) leave out two products over the long side, 1.5 mb^2 nb blocks, and take three over the short one, 1.5 mb^3, and a launch more:
-// worth it from 8192 blocks on.  us, one at a time against three and two: 300x1000 (2200 blocks) 114, 122; 512x1024 (4096) 137, 148; 512x2048 (12288) 154, 152; 512x4096 (28672) 179, 167; 1024x1536 (16384, but one and a half as wide as high) 216, 219;
-// 1024x4096 (98304) 382, 291; 4 of it 1251, 866.  A short side of up to kCoreSide blocks goes by the kernel above in any case.
+// Two steps at a time (below) leave out two products over the long side, 1.5 mb^2 nb blocks, and take three over the short one, 1.5 mb^3, and a launch more: worth it
+// from 8192 blocks on.  us of five steps, one at a time against two, one and two: 160x2000 (1400 blocks) 107, 107; 300x1000 (2200) 114, 121; 512x1024 (4096) 138, 144;
+// 8 of 160x2000 (11600) 143, 130; 512x2048 (12288) 153, 151; 1024x1536 (16384, but one and a half as wide as high) 214, 215; 512x4096 (28672) 177, 168; 12 of 200x2000
+// (32928) 213, 185; 1024x4096 (98304) 372, 313; 4 of it 1225, 979.  A short side of up to kCoreSide blocks goes by the kernel above in any case.
 bool is_wide(long long count, int mb, int nb) { return mb > kCoreSide && nb >= 2 * mb && count * (nb - mb) * mb * mb > 8192; }
 
 struct MuonPlan {
     int mb, nb, parts;
-    int squares;              // matrices of mb x mb: A and B, and where several steps are taken at a time another B and what they are multiplied to
+    int squares;              // matrices of mb x mb: A and B, and where two steps are taken at a time another B and what is multiplied
     size_t x_bytes, a_bytes, norm_bytes, part_bytes;
 };
 MuonPlan plan_of(long long count, long long rows, long long cols) {
@@ -742,19 +740,20 @@ bool bounds_of(const gleam_muon& p, double& sx, double& sa, double& sb, double& 
     return true;
 }
 
-// Several steps at a time, of wide matrices: B is a polynomial of A and commutes with it, so the next step's A is (B A) B, and the steps'
-// B multiply to one Q that X is multiplied by: instead of X X^T and B X, sums over the long side, three products of the short one.  What A is
-// rounded by, 2^-24 of its largest eigenvalue, is then not found again in the next X X^T: an eigenvalue near 0 grows by a^2 a step and Q changes by 2 b / a
-// of that, 2^-23 |b / a| (1 + a^2 + a^4) of itself after three steps (2.5e-5 of the smallest singular values with the default polynomial,
-// of which a step at a time leaves 2^-21 a^5 of the largest, 2.3e-4); so no more than three, and fewer where a is larger.
-// And Q has to be in reach of its scale, which is made for the largest value the steps' B could have, most_b^n of n steps, where what is there is about
-// a^n, and 1 beside it: above 2^12 of that its second parts would begin to go below the smallest float16 (at 2^16 of it; (1, -3, 6) has 2^21 for two
-// steps: 2500 x 700 X off by 1.2e-4 of itself together, 2.4e-7 one by one).
-int steps_at_once(const gleam_muon& h, double most_b) {
-    const double a2 = (double)h.a * h.a, loss = 0x1p-23 * std::fabs((double)h.b) / std::max(std::fabs((double)h.a), 1e-3);
-    const double over = most_b / std::min(std::max(std::fabs((double)h.a), 1e-6), 1.0);
-    auto may = [&](int n, double grown) { return loss * grown < 3e-5 && std::pow(over, n) <= 0x1p12; };
-    return may(3, 1.0 + a2 + a2 * a2) ? 3 : may(2, 1.0 + a2) ? 2 : 1;
+// Two steps at a time, of wide matrices and of short sides: B is a polynomial of A and commutes with it, so the next step's A is (B A) B, and the two B
+// multiply to one Q that X is multiplied by: instead of X X^T and B X, sums over the long side, three products of the short one.  What A is rounded by,
+// 2^-24 of its largest eigenvalue, is then not found again in the next X X^T: an eigenvalue near 0 grows by a^2 a step and Q changes by 2 b / a of that,
+// 2^-23 |b / a| (1 + a^2) of itself after two steps, 2.1e-6 with the default polynomial.  A third step would bring 2.5e-5, however many parts A has,
+// where float32 products leave X to 1e-6 (a strong direction over noise, 64 x 576: three steps together are 28 times as far from exact as float32 products,
+// two 1.1 times).  For the same reason the single step of an odd number is the second and not the last, by when the eigenvalues near 0 have grown
+// to what most of X is (96 x 200, an eighth of the directions strong, products emulated on the host: 1.0 times as far as float32 products, and 2.0).
+// And Q has to be in reach of its scale, which is made for the largest value that the steps' B could have, most_b^2, where what is there is about a^2, and 1
+// beside it: above 2^12 of that its second parts would begin to go below the smallest float16 (at 2^16 of it; (1, -3, 6) has 2^21: 2500 x 700 X off by
+// 1.2e-4 of itself together, 2.4e-7 one by one).
+bool may_go_together(const gleam_muon& h, double most_b) {
+    const double a = std::fabs((double)h.a), loss = 0x1p-23 * std::fabs((double)h.b) / std::max(a, 1e-3) * (1.0 + a * a);
+    const double over = most_b / std::min(std::max(a, 1e-6), 1.0);
+    return loss < 3e-5 && over * over <= 0x1p12;
 }
 
 }  // namespace
@@ -835,41 +834,28 @@ hipError_t muon_update(const gleam_muon& h, long long count, long long rows, lon
         a.sym_scale = (float)(s_to / (sl * sr));
         launch_product<kSym>(a, st);
     };
-    const bool core = p.mb <= kCoreSide;
-    const int most = core || p.squares > 2 ? steps_at_once(h, most_b) : 1, turns = (h.steps + most - 1) / most;
+    const bool core = p.mb <= kCoreSide, two = (core || p.squares > 2) && may_go_together(h, most_b);
     for (int k = 0, turn = 0; k < h.steps && e == hipSuccess; ++turn) {
-        const int now = (h.steps - k + turns - turn - 1) / (turns - turn);   // steps taken together, as even as they go
+        const int now = two && h.steps - k > 1 && !(turn == 1 && h.steps % 2) ? 2 : 1;   // steps taken together
         sym(a.x, sx, a.x, sx, a.nb, a.a, sa);
-        const char* q = nullptr;
-        double sq = sb;
+        const char* q = a.b = b[0];
+        const double sq = now == 1 ? sb : scale_of(most_b * most_b);
         if (core) {
             a.turn_scale = (float)(1.0 / sb);
-            for (int j = 1; j < now; ++j) {
-                const double s_to = scale_of(std::pow(most_b, j + 1));
-                a.q_scale[j - 1] = (float)(s_to / (sb * sq));
-                sq = s_to;
-            }
-            q = a.b = b[0];
-            const double work = 65536.0 * p.mb * p.mb * p.mb * count * (now == 1 ? 1 : 4 * now - 3);
+            a.q_scale = (float)(sq / (sb * sb));
+            const double work = 65536.0 * p.mb * p.mb * p.mb * count * (now == 1 ? 1 : 5);
             KernelScope ks("muon_core", work, 0.0, st, kProducts * work);
             hipLaunchKernelGGL(muon_core_kernel, grid_of(count), dim3(64 * p.mb * p.mb), 0, st, a, now);
-        }
-        for (int j = 0; j < (core ? 0 : now); ++j) {
-            a.b = b[j & 1];
+        } else {
             launch_product<kSquare>(a, st);
-            if (j + 1 < now) {
-                sym(a.b, sb, a.a, sa, a.mb, t, sa);      // B A, under the largest singular values of two X
-                sym(t, sa, a.b, sb, a.mb, a.a, sa);      // A of the next step
+            if (now == 2) {
+                sym(b[0], sb, a.a, sa, a.mb, t, sa);      // B A, under the largest singular values of two X
+                sym(t, sa, b[0], sb, a.mb, a.a, sa);      // A of the next step
+                a.b = b[1];
+                launch_product<kSquare>(a, st);
+                sym(b[1], sb, b[0], sb, a.mb, t, sq);     // Q; B A is not needed any more
+                q = t;
             }
-            if (j == 0) {
-                q = a.b;
-                continue;
-            }
-            char* to = j == 1 ? t : b[~j & 1];           // T is not needed any more; the B before neither
-            const double s_to = scale_of(std::pow(most_b, j + 1));
-            sym(a.b, sb, q, sq, a.mb, to, s_to);
-            q = to;
-            sq = s_to;
         }
         k += now;
         a.last = k == h.steps;

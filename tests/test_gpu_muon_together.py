@@ -34,3 +34,39 @@ def test_muon_of_polynomials_that_could_grow(coefficients, count, rows, cols):
     made for the largest."""
     err, bound = polynomial_error(count, rows, cols, coefficients, 2)
     assert err <= bound
+
+
+def gradient(kind, rows, cols):
+    rng = np.random.default_rng(rows)
+    noise, short = rng.normal(size=(rows, cols)), min(rows, cols)
+    if kind == "noise":
+        return noise
+    if kind == "direction":                                    # a single one, as strong as all of the noise or ten times as strong
+        return (3.0 if rows < cols else 1.0) * np.outer(rng.normal(size=rows), rng.normal(size=cols)) + noise
+    if kind == "directions":                                   # an eighth of the short side, from 1 to 0.01, over a floor of noise
+        few = max(1, short // 8)
+        return (rng.normal(size=(rows, few)) * np.logspace(0, -2, few)) @ rng.normal(size=(few, cols)) + 0.3 * noise
+    u, _, v = np.linalg.svd(noise, full_matrices=False)        # singular values spread evenly in their logarithm
+    return (u * np.logspace(0, -4, short)) @ v
+
+
+@pytest.mark.parametrize("kind", ["noise", "direction", "directions", "spread"])
+@pytest.mark.parametrize("count,rows,cols", [(4, 64, 64), (1, 192, 64), (2, 33, 250), (3, 30, 800), (3, 64, 576), (3, 96, 200), (3, 100, 900), (3, 900, 100), (2, 128, 2000), (70, 160, 320), (70, 320, 160), (12, 200, 2000), (1, 300, 2500), (1, 512, 2048), (1, 300, 400), (1, 130, 1000)])
+def test_muon_against_float32_products(count, rows, cols, kind):
+    """X after five steps of the default polynomial against the same steps in float32 products on the host: not more than four times as far from 64
+    bits.  A product's operands are off by half a step of 22 bits, 2^-23, each, and the product of the second parts that is left out is 2^-22 at
+    most: 2^-21, where operands of float32 are off by 2^-24 each, 2^-23."""
+    g = gradient(kind, rows, cols).astype(np.float32)
+    grad = torch.from_numpy(g).cuda().expand(count, rows, cols).contiguous()
+    theta, m = torch.zeros_like(grad), torch.zeros_like(grad)
+    step(theta, grad, m, lr=1.0, momentum=0.0)
+    want = mo.orthogonalise(g, 5, float(np.float32(1e-7)), DEFAULT)
+    x = (g / (np.linalg.norm(g.astype(np.float64)) + 1e-7)).astype(np.float32)
+    x = np.ascontiguousarray(x.T) if rows > cols else x
+    a, b, c = (np.float32(v) for v in mo.COEFFICIENTS)
+    for _ in range(5):
+        A = x @ x.T
+        x = a * x + (b * A + c * (A @ A)) @ x
+    ours, plain = rel_l2(-host(theta[-1]) / np.sqrt(max(1.0, rows / cols)), want), rel_l2(x.T if rows > cols else x, want)
+    print("muon", kind, count, rows, cols, "error", ours, "float32 products", plain, "ratio", ours / plain, flush=True)
+    assert ours <= 4 * plain
