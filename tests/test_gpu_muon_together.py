@@ -70,3 +70,35 @@ def test_muon_against_float32_products(count, rows, cols, kind):
     ours, plain = rel_l2(-host(theta[-1]) / np.sqrt(max(1.0, rows / cols)), want), rel_l2(x.T if rows > cols else x, want)
     print("muon", kind, count, rows, cols, "error", ours, "float32 products", plain, "ratio", ours / plain, flush=True)
     assert ours <= 4 * plain
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 7, 10])
+@pytest.mark.parametrize("count,rows,cols,gap", [(12, 200, 2000, 0), (12, 2000, 200, 3), (2, 520, 2100, 1)])
+def test_muon_of_wide_matrices_in_launches(count, rows, cols, gap, steps):
+    """Short sides of more than 128 and wide enough for several steps at a time; of 7 blocks (short sums of the short side) and of 17."""
+    check(count, rows, cols, steps=steps, gap=gap)
+
+
+@pytest.mark.parametrize("coefficients,steps", [((6.0, -10.0, 5.0), 2), ((6.0, -10.0, 5.0), 1), ((20.0, -20.0, 3.5), 2), ((1.5, -0.5, 0.0), 8), ((1.5, -0.5, 0.0), 5), ((1.0, 0.0, 0.0), 3)])
+@pytest.mark.parametrize("count,rows,cols", [(12, 200, 2000), (12, 2000, 200), (3, 90, 400)])
+def test_muon_of_wide_matrices_in_launches_and_other_polynomials(count, rows, cols, coefficients, steps):
+    """Also a slope that is too large for two steps at a time, and no A A."""
+    err, bound = polynomial_error(count, rows, cols, coefficients, steps)
+    assert err <= bound
+
+
+def test_muon_of_wide_matrices_in_launches_with_few_strong_directions():
+    check(12, 200, 2000, low=3)
+    check(12, 2000, 200, low=1)
+
+
+def test_muon_of_wide_matrices_in_launches_with_a_matrix_that_is_not_finite():
+    """Matrices of one call do not reach each other; a zero one stays."""
+    g = torch.randn(12, 200, 2000, device="cuda", generator=torch.Generator(device="cuda").manual_seed(6))
+    g[3], g[7, 5, 6] = 0.0, float("nan")
+    theta, m = torch.ones_like(g), torch.zeros_like(g)
+    step(theta, g, m, lr=1.0, momentum=0.0)
+    t = host(theta)
+    assert np.array_equal(t[3], np.ones((200, 2000))) and np.all(np.isnan(t[7])) and np.all(np.isfinite(np.delete(t, 7, 0)))
+    x = mo.orthogonalise(host(g[8]), 5, float(np.float32(1e-7)), DEFAULT)
+    assert np.linalg.norm(1.0 - t[8] - x) <= 8 * 2.0 ** -24 * sum(3.4445 ** k for k in range(6)) * np.linalg.norm(x) + 2.0 ** -24 * np.sqrt(t[8].size)   # 1 - X is rounded
