@@ -449,7 +449,7 @@ typedef struct {
     gleam_scan_strides x, r, i, h;
 } gleam_gatedscan_desc;
 
-/* Scratch of either direction; 0 where none is needed (then ws may be NULL). */
+/* Scratch of either direction; 0 where none is needed (then ws may be NULL).  Any description that one of the directions takes will do. */
 int gleam_gatedscan_workspace_bytes(const gleam_gatedscan_desc* desc, size_t* fwd_bytes, size_t* bwd_bytes);
 /* state_in: state before the first token, or NULL (zero).  state_out: state behind the last token, or NULL (not wanted); may be
  * state_in.  h may not overlap x, r or i. */

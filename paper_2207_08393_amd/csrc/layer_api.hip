@@ -291,7 +291,8 @@ int gleam_qknorm_bwd(const gleam_qknorm_desc* desc, const void* q, const void* k
 
 int gleam_gatedscan_workspace_bytes(const gleam_gatedscan_desc* desc, size_t* fwd_bytes, size_t* bwd_bytes) {
     if (!fwd_bytes || !bwd_bytes) return GLEAM_E_NULL;
-    const int rc = check_gatedscan(desc, false);
+    int rc = check_gatedscan(desc, false);
+    if (rc == GLEAM_E_DIMS) rc = check_gatedscan(desc, true);   // g_h may repeat, where h may not
     if (rc) return rc;
     *fwd_bytes = gatedscan_fwd_ws_bytes(*desc);
     *bwd_bytes = gatedscan_bwd_ws_bytes(*desc);

@@ -228,6 +228,20 @@ def test_gatedscan_of_inputs_that_stand_for_many(C, T, dtype):
     assert torch.equal(out[0], out[1]) and bool(torch.isfinite(out[0]).all())
 
 
+@pytest.mark.parametrize("T", [3, 200])
+@pytest.mark.parametrize("strides", [(0, 0, 0, 1), (0, 9, 0, 1), (9, 0, 9, 1)])
+def test_gatedscan_gradients_of_a_gradient_that_stands_for_many(strides, T):
+    """Backwards g_h is only read: with strides of 0, as a sum's gradient has them, it gives what its copy gives, bit by bit."""
+    B, P, C = 2, 3, 9
+    m = Scan(B, T, P, C, "f32", lengths=[T, T - 1])
+    g = torch.randn(T * C + B * P * 9 * T, device="cuda").as_strided((B, T, P, C), strides)
+    out = []
+    for m.x["g"] in (g, g.contiguous()):
+        out.append(m.bwd())
+    (a, al, aS), (b, bl, bS) = out
+    assert all(torch.equal(x, y) for x, y in zip((*a, al, aS), (*b, bl, bS))) and bool(torch.isfinite(torch.cat([x.flatten() for x in (*a, al, aS)])).all())
+
+
 def test_gatedscan_state_out_of_nothing_and_not_wanted():
     m = Scan(2, 140, 1, 6, "bf16", lengths=[140, 0], state=False)
     S = m.fwd()[1]

@@ -86,6 +86,20 @@ def test_gatedscan_refusals():
     assert L.gleam_gatedscan_workspace_bytes(changed(d, x=N(x.b, 0, x.p)), C.byref(n), C.byref(n)) == gb.GLEAM_OK   # arrays that are only read may repeat
 
 
+def test_gatedscan_workspace_of_either_direction():
+    """Backwards h's strides are those of a gradient that is only read; a description that neither direction takes is refused."""
+    L, d, n = gb.lib(), scan(), C.c_size_t(0)
+    query = lambda **more: L.gleam_gatedscan_workspace_bytes(changed(d, **more), C.byref(n), C.byref(n))  # noqa: E731
+    h, x = d.h, d.x
+    for repeated in (N(0, 0, 0), N(h.b, 0, h.p), N(0, h.t, h.p)):
+        assert query(h=repeated) == gb.GLEAM_OK and query(x=repeated, r=repeated, i=repeated) == gb.GLEAM_OK
+        assert query(h=repeated, x=N(x.b, 0, x.p)) == gb.GLEAM_E_DIMS
+        assert L.gleam_gatedscan_fwd(changed(d, h=repeated), *FAKE[:8], FAKE[8], 1 << 40, None) == gb.GLEAM_E_DIMS
+    y = torch.empty(2, 300, 1, 6)
+    e = gb.make_gatedscan(y, y, y, torch.empty(6).expand(2, 300, 1, 6))
+    assert gb.gleam_gatedscan_workspace_bytes(e) == gb.gleam_gatedscan_workspace_bytes(d)
+
+
 def test_gatedscan_binding_compares_arrays():
     x = torch.empty(1, 5, 2, 8)
     for bad in ((x, x, x, x[..., :4]), (x, x[:, :4], x, x), (x, x, x.bfloat16(), x), (x[0], x[0], x[0], x[0]), tuple(x.transpose(2, 3) for _ in range(4))):
