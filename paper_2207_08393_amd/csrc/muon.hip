@@ -348,7 +348,7 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(MuonArgs a) {
                 for (int q = 0; q < 4; ++q)
                     *(floatx4*)(lds[wave][i * W + j] + (q * 64 + lane) * 4) = floatx4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
     floatx16 sum;
-    if (MODE == kSquare && t.split == 0 && mine) sum = start_of_square(a, t.matrix, bi, bj);
+    if (MODE == kSquare && mine) sum = start_of_square(a, t.matrix, bi, bj);
     else
 #pragma unroll
         for (int i = 0; i < 16; ++i) sum[i] = 0.f;
@@ -367,12 +367,13 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(MuonArgs a) {
                 for (int e = 0; e < 4; ++e) sum[4 * q + e] += v[e];
             }
     }
-    if (!SHORT && a.splits > 1) {   // as the registers have it: [tile][split][block][four registers][lane]
-        float* to = a.part + ((t.tile * a.splits + t.split) * 4 + wave) * 1024 + lane * 4;
+    if constexpr (MODE == kSym && !SHORT)
+        if (a.splits > 1) {   // as the registers have it: [tile][split][block][four registers][lane]
+            float* to = a.part + ((t.tile * a.splits + t.split) * 4 + wave) * 1024 + lane * 4;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) *(floatx4*)(to + q * 256) = floatx4{sum[4 * q], sum[4 * q + 1], sum[4 * q + 2], sum[4 * q + 3]};
-        return;
-    }
+            for (int q = 0; q < 4; ++q) *(floatx4*)(to + q * 256) = floatx4{sum[4 * q], sum[4 * q + 1], sum[4 * q + 2], sum[4 * q + 3]};
+            return;
+        }
     float* tile = lds[wave][SHORT ? 0 : wave];   // read by this wave alone
     wave_sync();
     stage_block(sum, tile);
@@ -380,20 +381,19 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(MuonArgs a) {
     put_block<MODE>(a, t.matrix, bi, bj, tile);
 }
 
-// Sums the parts of a split product, a wave a block, in order.
-template <int MODE>
+// Sums the parts of a split X X^T, a wave a block, in order.
 __global__ __launch_bounds__(64) void muon_join_kernel(MuonArgs a) {
     __shared__ float lds[kTileFloats];
     constexpr int kBlocks = 4;
-    const int R = a.mb, Cb = MODE == kApply ? a.nb : a.mb, tr = (R + 1) / 2, tc = (Cb + 1) / 2;
-    const unsigned id = (unsigned)group_of_grid(), tile_id = id / kBlocks, per = MODE == kApply ? tr * tc : tr * (tr + 1) / 2;
+    const int R = a.mb, tr = (R + 1) / 2;
+    const unsigned id = (unsigned)group_of_grid(), tile_id = id / kBlocks, per = tr * (tr + 1) / 2;
     const unsigned matrix = tile_id / per;
     if (matrix >= (unsigned)a.count) return;
     const int block = (int)(id - tile_id * kBlocks), at = (int)(tile_id - matrix * per);
     Tile t;
-    place_tile<MODE>(at, tr, t);
+    place_tile<kSym>(at, tr, t);
     const int bi = 2 * t.ti + (block >> 1), bj = 2 * t.tj + (block & 1);
-    if (bi >= R || bj >= Cb || (MODE != kApply && bi > bj)) return;
+    if (bi > bj || bj >= R) return;
     const float* part = a.part + (long long)tile_id * a.splits * (kBlocks * 1024) + block * 1024 + (threadIdx.x & 63) * 4;
     floatx16 acc;
 #pragma unroll
@@ -409,7 +409,7 @@ __global__ __launch_bounds__(64) void muon_join_kernel(MuonArgs a) {
     }
     stage_block(acc, lds);
     wave_sync();
-    put_block<MODE>(a, matrix, bi, bj, lds);
+    put_block<kSym>(a, matrix, bi, bj, lds);
 }
 
 // Small matrices, of up to 16 blocks: all of a step in one workgroup.  A wave keeps one block of X in registers, as the matrix instruction returns
@@ -643,9 +643,9 @@ __global__ __launch_bounds__(64 * kCoreSide * kCoreSide) void muon_core_kernel(M
     small_across(block_at(a.b, matrix, mb, mb, 0, 0, 0), mb, bi, bj, v);
 }
 
-// Tiles of 64 x 64, and parts of the sum: a product of few tiles is split so that every CU has a workgroup, sums of 32 steps of 32 columns and more, no
-// part under eight (24 x 100 x 900, 29 steps: 122 us whole, 131 in three parts; 300 x 1000, 32 steps: 133 whole, 123 in four; one step of the
-// update at a time).
+// Tiles of 64 x 64, and parts of the sum: an X X^T of few tiles is split so that every CU has a workgroup, where the sum has 32 steps of 32 columns and more,
+// no part under eight.  us of the update, whole and split: 24 x 100 x 900 (29 steps) 109, 115; one 100 x 900 89, 87; 64 x 576 (18) 57, 61; 300 x 900 (29) 118, 116; 512 x 960 (30) 141, 168;
+// from 32 steps on 300 x 1000 121, 115; 100 x 1024 89, 85; 64 x 2048 73, 64; 512 x 2048 161, 151; 300 x 4000 181, 143.  The other products sum over the short side, and have 136 tiles where that is 32 steps.
 struct ProductPlan {
     bool is_short;            // sums of up to eight steps of 32 columns
     int splits;
@@ -657,7 +657,7 @@ ProductPlan product_plan(long long count, int mb, int nb, MuonProduct mode, int 
     p.tiles = mode == kApply ? tr * tc : tr * (tr + 1) / 2;
     long long s = 256 / (count * p.tiles);
     if (s > steps / 8) s = steps / 8;
-    if (steps < 32) s = 1;
+    if (mode != kSym || steps < 32) s = 1;
     p.splits = (int)(s < 1 ? 1 : s > 32 ? 32 : s);
     p.is_short = p.splits == 1 && steps <= 8;
     return p;
@@ -686,9 +686,7 @@ MuonPlan plan_of(long long count, long long rows, long long cols) {
     p.a_bytes = (size_t)count * p.mb * p.mb * 2 * kParts * kBlockBytes;
     p.squares = is_wide(count, p.mb, p.nb) ? 4 : 2;
     p.norm_bytes = (size_t)count * kMuonNorms * sizeof(double);
-    p.part_bytes = 0;
-    for (const ProductPlan& q : {product_plan(count, p.mb, p.nb, kSym, p.nb), product_plan(count, p.mb, p.nb, kSquare, p.mb), product_plan(count, p.mb, p.nb, kApply, p.mb)})
-        p.part_bytes = std::max(p.part_bytes, part_bytes(count, q));
+    p.part_bytes = part_bytes(count, product_plan(count, p.mb, p.nb, kSym, p.nb));
     return p;
 }
 
@@ -704,9 +702,9 @@ void launch_product(MuonArgs& a, hipStream_t st) {
         if (p.is_short) hipLaunchKernelGGL((muon_product_kernel<MODE, true>), grid, block, 0, st, a);
         else hipLaunchKernelGGL((muon_product_kernel<MODE, false>), grid, block, 0, st, a);
     }
-    if (p.splits == 1) return;
+    if (MODE != kSym || p.splits == 1) return;
     KernelScope ks("muon_join", 0.0, (double)part_bytes(a.count, p), st);
-    hipLaunchKernelGGL((muon_join_kernel<MODE>), grid_of(a.count * p.tiles * 4), dim3(64), 0, st, a);
+    hipLaunchKernelGGL(muon_join_kernel, grid_of(a.count * p.tiles * 4), dim3(64), 0, st, a);
 }
 
 // The power of two that takes v to (2^13, 2^14].
