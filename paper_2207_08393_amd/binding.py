@@ -633,7 +633,8 @@ def gleam_muon_workspace_bytes(count, rows, cols) -> int:
 def _matrices(t, like, what: str):
     """Address of float32 matrices [rows][cols] or [count][rows][cols] on the device, contiguous each, at equal distances as in `like`."""
     import torch
-    if (t.dtype is not torch.float32 or not t.is_cuda or t.shape != like.shape or t.stride() != like.stride() or t.dim() not in (2, 3) or
+    if (t.dtype is not torch.float32 or not t.is_cuda or t.shape != like.shape or t.dim() not in (2, 3) or
+            (t.stride() != like.stride() and any(n > 1 and x != y for n, x, y in zip(t.shape, t.stride(), like.stride()))) or
             (t.shape[-1] > 1 and t.stride(-1) != 1) or (t.shape[-2] > 1 and t.stride(-2) != t.shape[-1])):
         raise ValueError(f"{what}: shape {tuple(t.shape)} with strides {t.stride()} of {t.dtype} on {t.device}: float32 matrices on the GPU, contiguous "
                          f"each, of the shape and strides of theta, {tuple(like.shape)} and {like.stride()}, expected")

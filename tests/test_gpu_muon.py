@@ -173,6 +173,20 @@ def test_muon_of_many_matrices(count, rows, cols):
         assert np.abs(host(all_at_once[2][k]) - m).max() <= 2.0 ** -23 * np.abs(m).max()
 
 
+@pytest.mark.parametrize("count,rows,cols", [(1, 40, 50), (1, 1, 8), (3, 1, 8), (1, 100, 300)])
+def test_muon_of_strides_along_sides_of_one(count, rows, cols):
+    """Where there is one matrix, or one row, the distance to the next says nothing, and may differ from array to array."""
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    start = [torch.randn(count, rows, cols, device="cuda", generator=gen) for _ in range(3)]
+    want = [t.clone() for t in start]
+    step(*want, lr=0.1)
+    for k in range(3):
+        mine = [t.clone() for t in start]
+        mine[k] = mine[k].as_strided((count, rows, cols), (rows * cols + (5 if count == 1 else 0), cols + (7 if rows == 1 else 0), 1))
+        step(*mine, lr=0.1)
+        assert all(torch.equal(a, b) for a, b in zip(mine, want))
+
+
 @pytest.mark.parametrize("rows,cols", [(40, 50), (100, 300)])
 def test_muon_with_an_eps_that_is_no_guard(rows, cols):
     """1 / (|u| + eps) passes the range of a float32 where u is zero or tiny; X = u / (|u| + eps) does not."""
