@@ -41,7 +41,7 @@ def gradient(kind, rows, cols):
     noise, short = rng.normal(size=(rows, cols)), min(rows, cols)
     if kind == "noise":
         return noise
-    if kind == "direction":                                    # a single one, as strong as all of the noise or ten times as strong
+    if kind == "direction":                                    # a single one, as strong as all of the noise or three times that
         return (3.0 if rows < cols else 1.0) * np.outer(rng.normal(size=rows), rng.normal(size=cols)) + noise
     if kind == "directions":                                   # an eighth of the short side, from 1 to 0.01, over a floor of noise
         few = max(1, short // 8)
@@ -50,26 +50,38 @@ def gradient(kind, rows, cols):
     return (u * np.logspace(0, -4, short)) @ v
 
 
+def against_float32(count, g, steps):
+    rows, cols = g.shape
+    grad = torch.from_numpy(g).cuda().expand(count, rows, cols).contiguous()
+    theta, m = torch.zeros_like(grad), torch.zeros_like(grad)
+    step(theta, grad, m, lr=1.0, momentum=0.0, steps=steps)
+    want = mo.orthogonalise(g, steps, float(np.float32(1e-7)), DEFAULT)
+    x = (g / (np.linalg.norm(g.astype(np.float64)) + 1e-7)).astype(np.float32)
+    x = np.ascontiguousarray(x.T) if rows > cols else x
+    a, b, c = (np.float32(v) for v in mo.COEFFICIENTS)
+    for _ in range(steps):
+        A = x @ x.T
+        x = a * x + (b * A + c * (A @ A)) @ x
+    ours, plain = rel_l2(-host(theta[-1]) / np.sqrt(max(1.0, rows / cols)), want), rel_l2(x.T if rows > cols else x, want)
+    print("muon", count, rows, cols, steps, "error", ours, "float32 products", plain, "ratio", ours / plain, flush=True)
+    assert ours <= 4 * plain
+
+
 @pytest.mark.parametrize("kind", ["noise", "direction", "directions", "spread"])
-@pytest.mark.parametrize("count,rows,cols", [(4, 64, 64), (1, 192, 64), (2, 33, 250), (3, 30, 800), (3, 64, 576), (3, 96, 200), (3, 100, 900), (3, 900, 100), (2, 128, 2000), (70, 160, 320), (70, 320, 160), (12, 200, 2000), (1, 300, 2500), (1, 512, 2048), (1, 300, 400), (1, 130, 1000)])
+@pytest.mark.parametrize("count,rows,cols", [(4, 64, 64), (1, 192, 64), (2, 33, 250), (3, 30, 800), (3, 64, 576), (3, 96, 200), (3, 100, 900), (3, 900, 100), (2, 128, 2000),
+                                             (70, 160, 320), (70, 320, 160), (12, 200, 2000), (1, 300, 2500), (1, 512, 2048), (1, 300, 400), (1, 130, 1000)])
 def test_muon_against_float32_products(count, rows, cols, kind):
     """X after five steps of the default polynomial against the same steps in float32 products on the host: not more than four times as far from 64
     bits.  A product's operands are off by half a step of 22 bits, 2^-23, each, and the product of the second parts that is left out is 2^-22 at
     most: 2^-21, where operands of float32 are off by 2^-24 each, 2^-23."""
-    g = gradient(kind, rows, cols).astype(np.float32)
-    grad = torch.from_numpy(g).cuda().expand(count, rows, cols).contiguous()
-    theta, m = torch.zeros_like(grad), torch.zeros_like(grad)
-    step(theta, grad, m, lr=1.0, momentum=0.0)
-    want = mo.orthogonalise(g, 5, float(np.float32(1e-7)), DEFAULT)
-    x = (g / (np.linalg.norm(g.astype(np.float64)) + 1e-7)).astype(np.float32)
-    x = np.ascontiguousarray(x.T) if rows > cols else x
-    a, b, c = (np.float32(v) for v in mo.COEFFICIENTS)
-    for _ in range(5):
-        A = x @ x.T
-        x = a * x + (b * A + c * (A @ A)) @ x
-    ours, plain = rel_l2(-host(theta[-1]) / np.sqrt(max(1.0, rows / cols)), want), rel_l2(x.T if rows > cols else x, want)
-    print("muon", kind, count, rows, cols, "error", ours, "float32 products", plain, "ratio", ours / plain, flush=True)
-    assert ours <= 4 * plain
+    against_float32(count, gradient(kind, rows, cols).astype(np.float32), 5)
+
+
+@pytest.mark.parametrize("steps", [3, 4, 7, 10])
+@pytest.mark.parametrize("count,rows,cols", [(1, 64, 192), (3, 64, 576), (3, 200, 96), (12, 200, 2000), (1, 140, 170)])
+def test_muon_against_float32_products_of_other_step_counts(count, rows, cols, steps):
+    for kind in ("noise", "direction", "directions", "spread"):
+        against_float32(count, gradient(kind, rows, cols).astype(np.float32), steps)
 
 
 @pytest.mark.parametrize("steps", [1, 2, 3, 4, 7, 10])
