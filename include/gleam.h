@@ -431,7 +431,7 @@ int gleam_qknorm_bwd(const gleam_qknorm_desc* desc, const void* q, const void* k
                      void* g_q, void* g_k, float* g_gamma_q, float* g_gamma_k, void* ws, size_t ws_bytes, void* stream);
 
 /* ---- Gated scan -------------------------------------------------------------------------------------------------------------
- * A linear recurrence along the tokens whose memory the input itself opens and closes, channel by channel:
+ * A linear recurrence along the tokens whose memory the input itself opens and closes, channel by channel (the real-gated linear recurrent unit, De et al., 2024):
  *     s_t = sigmoid(r_t),   a_t = exp(-kappa softplus(lambda[c]) s_t),   h_t = a_t h_(t-1) + sqrt(1 - a_t^2) sigmoid(i_t) x_t
  * with x, r, i, h [B][T][P][C] and lambda [C] float32 (a parameter, with a gradient).  Its state is C numbers for each sequence and pixel.
  * Element [b][t][p][c] of an array lies at b*s.b + t*s.t + p*s.p + c (strides in elements, >= 0); arrays that are written - h, and in the

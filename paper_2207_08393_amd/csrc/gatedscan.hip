@@ -18,10 +18,11 @@
 // since gates and states are needed again on the way back; sequences longer than a workgroup's tokens take the same two launches.
 //
 // What bounds it: vector instructions, some 60 issue slots a token and channel forward (three exponentials, two quotients and a root count four
-// each).  20 x 192 x 160 pixels, 64 channels, bfloat16: 67 us, 4.7 TB/s and 96 % of the vector instructions' time, 2.4 ms as separate
-// products; 16384 tokens x 1024 channels: 27 + 8 + 29 us, 76 and 85 % in the two passes (26 us are its bytes, so that a scan that reads
+// each).  20 x 192 x 160 pixels, 64 channels, bfloat16: 67 us (float32 121, its bytes' time), 4.7 TB/s and 96 % of the vector
+// instructions' time, 2.4 ms as separate products; 16384 tokens x 1024 channels: 28 + 8 + 29 us, 76 and 85 % in the two passes (26 us are its bytes, so that a scan that reads
 // them once would still take some 40).  Gradients of 4 x 2048 x 1024: 19 + 6 + 38 + 5 us, 3.1 TB/s in the long pass (23 us of bytes in all);
-// 3 x 1001 x 301 in float32: 7 + 6 + 10 + 4, latency of four launches.  One token of 64 sequences, 1024 channels: 4.2 us, a launch.
+// 3 x 1001 x 301 in float32: 7 + 6 + 10 + 4, latency of four launches; 20 x 192 x 160 x 64 in bfloat16 162 us (106 of bytes), in float32 236 (212).
+// One token of 64 sequences, 1024 channels: 4.2 us, a launch.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>

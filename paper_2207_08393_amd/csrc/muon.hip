@@ -14,9 +14,9 @@
 // A and the polynomial B = a I + b A + c A^2 are symmetric: only blocks on and above the diagonal are computed, and written twice.
 //
 // What bounds it.  Matrices of up to 16 blocks: the latency of six phases a step, one workgroup (192 x 64: 35 us, of which a launch is 6).
-// Larger ones: launches and the latency of one wave's share while the chip is not full (24 x 100 x 900: 90 us, 12 of it bytes and matrix
-// instructions), then operands on their way through the L1 caches, 50 bytes a clock and CU (1024 x 4096: X X^T 28 us, 460 TFLOP/s of
-// float16 products, B X 35 us, 740 TFLOP/s; a library product of that type reaches 1211),
+// Larger ones: launches and the latency of one wave's share while the chip is not full (24 x 100 x 900: 104 to 109 us, 12 of it bytes and
+// matrix instructions), then operands on their way through the L1 caches, 50 bytes a clock and CU (1024 x 4096: X X^T 27 us, 480 TFLOP/s of
+// float16 products, B X 36 us, 720 TFLOP/s; a library product of that type reaches 1211),
 // and in a product of the short side, 10 us, the 120 CUs that 136 tiles leave without one.  Momentum and split move 12 and 16 bytes an element
 // at 4.4 and 5.2 TB/s.
 #include <hip/hip_runtime.h>
@@ -586,6 +586,7 @@ __global__ __launch_bounds__(64 * kSmallBlocks) void muon_small_kernel(MuonArgs 
 
 // One step or two (below) of a short side of up to four blocks, in one workgroup a matrix: from A to Q, the product of the steps' B.  A wave computes one
 // block of mb x mb of each product; the two operands stand in LDS as parts.  All these matrices are symmetric, so a block may be written as its transpose.
+// Latency bounds it: 24 of 100 x 900, 15.8 us for the five products of two steps and 7 for the one of a single step, where a launch takes 4.6 to 5 us.
 constexpr int kCoreSide = 4;
 __global__ __launch_bounds__(64 * kCoreSide * kCoreSide) void muon_core_kernel(MuonArgs a, int steps) {
     constexpr int kMost = kCoreSide * kCoreSide * 2 * kParts * kBlockBytes;
@@ -645,7 +646,8 @@ __global__ __launch_bounds__(64 * kCoreSide * kCoreSide) void muon_core_kernel(M
 
 // Tiles of 64 x 64, and parts of the sum: an X X^T of few tiles is split so that every CU has a workgroup, where the sum has 32 steps of 32 columns and more,
 // no part under eight.  us of the update, whole and split: 24 x 100 x 900 (29 steps) 109, 115; one 100 x 900 89, 87; 64 x 576 (18) 57, 61; 300 x 900 (29) 118, 116; 512 x 960 (30) 141, 168;
-// from 32 steps on 300 x 1000 121, 115; 100 x 1024 89, 85; 64 x 2048 73, 64; 512 x 2048 161, 151; 300 x 4000 181, 143.  The other products sum over the short side, and have 136 tiles where that is 32 steps.
+// from 32 steps on 300 x 1000 121, 115; 100 x 1024 89, 85; 64 x 2048 73, 64; 512 x 2048 161, 151; 300 x 4000 181, 143.
+// The other products sum over the short side, and have 136 tiles where that is 32 steps.
 struct ProductPlan {
     bool is_short;            // sums of up to eight steps of 32 columns
     int splits;

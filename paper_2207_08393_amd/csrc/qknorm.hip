@@ -10,7 +10,8 @@
 //
 // What bounds it: HBM, two passes over the arrays forward and three backward.  20 x 192 x 160 pixels, 4 + 4 heads of 16, bfloat16: 73 us for 157 MB
 // each way, 4.3 TB/s, half of the vector instructions' time (16 lanes that turn one token hold four rows; an angle in 64 bits is worked out
-// once for them).  Gradients of 16384 tokens, 16 + 4 heads of 128: 63 us for 252 MB, 4.0 TB/s, and 4.7 us for the sums.  One token of 64
+// once for them).  Gradients of 16384 tokens, 16 + 4 heads of 128: 63 us for 252 MB, 4.0 TB/s, and 4.8 us for the sums;
+// of 3 x 1001 tokens, 6 + 6 heads of 40, float32: 12 us, latency of the angles and then of the first row, and 3.8.  One token of 64
 // sequences: 4.9 us, latency of a launch, of the angle and of one row.
 #include <hip/hip_runtime.h>
 
